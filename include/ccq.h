@@ -61,7 +61,8 @@ typedef enum {
     CCQ_ERR_UNSUPPORTED = 2, /* a valid request this build does not implement     */
     CCQ_ERR_CUDA = 3,        /* a CUDA runtime/driver call failed                 */
     CCQ_ERR_TIMEOUT = 4,     /* an in-kernel bounded wait ran out (device status) */
-    CCQ_ERR_RANGE = 5        /* a chunk's gates left the range the kernel can factor (device status) */
+    CCQ_ERR_RANGE = 5,       /* a chunk's gates left the range the kernel can factor (device status) */
+    CCQ_ERR_INDEX = 6        /* a token id or action was outside its range (ccq_ops.h; device status) */
 } ccq_status;
 
 typedef enum { CCQ_BF16 = 0, CCQ_FP32 = 1 } ccq_dtype;
@@ -416,8 +417,9 @@ CCQ_API ccq_status ccq_gla_fwd_fixed_scratch(const void *q, const void *k, const
 /*
  * Synchronise `stream`, then read and clear the device status word that the
  * kernels write.  Returns CCQ_OK, CCQ_ERR_RANGE (a chunkwise CCQ-GLA kernel met
- * gates stronger than its factored decays can represent: see ccq_gla_fwd), CCQ_ERR_TIMEOUT (a kernel gave
- * up waiting; its outputs are not valid) or CCQ_ERR_CUDA.
+ * gates stronger than its factored decays can represent: see ccq_gla_fwd), CCQ_ERR_INDEX (an operator of
+ * ccq_ops.h met an index outside its range), CCQ_ERR_TIMEOUT (a kernel gave up waiting; its outputs are not
+ * valid) or CCQ_ERR_CUDA.
  */
 CCQ_API ccq_status ccq_device_status(void *stream);
 

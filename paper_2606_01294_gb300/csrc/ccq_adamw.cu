@@ -1,0 +1,350 @@
+// ccq_adamw.cu -- one AdamW update of many tensors in one launch, states in 32 or 8 bits (ccq_ops.h).
+//
+// Every element is read and written once: 28 bytes an element with everything in fp32, 16 with bf16 weights and
+// gradients, an fp32 master and 8-bit states.  HBM bounds it.  The tensors' addresses are the
+// launch's own arguments (constant memory), and a CTA finds its tensor among them by the tensors' first
+// chunks.  A warp updates kBlock consecutive elements, 8 a lane, which is also what shares a scale in the
+// 8-bit state: the block's largest moment is a warp's maximum, and the state never leaves registers between
+// its decoding and its rounding.
+// The 8-bit state's arithmetic up to the rounding is done without fused multiply-adds, so that its e4m3
+// codes are those of the formula's fp32 operations taken one by one.
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "ccq_ops.cuh"
+
+namespace ccq {
+namespace {
+
+constexpr int kBlock = CCQ_ADAMW_BLOCK;
+static_assert(kBlock == 32 * 8, "8 elements a lane");
+constexpr int kAdamThreads = 256;
+constexpr int kChunk = kBlock * (kAdamThreads / 32);  // elements of a CTA
+constexpr int kMaxTensors = 482;                      // of a launch: its arguments hold 32764 bytes
+
+struct AdamTensor {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *scale;
+    float *master;
+    int64_t n;
+    uint32_t first;  // chunk of the launch
+    uint32_t vec;    // every address allows 8 elements at a time
+};
+
+struct AdamConst {
+    float beta1, rest1, beta2, rest2;  // rest = 1 - beta
+    float keep;                        // 1 - lr weight_decay
+    float rate;                        // lr / (1 - beta1^step)
+    float root;                        // 1 / sqrt(1 - beta2^step)
+    float eps;
+    uint32_t turn;                     // step 0x9E3779B1
+    const float *grad_scale;
+};
+
+template <int CAP> struct AdamArgs {
+    AdamConst c;
+    int count;
+    AdamTensor t[CAP];
+};
+static_assert(sizeof(AdamArgs<kMaxTensors>) <= 32764, "a launch's arguments");
+
+// The two smallest non-negative e4m3 steps at a power-of-two scale: the bits of 2^e (as a float), at least 2^-100.
+__device__ __forceinline__ uint32_t scale_exponent(uint32_t top_bits) {
+    const int e = static_cast<int>((top_bits + 0x1FFFFFu) >> 23) - 8;  // the top three mantissa values fit below 448
+    return static_cast<uint32_t>(max(e, 27));
+}
+
+// e4m3 code of y = |x| / scale, rounded up where the fraction between neighbours reaches 2^20 - turn.
+__device__ __forceinline__ uint32_t encode(float y, uint32_t turn) {
+    const int normal = static_cast<int>((__float_as_uint(y) + turn) >> 20) - (120 << 3);
+    // below 2^-6 the neighbours are 2^-9 apart
+    const int small = static_cast<int>((static_cast<uint32_t>(y * 536870912.f) + turn) >> 20);
+    return static_cast<uint32_t>(min(y < 0.015625f ? small : normal, 127));
+}
+
+__device__ __forceinline__ void decode4(uint32_t codes, float *f) {
+    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes & 0xffffu), __NV_E4M3);
+    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes >> 16), __NV_E4M3);
+    const float2 x = __half22float2(__half2(a)), y = __half22float2(__half2(b));
+    f[0] = x.x; f[1] = x.y; f[2] = y.x; f[3] = y.y;
+}
+
+__device__ __forceinline__ uint32_t finite_bits(float x) {
+    const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
+    return b < 0x7f800000u ? b : 0u;
+}
+
+// Eight consecutive elements in the wide form; in the narrow one (unaligned tensors, a tensor's last block) lane l
+// holds elements l, l + 32, ... of the block, one access each.
+template <typename T> __device__ __forceinline__ void load8(const T *p, float (&f)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        unpack(load_stream<T, 8>(p), f);
+    } else {
+        float h[4];
+        const Pack<T, 4> a = load_stream<T, 4>(p), b = load_stream<T, 4>(p + 4);
+        unpack(a, h);
+        for (int i = 0; i < 4; ++i) f[i] = h[i];
+        unpack(b, h);
+        for (int i = 0; i < 4; ++i) f[4 + i] = h[i];
+    }
+}
+template <typename T> __device__ __forceinline__ void store8(T *p, const float (&f)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        Pack<T, 8> a;
+        pack(f, a);
+        store_stream<T, 8>(p, a);
+    } else {
+        Pack<T, 4> a;
+        const float lo[4] = {f[0], f[1], f[2], f[3]}, hi[4] = {f[4], f[5], f[6], f[7]};
+        pack(lo, a);
+        store_stream<T, 4>(p, a);
+        pack(hi, a);
+        store_stream<T, 4>(p + 4, a);
+    }
+}
+
+template <typename P, typename G, int BITS, int MASTER, int CAP>
+__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamArgs<CAP> a) {
+    // the last tensor whose first chunk is not past this one
+    int lo = 0, hi = a.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.t[mid].first <= blockIdx.x) lo = mid;
+        else hi = mid - 1;
+    }
+    const AdamTensor &t = a.t[lo];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t start = static_cast<int64_t>(blockIdx.x - t.first) * kChunk + warp * kBlock;
+    if (start >= t.n) return;
+    const int left = t.n - start < kBlock ? static_cast<int>(t.n - start) : kBlock;
+    const bool wide = t.vec && left == kBlock;
+    const float clip = a.c.grad_scale ? *a.c.grad_scale : 1.f;
+    P *param = static_cast<P *>(t.param) + start;
+    const G *grad = static_cast<const G *>(t.grad) + start;
+    float *master = MASTER ? t.master + start : nullptr;
+    float g[8], m[8], v[8], p[8];
+    float sm = 1.f, sv = 1.f;
+    float *scale = nullptr;
+    if constexpr (BITS == 8) {
+        scale = t.scale + start / kBlock * 2;
+        sm = scale[0];
+        sv = scale[1];
+    }
+    if (wide) {
+        load8(grad + lane * 8, g);
+        if constexpr (MASTER) load8(master + lane * 8, p);
+        else load8(param + lane * 8, p);
+        if constexpr (BITS == 8) {
+            const Pack<float, 2> cm = load_stream<float, 2>(reinterpret_cast<const float *>(static_cast<uint8_t *>(t.m) + start + lane * 8));
+            const Pack<float, 2> cv = load_stream<float, 2>(reinterpret_cast<const float *>(static_cast<uint8_t *>(t.v) + start + lane * 8));
+            decode4(cm.raw.x, m);
+            decode4(cm.raw.y, m + 4);
+            decode4(cv.raw.x, v);
+            decode4(cv.raw.y, v + 4);
+        } else {
+            load8(static_cast<const float *>(t.m) + start + lane * 8, m);
+            load8(static_cast<const float *>(t.v) + start + lane * 8, v);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int i = e * 32 + lane;
+            g[e] = p[e] = m[e] = v[e] = 0.f;
+            if (i >= left) continue;
+            g[e] = to_f32(grad[i]);
+            p[e] = MASTER ? master[i] : to_f32(param[i]);
+            if constexpr (BITS == 8) {
+                float f[4];
+                decode4(static_cast<const uint8_t *>(t.m)[start + i], f);
+                m[e] = f[0];
+                decode4(static_cast<const uint8_t *>(t.v)[start + i], f);
+                v[e] = f[0];
+            } else {
+                m[e] = static_cast<const float *>(t.m)[start + i];
+                v[e] = static_cast<const float *>(t.v)[start + i];
+            }
+        }
+    }
+    uint32_t top_m = 0, top_v = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float ge = __fmul_rn(g[e], clip);
+        float root;
+        if constexpr (BITS == 8) {
+            m[e] = __fmul_rn(m[e], sm);
+            const float r = __fmul_rn(v[e], sv);
+            v[e] = __fmul_rn(r, r);
+        }
+        m[e] = __fadd_rn(__fmul_rn(m[e], a.c.beta1), __fmul_rn(ge, a.c.rest1));
+        v[e] = __fadd_rn(__fmul_rn(v[e], a.c.beta2), __fmul_rn(__fmul_rn(ge, ge), a.c.rest2));
+        root = __fsqrt_rn(v[e]);
+        p[e] = p[e] * a.c.keep - a.c.rate * __fdividef(m[e], root * a.c.root + a.c.eps);
+        if constexpr (BITS == 8) {
+            v[e] = root;
+            top_m = max(top_m, finite_bits(m[e]));
+            top_v = max(top_v, finite_bits(root));
+        }
+    }
+    uint32_t code_m[8], code_v[8];
+    if constexpr (BITS == 8) {
+        const uint32_t em = scale_exponent(__reduce_max_sync(~0u, top_m));
+        const uint32_t ev = scale_exponent(__reduce_max_sync(~0u, top_v));
+        const float inv_m = __uint_as_float((254 - em) << 23), inv_v = __uint_as_float((254 - ev) << 23);
+        if (lane == 0) *reinterpret_cast<float2 *>(scale) = make_float2(__uint_as_float(em << 23), __uint_as_float(ev << 23));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t i = static_cast<uint32_t>(start) + (wide ? lane * 8 + e : e * 32 + lane);
+            const uint32_t turn = (i * 0x6A09E667u + a.c.turn) >> 12;
+            code_m[e] = encode(fabsf(m[e]) * inv_m, 0xFFFFFu - turn) | (m[e] < 0.f ? 128u : 0u);
+            code_v[e] = v[e] == 0.f ? 0u : max(encode(v[e] * inv_v, turn), 1u);
+        }
+    }
+    if (wide) {
+        store8(param + lane * 8, p);
+        if constexpr (MASTER) store8(master + lane * 8, p);
+        if constexpr (BITS == 8) {
+            auto word = [](const uint32_t *c) { return c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24; };
+            __stcs(reinterpret_cast<uint2 *>(static_cast<uint8_t *>(t.m) + start + lane * 8), make_uint2(word(code_m), word(code_m + 4)));
+            __stcs(reinterpret_cast<uint2 *>(static_cast<uint8_t *>(t.v) + start + lane * 8), make_uint2(word(code_v), word(code_v + 4)));
+        } else {
+            store8(static_cast<float *>(t.m) + start + lane * 8, m);
+            store8(static_cast<float *>(t.v) + start + lane * 8, v);
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int i = e * 32 + lane;
+        if (i >= left) continue;
+        param[i] = from_f32<P>(p[e]);
+        if constexpr (MASTER) master[i] = p[e];
+        if constexpr (BITS == 8) {
+            static_cast<uint8_t *>(t.m)[start + i] = static_cast<uint8_t>(code_m[e]);
+            static_cast<uint8_t *>(t.v)[start + i] = static_cast<uint8_t>(code_v[e]);
+        } else {
+            static_cast<float *>(t.m)[start + i] = m[e];
+            static_cast<float *>(t.v)[start + i] = v[e];
+        }
+    }
+}
+
+template <typename P, typename G, int BITS, int MASTER>
+cudaError_t launch_adamw(const AdamArgs<kMaxTensors> &a, unsigned chunks, cudaStream_t s) {
+    // a short list is passed as a short argument block
+    constexpr int kFew = 48;
+    if (a.count <= kFew) {
+        AdamArgs<kFew> few;
+        few.c = a.c;
+        few.count = a.count;
+        std::copy(a.t, a.t + a.count, few.t);
+        adamw_kernel<P, G, BITS, MASTER, kFew><<<chunks, kAdamThreads, 0, s>>>(few);
+    } else {
+        adamw_kernel<P, G, BITS, MASTER, kMaxTensors><<<chunks, kAdamThreads, 0, s>>>(a);
+    }
+    return cudaGetLastError();
+}
+
+ccq_status check_tensor(const ccq_adamw_tensor &t, int i, int pe, int ge, int bits, bool master) {
+    struct { const char *name; const void *p; int least; } need[] = {
+        {"param", t.param, pe}, {"grad", t.grad, ge}, {"m", t.m, bits / 8}, {"v", t.v, bits / 8},
+        {"scale", t.scale, bits == 8 ? 8 : 0}, {"master", t.master, master ? 4 : 0}};
+    for (const auto &q : need) {
+        if (!q.least) {
+            if (q.p) return op_fail(CCQ_ERR_INVALID_ARG, "tensor %d: %s is given but not used", i, q.name);
+        } else if (!q.p) {
+            return op_fail(CCQ_ERR_INVALID_ARG, "tensor %d: %s is NULL", i, q.name);
+        } else if (reinterpret_cast<uintptr_t>(q.p) % q.least) {
+            return op_fail(CCQ_ERR_INVALID_ARG, "tensor %d: %s is not aligned to %d bytes", i, q.name, q.least);
+        }
+    }
+    return CCQ_OK;
+}
+
+}  // namespace
+}  // namespace ccq
+
+using namespace ccq;
+
+extern "C" ccq_status ccq_adamw_step(const ccq_adamw_tensor *tensors, int count, ccq_dtype param_dtype, ccq_dtype grad_dtype,
+                                     int state_bits, const ccq_adamw_params *p, const float *grad_scale, void *stream) {
+    if (count < 0) return op_fail(CCQ_ERR_INVALID_ARG, "count=%d", count);
+    if (!p) return op_fail(CCQ_ERR_INVALID_ARG, "params is NULL");
+    if (count && !tensors) return op_fail(CCQ_ERR_INVALID_ARG, "tensors is NULL");
+    if (!valid_dtype(param_dtype) || !valid_dtype(grad_dtype))
+        return op_fail(CCQ_ERR_INVALID_ARG, "unknown dtype %d or grad dtype %d", param_dtype, grad_dtype);
+    if (state_bits != 8 && state_bits != 32) return op_fail(CCQ_ERR_INVALID_ARG, "state_bits=%d: 8 or 32", state_bits);
+    if (p->step < 1) return op_fail(CCQ_ERR_INVALID_ARG, "step=%lld must be >= 1", static_cast<long long>(p->step));
+    if (!(p->beta1 >= 0 && p->beta1 < 1) || !(p->beta2 >= 0 && p->beta2 < 1))
+        return op_fail(CCQ_ERR_INVALID_ARG, "betas must be in [0, 1)");
+    if (!(p->eps >= 0)) return op_fail(CCQ_ERR_INVALID_ARG, "eps must be >= 0");
+    if (grad_scale && reinterpret_cast<uintptr_t>(grad_scale) % 4)
+        return op_fail(CCQ_ERR_INVALID_ARG, "grad_scale is not aligned to 4 bytes");
+    const int pe = dtype_bytes(param_dtype), ge = dtype_bytes(grad_dtype);
+    bool master = false;
+    for (int i = 0; i < count; ++i)
+        if (tensors[i].n > 0) {
+            master = tensors[i].master != nullptr;
+            break;
+        }
+    if (master && param_dtype != CCQ_BF16)
+        return op_fail(CCQ_ERR_INVALID_ARG, "a master copy needs bf16 parameters");
+    for (int i = 0; i < count; ++i) {
+        if (tensors[i].n < 0) return op_fail(CCQ_ERR_INVALID_ARG, "tensor %d: n=%lld", i, static_cast<long long>(tensors[i].n));
+        if (tensors[i].n > (static_cast<int64_t>(1) << 40)) return op_fail(CCQ_ERR_UNSUPPORTED, "tensor %d: n above 2^40", i);
+        if (tensors[i].n == 0) continue;
+        ccq_status st = check_tensor(tensors[i], i, pe, ge, state_bits, master);
+        if (st != CCQ_OK) return st;
+    }
+    static thread_local AdamArgs<kMaxTensors> a;
+    const double b1 = p->beta1, b2 = p->beta2, c1 = 1 - pow(b1, static_cast<double>(p->step)),
+                 c2 = 1 - pow(b2, static_cast<double>(p->step));
+    a.c.beta1 = static_cast<float>(b1);
+    a.c.rest1 = static_cast<float>(1 - b1);
+    a.c.beta2 = static_cast<float>(b2);
+    a.c.rest2 = static_cast<float>(1 - b2);
+    a.c.keep = static_cast<float>(1 - p->lr * p->weight_decay);
+    a.c.rate = static_cast<float>(p->lr / c1);
+    a.c.root = static_cast<float>(1 / sqrt(c2));
+    a.c.eps = static_cast<float>(p->eps);
+    a.c.turn = static_cast<uint32_t>(p->step) * 0x9E3779B1u;
+    a.c.grad_scale = grad_scale;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    auto flush = [&](unsigned chunks) {
+        using B = __nv_bfloat16;
+        const bool pb = param_dtype == CCQ_BF16, gb = grad_dtype == CCQ_BF16, s8 = state_bits == 8;
+        if (!pb)
+            return gb ? (s8 ? launch_adamw<float, B, 8, 0>(a, chunks, s) : launch_adamw<float, B, 32, 0>(a, chunks, s))
+                      : (s8 ? launch_adamw<float, float, 8, 0>(a, chunks, s) : launch_adamw<float, float, 32, 0>(a, chunks, s));
+        if (!master)
+            return gb ? (s8 ? launch_adamw<B, B, 8, 0>(a, chunks, s) : launch_adamw<B, B, 32, 0>(a, chunks, s))
+                      : (s8 ? launch_adamw<B, float, 8, 0>(a, chunks, s) : launch_adamw<B, float, 32, 0>(a, chunks, s));
+        return gb ? (s8 ? launch_adamw<B, B, 8, 1>(a, chunks, s) : launch_adamw<B, B, 32, 1>(a, chunks, s))
+                  : (s8 ? launch_adamw<B, float, 8, 1>(a, chunks, s) : launch_adamw<B, float, 32, 1>(a, chunks, s));
+    };
+    a.count = 0;
+    int64_t chunks = 0;
+    const int64_t most = 0x7fffffff;  // CTAs of a launch
+    for (int i = 0; i < count; ++i) {
+        const ccq_adamw_tensor &t = tensors[i];
+        if (t.n == 0) continue;
+        const int64_t c = (t.n + kChunk - 1) / kChunk;
+        if (a.count == kMaxTensors || chunks + c > most) {
+            cudaError_t e = flush(static_cast<unsigned>(chunks));
+            if (e != cudaSuccess) return op_cuda(e, "AdamW launch");
+            a.count = 0;
+            chunks = 0;
+        }
+        auto at = [](const void *q, int bytes) { return reinterpret_cast<uintptr_t>(q) % bytes == 0; };
+        AdamTensor &d = a.t[a.count++];
+        d = {t.param, t.grad, t.m, t.v, t.scale, t.master, t.n, static_cast<uint32_t>(chunks), 0};
+        d.vec = at(t.param, 16) && at(t.grad, 16) && at(t.m, state_bits == 8 ? 8 : 16) && at(t.v, state_bits == 8 ? 8 : 16) &&
+                at(t.master, 16);
+        chunks += c;
+    }
+    return a.count ? op_cuda(flush(static_cast<unsigned>(chunks)), "AdamW launch") : CCQ_OK;
+}

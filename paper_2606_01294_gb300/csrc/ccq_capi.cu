@@ -215,6 +215,7 @@ const char *ccq_status_string(ccq_status s) {
         case CCQ_ERR_CUDA: return "CUDA error";
         case CCQ_ERR_TIMEOUT: return "a kernel's bounded wait timed out";
         case CCQ_ERR_RANGE: return "gates outside the range the chunkwise kernel can factor";
+        case CCQ_ERR_INDEX: return "an index outside its range";
     }
     return "unknown status";
 }
@@ -1111,6 +1112,9 @@ ccq_status ccq_device_status(void *stream) {
         if (v == static_cast<int>(CCQ_ERR_RANGE))  // the kernels write the status code itself
             return fail(CCQ_ERR_RANGE, "device status %d: a chunk's cumulative log gates over 16 tokens fell "
                                        "below about -87 (see ccq_gla_fwd); the outputs are not valid", v);
+        if (v == static_cast<int>(CCQ_ERR_INDEX))
+            return fail(CCQ_ERR_INDEX, "device status %d: a token id or action was outside its range (see "
+                                       "ccq_ops.h for what its row holds)", v);
         return fail(CCQ_ERR_TIMEOUT, "device status %d: an in-kernel wait gave up", v);
     }
     return CCQ_OK;

@@ -17,6 +17,8 @@ constexpr int kStatusTimeout = 4;
 // Status code a kernel writes when its inputs leave the range it can represent
 // (CCQ_ERR_RANGE); the kernel runs to completion, its outputs are not valid.
 constexpr int kStatusRange = 5;
+// Status code of an index outside its range (CCQ_ERR_INDEX).
+constexpr int kStatusIndex = 6;
 // A bounded wait gives up after this many SM clock cycles (about one second).
 constexpr long long kWaitLimitCycles = 2000000000LL;
 

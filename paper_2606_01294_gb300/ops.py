@@ -1,0 +1,375 @@
+"""Python binding of include/ccq_ops.h: the operators around the CCQ token mixer.
+
+The embedding lookup and its gradient, the (gated) group norm after the mixer's read and its gradient, the
+clipped policy loss with its gradient, the token log-probabilities, and the AdamW update of many tensors.  As in
+:mod:`.ccq`, this is argument marshalling only: tensors are CUDA tensors (there is no CPU path), outputs
+and workspaces are allocated with torch on the inputs' device, and every computation runs in the
+library's kernels on the current stream.
+
+Tensors of rows need contiguous rows; the rows themselves may lie apart (a slice of a wider projection), as
+long as one stride reaches them all.
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+from dataclasses import dataclass
+from typing import List, Optional
+
+import torch
+
+from . import ccq
+from .ccq import _check, _dtype_code, _ptr, _stream
+
+ACTIVATION = {"none": 0, "silu": 1, "sigmoid": 2}
+ADAMW_BLOCK = 256
+
+_VP, _I, _L, _F, _D, _Z = (ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_double,
+                           ctypes.c_size_t)
+
+
+class _PolicyParams(ctypes.Structure):
+    _fields_ = [("clip_low", _F), ("clip_high", _F), ("kl_coef", _F), ("temperature", _F), ("grad_scale", _F)]
+
+
+class _AdamWParams(ctypes.Structure):
+    _fields_ = [("lr", _D), ("beta1", _D), ("beta2", _D), ("eps", _D), ("weight_decay", _D), ("step", _L)]
+
+
+@functools.lru_cache(maxsize=1)
+def _library() -> ctypes.CDLL:
+    lib = ccq.load_library()
+    size = ctypes.POINTER(_Z)
+    for name, args in {
+            # table, dtype, stride | ids, id_bytes, n, rows, width, scale | out, stride | stream
+            "ccq_embed": [_VP, _I, _L, _VP, _I, _L, _L, _I, _F, _VP, _L, _VP],
+            # dout, dtype, stride | ids, id_bytes, n, rows, width, scale, padding | dtable, dtype, stride | ws | stream
+            "ccq_embed_grad": [_VP, _I, _L, _VP, _I, _L, _L, _I, _F, _L, _VP, _I, _L, _VP, _Z, _VP],
+            "ccq_embed_grad_workspace_size": [_L, _L, _I, size],
+            # x, gate (strides), weight, bias, dtypes, y, stride | tokens, channels, groups, centered, eps, act | stream
+            "ccq_group_norm": [_VP, _L, _VP, _L, _VP, _VP, _I, _I, _VP, _L, _L, _I, _I, _I, _F, _I, _VP],
+            # x, gate, weight, bias, dy, dtypes | dx, dgate, dweight, dbias | sizes, centered, eps, act | ws | stream
+            "ccq_group_norm_bwd": [_VP, _L, _VP, _L, _VP, _VP, _VP, _L, _I, _I, _VP, _L, _VP, _L, _VP, _VP, _L, _I,
+                                   _I, _I, _F, _I, _VP, _Z, _VP],
+            "ccq_group_norm_bwd_workspace_size": [_L, _I, _I, _I, size],
+            # logits, dtype, stride | actions, id_bytes | old, ref, adv, weights | n, vocab, params | loss, logp,
+            # dlogits, stride | ws | stream
+            "ccq_policy_loss": [_VP, _I, _L, _VP, _I, _VP, _VP, _VP, _VP, _L, _I, ctypes.POINTER(_PolicyParams), _VP,
+                                _VP, _VP, _L, _VP, _Z, _VP],
+            "ccq_policy_loss_workspace_size": [_L, size],
+            "ccq_token_logp": [_VP, _I, _L, _VP, _I, _L, _I, _F, _VP, _VP],
+            "ccq_adamw_step": [_VP, _I, _I, _I, _I, ctypes.POINTER(_AdamWParams), _VP, _VP]}.items():
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = args, _I
+    lib.ccq_default_policy_params.argtypes = [ctypes.POINTER(_PolicyParams)]
+    lib.ccq_default_policy_params.restype = None
+    return lib
+
+
+@functools.lru_cache(maxsize=256)
+def _size(fn, device, *args):
+    """Bytes from a workspace query: a function of the sizes (and of the device's SM count)."""
+    need = _Z(0)
+    _check(getattr(_library(), fn)(*args, ctypes.byref(need)))
+    return need.value
+
+
+def _workspace(workspace, need, device):
+    if workspace is None:
+        return torch.empty(max(need, 16), dtype=torch.uint8, device=device), max(need, 16)
+    _dense(workspace, "workspace", device)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _cuda(t, name, device=None):
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ValueError(f"{name} must be a CUDA tensor (there is no CPU path)")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    return t
+
+
+def _dense(t, name, device, dtype=None, shape=None):
+    _cuda(t, name, device)
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _rows(t, name, device=None, dtype=None, shape=None):
+    """The stride between the rows of a [..., width] tensor with contiguous rows."""
+    _cuda(t, name, device)
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dim() < 1:
+        raise ValueError(f"{name} must have at least one dimension")
+    if t.is_contiguous():
+        return t.shape[-1]
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must have contiguous rows (its last dimension)")
+    step, reach = None, 0
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if step is None:
+            step, reach = stride, stride * size
+        elif stride == reach:
+            reach = stride * size
+        else:
+            raise ValueError(f"{name}: one stride must reach all of its rows")
+    if step is not None and step < t.shape[-1]:
+        raise ValueError(f"{name}: its rows overlap")
+    return t.shape[-1] if step is None else step
+
+
+def _ids(t, name, device):
+    if t.dtype not in (torch.int64, torch.int32):
+        raise TypeError(f"{name} must be int64 or int32, got {t.dtype}")
+    _dense(t, name, device)
+    return t.element_size()
+
+
+# ---------------------------------------------------------------- embedding
+
+
+def embed(table, ids, *, scale: float = 1.0, out=None, stream=None):
+    """``scale * table[ids]`` (ccq_embed): table [rows, width] bf16 or fp32, ids int64 or int32 of any
+    shape; returns [*ids.shape, width].  An id outside the table gives a zero row and CCQ_ERR_INDEX
+    from :func:`ccq.device_status`."""
+    dev = _cuda(table, "table").device
+    if table.dim() != 2:
+        raise ValueError("table must be [rows, width]")
+    ts = _rows(table, "table")
+    width = _ids(ids, "ids", dev)
+    shape = ids.shape + (table.shape[1],)
+    if out is None:
+        out = torch.empty(shape, dtype=table.dtype, device=dev)
+    os = _rows(out, "out", dev, table.dtype, shape)
+    _check(_library().ccq_embed(table.data_ptr(), _dtype_code(table), ts, ids.data_ptr(), width, ids.numel(),
+                                table.shape[0], table.shape[1], scale, out.data_ptr(), os, _stream(dev, stream)))
+    return out
+
+
+def embed_grad(dout, ids, rows: int, *, scale: float = 1.0, padding_id: Optional[int] = None, dtype=None, out=None,
+               workspace=None, stream=None):
+    """Gradient of :func:`embed`'s table (ccq_embed_grad): row r is ``scale`` times the sum of dout over
+    the tokens with id r, summed in fp32 in a fixed order; rows without a token (and ``padding_id``'s) are zero.
+    dout [*ids.shape, width]; returns [rows, width] in ``dtype`` (dout's when not given) or ``out``."""
+    dev = _cuda(dout, "dout").device
+    id_bytes = _ids(ids, "ids", dev)
+    if dout.dim() < 1:
+        raise ValueError("dout must be [*ids.shape, width]")
+    width, n = dout.shape[-1], ids.numel()
+    ds = _rows(dout, "dout", dev, None, ids.shape + (width,))
+    if out is None:
+        out = torch.empty(rows, width, dtype=dtype or dout.dtype, device=dev)
+    os = _rows(out, "out", dev, dtype, (rows, width))
+    if padding_id is not None and not 0 <= padding_id < rows:
+        raise ValueError(f"padding_id {padding_id} is outside the table of {rows} rows")
+    workspace, nbytes = _workspace(workspace, _size("ccq_embed_grad_workspace_size", -1, n, rows, width), dev)
+    _check(_library().ccq_embed_grad(dout.data_ptr(), _dtype_code(dout), ds, ids.data_ptr(), id_bytes, n, rows, width,
+                                     scale, -1 if padding_id is None else padding_id, out.data_ptr(), _dtype_code(out),
+                                     os, workspace.data_ptr(), nbytes, _stream(dev, stream)))
+    return out
+
+
+# ---------------------------------------------------------------- group norm
+
+
+def _norm_args(x, weight, bias, gate, groups, activation):
+    dev = _cuda(x, "x").device
+    xs = _rows(x, "x")
+    channels = x.shape[-1]
+    if groups < 1 or channels % groups:
+        raise ValueError(f"{channels} channels do not divide into {groups} groups")
+    if activation not in ACTIVATION:
+        raise ValueError(f"unknown activation {activation!r}: one of {sorted(ACTIVATION)}")
+    gs = 0 if gate is None else _rows(gate, "gate", dev, x.dtype, x.shape)
+    param = weight if weight is not None else bias
+    pdt = _dtype_code(param) if param is not None else ccq.FP32
+    for p, name in ((weight, "weight"), (bias, "bias")):
+        if p is not None:
+            _dense(p, name, dev, param.dtype, (channels,))
+    return dev, xs, gs, channels, pdt, x.numel() // channels if channels else 0
+
+
+def group_norm(x, weight=None, bias=None, gate=None, *, groups: int, activation: str = "silu", centered: bool = True,
+               eps: float = 1e-5, out=None, stream=None):
+    """Group norm of every token's channels and an activation (ccq_group_norm): with ``groups`` = heads, what
+    follows the mixer's read.  x [..., channels] bf16 or fp32; weight, bias [channels] (None: 1 and
+    0); ``u * act(gate)`` with a gate of x's shape, ``act(u)`` without.  ``centered=False`` leaves the mean in
+    (a root-mean-square norm)."""
+    dev, xs, gs, channels, pdt, tokens = _norm_args(x, weight, bias, gate, groups, activation)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    os = _rows(out, "out", dev, x.dtype, x.shape)
+    _check(_library().ccq_group_norm(x.data_ptr(), xs, _ptr(gate), gs, _ptr(weight), _ptr(bias), _dtype_code(x), pdt,
+                                     out.data_ptr(), os, tokens, channels, groups, int(bool(centered)), eps,
+                                     ACTIVATION[activation], _stream(dev, stream)))
+    return out
+
+
+def group_norm_bwd(x, weight, bias, gate, dout, *, groups: int, activation: str = "silu", centered: bool = True,
+                   eps: float = 1e-5, out: Optional[dict] = None, workspace=None, stream=None):
+    """Gradients of :func:`group_norm` (ccq_group_norm_bwd): a dict of dx, dgate (where there is a gate), dweight
+    and dbias (where there are those).  Only the forward's inputs are needed.  ``out`` may hold preallocated
+    tensors under those names."""
+    dev, xs, gs, channels, pdt, tokens = _norm_args(x, weight, bias, gate, groups, activation)
+    ds = _rows(dout, "dout", dev, x.dtype, x.shape)
+    g = dict(out or {})
+    strides = {"dgate": 0}
+    for name, like in (("dx", x), ("dgate", gate)):
+        if like is not None:
+            if g.get(name) is None:
+                g[name] = torch.empty(x.shape, dtype=x.dtype, device=dev)
+            strides[name] = _rows(g[name], name, dev, x.dtype, x.shape)
+    for name, like in (("dweight", weight), ("dbias", bias)):
+        if like is not None:
+            if g.get(name) is None:
+                g[name] = torch.empty(like.shape, dtype=like.dtype, device=dev)
+            _dense(g[name], name, dev, like.dtype, like.shape)
+    workspace, nbytes = _workspace(workspace, _size("ccq_group_norm_bwd_workspace_size", dev.index, tokens, channels,
+                                                    groups, _dtype_code(x)), dev)
+    _check(_library().ccq_group_norm_bwd(
+        x.data_ptr(), xs, _ptr(gate), gs, _ptr(weight), _ptr(bias), dout.data_ptr(), ds, _dtype_code(x), pdt,
+        g["dx"].data_ptr(), strides["dx"], _ptr(g.get("dgate")), strides["dgate"], _ptr(g.get("dweight")),
+        _ptr(g.get("dbias")), tokens, channels, groups, int(bool(centered)), eps, ACTIVATION[activation],
+        workspace.data_ptr(), nbytes, _stream(dev, stream)))
+    return g
+
+
+# ---------------------------------------------------------------- policy loss
+
+
+def _tokens(logits, actions):
+    dev = _cuda(logits, "logits").device
+    if logits.dim() < 1:
+        raise ValueError("logits must be [..., vocab]")
+    ls = _rows(logits, "logits")
+    id_bytes = _ids(actions, "actions", dev)
+    if actions.shape != logits.shape[:-1]:
+        raise ValueError(f"actions have shape {tuple(actions.shape)}, expected {tuple(logits.shape[:-1])}")
+    return dev, ls, id_bytes
+
+
+def policy_loss(logits, actions, old_logp, advantages, *, ref_logp=None, weights=None, clip=(0.2, 0.2),
+                kl_coef: float = 0.0, temperature: float = 1.0, grad_scale: float = 1.0, grad: bool = True,
+                dlogits=None, workspace=None, stream=None):
+    """Clipped policy loss with a KL term and its gradient (ccq_policy_loss).  logits [..., vocab] bf16 or fp32;
+    actions [...] int64 or int32; old_logp, advantages, ref_logp (None: no KL term), weights (None: 1 / n)
+    [...] fp32.  A token of weight 0 is masked: nothing of it is read.  ``clip`` is (low, high), the ratio is held
+    in [1 - low, 1 + high].  Returns a dict of loss (a scalar tensor), logp [...] (0 where masked) and,
+    with ``grad``, dlogits (``grad_scale`` times the loss's gradient; ``dlogits`` may be the logits)."""
+    dev, ls, id_bytes = _tokens(logits, actions)
+    shape, vocab = actions.shape, logits.shape[-1]
+    for t, name in ((old_logp, "old_logp"), (advantages, "advantages"), (ref_logp, "ref_logp"), (weights, "weights")):
+        if t is not None or name in ("old_logp", "advantages"):
+            _dense(t, name, dev, torch.float32, shape)
+    loss = torch.empty((), dtype=torch.float32, device=dev)
+    logp = torch.empty(shape, dtype=torch.float32, device=dev)
+    gs = 0
+    if grad:
+        if dlogits is None:
+            dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+        gs = _rows(dlogits, "dlogits", dev, logits.dtype, logits.shape)
+    elif dlogits is not None:
+        raise ValueError("dlogits is given but grad is False")
+    n = actions.numel()
+    p = _PolicyParams(clip[0], clip[1], kl_coef, temperature, grad_scale)
+    workspace, nbytes = _workspace(workspace, _size("ccq_policy_loss_workspace_size", -1, n), dev)
+    _check(_library().ccq_policy_loss(
+        logits.data_ptr(), _dtype_code(logits), ls, actions.data_ptr(), id_bytes, old_logp.data_ptr(), _ptr(ref_logp),
+        advantages.data_ptr(), _ptr(weights), n, vocab, ctypes.byref(p), loss.data_ptr(), logp.data_ptr(),
+        _ptr(dlogits), gs, workspace.data_ptr(), nbytes, _stream(dev, stream)))
+    return {"loss": loss, "logp": logp, "dlogits": dlogits} if grad else {"loss": loss, "logp": logp}
+
+
+def token_logp(logits, actions, *, temperature: float = 1.0, out=None, stream=None):
+    """``log_softmax(logits / temperature)`` at the actions (ccq_token_logp), fp32 [...]: the old and reference
+    log-probabilities of a policy loss."""
+    dev, ls, id_bytes = _tokens(logits, actions)
+    if out is None:
+        out = torch.empty(actions.shape, dtype=torch.float32, device=dev)
+    _dense(out, "out", dev, torch.float32, actions.shape)
+    _check(_library().ccq_token_logp(logits.data_ptr(), _dtype_code(logits), ls, actions.data_ptr(), id_bytes,
+                                     actions.numel(), logits.shape[-1], temperature, out.data_ptr(),
+                                     _stream(dev, stream)))
+    return out
+
+
+# ---------------------------------------------------------------- AdamW
+
+
+@dataclass
+class AdamWState:
+    """Moments of a list of parameters: m and v as fp32 tensors, or as float8_e4m3fn tensors that hold m and the
+    square root of v over ``scale`` (fp32 [blocks, 2] per parameter, one row for ADAMW_BLOCK consecutive elements);
+    ``master`` the fp32 copies of bf16 parameters (None: none)."""
+    m: List[torch.Tensor]
+    v: List[torch.Tensor]
+    scale: Optional[List[torch.Tensor]] = None
+    master: Optional[List[torch.Tensor]] = None
+
+
+def adamw_state(params, *, bits: int = 32, master: bool = False) -> AdamWState:
+    """Zero moments for ``params`` (in 32 or 8 bits), and fp32 master copies of them where asked for."""
+    if bits not in (8, 32):
+        raise ValueError(f"bits={bits}: 8 or 32")
+    dtype = torch.float32 if bits == 32 else torch.float8_e4m3fn
+
+    def zeros(p):
+        return torch.zeros(p.shape, dtype=torch.float32 if bits == 32 else torch.uint8, device=p.device).view(dtype)
+
+    scale = None
+    if bits == 8:
+        scale = [torch.full((-(-p.numel() // ADAMW_BLOCK), 2), 2.0 ** -100, device=p.device) for p in params]
+    return AdamWState([zeros(p) for p in params], [zeros(p) for p in params], scale,
+                      [p.detach().float().clone() for p in params] if master else None)
+
+
+def _adamw_list(ts, name, count, device, dtype, numels):
+    if len(ts) != count:
+        raise ValueError(f"{name} has {len(ts)} tensors for {count} parameters")
+    for i, (t, n) in enumerate(zip(ts, numels)):
+        if t.dtype != dtype:
+            raise TypeError(f"{name}[{i}] must be {dtype}, got {t.dtype}")
+        if t.numel() != n or not t.is_contiguous() or t.device != device:
+            raise ValueError(f"{name}[{i}] must be a contiguous tensor of {n} elements on {device}")
+    return [t.data_ptr() for t in ts]
+
+
+def adamw_step(params, grads, state: AdamWState, step: int, *, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
+               weight_decay: float = 0.01, grad_scale: Optional[torch.Tensor] = None, stream=None):
+    """One AdamW update of all ``params`` (ccq_adamw_step), in place, with the moments of ``state``; ``step`` counts
+    from 1.  params and grads: lists of contiguous bf16 or fp32 tensors (one type for all params, one for all
+    grads).  ``grad_scale``: a CUDA fp32 scalar that multiplies the gradients (as from clipping their norm)."""
+    if not params:
+        return
+    first = _cuda(params[0], "params[0]")
+    dev, count = first.device, len(params)
+    numels = [p.numel() for p in params]
+    columns = [_adamw_list(params, "params", count, dev, first.dtype, numels),
+               _adamw_list(grads, "grads", count, dev, grads[0].dtype if grads else None, numels)]
+    bits = 8 if state.scale is not None else 32
+    dtype = torch.float8_e4m3fn if bits == 8 else torch.float32
+    columns += [_adamw_list(state.m, "state.m", count, dev, dtype, numels),
+                _adamw_list(state.v, "state.v", count, dev, dtype, numels)]
+    columns.append(_adamw_list(state.scale, "state.scale", count, dev, torch.float32,
+                               [-(-n // ADAMW_BLOCK) * 2 for n in numels]) if bits == 8 else [0] * count)
+    columns.append(_adamw_list(state.master, "state.master", count, dev, torch.float32, numels)
+                   if state.master is not None else [0] * count)
+    columns.append(numels)
+    table = (_L * (7 * count))(*[x for row in zip(*columns) for x in row])
+    if grad_scale is not None:
+        _dense(grad_scale, "grad_scale", dev, torch.float32)
+        if grad_scale.numel() != 1:
+            raise ValueError("grad_scale must be a scalar")
+    p = _AdamWParams(lr, betas[0], betas[1], eps, weight_decay, step)
+    _check(_library().ccq_adamw_step(ctypes.addressof(table), count, _dtype_code(first), _dtype_code(grads[0]), bits,
+                                     ctypes.byref(p), _ptr(grad_scale), _stream(dev, stream)))
