@@ -8,6 +8,8 @@
 #include <stdint.h>
 #include <stdio.h>
 
+#include <atomic>
+
 #include "../../include/ccq_ops.h"
 #include "ccq_internal.h"
 #include "sm100_ptx.cuh"
@@ -60,6 +62,18 @@ inline int sm_count_now() {
         counts[dev] = n;
     }
     return counts[dev];
+}
+
+// Opts a kernel into `bytes` of dynamic shared memory, once for a kernel and device.
+template <auto Kernel> cudaError_t allow_shared(int bytes) {
+    static std::atomic<int> allowed[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64 && allowed[dev].load(std::memory_order_relaxed) >= bytes) return cudaSuccess;
+    e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev >= 0 && dev < 64) allowed[dev].store(bytes, std::memory_order_relaxed);
+    return e;
 }
 
 // ---------------------------------------------------------------- elements and accesses
@@ -134,6 +148,18 @@ template <int W = 0, typename T, int N> __device__ __forceinline__ void pack(con
         set_word<W>(p.raw, __float_as_uint(f[W]));
         if constexpr (W + 1 < N) pack<W + 1>(f, p);
     }
+}
+
+// A thread's own asynchronous copy of one access to shared memory (4, 8 or 16 bytes), not kept in L1 where it is 16.
+template <int B> __device__ __forceinline__ void copy_async(void *dst, const void *src) {
+    if constexpr (B == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_addr(dst)), "l"(src), "n"(B) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void copy_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
 }
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
