@@ -48,23 +48,29 @@ __device__ __forceinline__ Row row_of(const PolicyArgs &a, int64_t i, bool note)
     return r;
 }
 
+struct RowScalars {
+    int action;
+    int row;  // of a batch
+    float weight, adv, old, ref, chosen;  // chosen: the action's logit
+};
+
 // The row's loss and c of the gradient, from its log-probability.
-__device__ __forceinline__ float row_loss(const PolicyArgs &a, int64_t i, float weight, float logp, float &c) {
-    const float adv = a.advantages[i];
-    const float ratio = expf(logp - a.old_logp[i]);
+__device__ __forceinline__ float row_loss(const PolicyArgs &a, const RowScalars &r, float logp, float &c) {
+    const float adv = r.adv;
+    const float ratio = expf(logp - r.old);
     const float open = ratio * adv;
     const float held = fminf(fmaxf(ratio, 1.f - a.p.clip_low), 1.f + a.p.clip_high) * adv;
     // a ratio or advantage that is not a number stays one
     float loss = open <= held || !(held < open) ? -open : -held;
     float slope = open <= held || !(held < open) ? -open : 0.f;
     if (a.ref_logp && a.p.kl_coef != 0.f) {
-        const float d = a.ref_logp[i] - logp;
+        const float d = r.ref - logp;
         const float em1 = expm1f(d);
         loss += a.p.kl_coef * (em1 - d);
         slope -= a.p.kl_coef * em1;
     }
-    c = a.p.grad_scale * weight * slope / a.p.temperature;
-    return weight * loss;
+    c = a.p.grad_scale * r.weight * slope / a.p.temperature;
+    return r.weight * loss;
 }
 
 constexpr int kRowThreads = 512;
@@ -129,7 +135,12 @@ template <typename T, int N> __global__ void __launch_bounds__(kRowThreads) poli
             if (a.score) {
                 a.logp[i] = logp;
             } else {
-                a.row_loss[i] = row_loss(a, i, row.weight, logp, c);
+                RowScalars r = {};
+                r.weight = row.weight;
+                r.adv = a.advantages[i];
+                r.old = a.old_logp[i];
+                if (a.ref_logp) r.ref = a.ref_logp[i];
+                a.row_loss[i] = row_loss(a, r, logp, c);
                 if (a.logp) a.logp[i] = logp;
             }
             bc[0] = m;
@@ -157,6 +168,396 @@ template <typename T, int N> __global__ void __launch_bounds__(kRowThreads) poli
     }
 }
 
+// ---------------------------------------------------------------- rows in shared memory
+
+// A cluster of `cs` CTAs takes a row, each a slice of its 16-byte granules, in one of kBuffers buffers of shared
+// memory: while a row is computed, the next ones come in and the gradient of the one before, written over its
+// logits, goes out, both as bulk copies.  Each logit is read from memory once.  A row that starts or ends inside a
+// granule (an odd vocabulary) has those elements fetched one by one a row ahead, and what belongs to its neighbours
+// replaced by -inf; the gradient's first and last elements are stored one by one.
+constexpr int kBuffers = 3;
+constexpr int kBatch = 256;  // rows whose scalars are held at once
+constexpr int kMaxCluster = 16;
+constexpr size_t kMaxSlice = 74240;  // bytes of a buffer: three and the scalars fit an SM
+constexpr float kLowest = -3.402823466e38f;
+
+struct Staging {
+    int per;  // granules of a slice
+    int cs;
+    int64_t clusters;
+};
+
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ void store_peer(float2 *p, int cta, float2 v) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr(p)), "r"(cta));
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(r), "f"(v.x), "f"(v.y) : "memory");
+}
+
+// (maximum, sum) pairs of a warp's lanes to those of all of them.  A sum is scaled to the common maximum; equal maxima
+// keep theirs as it is.
+__device__ __forceinline__ void join_warp(float &m, float &z, float scale) {
+    float top = m;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    z *= fast_exp2((m - top) * scale);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(~0u, z, o);
+    m = top;
+}
+
+// The larger of each pair of packed bf16 values (numbers before NaN; a NaN shows in the sum).
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 r = __hmax2(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+template <typename T> __device__ __forceinline__ float granule_max(const uint4 &a, const uint4 &b) {
+    if constexpr (IsBf16<T>::value) {
+        const uint32_t m = max_bf16x2(max_bf16x2(max_bf16x2(a.x, a.y), max_bf16x2(a.z, a.w)),
+                                      max_bf16x2(max_bf16x2(b.x, b.y), max_bf16x2(b.z, b.w)));
+        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+    } else {
+        const float x = fmaxf(fmaxf(__uint_as_float(a.x), __uint_as_float(a.y)), fmaxf(__uint_as_float(a.z), __uint_as_float(a.w)));
+        const float y = fmaxf(fmaxf(__uint_as_float(b.x), __uint_as_float(b.y)), fmaxf(__uint_as_float(b.z), __uint_as_float(b.w)));
+        return fmaxf(x, y);
+    }
+}
+
+// A granule's values as pairs, exp2((x - m) scale).
+template <typename T> __device__ __forceinline__ void granule_exp(const uint4 &r, uint64_t minus_m, uint64_t scale, uint64_t *e) {
+    constexpr int kPairs = IsBf16<T>::value ? 4 : 2;
+    uint64_t x[kPairs];
+    if constexpr (IsBf16<T>::value) {
+        x[0] = f2_from_bf16x2(r.x);
+        x[1] = f2_from_bf16x2(r.y);
+        x[2] = f2_from_bf16x2(r.z);
+        x[3] = f2_from_bf16x2(r.w);
+    } else {
+        x[0] = f2_make(__uint_as_float(r.x), __uint_as_float(r.y));
+        x[1] = f2_make(__uint_as_float(r.z), __uint_as_float(r.w));
+    }
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+        const float2 d = f2_split(f2_mul(f2_add(x[i], minus_m), scale));
+        e[i] = f2_make(fast_exp2(d.x), fast_exp2(d.y));
+    }
+}
+
+template <typename T, int THREADS, int GRAD>
+__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) policy_staged_kernel(PolicyArgs a, Staging g) {
+    constexpr int N = 16 / static_cast<int>(sizeof(T));
+    constexpr int kPairs = N / 2;
+    constexpr int kWarps = THREADS / 32;
+    extern __shared__ __align__(128) uint8_t dyn[];  // [kBuffers][per] granules, then the batch's scalars
+    __shared__ uint64_t full[kBuffers];
+    __shared__ int give_up;
+    __shared__ float2 pairs[kWarps], peers[2][kMaxCluster];
+    __shared__ uint32_t live_bits[kBatch / 32];
+    RowScalars *list = reinterpret_cast<RowScalars *>(dyn + static_cast<size_t>(kBuffers) * g.per * 16);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = static_cast<int>(blockIdx.x % g.cs);
+    const int64_t cluster = blockIdx.x / g.cs;
+    if (tid == 0) {
+        for (int b = 0; b < kBuffers; ++b) mbar_init(&full[b], 1);
+        give_up = 0;
+        fence_barrier_init();
+    }
+    __syncthreads();
+    if (g.cs > 1) cluster_barrier();  // every CTA of the cluster runs before its shared memory is written
+    const T *logits = static_cast<const T *>(a.logits);
+    T *dlogits = static_cast<T *>(a.dlogits);
+    const int first = rank * g.per;  // this slice's first granule
+    uint32_t loads = 0, rows = 0;    // issued (thread 0's count), and computed
+
+    // Elements of row i before its first granule's start, and the granules it touches.
+    auto offset_of = [](const void *row) { return static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)); };
+    auto buffer = [&](uint32_t k) { return reinterpret_cast<uint4 *>(dyn) + static_cast<size_t>(k % kBuffers) * g.per; };
+    auto slice_end = [&](int granules) { return granules - first < g.per ? granules - first : g.per; };
+    // Thread 0: the whole granules of row i's slice into the next buffer.
+    auto load_row = [&](int64_t i) {
+        const T *row = logits + i * a.logits_stride;
+        const int off = offset_of(row), whole = (off + a.vocab) / N;
+        const int lo = first > 0 || off == 0 ? 0 : 1, hi = slice_end(whole);
+        const uint32_t b = loads % kBuffers;
+        if (hi > lo) {
+            mbar_arrive_expect_tx(&full[b], static_cast<uint32_t>(hi - lo) * 16);
+            bulk_load(buffer(loads) + lo, row - off + static_cast<int64_t>(first + lo) * N, static_cast<uint32_t>(hi - lo) * 16, &full[b]);
+        } else {
+            mbar_arrive(&full[b]);
+        }
+        ++loads;
+    };
+    // Warp 1's lanes: the elements of the granules that row i shares with its neighbours, -inf in the others' places.
+    // `cell` is where the value belongs in the row's buffer (-1: nowhere in this slice).
+    auto edge_of = [&](int64_t i, int &cell) {
+        const T *row = logits + i * a.logits_stride;
+        const int off = offset_of(row), granules = (off + a.vocab + N - 1) / N;
+        const int tail = (off + a.vocab) % N;
+        cell = -1;
+        T v = from_f32<T>(-INFINITY);
+        const int e = lane % N, side = lane / N;
+        if (warp != 1 || side > 1) return v;
+        int at = -1;  // granule
+        if (side == 0 && off) at = 0;
+        if (side == 1 && tail && !(granules == 1 && off)) at = granules - 1;
+        if (at < first || at >= first + slice_end(granules)) return v;
+        cell = (at - first) * N + e;
+        const int64_t c = static_cast<int64_t>(at) * N + e - off;
+        if (c >= 0 && c < a.vocab) v = row[c];
+        return v;
+    };
+
+    for (int64_t start = cluster; start < a.n; start += g.clusters * kBatch) {
+        // the batch's scalars, and which of its rows are not masked
+        RowScalars mine[(kBatch + THREADS - 1) / THREADS];
+#pragma unroll
+        for (int q = 0; q < (kBatch + THREADS - 1) / THREADS; ++q) {
+            const int k = q * THREADS + tid;
+            const int64_t i = start + k * g.clusters;
+            bool live = false;
+            if (k < kBatch && i < a.n) {
+                const Row r = row_of(a, i, rank == 0);
+                live = r.action >= 0;
+                mine[q].action = r.action;
+                mine[q].row = k;
+                mine[q].weight = r.weight;
+                if (live) {
+                    mine[q].chosen = to_f32(logits[i * a.logits_stride + r.action]);
+                    mine[q].adv = a.score ? 0.f : a.advantages[i];
+                    mine[q].old = a.score ? 0.f : a.old_logp[i];
+                    mine[q].ref = a.ref_logp ? a.ref_logp[i] : 0.f;
+                } else if (rank == 0) {
+                    if (a.logp) a.logp[i] = a.score ? __int_as_float(0x7fc00000) : 0.f;
+                    if (!a.score) a.row_loss[i] = 0.f;
+                }
+            }
+            const uint32_t bits = __ballot_sync(~0u, live);
+            if (lane == 0 && k < kBatch) live_bits[k >> 5] = bits;
+        }
+        __syncthreads();
+        int count = 0;
+#pragma unroll
+        for (int w = 0; w < kBatch / 32; ++w) count += __popc(live_bits[w]);
+#pragma unroll
+        for (int q = 0; q < (kBatch + THREADS - 1) / THREADS; ++q) {
+            const int k = q * THREADS + tid;
+            if (k >= kBatch || !((live_bits[k >> 5] >> (k & 31)) & 1)) continue;
+            int at = __popc(live_bits[k >> 5] & ((1u << (k & 31)) - 1));
+            for (int w = 0; w < (k >> 5); ++w) at += __popc(live_bits[w]);
+            list[at] = mine[q];
+        }
+        __syncthreads();
+        auto row_index = [&](int j) { return start + list[j].row * g.clusters; };
+        if (tid == 0)
+            for (int j = 0; j < kBuffers - 1 && j < count; ++j) load_row(row_index(j));
+        if (count > 0) {
+            int cell;
+            const T v = edge_of(row_index(0), cell);
+            if (cell >= 0) reinterpret_cast<T *>(buffer(rows))[cell] = v;
+        }
+        if constexpr (GRAD) {
+            // masked rows: zeros, while the first rows come in
+            const int here = static_cast<int>(a.n - start < g.clusters * kBatch ? (a.n - start + g.clusters - 1) / g.clusters : kBatch);
+            for (int k = 0; k < here; ++k) {
+                if ((live_bits[k >> 5] >> (k & 31)) & 1) continue;
+                T *row = dlogits + (start + k * g.clusters) * a.dlogits_stride;
+                const int off = offset_of(row), granules = (off + a.vocab + N - 1) / N;
+                for (int c = tid; c < slice_end(granules); c += THREADS) {
+                    const int64_t e = static_cast<int64_t>(first + c) * N - off;
+                    if (e >= 0 && e + N <= a.vocab) {
+                        __stcs(reinterpret_cast<uint4 *>(row + e), make_uint4(0, 0, 0, 0));
+                    } else {
+                        for (int q = 0; q < N; ++q)
+                            if (e + q >= 0 && e + q < a.vocab) row[e + q] = from_f32<T>(0.f);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        for (int j = 0; j < count; ++j, ++rows) {
+            const RowScalars sc = list[j];
+            const int64_t i = start + sc.row * g.clusters;
+            const T *row = logits + i * a.logits_stride;
+            const int off = offset_of(row), granules = (off + a.vocab + N - 1) / N, mygran = slice_end(granules);
+            uint4 *buf = buffer(rows);
+            int edge_cell = -1;
+            T edge = from_f32<T>(0.f);
+            if (j + 1 < count) edge = edge_of(row_index(j + 1), edge_cell);
+            mbar_wait(&full[rows % kBuffers], (rows / kBuffers) & 1, &give_up, a.status);
+            // maximum and sum of this thread's values, two granules a step
+            float m = kLowest, z = 0.f;
+            {
+                constexpr uint32_t low = IsBf16<T>::value ? 0xff80ff80u : 0xff800000u;  // -inf
+                const uint64_t scale = f2_make(a.scale, a.scale);
+                uint64_t s0 = 0, s1 = 0;
+                for (int c = tid; c < mygran; c += 2 * THREADS) {
+                    const uint4 u = buf[c];
+                    uint4 v = make_uint4(low, low, low, low);
+                    if (c + THREADS < mygran) v = buf[c + THREADS];
+                    const float top = fmaxf(m, granule_max<T>(u, v));
+                    const float keep = fast_exp2((m - top) * a.scale);
+                    m = top;
+                    s0 = f2_mul(s0, f2_make(keep, keep));
+                    s1 = f2_mul(s1, f2_make(keep, keep));
+                    uint64_t e[kPairs];
+                    granule_exp<T>(u, f2_make(-m, -m), scale, e);
+#pragma unroll
+                    for (int q = 0; q < kPairs; ++q) s0 = f2_add(s0, e[q]);
+                    granule_exp<T>(v, f2_make(-m, -m), scale, e);
+#pragma unroll
+                    for (int q = 0; q < kPairs; ++q) s1 = f2_add(s1, e[q]);
+                }
+                const float2 t = f2_split(f2_add(s0, s1));
+                z = t.x + t.y;
+            }
+            join_warp(m, z, a.scale);
+            if (lane == 0) pairs[warp] = make_float2(m, z);
+            __syncthreads();
+            const bool alone = g.cs == 1;
+            if (alone || warp == 0) {
+                const float2 p = lane < kWarps ? pairs[lane] : make_float2(kLowest, 0.f);
+                m = p.x;
+                z = p.y;
+                join_warp(m, z, a.scale);
+            }
+            if (!alone) {
+                if (warp == 0 && lane < g.cs) store_peer(&peers[rows & 1][rank], lane, make_float2(m, z));
+                cluster_barrier();
+                const float2 p = lane < g.cs ? peers[rows & 1][lane] : make_float2(kLowest, 0.f);
+                m = p.x;
+                z = p.y;
+                join_warp(m, z, a.scale);
+            }
+            const float logp = (sc.chosen - m) * (a.scale * kLn2) - logf(z);
+            float c1 = 0.f, loss = 0.f;
+            if (!a.score) loss = row_loss(a, sc, logp, c1);
+            if (rank == 0 && tid == 0) {
+                if (a.logp) a.logp[i] = logp;
+                if (!a.score) a.row_loss[i] = loss;
+            }
+            if constexpr (GRAD) {
+                T *drow = dlogits + i * a.dlogits_stride;
+                const bool direct = offset_of(drow) != off;  // the two rows lie differently over their granules
+                const float c2 = -c1 / z;
+                const uint64_t scale = f2_make(a.scale, a.scale), minus_m = f2_make(-m, -m), mul = f2_make(c2, c2);
+                const int chosen = sc.action + off - first * N;  // the action's element of the slice
+                for (int c = tid; c < mygran; c += THREADS) {
+                    uint64_t e[kPairs];
+                    granule_exp<T>(buf[c], minus_m, scale, e);
+#pragma unroll
+                    for (int q = 0; q < kPairs; ++q) e[q] = f2_mul(e[q], mul);
+                    if (chosen >= c * N && chosen < c * N + N) {
+#pragma unroll
+                        for (int q = 0; q < kPairs; ++q) {
+                            const float2 t = f2_split(e[q]);
+                            e[q] = f2_make(t.x + (chosen == c * N + 2 * q ? c1 : 0.f), t.y + (chosen == c * N + 2 * q + 1 ? c1 : 0.f));
+                        }
+                    }
+                    const int64_t el = static_cast<int64_t>(first + c) * N - off;  // the granule's first element of the row
+                    const bool inside = el >= 0 && el + N <= a.vocab;
+                    if (inside && !direct) {
+                        uint4 o;
+                        if constexpr (IsBf16<T>::value) {
+                            o = make_uint4(bf16x2_from_f2(e[0]), bf16x2_from_f2(e[1]), bf16x2_from_f2(e[2]), bf16x2_from_f2(e[3]));
+                        } else {
+                            const float2 x = f2_split(e[0]), y = f2_split(e[1]);
+                            o = make_uint4(__float_as_uint(x.x), __float_as_uint(x.y), __float_as_uint(y.x), __float_as_uint(y.y));
+                        }
+                        buf[c] = o;
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < N; ++q) {
+                            const float2 t = f2_split(e[q / 2]);
+                            if (el + q >= 0 && el + q < a.vocab) drow[el + q] = from_f32<T>(q % 2 ? t.y : t.x);
+                        }
+                    }
+                }
+                fence_proxy_async_smem();
+            }
+            if (edge_cell >= 0) reinterpret_cast<T *>(buffer(rows + 1))[edge_cell] = edge;
+            __syncthreads();
+            if (tid == 0) {
+                if constexpr (GRAD) {
+                    T *drow = dlogits + i * a.dlogits_stride;
+                    if (offset_of(drow) == off) {
+                        const int whole = (off + a.vocab) / N, lo = first > 0 || off == 0 ? 0 : 1, hi = slice_end(whole);
+                        if (hi > lo) bulk_store(drow - off + static_cast<int64_t>(first + lo) * N, buf + lo, static_cast<uint32_t>(hi - lo) * 16);
+                    }
+                    tma_store_commit();
+                    tma_store_wait_read_but<1>();  // the row before has left its buffer
+                }
+                if (j + kBuffers - 1 < count) load_row(row_index(j + kBuffers - 1));
+            }
+        }
+        __syncthreads();  // the batch's scalars may go
+    }
+    if constexpr (GRAD) {
+        if (tid == 0) tma_store_wait_all();
+    }
+}
+
+struct StagePlan {
+    int threads, cs, per;
+    size_t smem;
+};
+
+// How rows are spread: the fewest CTAs a row whose slices fit three to an SM, and with few rows as many as there are
+// SMs for (slices of 8 KB at least).  False where even 16 CTAs do not hold a row: those are read twice.
+bool stage_plan(const PolicyArgs &a, int es, StagePlan *p) {
+    const int n = 16 / es;
+    const int64_t granules = (static_cast<int64_t>(a.vocab) + 2 * (n - 1)) / n + 1;
+    int cs = 1;
+    auto per = [&](int c) { return (granules + c - 1) / c; };
+    while (per(cs) * 16 > static_cast<int64_t>(kMaxSlice)) {
+        if (cs == kMaxCluster) return false;
+        cs *= 2;
+    }
+    while (cs < 8 && a.n * cs * 2 <= sm_count_now() && per(cs) * 16 >= 16384) cs *= 2;
+    p->cs = cs;
+    p->per = static_cast<int>(per(cs));
+    p->threads = p->per <= 512 ? 128 : p->per <= 1536 ? 256 : 512;
+    p->smem = static_cast<size_t>(kBuffers) * p->per * 16 + kBatch * sizeof(RowScalars);
+    return true;
+}
+
+template <typename T, int THREADS, int GRAD> cudaError_t launch_staged(const PolicyArgs &a, const StagePlan &p, cudaStream_t s) {
+    constexpr auto kernel = policy_staged_kernel<T, THREADS, GRAD>;
+    cudaError_t e = allow_shared<kernel>(232448 - 2048);
+    if (e != cudaSuccess) return e;
+    if (p.cs > 8 && (e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = p.smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = p.cs;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3(p.cs);
+    int clusters = 0;
+    if (p.cs > 1) {
+        if ((e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg)) != cudaSuccess) return e;
+    } else {
+        if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&clusters, kernel, THREADS, p.smem)) != cudaSuccess) return e;
+        clusters *= sm_count_now();
+    }
+    Staging g;
+    g.per = p.per;
+    g.cs = p.cs;
+    g.clusters = std::min<int64_t>(a.n, std::max(1, clusters));
+    cfg.gridDim = dim3(static_cast<unsigned>(g.clusters * p.cs));
+    return cudaLaunchKernelEx(&cfg, kernel, a, g);
+}
+
+template <typename T, int GRAD> cudaError_t launch_staged_threads(const PolicyArgs &a, const StagePlan &p, cudaStream_t s) {
+    return p.threads == 128 ? launch_staged<T, 128, GRAD>(a, p, s) : p.threads == 256 ? launch_staged<T, 256, GRAD>(a, p, s)
+                                                                                     : launch_staged<T, 512, GRAD>(a, p, s);
+}
+
 // loss = the rows' losses, by 1024 strided sums and a tree: an order that depends on n alone.
 constexpr int kLossThreads = 1024;
 __global__ void __launch_bounds__(kLossThreads) policy_loss_kernel(const float *row_loss, int64_t n, float *loss) {
@@ -181,6 +582,12 @@ template <typename T, int N> cudaError_t launch_rows(const PolicyArgs &a, cudaSt
 
 cudaError_t launch_policy(const PolicyArgs &a, ccq_dtype dtype, cudaStream_t s) {
     const int es = dtype_bytes(dtype);
+    StagePlan plan;
+    if (stage_plan(a, es, &plan)) {
+        if (dtype == CCQ_BF16)
+            return a.dlogits ? launch_staged_threads<__nv_bfloat16, 1>(a, plan, s) : launch_staged_threads<__nv_bfloat16, 0>(a, plan, s);
+        return a.dlogits ? launch_staged_threads<float, 1>(a, plan, s) : launch_staged_threads<float, 0>(a, plan, s);
+    }
     int b = access_bytes(static_cast<uintptr_t>(a.vocab) * es);
     b = row_access(a.logits, a.logits_stride, es, a.n, b);
     if (a.dlogits) b = row_access(a.dlogits, a.dlogits_stride, es, a.n, b);
