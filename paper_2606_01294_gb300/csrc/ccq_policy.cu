@@ -178,7 +178,8 @@ template <typename T, int N> __global__ void __launch_bounds__(kRowThreads) poli
 constexpr int kBuffers = 3;
 constexpr int kBatch = 256;  // rows whose scalars are held at once
 constexpr int kMaxCluster = 16;
-constexpr size_t kMaxSlice = 74240;  // bytes of a buffer: three and the scalars fit an SM
+constexpr int kGranules = 8;  // of a thread: their exponentials stay in registers until the row's sum is known
+constexpr size_t kMaxSlice = 512 * kGranules * 16;  // bytes of a buffer: three and the scalars fit an SM
 constexpr float kLowest = -3.402823466e38f;
 
 struct Staging {
@@ -213,15 +214,20 @@ __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
     const __nv_bfloat162 r = __hmax2(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b));
     return *reinterpret_cast<const uint32_t *>(&r);
 }
-template <typename T> __device__ __forceinline__ float granule_max(const uint4 &a, const uint4 &b) {
+// The largest of a thread's granules.
+template <typename T> __device__ __forceinline__ float granules_max(const uint4 (&r)[kGranules]) {
     if constexpr (IsBf16<T>::value) {
-        const uint32_t m = max_bf16x2(max_bf16x2(max_bf16x2(a.x, a.y), max_bf16x2(a.z, a.w)),
-                                      max_bf16x2(max_bf16x2(b.x, b.y), max_bf16x2(b.z, b.w)));
+        uint32_t m = r[0].x;
+#pragma unroll
+        for (int q = 0; q < kGranules; ++q) m = max_bf16x2(m, max_bf16x2(max_bf16x2(r[q].x, r[q].y), max_bf16x2(r[q].z, r[q].w)));
         return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
     } else {
-        const float x = fmaxf(fmaxf(__uint_as_float(a.x), __uint_as_float(a.y)), fmaxf(__uint_as_float(a.z), __uint_as_float(a.w)));
-        const float y = fmaxf(fmaxf(__uint_as_float(b.x), __uint_as_float(b.y)), fmaxf(__uint_as_float(b.z), __uint_as_float(b.w)));
-        return fmaxf(x, y);
+        float m = kLowest;
+#pragma unroll
+        for (int q = 0; q < kGranules; ++q)
+            m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(r[q].x), __uint_as_float(r[q].y)),
+                               fmaxf(__uint_as_float(r[q].z), __uint_as_float(r[q].w))));
+        return m;
     }
 }
 
@@ -246,7 +252,7 @@ template <typename T> __device__ __forceinline__ void granule_exp(const uint4 &r
 }
 
 template <typename T, int THREADS, int GRAD>
-__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) policy_staged_kernel(PolicyArgs a, Staging g) {
+__global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(PolicyArgs a, Staging g) {
     constexpr int N = 16 / static_cast<int>(sizeof(T));
     constexpr int kPairs = N / 2;
     constexpr int kWarps = THREADS / 32;
@@ -386,32 +392,30 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
             T edge = from_f32<T>(0.f);
             if (j + 1 < count) edge = edge_of(row_index(j + 1), edge_cell);
             mbar_wait(&full[rows % kBuffers], (rows / kBuffers) & 1, &give_up, a.status);
-            // maximum and sum of this thread's values, two granules a step
-            float m = kLowest, z = 0.f;
+            // this thread's exponentials, against its own maximum, and their sum
+            constexpr uint32_t low = IsBf16<T>::value ? 0xff80ff80u : 0xff800000u;  // -inf
+            const uint64_t scale = f2_make(a.scale, a.scale);
+            uint64_t e[kGranules][kPairs];
+            float m, z;
             {
-                constexpr uint32_t low = IsBf16<T>::value ? 0xff80ff80u : 0xff800000u;  // -inf
-                const uint64_t scale = f2_make(a.scale, a.scale);
-                uint64_t s0 = 0, s1 = 0;
-                for (int c = tid; c < mygran; c += 2 * THREADS) {
-                    const uint4 u = buf[c];
-                    uint4 v = make_uint4(low, low, low, low);
-                    if (c + THREADS < mygran) v = buf[c + THREADS];
-                    const float top = fmaxf(m, granule_max<T>(u, v));
-                    const float keep = fast_exp2((m - top) * a.scale);
-                    m = top;
-                    s0 = f2_mul(s0, f2_make(keep, keep));
-                    s1 = f2_mul(s1, f2_make(keep, keep));
-                    uint64_t e[kPairs];
-                    granule_exp<T>(u, f2_make(-m, -m), scale, e);
+                uint4 r[kGranules];
 #pragma unroll
-                    for (int q = 0; q < kPairs; ++q) s0 = f2_add(s0, e[q]);
-                    granule_exp<T>(v, f2_make(-m, -m), scale, e);
-#pragma unroll
-                    for (int q = 0; q < kPairs; ++q) s1 = f2_add(s1, e[q]);
+                for (int q = 0; q < kGranules; ++q) {
+                    r[q] = make_uint4(low, low, low, low);
+                    if (q * THREADS + tid < mygran) r[q] = buf[q * THREADS + tid];
                 }
-                const float2 t = f2_split(f2_add(s0, s1));
+                m = fmaxf(granules_max<T>(r), kLowest);
+                uint64_t sum[2] = {0, 0};
+#pragma unroll
+                for (int q = 0; q < kGranules; ++q) {
+                    granule_exp<T>(r[q], f2_make(-m, -m), scale, e[q]);
+#pragma unroll
+                    for (int k = 0; k < kPairs; ++k) sum[k & 1] = f2_add(sum[k & 1], e[q][k]);
+                }
+                const float2 t = f2_split(f2_add(sum[0], sum[1]));
                 z = t.x + t.y;
             }
+            const float own = m;
             join_warp(m, z, a.scale);
             if (lane == 0) pairs[warp] = make_float2(m, z);
             __syncthreads();
@@ -440,39 +444,40 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
             if constexpr (GRAD) {
                 T *drow = dlogits + i * a.dlogits_stride;
                 const bool direct = offset_of(drow) != off;  // the two rows lie differently over their granules
-                const float c2 = -c1 / z;
-                const uint64_t scale = f2_make(a.scale, a.scale), minus_m = f2_make(-m, -m), mul = f2_make(c2, c2);
-                const int chosen = sc.action + off - first * N;  // the action's element of the slice
-                for (int c = tid; c < mygran; c += THREADS) {
-                    uint64_t e[kPairs];
-                    granule_exp<T>(buf[c], minus_m, scale, e);
+                const float c2 = -c1 / z, mine2 = c2 * fast_exp2((own - m) * a.scale);
+                const uint64_t mul = f2_make(mine2, mine2);
+                // local granules that are stored element by element: those shared with the neighbours, or all
+                const int head = first == 0 && off ? 0 : -1, tail = (off + a.vocab) % N ? granules - 1 - first : -1;
 #pragma unroll
-                    for (int q = 0; q < kPairs; ++q) e[q] = f2_mul(e[q], mul);
-                    if (chosen >= c * N && chosen < c * N + N) {
+                for (int q = 0; q < kGranules; ++q) {
+                    const int c = q * THREADS + tid;
+                    if (c >= mygran) continue;
 #pragma unroll
-                        for (int q = 0; q < kPairs; ++q) {
-                            const float2 t = f2_split(e[q]);
-                            e[q] = f2_make(t.x + (chosen == c * N + 2 * q ? c1 : 0.f), t.y + (chosen == c * N + 2 * q + 1 ? c1 : 0.f));
-                        }
-                    }
-                    const int64_t el = static_cast<int64_t>(first + c) * N - off;  // the granule's first element of the row
-                    const bool inside = el >= 0 && el + N <= a.vocab;
-                    if (inside && !direct) {
+                    for (int k = 0; k < kPairs; ++k) e[q][k] = f2_mul(e[q][k], mul);
+                    if (c != head && c != tail && !direct) {
                         uint4 o;
                         if constexpr (IsBf16<T>::value) {
-                            o = make_uint4(bf16x2_from_f2(e[0]), bf16x2_from_f2(e[1]), bf16x2_from_f2(e[2]), bf16x2_from_f2(e[3]));
+                            o = make_uint4(bf16x2_from_f2(e[q][0]), bf16x2_from_f2(e[q][1]), bf16x2_from_f2(e[q][2]), bf16x2_from_f2(e[q][3]));
                         } else {
-                            const float2 x = f2_split(e[0]), y = f2_split(e[1]);
+                            const float2 x = f2_split(e[q][0]), y = f2_split(e[q][1]);
                             o = make_uint4(__float_as_uint(x.x), __float_as_uint(x.y), __float_as_uint(y.x), __float_as_uint(y.y));
                         }
                         buf[c] = o;
                     } else {
+                        const int64_t el = static_cast<int64_t>(first + c) * N - off;
 #pragma unroll
-                        for (int q = 0; q < N; ++q) {
-                            const float2 t = f2_split(e[q / 2]);
-                            if (el + q >= 0 && el + q < a.vocab) drow[el + q] = from_f32<T>(q % 2 ? t.y : t.x);
+                        for (int k = 0; k < N; ++k) {
+                            const float2 t = f2_split(e[q][k / 2]);
+                            if (el + k >= 0 && el + k < a.vocab) drow[el + k] = from_f32<T>(k % 2 ? t.y : t.x);
                         }
                     }
+                }
+                // the action's element, by the thread that has just stored its granule
+                const int at = sc.action + off - first * N, c = at / N;
+                if (at >= 0 && c < mygran && c % THREADS == tid) {
+                    const T v = from_f32<T>(c1 + c2 * fast_exp2((sc.chosen - m) * a.scale));
+                    if (c != head && c != tail && !direct) reinterpret_cast<T *>(buf)[at] = v;
+                    else drow[sc.action] = v;
                 }
                 fence_proxy_async_smem();
             }
@@ -517,7 +522,7 @@ bool stage_plan(const PolicyArgs &a, int es, StagePlan *p) {
     while (cs < 8 && a.n * cs * 2 <= sm_count_now() && per(cs) * 16 >= 16384) cs *= 2;
     p->cs = cs;
     p->per = static_cast<int>(per(cs));
-    p->threads = p->per <= 512 ? 128 : p->per <= 1536 ? 256 : 512;
+    p->threads = p->per <= 128 * kGranules ? 128 : p->per <= 256 * kGranules ? 256 : 512;
     p->smem = static_cast<size_t>(kBuffers) * p->per * 16 + kBatch * sizeof(RowScalars);
     return true;
 }
