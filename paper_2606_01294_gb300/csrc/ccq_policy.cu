@@ -54,6 +54,13 @@ struct RowScalars {
     float weight, adv, old, ref, chosen;  // chosen: the action's logit
 };
 
+// Whether the row is not masked; its weight and action are read together.
+__device__ __forceinline__ bool is_live(const PolicyArgs &a, int64_t i) {
+    const float w = a.weights ? a.weights[i] : 1.f;
+    const int64_t t = load_index(a.actions, a.id_bytes, i);
+    return w != 0.f && t >= 0 && t < a.vocab;
+}
+
 // The row's loss and c of the gradient, from its log-probability.
 __device__ __forceinline__ float row_loss(const PolicyArgs &a, const RowScalars &r, float logp, float &c) {
     const float adv = r.adv;
@@ -178,6 +185,7 @@ template <typename T, int N> __global__ void __launch_bounds__(kRowThreads) poli
 constexpr int kBuffers = 3;
 constexpr int kBatch = 256;  // rows whose scalars are held at once
 constexpr int kMaxCluster = 16;
+constexpr int kRanked = 16384;
 constexpr int kGranules = 8;  // of a thread: their exponentials stay in registers until the row's sum is known
 constexpr size_t kMaxSlice = 512 * kGranules * 16;  // bytes of a buffer: three and the scalars fit an SM
 constexpr float kLowest = -3.402823466e38f;
@@ -185,7 +193,9 @@ constexpr float kLowest = -3.402823466e38f;
 struct Staging {
     int per;  // granules of a slice
     int cs;
+    int ranked;  // rows are dealt out by their rank among the live ones
     int64_t clusters;
+    int64_t span;  // rows dealt out at a time, at most kBatch to a cluster
 };
 
 __device__ __forceinline__ void cluster_barrier() {
@@ -260,7 +270,9 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
     __shared__ uint64_t full[kBuffers];
     __shared__ int give_up;
     __shared__ float2 pairs[kWarps], peers[2][kMaxCluster];
-    __shared__ uint32_t live_bits[kBatch / 32];
+    __shared__ uint32_t live_bits[kBatch / 32], dead_bits[kBatch / 32];
+    __shared__ int live_rows[kBatch], dead_rows[kBatch], counts[2], warp_live[kWarps];
+    __shared__ uint32_t row_bits[kRanked / 32];
     RowScalars *list = reinterpret_cast<RowScalars *>(dyn + static_cast<size_t>(kBuffers) * g.per * 16);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = static_cast<int>(blockIdx.x % g.cs);
@@ -315,47 +327,118 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
         return v;
     };
 
-    for (int64_t start = cluster; start < a.n; start += g.clusters * kBatch) {
-        // the batch's scalars, and which of its rows are not masked
-        RowScalars mine[(kBatch + THREADS - 1) / THREADS];
+    for (int64_t start = 0; start < a.n; start += g.span) {
+        // this cluster's rows of the span: `live` ones to compute and `dead` (masked) ones to zero
+        const int64_t span = a.n - start < g.span ? a.n - start : g.span;
+        if (tid < 2) counts[tid] = 0;
+        __syncthreads();
+        if (g.ranked) {
+            // a bit for each row of the span, the live rows before each word of them, then every cluster takes each
+            // clusters-th of the live rows, and of the dead
+            const int words = static_cast<int>((span + 31) / 32);
+            for (int w = warp; w < words; w += kWarps * 4) {
+                bool live[4];
 #pragma unroll
-        for (int q = 0; q < (kBatch + THREADS - 1) / THREADS; ++q) {
-            const int k = q * THREADS + tid;
-            const int64_t i = start + k * g.clusters;
-            bool live = false;
-            if (k < kBatch && i < a.n) {
-                const Row r = row_of(a, i, rank == 0);
-                live = r.action >= 0;
-                mine[q].action = r.action;
-                mine[q].row = k;
-                mine[q].weight = r.weight;
-                if (live) {
-                    mine[q].chosen = to_f32(logits[i * a.logits_stride + r.action]);
-                    mine[q].adv = a.score ? 0.f : a.advantages[i];
-                    mine[q].old = a.score ? 0.f : a.old_logp[i];
-                    mine[q].ref = a.ref_logp ? a.ref_logp[i] : 0.f;
-                } else if (rank == 0) {
-                    if (a.logp) a.logp[i] = a.score ? __int_as_float(0x7fc00000) : 0.f;
-                    if (!a.score) a.row_loss[i] = 0.f;
+                for (int q = 0; q < 4; ++q) {
+                    const int64_t k = static_cast<int64_t>(w + q * kWarps) * 32 + lane;
+                    live[q] = k < span && is_live(a, start + k);
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t bits = __ballot_sync(~0u, live[q]);
+                    if (lane == 0 && w + q * kWarps < words) row_bits[w + q * kWarps] = bits;
                 }
             }
-            const uint32_t bits = __ballot_sync(~0u, live);
-            if (lane == 0 && k < kBatch) live_bits[k >> 5] = bits;
+            __syncthreads();
+            constexpr int kEach = (kRanked / 32 + THREADS - 1) / THREADS;  // words of a thread
+            int alive = 0;
+#pragma unroll
+            for (int q = 0; q < kEach; ++q)
+                if (tid * kEach + q < words) alive += __popc(row_bits[tid * kEach + q]);
+            int before = alive;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int t = __shfl_up_sync(~0u, before, o);
+                if (lane >= o) before += t;
+            }
+            if (lane == 31) warp_live[warp] = before;
+            __syncthreads();
+            before -= alive;
+            int all = 0;
+            for (int w = 0; w < kWarps; ++w) {
+                if (w < warp) before += warp_live[w];
+                all += warp_live[w];
+            }
+            const int c = static_cast<int>(cluster), cs = static_cast<int>(g.clusters);
+            for (int q = 0; q < kEach; ++q) {
+                const int w = tid * kEach + q;
+                if (w >= words) break;
+                const uint32_t bits = row_bits[w];
+                const int here = span - w * 32 < 32 ? static_cast<int>(span) - w * 32 : 32;
+                // the first live row at or after `before`, and the first dead one, that are this cluster's
+                for (int r = before + (c - before % cs + cs) % cs; r < before + __popc(bits); r += cs)
+                    live_rows[r / cs] = w * 32 + __fns(bits, 0, r - before + 1);
+                const int gone = w * 32 - before;
+                const uint32_t none = ~bits & (here < 32 ? (1u << here) - 1 : ~0u);
+                for (int r = gone + (c - gone % cs + cs) % cs; r < gone + __popc(none); r += cs)
+                    dead_rows[r / cs] = w * 32 + __fns(none, 0, r - gone + 1);
+                before += __popc(bits);
+            }
+            if (tid == 0) {
+                counts[0] = all > c ? (all - c + cs - 1) / cs : 0;
+                counts[1] = static_cast<int>(span) - all > c ? (static_cast<int>(span) - all - c + cs - 1) / cs : 0;
+            }
+        } else {
+            // every clusters-th row
+            for (int q = 0; q < kBatch; q += THREADS) {
+                const int k = q + tid;
+                const int64_t at = cluster + k * g.clusters;
+                const bool here = k < kBatch && at < span, live = here && is_live(a, start + at);
+                const uint32_t l = __ballot_sync(~0u, live), d = __ballot_sync(~0u, here && !live);
+                if (lane == 0 && k < kBatch) {
+                    live_bits[k >> 5] = l;
+                    dead_bits[k >> 5] = d;
+                }
+            }
+            __syncthreads();
+            for (int k = tid; k < kBatch; k += THREADS) {
+                const int w = k >> 5, bit = k & 31;
+                const bool live = (live_bits[w] >> bit) & 1;
+                if (!live && !((dead_bits[w] >> bit) & 1)) continue;
+                const uint32_t *bits = live ? live_bits : dead_bits;
+                int at = __popc(bits[w] & ((1u << bit) - 1));
+                for (int v = 0; v < w; ++v) at += __popc(bits[v]);
+                (live ? live_rows : dead_rows)[at] = static_cast<int>(cluster + k * g.clusters);
+            }
+            if (tid < 2) {
+                int all = 0;
+                for (int v = 0; v < kBatch / 32; ++v) all += __popc(tid ? dead_bits[v] : live_bits[v]);
+                counts[tid] = all;
+            }
         }
         __syncthreads();
-        int count = 0;
-#pragma unroll
-        for (int w = 0; w < kBatch / 32; ++w) count += __popc(live_bits[w]);
-#pragma unroll
-        for (int q = 0; q < (kBatch + THREADS - 1) / THREADS; ++q) {
-            const int k = q * THREADS + tid;
-            if (k >= kBatch || !((live_bits[k >> 5] >> (k & 31)) & 1)) continue;
-            int at = __popc(live_bits[k >> 5] & ((1u << (k & 31)) - 1));
-            for (int w = 0; w < (k >> 5); ++w) at += __popc(live_bits[w]);
-            list[at] = mine[q];
+        const int count = counts[0], dead = counts[1];
+        for (int k = tid; k < count; k += THREADS) {
+            const int64_t i = start + live_rows[k];
+            const Row r = row_of(a, i, false);
+            RowScalars sc;
+            sc.action = r.action;
+            sc.row = live_rows[k];
+            sc.weight = r.weight;
+            sc.chosen = to_f32(logits[i * a.logits_stride + r.action]);
+            sc.adv = a.score ? 0.f : a.advantages[i];
+            sc.old = a.score ? 0.f : a.old_logp[i];
+            sc.ref = a.ref_logp ? a.ref_logp[i] : 0.f;
+            list[k] = sc;
+        }
+        for (int k = tid; k < dead && rank == 0; k += THREADS) {
+            const int64_t i = start + dead_rows[k];
+            row_of(a, i, true);
+            if (a.logp) a.logp[i] = a.score ? __int_as_float(0x7fc00000) : 0.f;
+            if (!a.score) a.row_loss[i] = 0.f;
         }
         __syncthreads();
-        auto row_index = [&](int j) { return start + list[j].row * g.clusters; };
+        auto row_index = [&](int j) { return start + list[j].row; };
         if (tid == 0)
             for (int j = 0; j < kBuffers - 1 && j < count; ++j) load_row(row_index(j));
         if (count > 0) {
@@ -365,10 +448,8 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
         }
         if constexpr (GRAD) {
             // masked rows: zeros, while the first rows come in
-            const int here = static_cast<int>(a.n - start < g.clusters * kBatch ? (a.n - start + g.clusters - 1) / g.clusters : kBatch);
-            for (int k = 0; k < here; ++k) {
-                if ((live_bits[k >> 5] >> (k & 31)) & 1) continue;
-                T *row = dlogits + (start + k * g.clusters) * a.dlogits_stride;
+            for (int k = 0; k < dead; ++k) {
+                T *row = dlogits + (start + dead_rows[k]) * a.dlogits_stride;
                 const int off = offset_of(row), granules = (off + a.vocab + N - 1) / N;
                 for (int c = tid; c < slice_end(granules); c += THREADS) {
                     const int64_t e = static_cast<int64_t>(first + c) * N - off;
@@ -384,7 +465,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
         __syncthreads();
         for (int j = 0; j < count; ++j, ++rows) {
             const RowScalars sc = list[j];
-            const int64_t i = start + sc.row * g.clusters;
+            const int64_t i = start + sc.row;
             const T *row = logits + i * a.logits_stride;
             const int off = offset_of(row), granules = (off + a.vocab + N - 1) / N, mygran = slice_end(granules);
             uint4 *buf = buffer(rows);
@@ -529,7 +610,7 @@ bool stage_plan(const PolicyArgs &a, int es, StagePlan *p) {
 
 template <typename T, int THREADS, int GRAD> cudaError_t launch_staged(const PolicyArgs &a, const StagePlan &p, cudaStream_t s) {
     constexpr auto kernel = policy_staged_kernel<T, THREADS, GRAD>;
-    cudaError_t e = allow_shared<kernel>(232448 - 2048);
+    cudaError_t e = allow_shared<kernel>(static_cast<int>(kBuffers * kMaxSlice + kBatch * sizeof(RowScalars)));
     if (e != cudaSuccess) return e;
     if (p.cs > 8 && (e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -554,6 +635,11 @@ template <typename T, int THREADS, int GRAD> cudaError_t launch_staged(const Pol
     g.per = p.per;
     g.cs = p.cs;
     g.clusters = std::min<int64_t>(a.n, std::max(1, clusters));
+    g.span = g.clusters * kBatch;
+    // Masked rows cost a fraction of the others and come in no even order, so up to kRanked rows the live ones are dealt
+    // out by rank: every CTA reads all weights and actions once (about 2 us for 8192 rows).  Beyond, a cluster has hundreds
+    // of rows and the strided deal evens out by itself.
+    g.ranked = a.n <= std::min<int64_t>(kRanked, g.span);
     cfg.gridDim = dim3(static_cast<unsigned>(g.clusters * p.cs));
     return cudaLaunchKernelEx(&cfg, kernel, a, g);
 }
