@@ -25,6 +25,7 @@ struct PolicyArgs {
     const float *old_logp, *ref_logp, *advantages, *weights;
     ccq_policy_params p;
     float scale;      // log2(e) / temperature
+    float grad_mul;   // grad_scale / temperature
     float *logp, *row_loss;
     void *dlogits;
     int score;  // 1: log-probabilities alone
@@ -76,7 +77,7 @@ __device__ __forceinline__ float row_loss(const PolicyArgs &a, const RowScalars 
         loss += a.p.kl_coef * (em1 - d);
         slope -= a.p.kl_coef * em1;
     }
-    c = a.p.grad_scale * r.weight * slope / a.p.temperature;
+    c = r.weight * slope * a.grad_mul;
     return r.weight * loss;
 }
 
@@ -177,34 +178,62 @@ template <typename T, int N> __global__ void __launch_bounds__(kRowThreads) poli
 
 // ---------------------------------------------------------------- rows in shared memory
 
-// A cluster of `cs` CTAs takes a row, each a slice of its 16-byte granules, in one of kBuffers buffers of shared
-// memory: while a row is computed, the next ones come in and the gradient of the one before, written over its
-// logits, goes out, both as bulk copies.  Each logit is read from memory once.  A row that starts or ends inside a
+// A cluster of `cs` CTAs takes a row, each a slice of its 16-byte granules, in one of three to kMaxBuffers buffers of
+// shared memory: while a row is computed, the next ones come in and the gradients of the ones before, written over
+// their logits, go out, both as bulk copies.  Each logit is read from memory once.  A row that starts or ends inside a
 // granule (an odd vocabulary) has those elements fetched one by one a row ahead, and what belongs to its neighbours
 // replaced by -inf; the gradient's first and last elements are stored one by one.
-constexpr int kBuffers = 3;
-constexpr int kBatch = 256;  // rows whose scalars are held at once
+constexpr int kMaxBuffers = 8;
+// Rows whose scalars a CTA holds at once: the more CTAs share an SM, the fewer.
+constexpr int batch_rows(int threads) { return threads <= 128 ? 64 : 256; }
 constexpr int kMaxCluster = 16;
 constexpr int kRanked = 16384;
 constexpr int kGranules = 8;  // of a thread: their exponentials stay in registers until the row's sum is known
 constexpr size_t kMaxSlice = 512 * kGranules * 16;  // bytes of a buffer: three and the scalars fit an SM
+constexpr size_t kSmBytes = 206848;                      // of which an SM's CTAs share
 constexpr float kLowest = -3.402823466e38f;
 
 struct Staging {
     int per;  // granules of a slice
-    int cs;
+    int cs, buffers;
     int ranked;  // rows are dealt out by their rank among the live ones
     int64_t clusters;
-    int64_t span;  // rows dealt out at a time, at most kBatch to a cluster
+    int64_t span;  // rows dealt out at a time, at most batch_rows() to a cluster
 };
 
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
-__device__ __forceinline__ void store_peer(float2 *p, int cta, float2 v) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr(p)), "r"(cta));
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(r), "f"(v.x), "f"(v.y) : "memory");
+// Writes v to p in CTA `cta` of the cluster and tells that CTA's barrier of the 8 bytes.
+__device__ __forceinline__ void tell_peer(float2 *p, uint64_t *bar, int cta, float2 v) {
+    uint32_t to, at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_addr(p)), "r"(cta));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(bar)), "r"(cta));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(to),
+                 "l"(f2_make(v.x, v.y)), "r"(at)
+                 : "memory");
+}
+
+// mbar_wait for a barrier that the cluster's other CTAs complete.
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t parity, volatile int *abort, int *status) {
+    const long long start = clock64();
+    for (;;) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(smem_addr(bar)), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if (*abort) return false;
+        if (clock64() - start > kWaitLimitCycles) {
+            *abort = 1;
+            atomicExch(status, kStatusTimeout);
+            return false;
+        }
+    }
 }
 
 // (maximum, sum) pairs of a warp's lanes to those of all of them.  A sum is scaled to the common maximum; equal maxima
@@ -265,20 +294,22 @@ template <typename T, int THREADS, int GRAD>
 __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(PolicyArgs a, Staging g) {
     constexpr int N = 16 / static_cast<int>(sizeof(T));
     constexpr int kPairs = N / 2;
-    constexpr int kWarps = THREADS / 32;
-    extern __shared__ __align__(128) uint8_t dyn[];  // [kBuffers][per] granules, then the batch's scalars
-    __shared__ uint64_t full[kBuffers];
+    constexpr int kWarps = THREADS / 32, kBatch = batch_rows(THREADS);
+    extern __shared__ __align__(128) uint8_t dyn[];  // [buffers][per] granules, then the batch's scalars
+    __shared__ uint64_t full[kMaxBuffers], heard[2];
     __shared__ int give_up;
-    __shared__ float2 pairs[kWarps], peers[2][kMaxCluster];
+    __shared__ float2 pairs[kWarps];
+    __shared__ __align__(8) float2 peers[2][kMaxCluster];
     __shared__ uint32_t live_bits[kBatch / 32], dead_bits[kBatch / 32];
     __shared__ int live_rows[kBatch], dead_rows[kBatch], counts[2], warp_live[kWarps];
-    __shared__ uint32_t row_bits[kRanked / 32];
-    RowScalars *list = reinterpret_cast<RowScalars *>(dyn + static_cast<size_t>(kBuffers) * g.per * 16);
+    __shared__ uint32_t row_bits[THREADS == 512 ? kRanked / 32 : 1];
+    RowScalars *list = reinterpret_cast<RowScalars *>(dyn + static_cast<size_t>(g.buffers) * g.per * 16);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = static_cast<int>(blockIdx.x % g.cs);
     const int64_t cluster = blockIdx.x / g.cs;
     if (tid == 0) {
-        for (int b = 0; b < kBuffers; ++b) mbar_init(&full[b], 1);
+        for (int b = 0; b < kMaxBuffers; ++b) mbar_init(&full[b], 1);
+        for (int b = 0; b < 2; ++b) mbar_init(&heard[b], 1);
         give_up = 0;
         fence_barrier_init();
     }
@@ -287,27 +318,30 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
     const T *logits = static_cast<const T *>(a.logits);
     T *dlogits = static_cast<T *>(a.dlogits);
     const int first = rank * g.per;  // this slice's first granule
-    uint32_t loads = 0, rows = 0;    // issued (thread 0's count), and computed
+    // rows loaded (thread 0) and computed so far: their buffers and the barriers' phases
+    uint32_t load_at = 0, at = 0, phase = 0, rows = 0;
+    const int lag = g.buffers > 3 ? 2 : 1;  // rows whose gradients may still be leaving
+    const int ahead = g.buffers - lag;      // rows whose logits are under way or here
 
     // Elements of row i before its first granule's start, and the granules it touches.
     auto offset_of = [](const void *row) { return static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)); };
-    auto buffer = [&](uint32_t k) { return reinterpret_cast<uint4 *>(dyn) + static_cast<size_t>(k % kBuffers) * g.per; };
+    auto buffer = [&](uint32_t b) { return reinterpret_cast<uint4 *>(dyn) + static_cast<size_t>(b) * g.per; };
     auto slice_end = [&](int granules) { return granules - first < g.per ? granules - first : g.per; };
     // Thread 0: the whole granules of row i's slice into the next buffer.
     auto load_row = [&](int64_t i) {
         const T *row = logits + i * a.logits_stride;
         const int off = offset_of(row), whole = (off + a.vocab) / N;
         const int lo = first > 0 || off == 0 ? 0 : 1, hi = slice_end(whole);
-        const uint32_t b = loads % kBuffers;
+        const uint32_t b = load_at;
         if (hi > lo) {
             mbar_arrive_expect_tx(&full[b], static_cast<uint32_t>(hi - lo) * 16);
-            bulk_load(buffer(loads) + lo, row - off + static_cast<int64_t>(first + lo) * N, static_cast<uint32_t>(hi - lo) * 16, &full[b]);
+            bulk_load(buffer(b) + lo, row - off + static_cast<int64_t>(first + lo) * N, static_cast<uint32_t>(hi - lo) * 16, &full[b]);
         } else {
             mbar_arrive(&full[b]);
         }
-        ++loads;
+        load_at = load_at + 1 == static_cast<uint32_t>(g.buffers) ? 0 : load_at + 1;
     };
-    // Warp 1's lanes: the elements of the granules that row i shares with its neighbours, -inf in the others' places.
+    // The last warp's lanes: the elements of the granules that row i shares with its neighbours, -inf in the others' places.
     // `cell` is where the value belongs in the row's buffer (-1: nowhere in this slice).
     auto edge_of = [&](int64_t i, int &cell) {
         const T *row = logits + i * a.logits_stride;
@@ -316,7 +350,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
         cell = -1;
         T v = from_f32<T>(-INFINITY);
         const int e = lane % N, side = lane / N;
-        if (warp != 1 || side > 1) return v;
+        if (warp != kWarps - 1 || side > 1) return v;
         int at = -1;  // granule
         if (side == 0 && off) at = 0;
         if (side == 1 && tail && !(granules == 1 && off)) at = granules - 1;
@@ -332,7 +366,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
         const int64_t span = a.n - start < g.span ? a.n - start : g.span;
         if (tid < 2) counts[tid] = 0;
         __syncthreads();
-        if (g.ranked) {
+        if (THREADS == 512 && g.ranked) {
             // a bit for each row of the span, the live rows before each word of them, then every cluster takes each
             // clusters-th of the live rows, and of the dead
             const int words = static_cast<int>((span + 31) / 32);
@@ -440,11 +474,11 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
         __syncthreads();
         auto row_index = [&](int j) { return start + list[j].row; };
         if (tid == 0)
-            for (int j = 0; j < kBuffers - 1 && j < count; ++j) load_row(row_index(j));
+            for (int j = 0; j < ahead && j < count; ++j) load_row(row_index(j));
         if (count > 0) {
             int cell;
             const T v = edge_of(row_index(0), cell);
-            if (cell >= 0) reinterpret_cast<T *>(buffer(rows))[cell] = v;
+            if (cell >= 0) reinterpret_cast<T *>(buffer(at))[cell] = v;
         }
         if constexpr (GRAD) {
             // masked rows: zeros, while the first rows come in
@@ -468,11 +502,13 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
             const int64_t i = start + sc.row;
             const T *row = logits + i * a.logits_stride;
             const int off = offset_of(row), granules = (off + a.vocab + N - 1) / N, mygran = slice_end(granules);
-            uint4 *buf = buffer(rows);
+            const uint32_t next = at + 1 == static_cast<uint32_t>(g.buffers) ? 0 : at + 1;
+            uint4 *buf = buffer(at);
             int edge_cell = -1;
             T edge = from_f32<T>(0.f);
             if (j + 1 < count) edge = edge_of(row_index(j + 1), edge_cell);
-            mbar_wait(&full[rows % kBuffers], (rows / kBuffers) & 1, &give_up, a.status);
+            if (g.cs > 1 && tid == 0) mbar_arrive_expect_tx(&heard[rows & 1], static_cast<uint32_t>(g.cs) * 8);
+            mbar_wait(&full[at], phase, &give_up, a.status);
             // this thread's exponentials, against its own maximum, and their sum
             constexpr uint32_t low = IsBf16<T>::value ? 0xff80ff80u : 0xff800000u;  // -inf
             const uint64_t scale = f2_make(a.scale, a.scale);
@@ -508,8 +544,9 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
                 join_warp(m, z, a.scale);
             }
             if (!alone) {
-                if (warp == 0 && lane < g.cs) store_peer(&peers[rows & 1][rank], lane, make_float2(m, z));
-                cluster_barrier();
+                // (a CTA tells its row after the next only when all have told the next, so two sets of cells do)
+                if (warp == 0 && lane < g.cs) tell_peer(&peers[rows & 1][rank], &heard[rows & 1], lane, make_float2(m, z));
+                mbar_wait_cluster(&heard[rows & 1], (rows >> 1) & 1, &give_up, a.status);
                 const float2 p = lane < g.cs ? peers[rows & 1][lane] : make_float2(kLowest, 0.f);
                 m = p.x;
                 z = p.y;
@@ -562,7 +599,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
                 }
                 fence_proxy_async_smem();
             }
-            if (edge_cell >= 0) reinterpret_cast<T *>(buffer(rows + 1))[edge_cell] = edge;
+            if (edge_cell >= 0) reinterpret_cast<T *>(buffer(next))[edge_cell] = edge;
             __syncthreads();
             if (tid == 0) {
                 if constexpr (GRAD) {
@@ -572,20 +609,25 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
                         if (hi > lo) bulk_store(drow - off + static_cast<int64_t>(first + lo) * N, buf + lo, static_cast<uint32_t>(hi - lo) * 16);
                     }
                     tma_store_commit();
-                    tma_store_wait_read_but<1>();  // the row before has left its buffer
+                    // the row `lag` before this one has left the buffer that the next load takes
+                    if (lag == 1) tma_store_wait_read_but<1>();
+                    else tma_store_wait_read_but<2>();
                 }
-                if (j + kBuffers - 1 < count) load_row(row_index(j + kBuffers - 1));
+                if (j + ahead < count) load_row(row_index(j + ahead));
             }
+            at = next;
+            if (!at) phase ^= 1;
         }
         __syncthreads();  // the batch's scalars may go
     }
     if constexpr (GRAD) {
         if (tid == 0) tma_store_wait_all();
     }
+    if (g.cs > 1) cluster_barrier();  // no CTA leaves while others may still write to it
 }
 
 struct StagePlan {
-    int threads, cs, per;
+    int threads, cs, per, buffers;
     size_t smem;
 };
 
@@ -603,14 +645,18 @@ bool stage_plan(const PolicyArgs &a, int es, StagePlan *p) {
     while (cs < 8 && a.n * cs * 2 <= sm_count_now() && per(cs) * 16 >= 16384) cs *= 2;
     p->cs = cs;
     p->per = static_cast<int>(per(cs));
-    p->threads = p->per <= 128 * kGranules ? 128 : p->per <= 256 * kGranules ? 256 : 512;
-    p->smem = static_cast<size_t>(kBuffers) * p->per * 16 + kBatch * sizeof(RowScalars);
+    p->threads = p->per <= 32 * kGranules ? 32 : p->per <= 128 * kGranules ? 128 : p->per <= 256 * kGranules ? 256 : 512;
+    // what shared memory is left to an SM's 512 threads goes into more buffers: short rows need more of them under way
+    const size_t scalars = batch_rows(p->threads) * sizeof(RowScalars);
+    const size_t share = kSmBytes / (512 / p->threads) - scalars - 2048;
+    p->buffers = static_cast<int>(std::min<size_t>(kMaxBuffers, std::max<size_t>(3, share / (static_cast<size_t>(p->per) * 16))));
+    p->smem = static_cast<size_t>(p->buffers) * p->per * 16 + scalars;
     return true;
 }
 
 template <typename T, int THREADS, int GRAD> cudaError_t launch_staged(const PolicyArgs &a, const StagePlan &p, cudaStream_t s) {
     constexpr auto kernel = policy_staged_kernel<T, THREADS, GRAD>;
-    cudaError_t e = allow_shared<kernel>(static_cast<int>(kBuffers * kMaxSlice + kBatch * sizeof(RowScalars)));
+    cudaError_t e = allow_shared<kernel>(static_cast<int>(kSmBytes));
     if (e != cudaSuccess) return e;
     if (p.cs > 8 && (e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -634,18 +680,19 @@ template <typename T, int THREADS, int GRAD> cudaError_t launch_staged(const Pol
     Staging g;
     g.per = p.per;
     g.cs = p.cs;
+    g.buffers = p.buffers;
     g.clusters = std::min<int64_t>(a.n, std::max(1, clusters));
-    g.span = g.clusters * kBatch;
+    g.span = g.clusters * batch_rows(THREADS);
     // Masked rows cost a fraction of the others and come in no even order, so up to kRanked rows the live ones are dealt
-    // out by rank: every CTA reads all weights and actions once (about 2 us for 8192 rows).  Beyond, a cluster has hundreds
-    // of rows and the strided deal evens out by itself.
-    g.ranked = a.n <= std::min<int64_t>(kRanked, g.span);
+    // out by rank: every CTA reads all weights and actions once (about 2 us for 8192 rows).  Beyond, and with short rows,
+    // the strided deal evens out by itself.
+    g.ranked = a.weights && p.threads == 512 && a.n <= std::min<int64_t>(kRanked, g.span);
     cfg.gridDim = dim3(static_cast<unsigned>(g.clusters * p.cs));
     return cudaLaunchKernelEx(&cfg, kernel, a, g);
 }
 
 template <typename T, int GRAD> cudaError_t launch_staged_threads(const PolicyArgs &a, const StagePlan &p, cudaStream_t s) {
-    return p.threads == 128 ? launch_staged<T, 128, GRAD>(a, p, s) : p.threads == 256 ? launch_staged<T, 256, GRAD>(a, p, s)
+    return p.threads == 32 ? launch_staged<T, 32, GRAD>(a, p, s) : p.threads == 128 ? launch_staged<T, 128, GRAD>(a, p, s) : p.threads == 256 ? launch_staged<T, 256, GRAD>(a, p, s)
                                                                                      : launch_staged<T, 512, GRAD>(a, p, s);
 }
 
@@ -760,6 +807,7 @@ ccq_status ccq_policy_loss(const void *logits, ccq_dtype dtype, int64_t logits_s
     a.n = n; a.vocab = vocab;
     a.old_logp = old_logp; a.ref_logp = ref_logp; a.advantages = advantages; a.weights = weights;
     a.scale = kLog2e / a.p.temperature;
+    a.grad_mul = a.p.grad_scale / a.p.temperature;
     a.logp = logp; a.row_loss = static_cast<float *>(workspace);
     a.dlogits = dlogits; a.dlogits_stride = dlogits_stride;
     a.status = device_status_word();
