@@ -627,73 +627,136 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
 }
 
 struct StagePlan {
-    int threads, cs, per, buffers;
+    int threads, cs, per, buffers, clusters;  // clusters: those the device holds at once
     size_t smem;
 };
 
-// How rows are spread: the fewest CTAs a row whose slices fit three to an SM, and with few rows as many as there are
-// SMs for (slices of 8 KB at least).  False where even 16 CTAs do not hold a row: those are read twice.
-bool stage_plan(const PolicyArgs &a, int es, StagePlan *p) {
+int64_t row_granules(const PolicyArgs &a, int es) {
     const int n = 16 / es;
-    const int64_t granules = (static_cast<int64_t>(a.vocab) + 2 * (n - 1)) / n + 1;
-    int cs = 1;
-    auto per = [&](int c) { return (granules + c - 1) / c; };
-    while (per(cs) * 16 > static_cast<int64_t>(kMaxSlice)) {
-        if (cs == kMaxCluster) return false;
-        cs *= 2;
-    }
-    while (cs < 8 && a.n * cs * 2 <= sm_count_now() && per(cs) * 16 >= 16384) cs *= 2;
-    p->cs = cs;
-    p->per = static_cast<int>(per(cs));
-    p->threads = p->per <= 32 * kGranules ? 32 : p->per <= 128 * kGranules ? 128 : p->per <= 256 * kGranules ? 256 : 512;
-    // what shared memory is left to an SM's 512 threads goes into more buffers: short rows need more of them under way
-    const size_t scalars = batch_rows(p->threads) * sizeof(RowScalars);
-    const size_t share = kSmBytes / (512 / p->threads) - scalars - 2048;
-    p->buffers = static_cast<int>(std::min<size_t>(kMaxBuffers, std::max<size_t>(3, share / (static_cast<size_t>(p->per) * 16))));
-    p->smem = static_cast<size_t>(p->buffers) * p->per * 16 + scalars;
-    return true;
+    return (static_cast<int64_t>(a.vocab) + 2 * (n - 1)) / n + 1;
 }
 
-template <typename T, int THREADS, int GRAD> cudaError_t launch_staged(const PolicyArgs &a, const StagePlan &p, cudaStream_t s) {
+// A plan for slices of a cs-th of a row: the fewest threads that hold one, and shared memory for as many buffers as
+// an SM's 512 threads leave room for (short rows need more of them under way).
+StagePlan slice_plan(int64_t granules, int cs) {
+    StagePlan p = {};
+    p.cs = cs;
+    p.per = static_cast<int>((granules + cs - 1) / cs);
+    p.threads = p.per <= 32 * kGranules ? 32 : p.per <= 64 * kGranules ? 64 : p.per <= 128 * kGranules ? 128 : p.per <= 256 * kGranules ? 256 : 512;
+    const size_t scalars = batch_rows(p.threads) * sizeof(RowScalars);
+    const size_t share = kSmBytes / (512 / p.threads) - scalars - 2048;
+    p.buffers = static_cast<int>(std::min<size_t>(kMaxBuffers, std::max<size_t>(3, share / (static_cast<size_t>(p.per) * 16))));
+    p.smem = static_cast<size_t>(p.buffers) * p.per * 16 + scalars;
+    return p;
+}
+
+template <typename T, int THREADS, int GRAD> cudaError_t staged_config(const StagePlan &p, cudaLaunchConfig_t *cfg, cudaLaunchAttribute *at) {
     constexpr auto kernel = policy_staged_kernel<T, THREADS, GRAD>;
     cudaError_t e = allow_shared<kernel>(static_cast<int>(kSmBytes));
     if (e != cudaSuccess) return e;
     if (p.cs > 8 && (e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = p.smem;
-    cfg.stream = s;
+    *cfg = {};
+    cfg->gridDim = dim3(p.cs);
+    cfg->blockDim = dim3(THREADS);
+    cfg->dynamicSmemBytes = p.smem;
+    at->id = cudaLaunchAttributeClusterDimension;
+    at->val.clusterDim.x = p.cs;
+    at->val.clusterDim.y = at->val.clusterDim.z = 1;
+    cfg->attrs = at;
+    cfg->numAttrs = 1;
+    return cudaSuccess;
+}
+
+template <typename T, int THREADS, int GRAD> cudaError_t resident_clusters(StagePlan *p) {
+    constexpr auto kernel = policy_staged_kernel<T, THREADS, GRAD>;
+    cudaLaunchConfig_t cfg;
     cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = p.cs;
-    at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    cfg.gridDim = dim3(p.cs);
-    int clusters = 0;
-    if (p.cs > 1) {
-        if ((e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg)) != cudaSuccess) return e;
-    } else {
-        if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&clusters, kernel, THREADS, p.smem)) != cudaSuccess) return e;
-        clusters *= sm_count_now();
-    }
+    cudaError_t e = staged_config<T, THREADS, GRAD>(*p, &cfg, &at);
+    if (e != cudaSuccess) return e;
+    if (p->cs > 1) return cudaOccupancyMaxActiveClusters(&p->clusters, kernel, &cfg);
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->clusters, kernel, THREADS, p->smem);
+    p->clusters *= sm_count_now();
+    return e;
+}
+
+template <typename T, int THREADS, int GRAD> cudaError_t launch_staged(const PolicyArgs &a, const StagePlan &p, cudaStream_t s) {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute at;
+    cudaError_t e = staged_config<T, THREADS, GRAD>(p, &cfg, &at);
+    if (e != cudaSuccess) return e;
     Staging g;
     g.per = p.per;
     g.cs = p.cs;
     g.buffers = p.buffers;
-    g.clusters = std::min<int64_t>(a.n, std::max(1, clusters));
+    g.clusters = std::min<int64_t>(a.n, p.clusters);
     g.span = g.clusters * batch_rows(THREADS);
     // Masked rows cost a fraction of the others and come in no even order, so up to kRanked rows the live ones are dealt
     // out by rank: every CTA reads all weights and actions once (about 2 us for 8192 rows).  Beyond, and with short rows,
     // the strided deal evens out by itself.
-    g.ranked = a.weights && p.threads == 512 && a.n <= std::min<int64_t>(kRanked, g.span);
+    g.ranked = a.weights && THREADS == 512 && a.n <= std::min<int64_t>(kRanked, g.span);
     cfg.gridDim = dim3(static_cast<unsigned>(g.clusters * p.cs));
-    return cudaLaunchKernelEx(&cfg, kernel, a, g);
+    cfg.stream = s;
+    return cudaLaunchKernelEx(&cfg, policy_staged_kernel<T, THREADS, GRAD>, a, g);
 }
 
-template <typename T, int GRAD> cudaError_t launch_staged_threads(const PolicyArgs &a, const StagePlan &p, cudaStream_t s) {
-    return p.threads == 32 ? launch_staged<T, 32, GRAD>(a, p, s) : p.threads == 128 ? launch_staged<T, 128, GRAD>(a, p, s) : p.threads == 256 ? launch_staged<T, 256, GRAD>(a, p, s)
-                                                                                     : launch_staged<T, 512, GRAD>(a, p, s);
+// How rows are spread.  The time of a row is mostly latency (its loads, two reductions, its stores), so the rate goes
+// with the rows that the device holds at once: of the fewest CTAs a row with slices of up to 512, 256 and 128
+// threads, the one with the most clusters resident (8192 x 33000 bf16: 76, 101, 121 clusters take 308, 239 and
+// 205 us; 1500 x 128001: 38 each, 133, 131, 138 us).  With fewer rows than that, a row takes as many CTAs as
+// there are SMs for, in slices of 8 KB at least.  `found` is false where 16 CTAs do not hold a row: it is then read twice.
+template <typename T, int GRAD> cudaError_t stage_plan(const PolicyArgs &a, StagePlan *plan, bool *found) {
+    struct Known {
+        int64_t granules;
+        int device;
+        StagePlan plan;
+        bool found;
+    };
+    static thread_local Known last = {-1, -1, {}, false};
+    const int64_t granules = row_granules(a, sizeof(T));
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    auto query = [](StagePlan *p) {
+        return p->threads == 32 ? resident_clusters<T, 32, GRAD>(p) : p->threads == 64 ? resident_clusters<T, 64, GRAD>(p) : p->threads == 128 ? resident_clusters<T, 128, GRAD>(p)
+               : p->threads == 256 ? resident_clusters<T, 256, GRAD>(p) : resident_clusters<T, 512, GRAD>(p);
+    };
+    if (last.granules != granules || last.device != dev) {
+        Known k = {granules, dev, {}, false};
+        for (int threads : {512, 256, 128}) {
+            const int64_t cs = (granules + threads * kGranules - 1) / (threads * kGranules);
+            if (cs > kMaxCluster) continue;
+            StagePlan p = slice_plan(granules, static_cast<int>(cs));
+            if ((e = query(&p)) != cudaSuccess) return e;
+            if (p.clusters > k.plan.clusters) k.plan = p;
+        }
+        k.found = k.plan.clusters > 0;
+        // more CTAs a row where that leaves as many clusters (512 x 200000 fp32: 13 a row 172 us, 16 a row 162)
+        for (int cs = k.plan.cs + 1; k.found && k.plan.cs > 1 && cs <= kMaxCluster; ++cs) {
+            StagePlan p = slice_plan(granules, cs);
+            if ((e = query(&p)) != cudaSuccess) return e;
+            if (p.clusters < k.plan.clusters) break;
+            k.plan = p;
+        }
+        last = k;
+    }
+    *plan = last.plan;
+    *found = last.found;
+    if (!last.found || a.n * 2 > last.plan.clusters) return cudaSuccess;
+    int cs = last.plan.cs;
+    while (cs * 2 <= 8 && a.n * cs * 2 <= sm_count_now() && granules / cs >= 1024) cs *= 2;
+    if (cs == last.plan.cs) return cudaSuccess;
+    StagePlan p = slice_plan(granules, cs);
+    if ((e = query(&p)) != cudaSuccess) return e;
+    if (p.clusters > 0) *plan = p;
+    return cudaSuccess;
+}
+
+template <typename T, int GRAD> cudaError_t launch_staged_rows(const PolicyArgs &a, cudaStream_t s, bool *done) {
+    StagePlan p;
+    cudaError_t e = stage_plan<T, GRAD>(a, &p, done);
+    if (e != cudaSuccess || !*done) return e;
+    return p.threads == 32 ? launch_staged<T, 32, GRAD>(a, p, s) : p.threads == 64 ? launch_staged<T, 64, GRAD>(a, p, s) : p.threads == 128 ? launch_staged<T, 128, GRAD>(a, p, s)
+           : p.threads == 256 ? launch_staged<T, 256, GRAD>(a, p, s) : launch_staged<T, 512, GRAD>(a, p, s);
 }
 
 // loss = the rows' losses, by 1024 strided sums and a tree: an order that depends on n alone.
@@ -720,12 +783,13 @@ template <typename T, int N> cudaError_t launch_rows(const PolicyArgs &a, cudaSt
 
 cudaError_t launch_policy(const PolicyArgs &a, ccq_dtype dtype, cudaStream_t s) {
     const int es = dtype_bytes(dtype);
-    StagePlan plan;
-    if (stage_plan(a, es, &plan)) {
-        if (dtype == CCQ_BF16)
-            return a.dlogits ? launch_staged_threads<__nv_bfloat16, 1>(a, plan, s) : launch_staged_threads<__nv_bfloat16, 0>(a, plan, s);
-        return a.dlogits ? launch_staged_threads<float, 1>(a, plan, s) : launch_staged_threads<float, 0>(a, plan, s);
-    }
+    bool done = false;
+    cudaError_t e;
+    if (dtype == CCQ_BF16)
+        e = a.dlogits ? launch_staged_rows<__nv_bfloat16, 1>(a, s, &done) : launch_staged_rows<__nv_bfloat16, 0>(a, s, &done);
+    else
+        e = a.dlogits ? launch_staged_rows<float, 1>(a, s, &done) : launch_staged_rows<float, 0>(a, s, &done);
+    if (e != cudaSuccess || done) return e;
     int b = access_bytes(static_cast<uintptr_t>(a.vocab) * es);
     b = row_access(a.logits, a.logits_stride, es, a.n, b);
     if (a.dlogits) b = row_access(a.dlogits, a.dlogits_stride, es, a.n, b);
