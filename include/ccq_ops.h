@@ -45,9 +45,9 @@ CCQ_API ccq_status ccq_embed(const void *table, ccq_dtype dtype, int64_t table_s
  *   dtable     [rows, width] in grad_dtype, row stride dtable_stride; written in full.
  *   workspace  ccq_embed_grad_workspace_size() bytes, 16-byte aligned.
  * The ids are sorted (stably), then every run of equal ids is summed in fp32 in ascending
- * i within pieces whose bounds depend on the ids alone, and the pieces in order.  An id
+ * i within pieces whose bounds depend on the ids alone, and the pieces in a fixed order.  An id
  * outside [0, rows) contributes nothing and leaves CCQ_ERR_INDEX.
- * n <= 2^30, rows <= 2^30.
+ * n <= 2^30, rows <= 2^23.
  */
 CCQ_API ccq_status ccq_embed_grad(const void *dout, ccq_dtype dtype, int64_t dout_stride, const void *ids,
                                   int id_bytes, int64_t n, int64_t rows, int width, float scale,

@@ -5,14 +5,13 @@
 //
 // Gradient: dtable[r] = scale * sum of dout[i] over the i with ids[i] = r.  Each row of dout is read
 // once and each row of dtable written once; no sum depends on the order of atomics:
-//   1. embed_sort_kernel: a stable radix sort of (id, i), one cluster of 8 CTAs, all passes in one launch.
-//      It also marks where each piece of the path below begins.
-//   2. embed_sum_kernel: the sorted entries and the rows' ends form one path of n + rows steps (the
-//      entries of row 0, its end, the entries of row 1, its end, ...).  The path is cut into pieces of
-//      kPiece steps, so frequent ids and empty rows cost the same everywhere.  A warp takes a piece of a
-//      column slice: it adds the entries and writes a row at its end.  What it holds of a row that began in
-//      an earlier piece, or ends in a later one, goes to the workspace.
-//   3. embed_join_kernel: adds the parts of the rows that span pieces, in order.
+//   1. embed_sort_kernel: one cluster of 8 CTAs sorts (id, i) stably, all passes in one launch; meanwhile the other CTAs
+//      write the rows that no id names (most of a vocabulary's), which hides the sort's latency.
+//   2. embed_sum_kernel: the sorted entries are cut into pieces of kPiece, so that frequent ids cost no
+//      more than others.  A warp takes a piece of a column slice, adds its entries and writes a row where its
+//      run of equal ids ends.  A run that ends in the next piece is finished by the piece in which it begins; of
+//      longer ones every piece leaves its part in the workspace.
+//   3. embed_join_kernel: adds the parts of the runs over three pieces and more, in order.
 #include <algorithm>
 
 #include "ccq_ops.cuh"
@@ -82,9 +81,9 @@ cudaError_t launch_embed(const void *table, int64_t table_stride, const void *id
 constexpr int kSortCtas = 8;
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kMaxDigit = 10;  // bits of a pass
-constexpr int kHeld = 4;       // entries a lane keeps in registers; with more, a pass reads them twice
-constexpr int kPiece = 32;     // path steps of a piece
+constexpr int kMaxDigit = 9;  // bits of a pass
+constexpr int kHeld = 8;      // entries a lane keeps in registers; up to these, the passes exchange them in shared memory
+constexpr int kPiece = 32;    // entries of a piece, one a lane
 
 struct SortArgs {
     const void *ids;
@@ -92,83 +91,140 @@ struct SortArgs {
     int n;
     int64_t rows, padding;
     int passes, digit;
-    uint32_t *key[2];
-    uint32_t *pos[2];
-    int *piece_start;  // [pieces + 1]: entries before each piece's first step
-    int pieces;
-    int *joins;        // count, then the pieces that end a row from an earlier one (embed_sum_kernel)
+    uint2 *list[2];    // (key, position); the last pass writes list[(passes - 1) & 1], or list[0] where entries are held
+    int *joins;  // count, then the pieces that end a run over three pieces and more (embed_sum_kernel)
     int *status;
+    uint8_t *dtable;  // the CTAs behind the first cluster write its rows without entries
+    int64_t row_bytes, row_stride;
+    int access, present_words;  // bytes of a store, and words of a CTA's bitmap of its rows
 };
 
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
+// Entries of a warp, a multiple of 32.
+__host__ __device__ inline int warp_entries(int n) { return ((n + kSortCtas * kSortWarps - 1) / (kSortCtas * kSortWarps) + 31) & ~31; }
+__host__ __device__ inline bool sort_holds(int n) { return warp_entries(n) <= 32 * kHeld; }
+constexpr int kSortMostShared = 204800;  // bytes; bounds the rows too (a bitmap of each CTA's)
+inline int sort_shared_words(int digit) { return kSortWarps * ((1 << digit) + 1) + (kSortCtas + 1) * (1 << digit); }
 
-__device__ __forceinline__ void cluster_store(uint32_t *p, int cta, uint32_t v) {
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_address(const void *p, int cta) {
     uint32_t a;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(cta));
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
+    return a;
+}
+__device__ __forceinline__ void cluster_store(uint32_t *p, int cta, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_address(p, cta)), "r"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_store(uint2 *p, int cta, uint2 v) {
+    asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(cluster_address(p, cta)), "r"(v.x), "r"(v.y) : "memory");
+}
+// Zeros to the rows that no id names: CTA `part` of `parts` looks after the rows r with r % parts = part.
+__device__ __forceinline__ void zero_absent_rows(const SortArgs &a, int part, int parts, uint32_t *present) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int64_t mine = a.rows > part ? (a.rows - part + parts - 1) / parts : 0;
+    for (int w = tid; w < a.present_words; w += kSortThreads) present[w] = 0;
+    __syncthreads();
+    auto see = [&](int64_t id) {
+        if (id < 0 || id >= a.rows || id == a.padding) return;
+        const uint32_t r = static_cast<uint32_t>(id), q = r / static_cast<uint32_t>(parts);
+        if (r - q * parts == static_cast<uint32_t>(part)) atomicOr(&present[q >> 5], 1u << (q & 31));
+    };
+    constexpr int kAtOnce = 8;
+    for (int i0 = tid; i0 < a.n; i0 += kAtOnce * kSortThreads) {
+        int64_t id[kAtOnce];
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+            const int i = i0 + q * kSortThreads;
+            id[q] = i >= a.n ? -1 : a.id_bytes == 8 ? static_cast<const int64_t *>(a.ids)[i] : static_cast<const int32_t *>(a.ids)[i];
+        }
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) see(id[q]);
+    }
+    __syncthreads();
+    for (int64_t q = warp; q < mine; q += kSortWarps) {
+        if ((present[q >> 5] >> (q & 31)) & 1) continue;
+        uint8_t *row = a.dtable + (q * parts + part) * a.row_stride;
+        if (a.access == 16) {
+            for (int64_t c = lane * 16; c < a.row_bytes; c += 512) __stcs(reinterpret_cast<uint4 *>(row + c), make_uint4(0, 0, 0, 0));
+        } else if (a.access >= 4) {
+            for (int64_t c = lane * 4; c < a.row_bytes; c += 128) __stcs(reinterpret_cast<uint32_t *>(row + c), 0u);
+        } else {
+            for (int64_t c = lane * 2; c < a.row_bytes; c += 64) __stcs(reinterpret_cast<uint16_t *>(row + c), static_cast<uint16_t>(0));
+        }
+    }
 }
 
 // Every warp owns a contiguous range of the entries, warps and CTAs in order, so ranks within a warp, sums over
 // the warps before it and over the CTAs before that keep equal digits in order.  Invalid and padding ids get the
-// key `rows`, behind every row.  All passes run in one launch: n = 16384 takes two and about a sixth of the whole call.
+// key `rows`, behind every row.  All passes run in one launch.  Its time is latency: n = 16384 takes two passes of about
+// five barriers each.  A lane finds the others with its digit by a ballot for each bit (match.any takes a time that grows with
+// the number of different digits, 2000 cycles a step for 32 warps of random ones), and up to 65536 entries pass from CTA to
+// CTA in shared memory (through global memory a pass took 6000 cycles for its stores and loads alone).
 __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads) embed_sort_kernel(SortArgs a) {
-    extern __shared__ uint32_t smem[];
-    const int bins = 1 << a.digit;
-    uint32_t *counts = smem;                     // [kSortWarps][bins]: a warp's entries, then its first slot of each bin
-    uint32_t *totals = smem + kSortWarps * bins;  // [kSortCtas][bins]: every CTA's entries
+    extern __shared__ __align__(16) uint32_t smem[];
+    if (blockIdx.x >= kSortCtas) {  // (whole clusters)
+        zero_absent_rows(a, blockIdx.x - kSortCtas, gridDim.x - kSortCtas, smem);
+        return;
+    }
+    const int bins = 1 << a.digit, row = bins + 1;  // (a column of counts spans all banks)
+    uint32_t *counts = smem;                         // [kSortWarps][row]: a warp's entries, then those of the warps before it
+    uint32_t *totals = counts + kSortWarps * row;    // [kSortCtas][bins]: every CTA's entries
+    uint32_t *base = totals + kSortCtas * bins;      // [bins]: this CTA's first slot
+    uint2 *xchg = reinterpret_cast<uint2 *>(smem + ((kSortWarps * row + (kSortCtas + 1) * bins + 1) & ~1));  // this CTA's slots
     __shared__ uint32_t scan[kSortWarps];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
-    const int per = ((a.n + kSortCtas * kSortWarps - 1) / (kSortCtas * kSortWarps) + 31) & ~31;
+    const int per = warp_entries(a.n), mine_slots = per * kSortWarps;
+    const bool held = sort_holds(a.n);
     const int64_t lo64 = static_cast<int64_t>(cta * kSortWarps + warp) * per;
     const int lo = static_cast<int>(lo64 < a.n ? lo64 : a.n);
     const int hi = lo + (a.n - lo < per ? a.n - lo : per);
-    const bool held = per <= 32 * kHeld;
-    uint32_t *mine = counts + warp * bins;
+    uint32_t *mine = counts + warp * row;
+    cluster_arrive();  // waited for before the first store to another CTA: all run by then
     if (cta == 0 && tid == 0) a.joins[0] = 0;
-    cluster_sync();  // every CTA runs before its shared memory is written
+    auto key_from = [&](int64_t id) -> uint32_t {
+        if (id < 0 || id >= a.rows) {
+            note_index(a.status);
+            return static_cast<uint32_t>(a.rows);
+        }
+        return static_cast<uint32_t>(id == a.padding ? a.rows : id);
+    };
+    uint2 kp[kHeld];
+    uint32_t slot[kHeld];
+    if (held) {
+        int64_t id[kHeld];
+        if (a.id_bytes == 8) {
+#pragma unroll
+            for (int q = 0; q < kHeld; ++q) id[q] = lo + q * 32 + lane < hi ? static_cast<const int64_t *>(a.ids)[lo + q * 32 + lane] : 0;
+        } else {
+#pragma unroll
+            for (int q = 0; q < kHeld; ++q) id[q] = lo + q * 32 + lane < hi ? static_cast<const int32_t *>(a.ids)[lo + q * 32 + lane] : 0;
+        }
+#pragma unroll
+        for (int q = 0; q < kHeld; ++q) kp[q] = make_uint2(key_from(id[q]), static_cast<uint32_t>(lo + q * 32 + lane));
+    }
     for (int pass = 0; pass < a.passes; ++pass) {
         const int shift = pass * a.digit;
-        const uint32_t *key = a.key[(pass + 1) & 1], *pos = a.pos[(pass + 1) & 1];
-        uint32_t *key_out = a.key[pass & 1], *pos_out = a.pos[pass & 1];
-        auto key_from = [&](int64_t id) -> uint32_t {
-            if (id < 0 || id >= a.rows) {
-                note_index(a.status);
-                return static_cast<uint32_t>(a.rows);
-            }
-            return static_cast<uint32_t>(id == a.padding ? a.rows : id);
+        const uint2 *from = a.list[(pass + 1) & 1];
+        uint2 *to = a.list[pass & 1];
+        auto entry = [&](int i) {
+            return pass ? from[i] : make_uint2(key_from(load_index(a.ids, a.id_bytes, i)), static_cast<uint32_t>(i));
         };
-        auto key_of = [&](int i) -> uint32_t { return pass ? key[i] : key_from(load_index(a.ids, a.id_bytes, i)); };
-        uint32_t k[kHeld], p[kHeld], slot[kHeld];
         if (held && pass) {
 #pragma unroll
-            for (int q = 0; q < kHeld; ++q) {
-                const int i = lo + q * 32 + lane;
-                k[q] = i < hi ? key[i] : 0;
-                p[q] = i < hi ? pos[i] : 0;
-            }
-        } else if (held) {
-            int64_t id[kHeld];
-            if (a.id_bytes == 8) {
-#pragma unroll
-                for (int q = 0; q < kHeld; ++q) id[q] = lo + q * 32 + lane < hi ? static_cast<const int64_t *>(a.ids)[lo + q * 32 + lane] : 0;
-            } else {
-#pragma unroll
-                for (int q = 0; q < kHeld; ++q) id[q] = lo + q * 32 + lane < hi ? static_cast<const int32_t *>(a.ids)[lo + q * 32 + lane] : 0;
-            }
-#pragma unroll
-            for (int q = 0; q < kHeld; ++q) {
-                p[q] = static_cast<uint32_t>(lo + q * 32 + lane);
-                k[q] = key_from(id[q]);
-            }
+            for (int q = 0; q < kHeld; ++q)
+                if (lo + q * 32 + lane < hi) kp[q] = xchg[warp * per + q * 32 + lane];
         }
-        for (int i = tid; i < kSortWarps * bins; i += kSortThreads) counts[i] = 0;
+        for (int i = tid; i < kSortWarps * row; i += kSortThreads) counts[i] = 0;
         __syncthreads();
         // an entry's place among its warp's of the same digit
-        auto place = [&](uint32_t key_, bool live) -> uint32_t {
-            const uint32_t d = live ? (key_ >> shift) & (bins - 1) : ~0u;
-            const uint32_t same = __match_any_sync(~0u, d);
+        auto place = [&](uint32_t key, bool live) -> uint32_t {
+            const uint32_t d = (key >> shift) & (bins - 1);
+            uint32_t same = __ballot_sync(~0u, live);
+            for (int bit = 0; bit < a.digit; ++bit) {
+                const bool set = (d >> bit) & 1;
+                const uint32_t with = __ballot_sync(~0u, set);
+                same &= set ? with : ~with;
+            }
             const int rank = __popc(same & ((1u << lane) - 1));
             uint32_t at = 0;
             if (live) at = mine[d] + rank;
@@ -180,28 +236,39 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
         if (held) {
 #pragma unroll
             for (int q = 0; q < kHeld; ++q)
-                if (lo + q * 32 < hi) slot[q] = place(k[q], lo + q * 32 + lane < hi);
+                if (lo + q * 32 < hi) slot[q] = place(kp[q].x, lo + q * 32 + lane < hi);
         } else {
-            for (int i0 = lo; i0 < hi; i0 += 32) place(i0 + lane < hi ? key_of(i0 + lane) : 0, i0 + lane < hi);
+            for (int i0 = lo; i0 < hi; i0 += 32) place(i0 + lane < hi ? entry(i0 + lane).x : 0, i0 + lane < hi);
         }
         __syncthreads();
-        // this CTA's entries of every bin to all CTAs
-        if (tid < bins) {
-            uint32_t sum = 0;
-#pragma unroll 8
-            for (int w = 0; w < kSortWarps; ++w) sum += counts[w * bins + tid];
-            for (int c = 0; c < kSortCtas; ++c) cluster_store(&totals[cta * bins + tid], c, sum);
+        if (pass == 0) cluster_wait();
+        // a warp scans the warps' counts of a bin, a lane each, and tells every CTA this one's total
+        for (int bin = warp; bin < bins; bin += kSortWarps) {
+            const uint32_t own = counts[lane * row + bin];
+            uint32_t inc = own;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t t = __shfl_up_sync(~0u, inc, o);
+                if (lane >= o) inc += t;
+            }
+            counts[lane * row + bin] = inc - own;
+            const uint32_t total = __shfl_sync(~0u, inc, 31);
+            if (lane < kSortCtas) cluster_store(&totals[cta * bins + bin], lane, total);
         }
-        cluster_sync();
+        cluster_arrive();
+        cluster_wait();
         uint32_t all = 0, before = 0;
-        if (tid < bins)
+        if (tid < bins) {
+#pragma unroll
             for (int c = 0; c < kSortCtas; ++c) {
                 const uint32_t t = totals[c * bins + tid];
                 if (c < cta) before += t;
                 all += t;
             }
+        }
         // exclusive scan of `all` over the bins
         uint32_t inc = all;
+#pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const uint32_t t = __shfl_up_sync(~0u, inc, o);
             if (lane >= o) inc += t;
@@ -209,58 +276,36 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
         if (lane == 31) scan[warp] = inc;
         __syncthreads();
         if (tid < bins) {
-            uint32_t base = inc - all + before;
-            for (int w = 0; w < warp; ++w) base += scan[w];
-#pragma unroll 8
-            for (int w = 0; w < kSortWarps; ++w) {
-                const uint32_t c = counts[w * bins + tid];
-                counts[w * bins + tid] = base;
-                base += c;
-            }
+            uint32_t b = inc - all + before;
+            for (int w = 0; w < warp; ++w) b += scan[w];
+            base[tid] = b;
         }
         __syncthreads();
         if (held) {
 #pragma unroll
             for (int q = 0; q < kHeld; ++q) {
                 if (lo + q * 32 + lane >= hi) continue;
-                const uint32_t at = slot[q] + mine[(k[q] >> shift) & (bins - 1)];
-                key_out[at] = k[q];
-                pos_out[at] = p[q];
+                const uint32_t d = (kp[q].x >> shift) & (bins - 1);
+                const uint32_t at = slot[q] + mine[d] + base[d], owner = at / static_cast<uint32_t>(mine_slots);
+                cluster_store(&xchg[at - owner * mine_slots], static_cast<int>(owner), kp[q]);
             }
         } else {
+            // (place() counts on from the warps before this one)
             for (int i0 = lo; i0 < hi; i0 += 32) {
-                const int i = i0 + lane;
-                const bool live = i < hi;
-                const uint32_t kk = live ? key_of(i) : 0, at = place(kk, live);
-                if (live) {
-                    key_out[at] = kk;
-                    pos_out[at] = pass ? pos[i] : static_cast<uint32_t>(i);
-                }
+                const bool live = i0 + lane < hi;
+                const uint2 e = live ? entry(i0 + lane) : make_uint2(0, 0);
+                const uint32_t at = place(e.x, live) + base[(e.x >> shift) & (bins - 1)];
+                if (live) to[at] = e;
             }
         }
-        cluster_sync();  // the next pass reads what the other CTAs wrote, and `totals` may be written again
+        cluster_arrive();  // the next pass reads what the other CTAs wrote, and `totals` may be written again
+        cluster_wait();
     }
-    // Entry i is step i + key[i] of the path, so it is the first of the pieces that start after entry i - 1's step and
-    // not after its own; those that start after the last entry's have none.
-    const uint32_t *key = a.key[(a.passes + 1) & 1];
-    for (int i0 = (cta * kSortWarps + warp) * 32; i0 <= a.n; i0 += kSortCtas * kSortThreads) {
-        const int i = i0 + lane;
-        int64_t first = 0, last = -1;
-        if (i <= a.n) {
-            first = i ? (static_cast<int64_t>(i - 1) + key[i - 1]) / kPiece + 1 : 0;
-            last = i < a.n ? (static_cast<int64_t>(i) + key[i]) / kPiece : a.pieces;
-        }
-        // long gaps are filled by the whole warp
-        uint32_t wide = __ballot_sync(~0u, last - first >= 4);
-        if (last - first < 4)
-            for (int64_t q = first; q <= last; ++q) a.piece_start[q] = i;
-        while (wide) {
-            const int src = __ffs(wide) - 1;
-            wide &= wide - 1;
-            const int64_t f = __shfl_sync(~0u, first, src), l = __shfl_sync(~0u, last, src);
-            for (int64_t q = f + lane; q <= l; q += 32) a.piece_start[q] = i0 + src;
-        }
-    }
+    if (!held) return;
+    // this CTA's slots
+    const int first_slot = static_cast<int>(static_cast<int64_t>(cta) * mine_slots < a.n ? cta * mine_slots : a.n);
+    const int slots = a.n - first_slot < mine_slots ? a.n - first_slot : mine_slots;
+    for (int j = tid; j < slots; j += kSortThreads) a.list[0][first_slot + j] = xchg[j];
 }
 
 // ---------------------------------------------------------------- sums
@@ -268,14 +313,13 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
 struct SumArgs {
     const void *dout;
     int64_t dout_stride;
-    const uint32_t *key, *pos;  // sorted entries
-    const int *piece_start;
+    const uint2 *list;  // sorted (key, position)
     int *joins;
     int n, rows, width, packs;
     float scale;
     void *dtable;
     int64_t dtable_stride;
-    float *part;  // [pieces][2][width]: what a piece holds of a row from before it, and of a row it leaves open
+    float *part;  // [pieces][2][width]: what a piece holds of a run from before it, and of a run it leaves open
     int pieces;
 };
 
@@ -294,76 +338,69 @@ template <typename T, typename O, int N> __global__ void __launch_bounds__(kSumT
     const bool live = c < a.packs;
     const T *dout = static_cast<const T *>(a.dout) + static_cast<int64_t>(c) * N;
     O *dtable = static_cast<O *>(a.dtable) + static_cast<int64_t>(c) * N;
-    const int64_t step0 = piece * kPiece, step1 = step0 + kPiece;
-    const int last = a.pieces;
-    const int before = piece > 0 ? a.piece_start[piece - 1] : 0;
-    int i0 = a.piece_start[piece];
-    const int i1 = a.piece_start[piece + 1], i2 = a.piece_start[piece + 2 < last ? piece + 2 : last];
-    int v = static_cast<int>(step0 - i0 < a.rows ? step0 - i0 : a.rows);
-    int v1 = static_cast<int>(step1 - i1 < a.rows ? step1 - i1 : a.rows);
-    const int64_t v2 = piece + 2 < last ? step1 + kPiece - i2 : a.rows;  // rows that end before the piece after the next
-    // the piece's entries and those of the next, one a lane (there are at most kPiece each), and the entry before each
-    uint32_t key = ~0u, pos = 0, key2 = ~0u, pos2 = 0;
-    if (i0 + lane < i1) {
-        key = a.key[i0 + lane];
-        pos = a.pos[i0 + lane];
-    }
-    if (i1 + lane < i2) {
-        key2 = a.key[i1 + lane];
-        pos2 = a.pos[i1 + lane];
-    }
-    const uint32_t before0 = i0 > 0 ? a.key[i0 - 1] : ~0u, before1 = before > 0 ? a.key[before - 1] : ~0u;
-    // the sum in hand belongs to a row with entries before this piece
-    bool head = v < a.rows && before0 == static_cast<uint32_t>(v);
-    int skip = 0;  // entries that the piece before takes
-    if (head && before1 != static_cast<uint32_t>(v) && v < v1) {
-        // the row began in the piece before and ends here: that piece finishes it
-        skip = __popc(__ballot_sync(~0u, key == static_cast<uint32_t>(v)));
+    const int i0 = static_cast<int>(piece * kPiece);
+    const uint32_t none = ~0u;
+    // this piece's entries and those of the next, one a lane, and the keys of the entries before this piece, before the
+    // one before it, and behind the next
+    const uint2 e = i0 + lane < a.n ? a.list[i0 + lane] : make_uint2(none, 0);
+    const uint2 e2 = i0 + kPiece + lane < a.n ? a.list[i0 + kPiece + lane] : make_uint2(none, 0);
+    const uint32_t before0 = i0 > 0 ? a.list[i0 - 1].x : none, before1 = i0 > kPiece ? a.list[i0 - kPiece - 1].x : none;
+    const uint32_t behind2 = i0 + 2 * kPiece < a.n ? a.list[i0 + 2 * kPiece].x : none;
+    const uint32_t first = __shfl_sync(~0u, e.x, 0), last = __shfl_sync(~0u, e.x, kPiece - 1), next = __shfl_sync(~0u, e2.x, 0);
+    // entries behind the last row's (invalid and padding ids) are left out
+    const int own = __popc(__ballot_sync(~0u, e.x < static_cast<uint32_t>(a.rows)));
+    if (!own) return;
+    const uint32_t same = __ballot_sync(~0u, e.x == first);
+    bool head = before0 == first;  // the first run has entries before this piece
+    int skip = 0;
+    // a run that began in the piece before and ends here is finished there
+    if (head && before1 != first && !(same == ~0u && next == first)) {
+        skip = __popc(same);
         head = false;
-        ++v;
     }
-    // the row left open at the end of this piece ends in the next one: finished here, if it began here
+    // the last run, if it goes on in the next piece: finished here, if it began here and ends there
     int more = 0;
-    const uint32_t open = static_cast<uint32_t>(v1);
-    if (v1 < a.rows && v1 < v2 && (v < v1 || !head)) {
-        const uint32_t last_key = i1 > 0 ? a.key[i1 - 1] : ~0u;
-        if (last_key == open && i1 > i0 + skip) {
-            more = __popc(__ballot_sync(~0u, key2 == open));
-            ++v1;
+    bool open = own == kPiece && next == last;
+    if (open && skip < kPiece && !(head && same == ~0u)) {
+        const uint32_t on = __ballot_sync(~0u, e2.x == last);
+        if (!(on == ~0u && behind2 == last)) {
+            more = __popc(on);
+            open = false;
         }
     }
-    if (head && v < v1 && slice == 0 && lane == 0) a.joins[1 + atomicAdd(a.joins, 1)] = static_cast<int>(piece);
+    if (skip == kPiece) open = false;
     float acc[N];
 #pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] = 0.f;
-    auto end_row = [&] {
+    for (int q = 0; q < N; ++q) acc[q] = 0.f;
+    auto end_run = [&](uint32_t row) {
         if (live) {
             if (head) {
                 float *to = a.part + piece * 2 * a.width + c * N;
 #pragma unroll
-                for (int e = 0; e < N; ++e) to[e] = acc[e];
+                for (int q = 0; q < N; ++q) to[q] = acc[q];
             } else {
                 Pack<O, N> o;
                 float f[N];
 #pragma unroll
-                for (int e = 0; e < N; ++e) f[e] = acc[e] * a.scale;
+                for (int q = 0; q < N; ++q) f[q] = acc[q] * a.scale;
                 pack(f, o);
-                store_stream<O, N>(dtable + static_cast<int64_t>(v) * a.dtable_stride, o);
+                store_stream<O, N>(dtable + static_cast<int64_t>(row) * a.dtable_stride, o);
             }
         }
+        if (head && slice == 0 && lane == 0) a.joins[1 + atomicAdd(a.joins, 1)] = static_cast<int>(piece);
         head = false;
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] = 0.f;
-        ++v;
+        for (int q = 0; q < N; ++q) acc[q] = 0.f;
     };
-    // entries behind the last row's (invalid and padding ids) are left out
-    const int own = __popc(__ballot_sync(~0u, key < static_cast<uint32_t>(a.rows))), count = own + more;
+    const int count = own + more;
+    if (skip >= count) return;
+    uint32_t run = skip < own ? __shfl_sync(~0u, e.x, skip) : last;
     for (int q0 = skip; q0 < count; q0 += kFlight) {
         Pack<T, N> x[kFlight];
 #pragma unroll
         for (int q = 0; q < kFlight; ++q) {
             const int at = q0 + q;
-            const uint32_t row = at < own ? __shfl_sync(~0u, pos, at & 31) : __shfl_sync(~0u, pos2, (at - own) & 31);
+            const uint32_t row = at < own ? __shfl_sync(~0u, e.y, at & 31) : __shfl_sync(~0u, e2.y, (at - own) & 31);
             x[q].raw = {};
             if (live && at < count) x[q] = load_stream<T, N>(dout + static_cast<int64_t>(row) * a.dout_stride);
         }
@@ -371,24 +408,28 @@ template <typename T, typename O, int N> __global__ void __launch_bounds__(kSumT
         for (int q = 0; q < kFlight; ++q) {
             const int at = q0 + q;
             if (at >= count) break;
-            const uint32_t k = at < own ? __shfl_sync(~0u, key, at & 31) : open;
-            while (v < static_cast<int>(k)) end_row();
+            const uint32_t k = at < own ? __shfl_sync(~0u, e.x, at & 31) : last;
+            if (k != run) {
+                end_run(run);
+                run = k;
+            }
             float f[N];
             unpack(x[q], f);
 #pragma unroll
-            for (int e = 0; e < N; ++e) acc[e] += f[e];
+            for (int d = 0; d < N; ++d) acc[d] += f[d];
         }
     }
-    while (v < v1) end_row();
-    if (live && v < a.rows) {
+    if (!open) {
+        end_run(run);
+    } else if (live) {
         float *to = a.part + (piece * 2 + 1) * a.width + c * N;
 #pragma unroll
-        for (int e = 0; e < N; ++e) to[e] = acc[e];
+        for (int q = 0; q < N; ++q) to[q] = acc[q];
     }
 }
 
-// The rows that span pieces: the parts of the pieces before the one that ends the row, then that one's.  A CTA takes 64
-// columns of a row, 16 threads 4 columns each, in 16 strided sums over the pieces that are then added in order.
+// The runs over three pieces and more: the parts of the pieces before the one that ends the run, then that one's.  A CTA takes
+// 64 columns of a row, 16 threads 4 columns each, in 16 strided sums over the pieces that are then added in order.
 constexpr int kJoinColumns = 64;
 constexpr int kJoinCtas = 608;
 template <typename O> __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(SumArgs a) {
@@ -399,36 +440,34 @@ template <typename O> __global__ void __launch_bounds__(kSumThreads) embed_join_
     for (int64_t job = blockIdx.x; job < static_cast<int64_t>(count) * chunks; job += gridDim.x) {
         const int64_t piece = a.joins[1 + job / chunks];
         const int c0 = static_cast<int>(job % chunks) * kJoinColumns;
-        const int v = static_cast<int>(piece * kPiece - a.piece_start[piece]);
-        // the first piece with entries of row v: its first entry's, at step lo + v; a warp tries 32 places at a time
-        int lo = 0, hi = a.piece_start[piece];
+        const uint32_t row = a.list[piece * kPiece].x;
+        // the run's first entry; a warp tries 32 places at a time
+        int lo = 0, hi = static_cast<int>(piece * kPiece);
         while (lo < hi) {
             const int stride = (hi - lo + 31) / 32, at = lo + (threadIdx.x & 31) * stride;
-            const uint32_t below = __ballot_sync(~0u, at < hi && a.key[at < hi ? at : hi - 1] < static_cast<uint32_t>(v));
+            const uint32_t below = __ballot_sync(~0u, at < hi && a.list[at < hi ? at : hi - 1].x < row);
             if (!below) break;
-            const int top = __popc(below) - 1;  // the last place whose key is below v
-            const int from = lo + top * stride;
+            const int from = lo + (__popc(below) - 1) * stride;  // the last place whose key is below
             hi = from + stride < hi ? from + stride : hi;
             lo = from + 1;
         }
-        const int64_t first = (static_cast<int64_t>(lo) + v) / kPiece;
         float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int64_t p = first + group; p <= piece; p += 16) {
+        for (int64_t p = lo / kPiece + group; p <= piece; p += 16) {
             const float *from = a.part + (p * 2 + (p < piece)) * a.width + c0 + column;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (c0 + column + e < a.width) s[e] += from[e];
+            for (int q = 0; q < 4; ++q)
+                if (c0 + column + q < a.width) s[q] += from[q];
         }
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sums[group][column + e] = s[e];
+        for (int q = 0; q < 4; ++q) sums[group][column + q] = s[q];
         __syncthreads();
         if (threadIdx.x < kJoinColumns && c0 + static_cast<int>(threadIdx.x) < a.width) {
             float t = 0.f;
 #pragma unroll
             for (int g = 0; g < 16; ++g) t += sums[g][threadIdx.x];
-            static_cast<O *>(a.dtable)[static_cast<int64_t>(v) * a.dtable_stride + c0 + threadIdx.x] = from_f32<O>(t * a.scale);
+            static_cast<O *>(a.dtable)[static_cast<int64_t>(row) * a.dtable_stride + c0 + threadIdx.x] = from_f32<O>(t * a.scale);
         }
     }
 }
@@ -449,14 +488,31 @@ int key_bits(int64_t rows) {  // keys 0 .. rows
     return b;
 }
 
-int64_t piece_count(int64_t n, int64_t rows) { return (n + rows + kPiece - 1) / kPiece; }
+// CTAs that write zeros while the sort's cluster works: the clusters that are resident at once, without that one.
+cudaError_t zero_ctas(int *parts) {
+    static std::atomic<int> known[64];
+    int dev = 0, clusters = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64 && (*parts = known[dev].load(std::memory_order_relaxed)) > 0) return cudaSuccess;
+    if ((e = allow_shared<embed_sort_kernel>(kSortMostShared)) != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kSortCtas);
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.dynamicSmemBytes = kSortMostShared;
+    if ((e = cudaOccupancyMaxActiveClusters(&clusters, embed_sort_kernel, &cfg)) != cudaSuccess) return e;
+    *parts = kSortCtas * std::max(1, clusters - 1);
+    if (dev >= 0 && dev < 64) known[dev].store(*parts, std::memory_order_relaxed);
+    return cudaSuccess;
+}
+
+int64_t piece_count(int64_t n) { return (n + kPiece - 1) / kPiece; }
 
 size_t round16(size_t x) { return (x + 15) & ~static_cast<size_t>(15); }
 
-size_t grad_workspace(int64_t n, int64_t rows, int width) {
-    const size_t pieces = static_cast<size_t>(piece_count(n, rows));
-    return 4 * round16(static_cast<size_t>(n) * 4) + 2 * round16((pieces + 1) * 4) +
-           round16(pieces * 2 * width * sizeof(float));
+size_t grad_workspace(int64_t n, int width) {
+    const size_t pieces = static_cast<size_t>(piece_count(n));
+    return 2 * round16(static_cast<size_t>(n) * 8) + round16((pieces + 1) * 4) + round16(pieces * 2 * width * sizeof(float));
 }
 
 ccq_status check_sizes(int64_t n, int64_t rows, int width) {
@@ -469,8 +525,8 @@ ccq_status check_sizes(int64_t n, int64_t rows, int width) {
 ccq_status check_grad_sizes(int64_t n, int64_t rows, int width) {
     ccq_status st = check_sizes(n, rows, width);
     if (st != CCQ_OK) return st;
-    if (n > (1 << 30) || rows > (1 << 30))
-        return op_fail(CCQ_ERR_UNSUPPORTED, "n=%lld rows=%lld: supported up to 2^30", static_cast<long long>(n),
+    if (n > (1 << 30) || rows > (1 << 23))
+        return op_fail(CCQ_ERR_UNSUPPORTED, "n=%lld rows=%lld: supported up to 2^30 and 2^23", static_cast<long long>(n),
                        static_cast<long long>(rows));
     return CCQ_OK;
 }
@@ -526,7 +582,7 @@ ccq_status ccq_embed_grad_workspace_size(int64_t n, int64_t rows, int width, siz
     ccq_status st = check_grad_sizes(n, rows, width);
     if (st != CCQ_OK) return st;
     if (!bytes) return op_fail(CCQ_ERR_INVALID_ARG, "bytes is NULL");
-    *bytes = grad_workspace(n, rows, width);
+    *bytes = grad_workspace(n, width);
     return CCQ_OK;
 }
 
@@ -543,13 +599,14 @@ ccq_status ccq_embed_grad(const void *dout, ccq_dtype dtype, int64_t dout_stride
     if (padding_id >= rows)
         return op_fail(CCQ_ERR_INVALID_ARG, "padding_id=%lld is outside the table of %lld rows",
                        static_cast<long long>(padding_id), static_cast<long long>(rows));
-    const size_t need = grad_workspace(n, rows, width);
+    const size_t need = grad_workspace(n, width);
     if ((st = op_pointer("workspace", workspace, 16)) != CCQ_OK) return st;
     if (workspace_bytes < need)
         return op_fail(CCQ_ERR_INVALID_ARG, "workspace of %zu bytes, needs %zu", workspace_bytes, need);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const size_t list = round16(static_cast<size_t>(n) * 4);
+    const size_t list = round16(static_cast<size_t>(n) * 8);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
+    const int eo = dtype_bytes(grad_dtype), out_bytes = row_access(dtable, dtable_stride, eo, rows, access_bytes(static_cast<uintptr_t>(width) * eo));
     SortArgs so = {};
     so.ids = ids;
     so.id_bytes = id_bytes;
@@ -559,39 +616,38 @@ ccq_status ccq_embed_grad(const void *dout, ccq_dtype dtype, int64_t dout_stride
     const int bits = key_bits(rows);
     so.passes = (bits + kMaxDigit - 1) / kMaxDigit;
     so.digit = (bits + so.passes - 1) / so.passes;
-    for (int k = 0; k < 2; ++k) {
-        so.key[k] = reinterpret_cast<uint32_t *>(ws + (2 * k) * list);
-        so.pos[k] = reinterpret_cast<uint32_t *>(ws + (2 * k + 1) * list);
-    }
+    for (int k = 0; k < 2; ++k) so.list[k] = reinterpret_cast<uint2 *>(ws + k * list);
+    so.joins = reinterpret_cast<int *>(ws + 2 * list);
     so.status = device_status_word();
-    so.pieces = static_cast<int>(piece_count(n, rows));
-    so.piece_start = reinterpret_cast<int *>(ws + 4 * list);
-    const size_t starts = round16((static_cast<size_t>(so.pieces) + 1) * 4);
-    so.joins = reinterpret_cast<int *>(ws + 4 * list + starts);
-    const size_t smem = (kSortWarps + kSortCtas) * (static_cast<size_t>(1) << so.digit) * sizeof(uint32_t);
-    cudaError_t e = allow_shared<embed_sort_kernel>((kSortWarps + kSortCtas) * (1 << kMaxDigit) * static_cast<int>(sizeof(uint32_t)));
+    so.dtable = static_cast<uint8_t *>(dtable);
+    so.row_bytes = static_cast<int64_t>(width) * eo;
+    so.row_stride = dtable_stride * eo;
+    so.access = out_bytes;
+    int parts = 0;
+    cudaError_t e = zero_ctas(&parts);
     if (e != cudaSuccess) return op_cuda(e, "sort kernel attribute");
-    embed_sort_kernel<<<kSortCtas, kSortThreads, smem, s>>>(so);
+    so.present_words = static_cast<int>((rows + static_cast<int64_t>(parts) * 32 - 1) / (static_cast<int64_t>(parts) * 32));
+    const size_t slots = sort_holds(so.n) ? static_cast<size_t>(warp_entries(so.n)) * kSortWarps : 0;
+    const size_t smem = std::max(sort_shared_words(so.digit) * sizeof(uint32_t) + 8 + slots * sizeof(uint2), so.present_words * sizeof(uint32_t));
+    embed_sort_kernel<<<kSortCtas + parts, kSortThreads, smem, s>>>(so);
     if ((e = cudaGetLastError()) != cudaSuccess) return op_cuda(e, "sort launch");
+    if (n == 0) return CCQ_OK;
     SumArgs a = {};
     a.dout = dout;
     a.dout_stride = dout_stride;
-    a.key = so.key[(so.passes + 1) & 1];
-    a.pos = so.pos[(so.passes + 1) & 1];
+    a.list = so.list[sort_holds(so.n) ? 0 : (so.passes - 1) & 1];
     a.n = so.n;
     a.rows = static_cast<int>(rows);
     a.width = width;
     a.scale = scale;
     a.dtable = dtable;
     a.dtable_stride = dtable_stride;
-    a.piece_start = so.piece_start;
     a.joins = so.joins;
-    a.part = reinterpret_cast<float *>(ws + 4 * list + 2 * starts);
-    a.pieces = so.pieces;
-    const int es = dtype_bytes(dtype), eo = dtype_bytes(grad_dtype);
+    a.pieces = static_cast<int>(piece_count(n));
+    a.part = reinterpret_cast<float *>(ws + 2 * list + round16((static_cast<size_t>(a.pieces) + 1) * 4));
+    const int es = dtype_bytes(dtype);
     // elements an access may hold in both operands, at most 16 bytes of the wider type
-    int b = row_access(dtable, dtable_stride, eo, rows, access_bytes(static_cast<uintptr_t>(width) * eo)) / eo;
-    if (n > 0) b = std::min(b, row_access(dout, dout_stride, es, n, access_bytes(static_cast<uintptr_t>(width) * es)) / es);
+    const int b = std::min(out_bytes / eo, row_access(dout, dout_stride, es, n, access_bytes(static_cast<uintptr_t>(width) * es)) / es);
     using B = __nv_bfloat16;
     if (dtype == CCQ_BF16 && grad_dtype == CCQ_BF16)
         e = b >= 8 ? launch_sum<B, B, 8>(a, s) : b >= 2 ? launch_sum<B, B, 2>(a, s) : launch_sum<B, B, 1>(a, s);
