@@ -5,7 +5,7 @@
 //
 // Gradient: dtable[r] = scale * sum of dout[i] over the i with ids[i] = r.  Each row of dout is read
 // once and each row of dtable written once; no sum depends on the order of atomics:
-//   1. embed_sort_kernel: one cluster of 8 CTAs sorts (id, i) stably, all passes in one launch; meanwhile the other CTAs
+//   1. embed_sort_kernel: one cluster of CTAs sorts (id, i) stably, all passes in one launch; the clusters beside it
 //      write the rows that no id names (most of a vocabulary's), which hides the sort's latency.
 //   2. embed_sum_kernel: the sorted entries are cut into pieces of kPiece, so that frequent ids cost no
 //      more than others.  A warp takes a piece of a column slice, adds its entries and writes a row where its
@@ -32,32 +32,44 @@ __global__ void __launch_bounds__(kLookupThreads) embed_kernel(const T *__restri
                                                                int64_t out_stride, int *status) {
     const int64_t first = (static_cast<int64_t>(blockIdx.x) * kLookupRows) * blockDim.y + threadIdx.y;
     int64_t id[kLookupRows];
+    bool known[kLookupRows];
 #pragma unroll
     for (int r = 0; r < kLookupRows; ++r) {
         const int64_t i = first + r * blockDim.y;
-        id[r] = i < n ? load_index(ids, id_bytes, i) : -1;
-        if (i < n && (id[r] < 0 || id[r] >= rows)) {
-            id[r] = -1;
-            if (threadIdx.x == 0 && blockIdx.y == 0) note_index(status);
+        id[r] = i < n ? load_index(ids, id_bytes, i) : 0;
+        known[r] = id[r] >= 0 && id[r] < rows;
+        if (!known[r]) {
+            id[r] = 0;
+            if (threadIdx.x == 0) note_index(status);
         }
     }
-    for (int c = blockIdx.y * blockDim.x + threadIdx.x; c < packs; c += gridDim.y * blockDim.x) {
-        Pack<T, N> v[kLookupRows];
+    constexpr int K = N * sizeof(T) <= 4 ? 4 : 1;  // columns at once: narrow accesses need more of them
+    for (int c0 = threadIdx.x; c0 < packs; c0 += K * blockDim.x) {
+        Pack<T, N> v[kLookupRows][K];
 #pragma unroll
         for (int r = 0; r < kLookupRows; ++r) {
-            v[r].raw = {};
-            if (id[r] >= 0) v[r] = load_plain<T, N>(table + id[r] * table_stride + static_cast<int64_t>(c) * N);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                // (without conditions, so that all loads stay under way: past the end the last access, for an id outside row 0)
+                const int c = min(c0 + k * static_cast<int>(blockDim.x), packs - 1);
+                v[r][k] = load_plain<T, N>(table + id[r] * table_stride + static_cast<int64_t>(c) * N);
+            }
         }
 #pragma unroll
         for (int r = 0; r < kLookupRows; ++r) {
             const int64_t i = first + r * blockDim.y;
             if (i >= n) continue;
-            float f[N];
-            unpack(v[r], f);
 #pragma unroll
-            for (int e = 0; e < N; ++e) f[e] *= scale;
-            pack(f, v[r]);
-            store_stream<T, N>(out + i * out_stride + static_cast<int64_t>(c) * N, v[r]);
+            for (int k = 0; k < K; ++k) {
+                const int c = c0 + k * blockDim.x;
+                if (c >= packs) continue;
+                float f[N];
+                unpack(v[r][k], f);
+#pragma unroll
+                for (int e = 0; e < N; ++e) f[e] = known[r] ? f[e] * scale : 0.f;
+                pack(f, v[r][k]);
+                store_stream<T, N>(out + i * out_stride + static_cast<int64_t>(c) * N, v[r][k]);
+            }
         }
     }
 }
@@ -69,7 +81,7 @@ cudaError_t launch_embed(const void *table, int64_t table_stride, const void *id
     int tx = 32;
     while (tx < kLookupThreads && tx < packs) tx *= 2;
     const int ty = kLookupThreads / tx;
-    const dim3 grid(static_cast<unsigned>((n + ty * kLookupRows - 1) / (ty * kLookupRows)), 1);
+    const unsigned grid = static_cast<unsigned>((n + ty * kLookupRows - 1) / (ty * kLookupRows));
     embed_kernel<T, N><<<grid, dim3(tx, ty), 0, s>>>(
         static_cast<const T *>(table), table_stride, ids, id_bytes, n, rows, packs, scale, static_cast<T *>(out),
         out_stride, device_status_word());
@@ -78,7 +90,7 @@ cudaError_t launch_embed(const void *table, int64_t table_stride, const void *id
 
 // ---------------------------------------------------------------- sort
 
-constexpr int kSortCtas = 8;
+constexpr int kMostCtas = 16;  // of the sort's cluster
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kMaxDigit = 9;  // bits of a pass
@@ -92,18 +104,19 @@ struct SortArgs {
     int64_t rows, padding;
     int passes, digit;
     uint2 *list[2];    // (key, position); the last pass writes list[(passes - 1) & 1], or list[0] where entries are held
-    int *joins;  // count, then the pieces that end a run over three pieces and more (embed_sum_kernel)
+    int *joins;  // their count, set to 0 (embed_sum_kernel)
     int *status;
+    int ctas;  // of a cluster
     uint8_t *dtable;  // the CTAs behind the first cluster write its rows without entries
     int64_t row_bytes, row_stride;
     int access, present_words;  // bytes of a store, and words of a CTA's bitmap of its rows
 };
 
 // Entries of a warp, a multiple of 32.
-__host__ __device__ inline int warp_entries(int n) { return ((n + kSortCtas * kSortWarps - 1) / (kSortCtas * kSortWarps) + 31) & ~31; }
-__host__ __device__ inline bool sort_holds(int n) { return warp_entries(n) <= 32 * kHeld; }
-constexpr int kSortMostShared = 204800;  // bytes; bounds the rows too (a bitmap of each CTA's)
-inline int sort_shared_words(int digit) { return kSortWarps * ((1 << digit) + 1) + (kSortCtas + 1) * (1 << digit); }
+__host__ __device__ inline int warp_entries(int n, int ctas) { return ((n + ctas * kSortWarps - 1) / (ctas * kSortWarps) + 31) & ~31; }
+__host__ __device__ inline bool sort_holds(int n, int ctas) { return warp_entries(n, ctas) <= 32 * kHeld; }
+constexpr int kSortMostShared = 204800;  // bytes
+inline int sort_shared_words(int digit, int ctas) { return kSortWarps * ((1 << digit) + 1) + (ctas + 1) * (1 << digit); }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
@@ -112,23 +125,19 @@ __device__ __forceinline__ uint32_t cluster_address(const void *p, int cta) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(cta));
     return a;
 }
-__device__ __forceinline__ void cluster_store(uint32_t *p, int cta, uint32_t v) {
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_address(p, cta)), "r"(v) : "memory");
+__device__ __forceinline__ void cluster_store(uint4 *p, int cta, uint4 v) {
+    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_address(p, cta)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+                 : "memory");
 }
 __device__ __forceinline__ void cluster_store(uint2 *p, int cta, uint2 v) {
     asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(cluster_address(p, cta)), "r"(v.x), "r"(v.y) : "memory");
 }
 // Zeros to the rows that no id names: CTA `part` of `parts` looks after the rows r with r % parts = part.
-__device__ __forceinline__ void zero_absent_rows(const SortArgs &a, int part, int parts, uint32_t *present) {
+__device__ __forceinline__ void zero_absent_rows(const SortArgs &a, uint32_t part, uint32_t parts, uint32_t *present) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t mine = a.rows > part ? (a.rows - part + parts - 1) / parts : 0;
     for (int w = tid; w < a.present_words; w += kSortThreads) present[w] = 0;
     __syncthreads();
-    auto see = [&](int64_t id) {
-        if (id < 0 || id >= a.rows || id == a.padding) return;
-        const uint32_t r = static_cast<uint32_t>(id), q = r / static_cast<uint32_t>(parts);
-        if (r - q * parts == static_cast<uint32_t>(part)) atomicOr(&present[q >> 5], 1u << (q & 31));
-    };
     constexpr int kAtOnce = 8;
     for (int i0 = tid; i0 < a.n; i0 += kAtOnce * kSortThreads) {
         int64_t id[kAtOnce];
@@ -138,7 +147,11 @@ __device__ __forceinline__ void zero_absent_rows(const SortArgs &a, int part, in
             id[q] = i >= a.n ? -1 : a.id_bytes == 8 ? static_cast<const int64_t *>(a.ids)[i] : static_cast<const int32_t *>(a.ids)[i];
         }
 #pragma unroll
-        for (int q = 0; q < kAtOnce; ++q) see(id[q]);
+        for (int q = 0; q < kAtOnce; ++q) {
+            if (id[q] < 0 || id[q] >= a.rows || id[q] == a.padding) continue;
+            const uint32_t r = static_cast<uint32_t>(id[q]), at = r / parts;
+            if (r - at * parts == part) atomicOr(&present[at >> 5], 1u << (at & 31));
+        }
     }
     __syncthreads();
     for (int64_t q = warp; q < mine; q += kSortWarps) {
@@ -160,27 +173,28 @@ __device__ __forceinline__ void zero_absent_rows(const SortArgs &a, int part, in
 // five barriers each.  A lane finds the others with its digit by a ballot for each bit (match.any takes a time that grows with
 // the number of different digits, 2000 cycles a step for 32 warps of random ones), and up to 65536 entries pass from CTA to
 // CTA in shared memory (through global memory a pass took 6000 cycles for its stores and loads alone).
-__global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads) embed_sort_kernel(SortArgs a) {
+__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortArgs a) {
     extern __shared__ __align__(16) uint32_t smem[];
-    if (blockIdx.x >= kSortCtas) {  // (whole clusters)
-        zero_absent_rows(a, blockIdx.x - kSortCtas, gridDim.x - kSortCtas, smem);
+    const int ctas = a.ctas;
+    if (static_cast<int>(blockIdx.x) >= ctas) {  // (whole clusters)
+        zero_absent_rows(a, blockIdx.x - ctas, gridDim.x - ctas, smem);
         return;
     }
     const int bins = 1 << a.digit, row = bins + 1;  // (a column of counts spans all banks)
     uint32_t *counts = smem;                         // [kSortWarps][row]: a warp's entries, then those of the warps before it
-    uint32_t *totals = counts + kSortWarps * row;    // [kSortCtas][bins]: every CTA's entries
-    uint32_t *base = totals + kSortCtas * bins;      // [bins]: this CTA's first slot
-    uint2 *xchg = reinterpret_cast<uint2 *>(smem + ((kSortWarps * row + (kSortCtas + 1) * bins + 1) & ~1));  // this CTA's slots
+    uint32_t *totals = counts + kSortWarps * row;    // [ctas][bins]: every CTA's entries (16-byte aligned: 32 rows)
+    uint32_t *base = totals + ctas * bins;      // [bins]: this CTA's entries, then its first slot
+    uint2 *xchg = reinterpret_cast<uint2 *>(smem + ((kSortWarps * row + (ctas + 1) * bins + 1) & ~1));  // this CTA's slots
     __shared__ uint32_t scan[kSortWarps];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
-    const int per = warp_entries(a.n), mine_slots = per * kSortWarps;
-    const bool held = sort_holds(a.n);
+    const int per = warp_entries(a.n, ctas), mine_slots = per * kSortWarps;
+    const bool held = sort_holds(a.n, ctas);
     const int64_t lo64 = static_cast<int64_t>(cta * kSortWarps + warp) * per;
     const int lo = static_cast<int>(lo64 < a.n ? lo64 : a.n);
     const int hi = lo + (a.n - lo < per ? a.n - lo : per);
     uint32_t *mine = counts + warp * row;
     cluster_arrive();  // waited for before the first store to another CTA: all run by then
-    if (cta == 0 && tid == 0) a.joins[0] = 0;
+    if (cta == 0 && tid == 0) *a.joins = 0;
     auto key_from = [&](int64_t id) -> uint32_t {
         if (id < 0 || id >= a.rows) {
             note_index(a.status);
@@ -242,25 +256,40 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
         }
         __syncthreads();
         if (pass == 0) cluster_wait();
-        // a warp scans the warps' counts of a bin, a lane each, and tells every CTA this one's total
-        for (int bin = warp; bin < bins; bin += kSortWarps) {
-            const uint32_t own = counts[lane * row + bin];
-            uint32_t inc = own;
+        // counts become those of the warps before; four lanes share a bin's 32 (their banks differ)
+        for (int bin = tid >> 2; bin < bins; bin += kSortThreads / 4) {
+            constexpr int kShare = kSortWarps / 4;
+            uint32_t *from = counts + (tid & 3) * kShare * row + bin, c[kShare], sum = 0;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t t = __shfl_up_sync(~0u, inc, o);
-                if (lane >= o) inc += t;
+            for (int w = 0; w < kShare; ++w) c[w] = from[w * row];
+#pragma unroll
+            for (int w = 0; w < kShare; ++w) sum += c[w];
+            uint32_t inc = sum;
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) {
+                const uint32_t t = __shfl_up_sync(0xfu << (lane & 28), inc, o, 4);
+                if ((tid & 3) >= o) inc += t;
             }
-            counts[lane * row + bin] = inc - own;
-            const uint32_t total = __shfl_sync(~0u, inc, 31);
-            if (lane < kSortCtas) cluster_store(&totals[cta * bins + bin], lane, total);
+            if ((tid & 3) == 3) base[bin] = inc;
+            uint32_t at = inc - sum;
+#pragma unroll
+            for (int w = 0; w < kShare; ++w) {
+                from[w * row] = at;
+                at += c[w];
+            }
+        }
+        __syncthreads();
+        // this CTA's entries of every bin to all CTAs, four bins a store
+        for (int q = tid; q < ctas * bins / 4; q += kSortThreads) {
+            const int to = q / (bins / 4), quad = q - to * (bins / 4);
+            cluster_store(reinterpret_cast<uint4 *>(&totals[cta * bins]) + quad, to, reinterpret_cast<const uint4 *>(base)[quad]);
         }
         cluster_arrive();
         cluster_wait();
         uint32_t all = 0, before = 0;
         if (tid < bins) {
-#pragma unroll
-            for (int c = 0; c < kSortCtas; ++c) {
+#pragma unroll 4
+            for (int c = 0; c < ctas; ++c) {
                 const uint32_t t = totals[c * bins + tid];
                 if (c < cta) before += t;
                 all += t;
@@ -314,7 +343,8 @@ struct SumArgs {
     const void *dout;
     int64_t dout_stride;
     const uint2 *list;  // sorted (key, position)
-    int *joins;
+    int *count;   // of joins
+    int2 *joins;  // (first, last piece) of the runs over three pieces and more
     int n, rows, width, packs;
     float scale;
     void *dtable;
@@ -325,18 +355,24 @@ struct SumArgs {
 
 constexpr int kSumThreads = 256;
 
-template <typename T, typename O, int N> __global__ void __launch_bounds__(kSumThreads, 4) embed_sum_kernel(SumArgs a) {
+template <typename T, typename O, int N> __global__ void __launch_bounds__(kSumThreads, N <= 2 ? 3 : 4) embed_sum_kernel(SumArgs a) {
+    constexpr int K = N <= 2 ? 4 : 1;        // accesses of a lane
     constexpr int kFlight = N >= 8 ? 4 : 8;  // entries whose loads are under way at once
     grid_wait();
     const int lane = threadIdx.x & 31;
-    const int slices = (a.packs + 31) / 32;
+    const int slices = (a.packs + 32 * K - 1) / (32 * K);
     const int64_t warp = static_cast<int64_t>(blockIdx.x) * (kSumThreads / 32) + (threadIdx.x >> 5);
     const int64_t piece = warp / slices;
     if (piece >= a.pieces) return;
     const int slice = static_cast<int>(warp - piece * slices);
-    const int c = slice * 32 + lane;
-    const bool live = c < a.packs;
-    const T *dout = static_cast<const T *>(a.dout) + static_cast<int64_t>(c) * N;
+    const int c = slice * 32 * K + lane;
+    const int live = c < a.packs ? (a.packs - c + 31) / 32 : 0;  // accesses of this lane within the row (K or more: all)
+    // Loads are made without conditions, so that all stay under way: a lane past the row's end reads its last access, and what
+    // is past the last entry the batch's first.
+    const T *dout = static_cast<const T *>(a.dout);
+    int offset[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) offset[j] = (c + 32 * j < a.packs ? c + 32 * j : a.packs - 1) * N;
     O *dtable = static_cast<O *>(a.dtable) + static_cast<int64_t>(c) * N;
     const int i0 = static_cast<int>(piece * kPiece);
     const uint32_t none = ~0u;
@@ -369,40 +405,65 @@ template <typename T, typename O, int N> __global__ void __launch_bounds__(kSumT
         }
     }
     if (skip == kPiece) open = false;
-    float acc[N];
+    float acc[K][N];
+    auto clear = [&] {
 #pragma unroll
-    for (int q = 0; q < N; ++q) acc[q] = 0.f;
+        for (int j = 0; j < K; ++j)
+#pragma unroll
+            for (int q = 0; q < N; ++q) acc[j][q] = 0.f;
+    };
+    auto leave = [&](int which) {  // the sums to the workspace
+        float *to = a.part + (piece * 2 + which) * a.width + c * N;
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+            if (j < live)
+#pragma unroll
+                for (int q = 0; q < N; ++q) to[j * 32 * N + q] = acc[j][q];
+    };
+    clear();
     auto end_run = [&](uint32_t row) {
-        if (live) {
-            if (head) {
-                float *to = a.part + piece * 2 * a.width + c * N;
+        if (head) {
+            leave(0);
+        } else {
 #pragma unroll
-                for (int q = 0; q < N; ++q) to[q] = acc[q];
-            } else {
+            for (int j = 0; j < K; ++j) {
+                if (j >= live) continue;
                 Pack<O, N> o;
                 float f[N];
 #pragma unroll
-                for (int q = 0; q < N; ++q) f[q] = acc[q] * a.scale;
+                for (int q = 0; q < N; ++q) f[q] = acc[j][q] * a.scale;
                 pack(f, o);
-                store_stream<O, N>(dtable + static_cast<int64_t>(row) * a.dtable_stride, o);
+                store_stream<O, N>(dtable + static_cast<int64_t>(row) * a.dtable_stride + j * 32 * N, o);
             }
         }
-        if (head && slice == 0 && lane == 0) a.joins[1 + atomicAdd(a.joins, 1)] = static_cast<int>(piece);
+        if (head && slice == 0) {
+            // for the join: the piece with the run's first entry; the warp tries 32 places at a time
+            int lo = 0, hi = i0;
+            while (lo < hi) {
+                const int stride = (hi - lo + 31) / 32, at = lo + lane * stride;
+                const uint32_t below = __ballot_sync(~0u, at < hi && a.list[at < hi ? at : hi - 1].x < row);
+                if (!below) break;
+                const int from = lo + (__popc(below) - 1) * stride;  // the last place whose key is below
+                hi = from + stride < hi ? from + stride : hi;
+                lo = from + 1;
+            }
+            if (lane == 0) a.joins[atomicAdd(a.count, 1)] = make_int2(lo / kPiece, static_cast<int>(piece));
+        }
         head = false;
-#pragma unroll
-        for (int q = 0; q < N; ++q) acc[q] = 0.f;
+        clear();
     };
     const int count = own + more;
     if (skip >= count) return;
     uint32_t run = skip < own ? __shfl_sync(~0u, e.x, skip) : last;
     for (int q0 = skip; q0 < count; q0 += kFlight) {
-        Pack<T, N> x[kFlight];
+        Pack<T, N> x[kFlight][K];
 #pragma unroll
         for (int q = 0; q < kFlight; ++q) {
-            const int at = q0 + q;
+            const int at = q0 + q < count ? q0 + q : q0;
             const uint32_t row = at < own ? __shfl_sync(~0u, e.y, at & 31) : __shfl_sync(~0u, e2.y, (at - own) & 31);
-            x[q].raw = {};
-            if (live && at < count) x[q] = load_stream<T, N>(dout + static_cast<int64_t>(row) * a.dout_stride);
+            const T *from = dout + static_cast<int64_t>(row) * a.dout_stride;
+#pragma unroll
+            for (int j = 0; j < K; ++j) x[q][j] = load_stream<T, N>(from + offset[j]);
         }
 #pragma unroll
         for (int q = 0; q < kFlight; ++q) {
@@ -413,19 +474,17 @@ template <typename T, typename O, int N> __global__ void __launch_bounds__(kSumT
                 end_run(run);
                 run = k;
             }
-            float f[N];
-            unpack(x[q], f);
 #pragma unroll
-            for (int d = 0; d < N; ++d) acc[d] += f[d];
+            for (int j = 0; j < K; ++j) {
+                float f[N];
+                unpack(x[q][j], f);
+#pragma unroll
+                for (int d = 0; d < N; ++d) acc[j][d] += f[d];
+            }
         }
     }
-    if (!open) {
-        end_run(run);
-    } else if (live) {
-        float *to = a.part + (piece * 2 + 1) * a.width + c * N;
-#pragma unroll
-        for (int q = 0; q < N; ++q) to[q] = acc[q];
-    }
+    if (!open) end_run(run);
+    else leave(1);
 }
 
 // The runs over three pieces and more: the parts of the pieces before the one that ends the run, then that one's.  A CTA takes
@@ -435,25 +494,15 @@ constexpr int kJoinCtas = 608;
 template <typename O> __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(SumArgs a) {
     __shared__ float sums[16][kJoinColumns + 1];
     grid_wait();
-    const int count = a.joins[0], chunks = (a.width + kJoinColumns - 1) / kJoinColumns;
+    const int count = *a.count, chunks = (a.width + kJoinColumns - 1) / kJoinColumns;
     const int column = (threadIdx.x & 15) * 4, group = threadIdx.x >> 4;
     for (int64_t job = blockIdx.x; job < static_cast<int64_t>(count) * chunks; job += gridDim.x) {
-        const int64_t piece = a.joins[1 + job / chunks];
-        const int c0 = static_cast<int>(job % chunks) * kJoinColumns;
-        const uint32_t row = a.list[piece * kPiece].x;
-        // the run's first entry; a warp tries 32 places at a time
-        int lo = 0, hi = static_cast<int>(piece * kPiece);
-        while (lo < hi) {
-            const int stride = (hi - lo + 31) / 32, at = lo + (threadIdx.x & 31) * stride;
-            const uint32_t below = __ballot_sync(~0u, at < hi && a.list[at < hi ? at : hi - 1].x < row);
-            if (!below) break;
-            const int from = lo + (__popc(below) - 1) * stride;  // the last place whose key is below
-            hi = from + stride < hi ? from + stride : hi;
-            lo = from + 1;
-        }
+        const int2 span = a.joins[job / chunks];
+        const int piece = span.y, c0 = static_cast<int>(job % chunks) * kJoinColumns;
+        const uint32_t row = a.list[static_cast<int64_t>(piece) * kPiece].x;
         float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int64_t p = lo / kPiece + group; p <= piece; p += 16) {
+        for (int64_t p = span.x + group; p <= piece; p += 16) {
             const float *from = a.part + (p * 2 + (p < piece)) * a.width + c0 + column;
 #pragma unroll
             for (int q = 0; q < 4; ++q)
@@ -474,7 +523,8 @@ template <typename O> __global__ void __launch_bounds__(kSumThreads) embed_join_
 
 template <typename T, typename O, int N> cudaError_t launch_sum(SumArgs a, cudaStream_t s) {
     a.packs = a.width / N;
-    const int64_t warps = static_cast<int64_t>(a.pieces) * ((a.packs + 31) / 32);
+    const int columns = N <= 2 ? 128 : 32;  // accesses of a warp
+    const int64_t warps = static_cast<int64_t>(a.pieces) * ((a.packs + columns - 1) / columns);
     const int per = kSumThreads / 32;
     cudaError_t e = launch_after(embed_sum_kernel<T, O, N>, static_cast<unsigned>((warps + per - 1) / per), kSumThreads,
                                  0, s, a);
@@ -488,21 +538,36 @@ int key_bits(int64_t rows) {  // keys 0 .. rows
     return b;
 }
 
-// CTAs that write zeros while the sort's cluster works: the clusters that are resident at once, without that one.
-cudaError_t zero_ctas(int *parts) {
-    static std::atomic<int> known[64];
-    int dev = 0, clusters = 0;
+// CTAs of the sort's cluster.  More make it faster (16384 ids: about 30, 20 and 16 us with 4, 8 and 16) and leave fewer SMs
+// to write zeros beside it (148, 112, 96): few where the rows that surely have no entry are many, 16 (beyond the
+// portable size) where ids are.  16384 x 2048 into 32000 rows: 70, 74, 80 us; 60000 x 64 into 100000: 82, 53, 47.
+int sort_ctas(int64_t n, int64_t rows, size_t row_bytes) {
+    if (n > 32768) return kMostCtas;
+    return rows > n && static_cast<size_t>(rows - n) * row_bytes > (static_cast<size_t>(64) << 20) ? 4 : 8;
+}
+
+// The sort's launch with clusters of `ctas`; `clusters`: those resident at once, asked for once a device and size.
+cudaError_t sort_config(int ctas, cudaLaunchConfig_t *cfg, cudaLaunchAttribute *at, int *clusters) {
+    static std::atomic<int> known[64][kMostCtas + 1];
+    int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (dev >= 0 && dev < 64 && (*parts = known[dev].load(std::memory_order_relaxed)) > 0) return cudaSuccess;
+    *cfg = {};
+    cfg->gridDim = dim3(ctas);
+    cfg->blockDim = dim3(kSortThreads);
+    cfg->dynamicSmemBytes = kSortMostShared;
+    at->id = cudaLaunchAttributeClusterDimension;
+    at->val.clusterDim.x = ctas;
+    at->val.clusterDim.y = at->val.clusterDim.z = 1;
+    cfg->attrs = at;
+    cfg->numAttrs = 1;
+    const bool keep = dev >= 0 && dev < 64;
+    if (keep && (*clusters = known[dev][ctas].load(std::memory_order_relaxed)) > 0) return cudaSuccess;
     if ((e = allow_shared<embed_sort_kernel>(kSortMostShared)) != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kSortCtas);
-    cfg.blockDim = dim3(kSortThreads);
-    cfg.dynamicSmemBytes = kSortMostShared;
-    if ((e = cudaOccupancyMaxActiveClusters(&clusters, embed_sort_kernel, &cfg)) != cudaSuccess) return e;
-    *parts = kSortCtas * std::max(1, clusters - 1);
-    if (dev >= 0 && dev < 64) known[dev].store(*parts, std::memory_order_relaxed);
+    if ((e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
+    if ((e = cudaOccupancyMaxActiveClusters(clusters, embed_sort_kernel, cfg)) != cudaSuccess) return e;
+    *clusters = std::max(2, *clusters);
+    if (keep) known[dev][ctas].store(*clusters, std::memory_order_relaxed);
     return cudaSuccess;
 }
 
@@ -512,7 +577,7 @@ size_t round16(size_t x) { return (x + 15) & ~static_cast<size_t>(15); }
 
 size_t grad_workspace(int64_t n, int width) {
     const size_t pieces = static_cast<size_t>(piece_count(n));
-    return 2 * round16(static_cast<size_t>(n) * 8) + round16((pieces + 1) * 4) + round16(pieces * 2 * width * sizeof(float));
+    return 2 * round16(static_cast<size_t>(n) * 8) + 16 + round16(pieces * 8) + round16(pieces * 2 * width * sizeof(float));
 }
 
 ccq_status check_sizes(int64_t n, int64_t rows, int width) {
@@ -615,36 +680,45 @@ ccq_status ccq_embed_grad(const void *dout, ccq_dtype dtype, int64_t dout_stride
     so.padding = padding_id;
     const int bits = key_bits(rows);
     so.passes = (bits + kMaxDigit - 1) / kMaxDigit;
-    so.digit = (bits + so.passes - 1) / so.passes;
+    so.digit = std::max(2, (bits + so.passes - 1) / so.passes);  // (bins are told four at a time)
     for (int k = 0; k < 2; ++k) so.list[k] = reinterpret_cast<uint2 *>(ws + k * list);
     so.joins = reinterpret_cast<int *>(ws + 2 * list);
     so.status = device_status_word();
+    so.ctas = sort_ctas(n, rows, static_cast<size_t>(width) * eo);
+    const bool held = sort_holds(so.n, so.ctas);
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute at;
+    int clusters = 0;
+    cudaError_t e = sort_config(so.ctas, &cfg, &at, &clusters);
+    if (e != cudaSuccess) return op_cuda(e, "sort kernel configuration");
+    const int parts = (clusters - 1) * so.ctas;
     so.dtable = static_cast<uint8_t *>(dtable);
     so.row_bytes = static_cast<int64_t>(width) * eo;
     so.row_stride = dtable_stride * eo;
     so.access = out_bytes;
-    int parts = 0;
-    cudaError_t e = zero_ctas(&parts);
-    if (e != cudaSuccess) return op_cuda(e, "sort kernel attribute");
     so.present_words = static_cast<int>((rows + static_cast<int64_t>(parts) * 32 - 1) / (static_cast<int64_t>(parts) * 32));
-    const size_t slots = sort_holds(so.n) ? static_cast<size_t>(warp_entries(so.n)) * kSortWarps : 0;
-    const size_t smem = std::max(sort_shared_words(so.digit) * sizeof(uint32_t) + 8 + slots * sizeof(uint2), so.present_words * sizeof(uint32_t));
-    embed_sort_kernel<<<kSortCtas + parts, kSortThreads, smem, s>>>(so);
-    if ((e = cudaGetLastError()) != cudaSuccess) return op_cuda(e, "sort launch");
+    const size_t slots = held ? static_cast<size_t>(warp_entries(so.n, so.ctas)) * kSortWarps : 0;
+    cfg.gridDim = dim3(so.ctas + parts);
+    cfg.dynamicSmemBytes = std::max(sort_shared_words(so.digit, so.ctas) * sizeof(uint32_t) + 8 + slots * sizeof(uint2),
+                                    so.present_words * sizeof(uint32_t));
+    cfg.stream = s;
+    e = cudaLaunchKernelEx(&cfg, embed_sort_kernel, so);
+    if (e != cudaSuccess) return op_cuda(e, "sort launch");
     if (n == 0) return CCQ_OK;
     SumArgs a = {};
     a.dout = dout;
     a.dout_stride = dout_stride;
-    a.list = so.list[sort_holds(so.n) ? 0 : (so.passes - 1) & 1];
+    a.list = so.list[held ? 0 : (so.passes - 1) & 1];
     a.n = so.n;
     a.rows = static_cast<int>(rows);
     a.width = width;
     a.scale = scale;
     a.dtable = dtable;
     a.dtable_stride = dtable_stride;
-    a.joins = so.joins;
+    a.count = so.joins;
+    a.joins = reinterpret_cast<int2 *>(ws + 2 * list + 16);
     a.pieces = static_cast<int>(piece_count(n));
-    a.part = reinterpret_cast<float *>(ws + 2 * list + round16((static_cast<size_t>(a.pieces) + 1) * 4));
+    a.part = reinterpret_cast<float *>(ws + 2 * list + 16 + round16(static_cast<size_t>(a.pieces) * 8));
     const int es = dtype_bytes(dtype);
     // elements an access may hold in both operands, at most 16 bytes of the wider type
     const int b = std::min(out_bytes / eo, row_access(dout, dout_stride, es, n, access_bytes(static_cast<uintptr_t>(width) * es)) / es);

@@ -9,6 +9,7 @@
 #include <stdio.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "../../include/ccq_ops.h"
 #include "ccq_internal.h"
@@ -84,28 +85,36 @@ template <> struct RawOf<8> { using type = uint2; };
 template <> struct RawOf<4> { using type = uint32_t; };
 template <> struct RawOf<2> { using type = uint16_t; };
 
-// N elements of T as one access.
+// N elements of T as one access.  A single bf16 is held in a 32-bit register: with 16-bit ones the compiler packs two
+// loads' results into one register, and each load is then waited for as it is made.
 template <typename T, int N> struct Pack {
-    using Raw = typename RawOf<N * static_cast<int>(sizeof(T))>::type;
+    using Mem = typename RawOf<N * static_cast<int>(sizeof(T))>::type;
+    using Raw = typename std::conditional<sizeof(Mem) == 2, uint32_t, Mem>::type;
     Raw raw;
 };
 
 // Read once, not kept in L1 (the data streams through).
 template <typename T, int N> __device__ __forceinline__ Pack<T, N> load_stream(const T *p) {
     Pack<T, N> r;
-    r.raw = __ldcs(reinterpret_cast<const typename Pack<T, N>::Raw *>(p));
+    if constexpr (N * sizeof(T) == 2)
+        asm volatile("ld.global.cs.u16 %0, [%1];" : "=r"(r.raw) : "l"(p));
+    else
+        r.raw = __ldcs(reinterpret_cast<const typename Pack<T, N>::Mem *>(p));
     return r;
 }
 template <typename T, int N> __device__ __forceinline__ Pack<T, N> load_plain(const T *p) {
     Pack<T, N> r;
-    r.raw = *reinterpret_cast<const typename Pack<T, N>::Raw *>(p);
+    if constexpr (N * sizeof(T) == 2)
+        asm volatile("ld.global.u16 %0, [%1];" : "=r"(r.raw) : "l"(p));
+    else
+        r.raw = *reinterpret_cast<const typename Pack<T, N>::Mem *>(p);
     return r;
 }
 template <typename T, int N> __device__ __forceinline__ void store_stream(T *p, const Pack<T, N> &v) {
-    __stcs(reinterpret_cast<typename Pack<T, N>::Raw *>(p), v.raw);
+    __stcs(reinterpret_cast<typename Pack<T, N>::Mem *>(p), static_cast<typename Pack<T, N>::Mem>(v.raw));
 }
 template <typename T, int N> __device__ __forceinline__ void store_plain(T *p, const Pack<T, N> &v) {
-    *reinterpret_cast<typename Pack<T, N>::Raw *>(p) = v.raw;
+    *reinterpret_cast<typename Pack<T, N>::Mem *>(p) = static_cast<typename Pack<T, N>::Mem>(v.raw);
 }
 
 template <int W> __device__ __forceinline__ uint32_t word_of(const uint4 &r) {
@@ -113,15 +122,11 @@ template <int W> __device__ __forceinline__ uint32_t word_of(const uint4 &r) {
 }
 template <int W> __device__ __forceinline__ uint32_t word_of(const uint2 &r) { return W == 0 ? r.x : r.y; }
 template <int W> __device__ __forceinline__ uint32_t word_of(uint32_t r) { return r; }
-template <int W> __device__ __forceinline__ uint32_t word_of(uint16_t r) { return r; }
 template <int W> __device__ __forceinline__ void set_word(uint4 &r, uint32_t w) {
     (W == 0 ? r.x : W == 1 ? r.y : W == 2 ? r.z : r.w) = w;
 }
 template <int W> __device__ __forceinline__ void set_word(uint2 &r, uint32_t w) { (W == 0 ? r.x : r.y) = w; }
 template <int W> __device__ __forceinline__ void set_word(uint32_t &r, uint32_t w) { r = w; }
-template <int W> __device__ __forceinline__ void set_word(uint16_t &r, uint32_t w) {
-    r = static_cast<uint16_t>(w);
-}
 
 template <typename T> struct IsBf16 { static constexpr bool value = false; };
 template <> struct IsBf16<__nv_bfloat16> { static constexpr bool value = true; };
