@@ -330,14 +330,15 @@ __global__ void __launch_bounds__(kThreads, resident(N * K, BWD)) norm_kernel(No
             }
             copy_commit();
         } else {
+            // without conditions, so that all loads stay under way: past the end of the tokens the slot's first token (or the
+            // first of all), past the group's end its last access, which take() drops
+            const uint32_t from = turn < mine ? t : mine > 0 ? row0 : 0;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                px[k].raw = pg[k].raw = pd[k].raw = {};
-                if (turn < mine && k < accesses) {
-                    px[k] = load_stream<T, N>(row_at(X, t, x_row) + k * TEAM * N);
-                    if (gated) pg[k] = load_stream<T, N>(row_at(G, t, g_row) + k * TEAM * N);
-                    if constexpr (BWD) pd[k] = load_stream<T, N>(row_at(DY, t, dy_row) + k * TEAM * N);
-                }
+                const int c = (k < accesses ? k * TEAM : accesses > 0 ? (accesses - 1) * TEAM : -l) * N;
+                px[k] = load_stream<T, N>(row_at(X, from, x_row) + c);
+                if (gated) pg[k] = load_stream<T, N>(row_at(G, from, g_row) + c);
+                if constexpr (BWD) pd[k] = load_stream<T, N>(row_at(DY, from, dy_row) + c);
             }
         }
     };
@@ -380,6 +381,10 @@ __global__ void __launch_bounds__(kThreads, resident(N * K, BWD)) norm_kernel(No
                     unpack(p, f);
                 } else {
                     unpack(held[k], f);
+                    if (k >= accesses) {
+#pragma unroll
+                        for (int e = 0; e < N; ++e) f[e] = 0.f;
+                    }
                 }
 #pragma unroll
                 for (int e = 0; e < N; ++e) v[k * N + e] = f[e];
@@ -388,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, resident(N * K, BWD)) norm_kernel(No
         float x[E], g[E], dy[E];
         take(0, px, x);
         if constexpr (S == 0) {
-            take(1, pg, g);
+            if (gated) take(1, pg, g);
             if constexpr (BWD) take(2, pd, dy);
         }
         if constexpr (S == 0) fetch(turn + 1);
@@ -584,7 +589,7 @@ Shape shape_of(int64_t tokens, int channels, int groups, int n, int bwd) {
     while (s.k < kmax && 32 * s.k < packs) s.k = n == 1 || n == 2 ? s.k * 4 : s.k * 2;
     s.k = std::min(s.k, kmax);
     if (32 * s.k >= packs) {
-        s.team = s.k > 1 ? 32 : packs <= 1 ? 1 : packs <= 4 ? 4 : packs <= 8 ? 8 : packs <= 16 ? 16 : 32;
+        s.team = s.k == 4 && n <= 2 ? (packs <= 32 ? 8 : packs <= 64 ? 16 : 32) : s.k > 1 ? 32 : packs <= 1 ? 1 : packs <= 4 ? 4 : packs <= 8 ? 8 : packs <= 16 ? 16 : 32;
     } else if (kThreads * kmax >= packs) {
         s.k = kThreads >= packs ? 1 : kmax;
         s.team = kThreads;
@@ -622,6 +627,10 @@ template <typename T, int N, int K, int BWD> cudaError_t launch_one(const NormAr
             case 8: return launch_team<T, N, K, 8, BWD>(a, sh, s);
             case 16: return launch_team<T, N, K, 16, BWD>(a, sh, s);
         }
+    }
+    if constexpr (K == 4 && N <= 2) {
+        if (sh.team == 8) return launch_team<T, N, K, 8, BWD>(a, sh, s);
+        if (sh.team == 16) return launch_team<T, N, K, 16, BWD>(a, sh, s);
     }
     if constexpr (K == 1 || N * K == kMaxElems)
         if (sh.team == kWide) return launch_team<T, N, K, kWide, BWD>(a, sh, s);
