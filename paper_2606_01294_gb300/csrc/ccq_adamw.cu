@@ -53,18 +53,25 @@ template <int CAP> struct AdamArgs {
 };
 static_assert(sizeof(AdamArgs<kMaxTensors>) <= 32764, "a launch's arguments");
 
-// The two smallest non-negative e4m3 steps at a power-of-two scale: the bits of 2^e (as a float), at least 2^-100.
-__device__ __forceinline__ uint32_t scale_exponent(uint32_t top_bits) {
-    const int e = static_cast<int>((top_bits + 0x1FFFFFu) >> 23) - 8;  // the top three mantissa values fit below 448
+// The exponent field of the smallest power of two 2^e >= 2^-100 with top <= 448 * 2^e (448 = 1.75 * 2^8).
+__device__ __forceinline__ uint32_t scale_exponent(float top) {
+    const int e = static_cast<int>((__float_as_uint(top) + 0x1FFFFFu) >> 23) - 8;
     return static_cast<uint32_t>(max(e, 27));
 }
 
-// e4m3 code of y = |x| / scale, rounded up where the fraction between neighbours reaches 2^20 - turn.
+// e4m3 code of y = |x| / scale, rounded up where the fraction between neighbours reaches 2^20 - turn.  Below 2^-6 the
+// neighbours are 2^-9 apart: there 2^-6 + y has them in its upper three mantissa bits (the sum is cut, not
+// rounded).  Not a number, and infinity: 127.
 __device__ __forceinline__ uint32_t encode(float y, uint32_t turn) {
-    const int normal = static_cast<int>((__float_as_uint(y) + turn) >> 20) - (120 << 3);
-    // below 2^-6 the neighbours are 2^-9 apart
-    const int small = static_cast<int>((static_cast<uint32_t>(y * 536870912.f) + turn) >> 20);
-    return static_cast<uint32_t>(min(y < 0.015625f ? small : normal, 127));
+    const bool small = y < 0.015625f;
+    const float z = small ? __fadd_rz(y, 0.015625f) : y;
+    return min(((__float_as_uint(z) + turn) >> 20) - (small ? 121u << 3 : 120u << 3), 127u);
+}
+
+__device__ __forceinline__ float fast_rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 __device__ __forceinline__ void decode4(uint32_t codes, float *f) {
@@ -72,11 +79,6 @@ __device__ __forceinline__ void decode4(uint32_t codes, float *f) {
     const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes >> 16), __NV_E4M3);
     const float2 x = __half22float2(__half2(a)), y = __half22float2(__half2(b));
     f[0] = x.x; f[1] = x.y; f[2] = y.x; f[3] = y.y;
-}
-
-__device__ __forceinline__ uint32_t finite_bits(float x) {
-    const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
-    return b < 0x7f800000u ? b : 0u;
 }
 
 // Eight consecutive elements in the wide form; in the narrow one (unaligned tensors, a tensor's last block) lane l
@@ -170,37 +172,68 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
             }
         }
     }
-    uint32_t top_m = 0, top_v = 0;
+    // two elements an operation; every product and sum of the moments is rounded by itself
+    float top_m = 0.f, top_v = 0.f;
+    auto two = [](float x) { return f2_make(x, x); };
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float ge = __fmul_rn(g[e], clip);
-        float root;
+    for (int e = 0; e < 8; e += 2) {
+        const uint64_t ge = f2_mul(f2_make(g[e], g[e + 1]), two(clip));
+        uint64_t me = f2_make(m[e], m[e + 1]), ve = f2_make(v[e], v[e + 1]);
         if constexpr (BITS == 8) {
-            m[e] = __fmul_rn(m[e], sm);
-            const float r = __fmul_rn(v[e], sv);
-            v[e] = __fmul_rn(r, r);
+            me = f2_mul(me, two(sm));
+            ve = f2_mul(ve, two(sv));
+            ve = f2_mul(ve, ve);
         }
-        m[e] = __fadd_rn(__fmul_rn(m[e], a.c.beta1), __fmul_rn(ge, a.c.rest1));
-        v[e] = __fadd_rn(__fmul_rn(v[e], a.c.beta2), __fmul_rn(__fmul_rn(ge, ge), a.c.rest2));
-        root = __fsqrt_rn(v[e]);
-        p[e] = p[e] * a.c.keep - a.c.rate * __fdividef(m[e], root * a.c.root + a.c.eps);
+        // (the sums one by one: a packed sum of packed products is contracted, whatever their rounding says)
+        const float2 ma = f2_split(f2_mul(me, two(a.c.beta1))), mb = f2_split(f2_mul(ge, two(a.c.rest1)));
+        const float2 va = f2_split(f2_mul(ve, two(a.c.beta2))), vb = f2_split(f2_mul(f2_mul(ge, ge), two(a.c.rest2)));
+        const float2 m2 = make_float2(__fadd_rn(ma.x, mb.x), __fadd_rn(ma.y, mb.y));
+        const float2 v2 = make_float2(__fadd_rn(va.x, vb.x), __fadd_rn(va.y, vb.y));
+        me = f2_make(m2.x, m2.y);
+        const float r0 = __fsqrt_rn(v2.x), r1 = __fsqrt_rn(v2.y);
+        const float2 d = f2_split(f2_fma(f2_make(r0, r1), two(a.c.root), two(a.c.eps)));
+        const uint64_t step = f2_mul(f2_mul(me, two(-a.c.rate)), f2_make(fast_rcp(d.x), fast_rcp(d.y)));
+        const float2 q = f2_split(f2_fma(f2_make(p[e], p[e + 1]), two(a.c.keep), step));
+        p[e] = q.x;
+        p[e + 1] = q.y;
+        m[e] = m2.x;
+        m[e + 1] = m2.y;
         if constexpr (BITS == 8) {
-            v[e] = root;
-            top_m = max(top_m, finite_bits(m[e]));
-            top_v = max(top_v, finite_bits(root));
+            v[e] = r0;
+            v[e + 1] = r1;
+            // (the larger number of a number and a NaN)
+            top_m = fmaxf(fmaxf(top_m, fabsf(m2.x)), fabsf(m2.y));
+            top_v = fmaxf(fmaxf(top_v, r0), r1);
+        } else {
+            v[e] = v2.x;
+            v[e + 1] = v2.y;
         }
     }
     uint32_t code_m[8], code_v[8];
     if constexpr (BITS == 8) {
-        const uint32_t em = scale_exponent(__reduce_max_sync(~0u, top_m));
-        const uint32_t ev = scale_exponent(__reduce_max_sync(~0u, top_v));
+        // non-negative floats order as their bits do
+        top_m = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top_m)));
+        top_v = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top_v)));
+        if (!(top_m < INFINITY) || !(top_v < INFINITY)) {  // an infinite moment is its own element's alone
+            top_m = top_v = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (fabsf(m[e]) < INFINITY) top_m = fmaxf(top_m, fabsf(m[e]));
+                if (v[e] < INFINITY) top_v = fmaxf(top_v, v[e]);
+            }
+            top_m = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top_m)));
+            top_v = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top_v)));
+        }
+        const uint32_t em = scale_exponent(top_m), ev = scale_exponent(top_v);
         const float inv_m = __uint_as_float((254 - em) << 23), inv_v = __uint_as_float((254 - ev) << 23);
         if (lane == 0) *reinterpret_cast<float2 *>(scale) = make_float2(__uint_as_float(em << 23), __uint_as_float(ev << 23));
+        const uint32_t hop = wide ? 1u : 32u;
+        uint32_t word = (static_cast<uint32_t>(start) + (wide ? lane * 8 : lane)) * 0x6A09E667u + a.c.turn;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint32_t i = static_cast<uint32_t>(start) + (wide ? lane * 8 + e : e * 32 + lane);
-            const uint32_t turn = (i * 0x6A09E667u + a.c.turn) >> 12;
-            code_m[e] = encode(fabsf(m[e]) * inv_m, 0xFFFFFu - turn) | (m[e] < 0.f ? 128u : 0u);
+            const uint32_t turn = word >> 12;
+            word += hop * 0x6A09E667u;
+            code_m[e] = encode(fabsf(m[e]) * inv_m, turn ^ 0xFFFFFu) | (m[e] < 0.f ? 128u : 0u);
             code_v[e] = v[e] == 0.f ? 0u : max(encode(v[e] * inv_v, turn), 1u);
         }
     }

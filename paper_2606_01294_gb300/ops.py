@@ -13,7 +13,9 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import struct
 from dataclasses import dataclass
+from itertools import chain
 from typing import List, Optional
 
 import torch
@@ -333,15 +335,20 @@ def adamw_state(params, *, bits: int = 32, master: bool = False) -> AdamWState:
                       [p.detach().float().clone() for p in params] if master else None)
 
 
-def _adamw_list(ts, name, count, device, dtype, numels):
+def _adamw_list(ts, name, count, index, dtype, numels):
+    """The addresses of a list that goes with the parameters.  (One expression a tensor: with a hundred of them the
+    host's work is most of a call.)"""
     if len(ts) != count:
         raise ValueError(f"{name} has {len(ts)} tensors for {count} parameters")
-    for i, (t, n) in enumerate(zip(ts, numels)):
-        if t.dtype != dtype:
-            raise TypeError(f"{name}[{i}] must be {dtype}, got {t.dtype}")
-        if t.numel() != n or not t.is_contiguous() or t.device != device:
-            raise ValueError(f"{name}[{i}] must be a contiguous tensor of {n} elements on {device}")
-    return [t.data_ptr() for t in ts]
+    at = [t.data_ptr() for t, n in zip(ts, numels)
+          if t.dtype is dtype and t.get_device() == index and t.numel() == n and t.is_contiguous()]
+    if len(at) != count:
+        for i, (t, n) in enumerate(zip(ts, numels)):
+            if t.dtype != dtype:
+                raise TypeError(f"{name}[{i}] must be {dtype}, got {t.dtype}")
+            if t.numel() != n or not t.is_contiguous() or t.get_device() != index:
+                raise ValueError(f"{name}[{i}] must be a contiguous tensor of {n} elements on cuda:{index}")
+    return at
 
 
 def adamw_step(params, grads, state: AdamWState, step: int, *, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
@@ -352,24 +359,24 @@ def adamw_step(params, grads, state: AdamWState, step: int, *, lr: float, betas=
     if not params:
         return
     first = _cuda(params[0], "params[0]")
-    dev, count = first.device, len(params)
+    dev, index, count = first.device, first.get_device(), len(params)
     numels = [p.numel() for p in params]
-    columns = [_adamw_list(params, "params", count, dev, first.dtype, numels),
-               _adamw_list(grads, "grads", count, dev, grads[0].dtype if grads else None, numels)]
-    bits = 8 if state.scale is not None else 32
-    dtype = torch.float8_e4m3fn if bits == 8 else torch.float32
-    columns += [_adamw_list(state.m, "state.m", count, dev, dtype, numels),
-                _adamw_list(state.v, "state.v", count, dev, dtype, numels)]
-    columns.append(_adamw_list(state.scale, "state.scale", count, dev, torch.float32,
-                               [-(-n // ADAMW_BLOCK) * 2 for n in numels]) if bits == 8 else [0] * count)
-    columns.append(_adamw_list(state.master, "state.master", count, dev, torch.float32, numels)
-                   if state.master is not None else [0] * count)
-    columns.append(numels)
-    table = (_L * (7 * count))(*[x for row in zip(*columns) for x in row])
+    bits = 32 if state.scale is None else 8
+    dtype = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    none = [0] * count
+    rows = zip(_adamw_list(params, "params", count, index, first.dtype, numels),
+               _adamw_list(grads, "grads", count, index, grads[0].dtype if grads else None, numels),
+               _adamw_list(state.m, "state.m", count, index, dtype, numels),
+               _adamw_list(state.v, "state.v", count, index, dtype, numels),
+               none if bits == 32 else _adamw_list(state.scale, "state.scale", count, index, torch.float32,
+                                                   [-(-n // ADAMW_BLOCK) * 2 for n in numels]),
+               none if state.master is None else _adamw_list(state.master, "state.master", count, index, torch.float32,
+                                                             numels), numels)
+    table = struct.pack(f"{7 * count}q", *chain.from_iterable(rows))
     if grad_scale is not None:
         _dense(grad_scale, "grad_scale", dev, torch.float32)
         if grad_scale.numel() != 1:
             raise ValueError("grad_scale must be a scalar")
     p = _AdamWParams(lr, betas[0], betas[1], eps, weight_decay, step)
-    _check(_library().ccq_adamw_step(ctypes.addressof(table), count, _dtype_code(first), _dtype_code(grads[0]), bits,
+    _check(_library().ccq_adamw_step(table, count, _dtype_code(first), _dtype_code(grads[0]), bits,
                                      ctypes.byref(p), _ptr(grad_scale), _stream(dev, stream)))
