@@ -59,15 +59,19 @@ __device__ __forceinline__ uint32_t scale_exponent(float top) {
     return static_cast<uint32_t>(max(e, 27));
 }
 
-// e4m3 code of y = |x| / scale, rounded up where the fraction between neighbours reaches 2^20 - turn.  Below 2^-6 the
-// neighbours are 2^-9 apart: there 2^-6 + y has them in its upper three mantissa bits (the sum is cut, not
-// rounded).  Not a number, and infinity: 127.
-__device__ __forceinline__ uint32_t encode(float y, uint32_t turn) {
-    const bool small = y < 0.015625f;
-    const float z = small ? __fadd_rz(y, 0.015625f) : y;
-    return min(((__float_as_uint(z) + turn) >> 20) - (small ? 121u << 3 : 120u << 3), 127u);
+// y = |x| / scale as a number whose upper bits are its e4m3 code: below 2^-6 the neighbours are 2^-9 apart, and
+// 2^-7 + y / 2 (cut, not rounded) has them in its upper three mantissa bits.  Not a number, and infinity: the code 127.
+__device__ __forceinline__ uint32_t code_bits(float y) {
+    return __float_as_uint(y < 0.015625f ? __fmaf_rz(y, 0.5f, 0.0078125f) : fminf(y, 480.f));
 }
+// The code, rounded up where the fraction between neighbours reaches 2^20 - turn.
+__device__ __forceinline__ uint32_t encode(float y, uint32_t turn) { return ((code_bits(y) + turn) >> 20) - (120u << 3); }
 
+__device__ __forceinline__ float approx_sqrt(float x) {
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ float fast_rcp(float x) {
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -111,7 +115,7 @@ template <typename T> __device__ __forceinline__ void store8(T *p, const float (
 }
 
 template <typename P, typename G, int BITS, int MASTER, int CAP>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamArgs<CAP> a) {
+__global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_constant__ AdamArgs<CAP> a) {
     // the last tensor whose first chunk is not past this one
     int lo = 0, hi = a.count - 1;
     while (lo < hi) {
@@ -173,7 +177,7 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
         }
     }
     // two elements an operation; every product and sum of the moments is rounded by itself
-    float top_m = 0.f, top_v = 0.f;
+    float top_m = 0.f, top_v = 0.f, root[8];
     auto two = [](float x) { return f2_make(x, x); };
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
@@ -190,7 +194,7 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
         const float2 m2 = make_float2(__fadd_rn(ma.x, mb.x), __fadd_rn(ma.y, mb.y));
         const float2 v2 = make_float2(__fadd_rn(va.x, vb.x), __fadd_rn(va.y, vb.y));
         me = f2_make(m2.x, m2.y);
-        const float r0 = __fsqrt_rn(v2.x), r1 = __fsqrt_rn(v2.y);
+        const float r0 = approx_sqrt(v2.x), r1 = approx_sqrt(v2.y);
         const float2 d = f2_split(f2_fma(f2_make(r0, r1), two(a.c.root), two(a.c.eps)));
         const uint64_t step = f2_mul(f2_mul(me, two(-a.c.rate)), f2_make(fast_rcp(d.x), fast_rcp(d.y)));
         const float2 q = f2_split(f2_fma(f2_make(p[e], p[e + 1]), two(a.c.keep), step));
@@ -198,15 +202,14 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
         p[e + 1] = q.y;
         m[e] = m2.x;
         m[e + 1] = m2.y;
+        v[e] = v2.x;
+        v[e + 1] = v2.y;
         if constexpr (BITS == 8) {
-            v[e] = r0;
-            v[e + 1] = r1;
+            root[e] = r0;
+            root[e + 1] = r1;
             // (the larger number of a number and a NaN)
             top_m = fmaxf(fmaxf(top_m, fabsf(m2.x)), fabsf(m2.y));
-            top_v = fmaxf(fmaxf(top_v, r0), r1);
-        } else {
-            v[e] = v2.x;
-            v[e + 1] = v2.y;
+            top_v = fmaxf(fmaxf(top_v, v2.x), v2.y);
         }
     }
     uint32_t code_m[8], code_v[8];
@@ -224,17 +227,30 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
             top_m = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top_m)));
             top_v = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top_v)));
         }
-        const uint32_t em = scale_exponent(top_m), ev = scale_exponent(top_v);
+        const uint32_t em = scale_exponent(top_m), ev = scale_exponent(__fsqrt_rn(top_v));
         const float inv_m = __uint_as_float((254 - em) << 23), inv_v = __uint_as_float((254 - ev) << 23);
         if (lane == 0) *reinterpret_cast<float2 *>(scale) = make_float2(__uint_as_float(em << 23), __uint_as_float(ev << 23));
         const uint32_t hop = wide ? 1u : 32u;
-        uint32_t word = (static_cast<uint32_t>(start) + (wide ? lane * 8 : lane)) * 0x6A09E667u + a.c.turn;
+        const uint32_t word0 = (static_cast<uint32_t>(start) + (wide ? lane * 8 : lane)) * 0x6A09E667u + a.c.turn;
+        uint32_t word = word0, near = ~0u;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const uint32_t turn = word >> 12;
             word += hop * 0x6A09E667u;
-            code_m[e] = encode(fabsf(m[e]) * inv_m, turn ^ 0xFFFFFu) | (m[e] < 0.f ? 128u : 0u);
-            code_v[e] = v[e] == 0.f ? 0u : max(encode(v[e] * inv_v, turn), 1u);
+            code_m[e] = encode(fabsf(m[e]) * inv_m, turn ^ 0xFFFFFu) | ((__float_as_uint(m[e]) >> 24) & 128u);
+            const uint32_t at = code_bits(root[e] * inv_v) + turn;
+            code_v[e] = max((at >> 20) - (120u << 3), min(__float_as_uint(v[e]), 1u));
+            near = min(near, (at + 8u) & 0xFFFFFu);
+        }
+        // The approximate root is within two units in the last place; where that could pass a threshold (a few elements of a
+        // million), the rounded root decides.
+        if (near < 16u) {
+            word = word0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                code_v[e] = max(encode(__fsqrt_rn(v[e]) * inv_v, word >> 12), min(__float_as_uint(v[e]), 1u));
+                word += hop * 0x6A09E667u;
+            }
         }
     }
     if (wide) {
