@@ -38,8 +38,13 @@ class _AdamWParams(ctypes.Structure):
     _fields_ = [("lr", _D), ("beta1", _D), ("beta2", _D), ("eps", _D), ("weight_decay", _D), ("step", _L)]
 
 
-@functools.lru_cache(maxsize=1)
+_lib = None
+
+
 def _library() -> ctypes.CDLL:
+    global _lib
+    if _lib is not None:
+        return _lib
     lib = ccq.load_library()
     size = ctypes.POINTER(_Z)
     for name, args in {
@@ -65,6 +70,7 @@ def _library() -> ctypes.CDLL:
         fn.argtypes, fn.restype = args, _I
     lib.ccq_default_policy_params.argtypes = [ctypes.POINTER(_PolicyParams)]
     lib.ccq_default_policy_params.restype = None
+    _lib = lib
     return lib
 
 
@@ -92,6 +98,9 @@ def _cuda(t, name, device=None):
 
 
 def _dense(t, name, device, dtype=None, shape=None):
+    if (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.is_contiguous()
+            and (dtype is None or t.dtype is dtype) and (shape is None or t.shape == shape)):
+        return t
     _cuda(t, name, device)
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
@@ -103,7 +112,11 @@ def _dense(t, name, device, dtype=None, shape=None):
 
 
 def _rows(t, name, device=None, dtype=None, shape=None):
-    """The stride between the rows of a [..., width] tensor with contiguous rows."""
+    """The stride between the rows of a [..., width] tensor with contiguous rows.  (A tensor as most are passes on one
+    expression: the small cases' time is the host's.)"""
+    if (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and (device is None or t.device == device)
+            and (dtype is None or t.dtype is dtype) and (shape is None or t.shape == shape) and t.dim() > 0):
+        return t.shape[-1]
     _cuda(t, name, device)
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
@@ -131,6 +144,11 @@ def _rows(t, name, device=None, dtype=None, shape=None):
 
 
 def _ids(t, name, device):
+    if isinstance(t, torch.Tensor) and t.device == device and t.is_cuda and t.is_contiguous():
+        if t.dtype is torch.int64:
+            return 8
+        if t.dtype is torch.int32:
+            return 4
     if t.dtype not in (torch.int64, torch.int32):
         raise TypeError(f"{name} must be int64 or int32, got {t.dtype}")
     _dense(t, name, device)
@@ -144,17 +162,18 @@ def embed(table, ids, *, scale: float = 1.0, out=None, stream=None):
     """``scale * table[ids]`` (ccq_embed): table [rows, width] bf16 or fp32, ids int64 or int32 of any
     shape; returns [*ids.shape, width].  An id outside the table gives a zero row and CCQ_ERR_INDEX
     from :func:`ccq.device_status`."""
-    dev = _cuda(table, "table").device
+    ts = _rows(table, "table")
     if table.dim() != 2:
         raise ValueError("table must be [rows, width]")
-    ts = _rows(table, "table")
-    width = _ids(ids, "ids", dev)
-    shape = ids.shape + (table.shape[1],)
+    dev = table.device
+    id_bytes = _ids(ids, "ids", dev)
+    rows, width = table.shape
     if out is None:
-        out = torch.empty(shape, dtype=table.dtype, device=dev)
-    os = _rows(out, "out", dev, table.dtype, shape)
-    _check(_library().ccq_embed(table.data_ptr(), _dtype_code(table), ts, ids.data_ptr(), width, ids.numel(),
-                                table.shape[0], table.shape[1], scale, out.data_ptr(), os, _stream(dev, stream)))
+        out, os = torch.empty((*ids.shape, width), dtype=table.dtype, device=dev), width
+    else:
+        os = _rows(out, "out", dev, table.dtype, ids.shape + (width,))
+    _check(_library().ccq_embed(table.data_ptr(), _dtype_code(table), ts, ids.data_ptr(), id_bytes, ids.numel(), rows,
+                                width, scale, out.data_ptr(), os, _stream(dev, stream)))
     return out
 
 
@@ -163,15 +182,15 @@ def embed_grad(dout, ids, rows: int, *, scale: float = 1.0, padding_id: Optional
     """Gradient of :func:`embed`'s table (ccq_embed_grad): row r is ``scale`` times the sum of dout over
     the tokens with id r, summed in fp32 in a fixed order; rows without a token (and ``padding_id``'s) are zero.
     dout [*ids.shape, width]; returns [rows, width] in ``dtype`` (dout's when not given) or ``out``."""
-    dev = _cuda(dout, "dout").device
+    _rows(dout, "dout")
+    dev = dout.device
     id_bytes = _ids(ids, "ids", dev)
-    if dout.dim() < 1:
-        raise ValueError("dout must be [*ids.shape, width]")
     width, n = dout.shape[-1], ids.numel()
     ds = _rows(dout, "dout", dev, None, ids.shape + (width,))
     if out is None:
-        out = torch.empty(rows, width, dtype=dtype or dout.dtype, device=dev)
-    os = _rows(out, "out", dev, dtype, (rows, width))
+        out, os = torch.empty((rows, width), dtype=dtype or dout.dtype, device=dev), width
+    else:
+        os = _rows(out, "out", dev, dtype, (rows, width))
     if padding_id is not None and not 0 <= padding_id < rows:
         raise ValueError(f"padding_id {padding_id} is outside the table of {rows} rows")
     workspace, nbytes = _workspace(workspace, _size("ccq_embed_grad_workspace_size", -1, n, rows, width), dev)
@@ -185,9 +204,8 @@ def embed_grad(dout, ids, rows: int, *, scale: float = 1.0, padding_id: Optional
 
 
 def _norm_args(x, weight, bias, gate, groups, activation):
-    dev = _cuda(x, "x").device
     xs = _rows(x, "x")
-    channels = x.shape[-1]
+    dev, channels = x.device, x.shape[-1]
     if groups < 1 or channels % groups:
         raise ValueError(f"{channels} channels do not divide into {groups} groups")
     if activation not in ACTIVATION:
@@ -195,9 +213,10 @@ def _norm_args(x, weight, bias, gate, groups, activation):
     gs = 0 if gate is None else _rows(gate, "gate", dev, x.dtype, x.shape)
     param = weight if weight is not None else bias
     pdt = _dtype_code(param) if param is not None else ccq.FP32
-    for p, name in ((weight, "weight"), (bias, "bias")):
-        if p is not None:
-            _dense(p, name, dev, param.dtype, (channels,))
+    if weight is not None:
+        _dense(weight, "weight", dev, param.dtype, (channels,))
+    if bias is not None:
+        _dense(bias, "bias", dev, param.dtype, (channels,))
     return dev, xs, gs, channels, pdt, x.numel() // channels if channels else 0
 
 
@@ -209,8 +228,9 @@ def group_norm(x, weight=None, bias=None, gate=None, *, groups: int, activation:
     (a root-mean-square norm)."""
     dev, xs, gs, channels, pdt, tokens = _norm_args(x, weight, bias, gate, groups, activation)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-    os = _rows(out, "out", dev, x.dtype, x.shape)
+        out, os = torch.empty(x.shape, dtype=x.dtype, device=dev), channels
+    else:
+        os = _rows(out, "out", dev, x.dtype, x.shape)
     _check(_library().ccq_group_norm(x.data_ptr(), xs, _ptr(gate), gs, _ptr(weight), _ptr(bias), _dtype_code(x), pdt,
                                      out.data_ptr(), os, tokens, channels, groups, int(bool(centered)), eps,
                                      ACTIVATION[activation], _stream(dev, stream)))
@@ -229,13 +249,15 @@ def group_norm_bwd(x, weight, bias, gate, dout, *, groups: int, activation: str 
     for name, like in (("dx", x), ("dgate", gate)):
         if like is not None:
             if g.get(name) is None:
-                g[name] = torch.empty(x.shape, dtype=x.dtype, device=dev)
-            strides[name] = _rows(g[name], name, dev, x.dtype, x.shape)
+                g[name], strides[name] = torch.empty(x.shape, dtype=x.dtype, device=dev), channels
+            else:
+                strides[name] = _rows(g[name], name, dev, x.dtype, x.shape)
     for name, like in (("dweight", weight), ("dbias", bias)):
         if like is not None:
             if g.get(name) is None:
                 g[name] = torch.empty(like.shape, dtype=like.dtype, device=dev)
-            _dense(g[name], name, dev, like.dtype, like.shape)
+            else:
+                _dense(g[name], name, dev, like.dtype, like.shape)
     workspace, nbytes = _workspace(workspace, _size("ccq_group_norm_bwd_workspace_size", dev.index, tokens, channels,
                                                     groups, _dtype_code(x)), dev)
     _check(_library().ccq_group_norm_bwd(
@@ -250,10 +272,8 @@ def group_norm_bwd(x, weight, bias, gate, dout, *, groups: int, activation: str 
 
 
 def _tokens(logits, actions):
-    dev = _cuda(logits, "logits").device
-    if logits.dim() < 1:
-        raise ValueError("logits must be [..., vocab]")
     ls = _rows(logits, "logits")
+    dev = logits.device
     id_bytes = _ids(actions, "actions", dev)
     if actions.shape != logits.shape[:-1]:
         raise ValueError(f"actions have shape {tuple(actions.shape)}, expected {tuple(logits.shape[:-1])}")
@@ -270,16 +290,20 @@ def policy_loss(logits, actions, old_logp, advantages, *, ref_logp=None, weights
     with ``grad``, dlogits (``grad_scale`` times the loss's gradient; ``dlogits`` may be the logits)."""
     dev, ls, id_bytes = _tokens(logits, actions)
     shape, vocab = actions.shape, logits.shape[-1]
-    for t, name in ((old_logp, "old_logp"), (advantages, "advantages"), (ref_logp, "ref_logp"), (weights, "weights")):
-        if t is not None or name in ("old_logp", "advantages"):
-            _dense(t, name, dev, torch.float32, shape)
+    _dense(old_logp, "old_logp", dev, torch.float32, shape)
+    _dense(advantages, "advantages", dev, torch.float32, shape)
+    if ref_logp is not None:
+        _dense(ref_logp, "ref_logp", dev, torch.float32, shape)
+    if weights is not None:
+        _dense(weights, "weights", dev, torch.float32, shape)
     loss = torch.empty((), dtype=torch.float32, device=dev)
     logp = torch.empty(shape, dtype=torch.float32, device=dev)
     gs = 0
     if grad:
         if dlogits is None:
-            dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
-        gs = _rows(dlogits, "dlogits", dev, logits.dtype, logits.shape)
+            dlogits, gs = torch.empty(logits.shape, dtype=logits.dtype, device=dev), vocab
+        else:
+            gs = _rows(dlogits, "dlogits", dev, logits.dtype, logits.shape)
     elif dlogits is not None:
         raise ValueError("dlogits is given but grad is False")
     n = actions.numel()
@@ -298,7 +322,8 @@ def token_logp(logits, actions, *, temperature: float = 1.0, out=None, stream=No
     dev, ls, id_bytes = _tokens(logits, actions)
     if out is None:
         out = torch.empty(actions.shape, dtype=torch.float32, device=dev)
-    _dense(out, "out", dev, torch.float32, actions.shape)
+    else:
+        _dense(out, "out", dev, torch.float32, actions.shape)
     _check(_library().ccq_token_logp(logits.data_ptr(), _dtype_code(logits), ls, actions.data_ptr(), id_bytes,
                                      actions.numel(), logits.shape[-1], temperature, out.data_ptr(),
                                      _stream(dev, stream)))
