@@ -354,8 +354,9 @@ struct SumArgs {
 };
 
 constexpr int kSumThreads = 256;
+constexpr int kJoinThreads = 256;
 
-template <typename T, typename O, int N> __global__ void __launch_bounds__(kSumThreads, N <= 2 ? 3 : 4) embed_sum_kernel(SumArgs a) {
+template <typename T, typename O, int N> __global__ void __launch_bounds__(kSumThreads, (N <= 2 ? 768 : 1024) / kSumThreads) embed_sum_kernel(SumArgs a) {
     constexpr int K = N <= 2 ? 4 : 1;        // accesses of a lane
     constexpr int kFlight = N >= 8 ? 4 : 8;  // entries whose loads are under way at once
     grid_wait();
@@ -491,7 +492,7 @@ template <typename T, typename O, int N> __global__ void __launch_bounds__(kSumT
 // 64 columns of a row, 16 threads 4 columns each, in 16 strided sums over the pieces that are then added in order.
 constexpr int kJoinColumns = 64;
 constexpr int kJoinCtas = 608;
-template <typename O> __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(SumArgs a) {
+template <typename O> __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(SumArgs a) {
     __shared__ float sums[16][kJoinColumns + 1];
     grid_wait();
     const int count = *a.count, chunks = (a.width + kJoinColumns - 1) / kJoinColumns;
@@ -529,7 +530,7 @@ template <typename T, typename O, int N> cudaError_t launch_sum(SumArgs a, cudaS
     cudaError_t e = launch_after(embed_sum_kernel<T, O, N>, static_cast<unsigned>((warps + per - 1) / per), kSumThreads,
                                  0, s, a);
     if (e != cudaSuccess) return e;
-    return launch_after(embed_join_kernel<O>, kJoinCtas, kSumThreads, 0, s, a);
+    return launch_after(embed_join_kernel<O>, kJoinCtas, kJoinThreads, 0, s, a);
 }
 
 int key_bits(int64_t rows) {  // keys 0 .. rows
