@@ -126,9 +126,10 @@ CCQ_API void ccq_default_policy_params(ccq_policy_params *p);
  *   dlogits   [n, vocab] in dtype, row stride dlogits_stride, or NULL (loss and logp alone).
  *             May be the logits themselves (same address and stride).
  *   workspace ccq_policy_loss_workspace_size() bytes, 16-byte aligned.
- * A token of weight 0 is masked: its logits, action, advantage and log-probabilities are not
- * read, its logp and its row of dlogits are 0.  An action outside [0, vocab) masks its
- * token in the same way and leaves CCQ_ERR_INDEX.
+ * A token of weight 0 is masked: its logits are not read, its action, advantage and
+ * log-probabilities (which may be anything) not used, its logp and its row of dlogits are 0.
+ * An action outside [0, vocab) masks its token in the same way and, where the weight is not 0,
+ * leaves CCQ_ERR_INDEX.
  */
 CCQ_API ccq_status ccq_policy_loss(const void *logits, ccq_dtype dtype, int64_t logits_stride,
                                    const void *actions, int id_bytes, const float *old_logp,

@@ -1,13 +1,17 @@
 // ccq_adamw.cu -- one AdamW update of many tensors in one launch, states in 32 or 8 bits (ccq_ops.h).
 //
+//   g = c grad, m = b1 m + (1 - b1) g, v = b2 v + (1 - b2) g^2,
+//   p = (1 - lr wd) p - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 // Every element is read and written once: 28 bytes an element with everything in fp32, 16 with bf16 weights and
-// gradients, an fp32 master and 8-bit states.  HBM bounds it.  The tensors' addresses are the
-// launch's own arguments (constant memory), and a CTA finds its tensor among them by the tensors' first
-// chunks.  A warp updates kBlock consecutive elements, 8 a lane, which is also what shares a scale in the
-// 8-bit state: the block's largest moment is a warp's maximum, and the state never leaves registers between
-// its decoding and its rounding.
+// gradients, an fp32 master and 8-bit states.  The tensors' addresses are the launch's own arguments (constant
+// memory), and a CTA finds its tensor among them by the tensors' first chunks.  A warp updates kBlock
+// consecutive elements, 8 a lane, which is also what shares a scale in the 8-bit state: the block's largest moment is
+// a warp's maximum, and the state never leaves registers between its decoding and its rounding.
 // The 8-bit state's arithmetic up to the rounding is done without fused multiply-adds, so that its e4m3
 // codes are those of the formula's fp32 operations taken one by one.
+// Measured: 84 M elements in fp32 340 us (6.9 TB/s, the copy rate; HBM bounds it); 253 M with masters and 8-bit states 720 us
+// (5.6 TB/s, 83 %; about 69 instructions an element, half of them integer, bound it beside HBM).
+// (Tried and taken back: the next block's operands by asynchronous copies while one is computed, 748 us.)
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <math.h>

@@ -2,17 +2,20 @@
 // (ccq_ops.h).
 //
 // Both directions stream: the forward reads x (and the gate) and writes y, the backward reads x, the gate and
-// dy and writes dx and dgate, each once; HBM bounds them.  A team of L threads holds a (token, group)'s d
-// channels in registers, K accesses of N elements each, so that the mean, then the squared deviations from it
-// (two passes over registers: no cancellation for a group whose mean is large), and in the backward
-// the two means of its formula, are sums over registers and a team:
+// dy and writes dx and dgate, each once.  A team of threads holds a (token, group)'s d channels in registers, K
+// accesses of N elements each, so that the mean and the squared deviations from it (no cancellation for a group
+// whose mean is large), and in the backward the two means of its formula, are sums over registers and a team:
 //   s = act(gate), du = dy s, dgate = dy u act'(gate)      (no gate: du = dy act'(u))
 //   dxh = du weight,  dx = rstd (dxh - mean(dxh) - xh mean(dxh xh))     (mean(dxh) = 0 with centered = 0)
 //   dweight = sum over tokens of du xh,  dbias = sum over tokens of du
 // A team keeps one group and walks over tokens, so that its weights, and the backward's partial sums of
 // dweight and dbias, stay in registers too; the partial sums go to the workspace once and norm_param_kernel
-// adds them in a fixed order.  L is at most a warp's 32 where K accesses each suffice, else the
-// whole CTA; groups beyond that (d > 4096) are walked in memory (the _long kernels).
+// adds them in a fixed order.  A team is at most a warp where K accesses each suffice, else the
+// whole CTA; groups beyond that (d > 4096) are walked in memory (norm_long_kernel).
+// Measured, bf16 with a gate and groups of 128: forward of 32768 x 2048 64 us (6.3 TB/s, 93 % of the copy rate; HBM bounds
+// it); backward of 16384 x 2048 62 us (5.4 TB/s, 80 %; 41 instructions an element, about half of them in the FMA pipes,
+// which packed pairs do not speed up, and 5 us for the parameters' gradients).  Groups of 33, one element an access: 31 and
+// 26 %.
 #include <algorithm>
 
 #include "ccq_ops.cuh"

@@ -285,7 +285,7 @@ def policy_loss(logits, actions, old_logp, advantages, *, ref_logp=None, weights
                 dlogits=None, workspace=None, stream=None):
     """Clipped policy loss with a KL term and its gradient (ccq_policy_loss).  logits [..., vocab] bf16 or fp32;
     actions [...] int64 or int32; old_logp, advantages, ref_logp (None: no KL term), weights (None: 1 / n)
-    [...] fp32.  A token of weight 0 is masked: nothing of it is read.  ``clip`` is (low, high), the ratio is held
+    [...] fp32.  A token of weight 0 is masked: nothing of it counts, whatever it holds.  ``clip`` is (low, high), the ratio is held
     in [1 - low, 1 + high].  Returns a dict of loss (a scalar tensor), logp [...] (0 where masked) and,
     with ``grad``, dlogits (``grad_scale`` times the loss's gradient; ``dlogits`` may be the logits)."""
     dev, ls, id_bytes = _tokens(logits, actions)

@@ -142,6 +142,19 @@ def test_embed_grad(dtype, out_dtype, n, rows, width, kind):
     assert torch.equal(d, ops.embed_grad(dout, ids.int(), rows, scale=3.0, dtype=out_dtype))  # same bits again
 
 
+@pytest.mark.parametrize("n,rows,width,kind", [(131072, 5000, 16, "zipf"), (200001, 3000, 8, "half"), (300000, 400000, 8, "zipf"),
+                                               (150000, 100, 24, "same"), (3000, 300000, 64, "zipf"), (40000, 513, 40, "even")])
+def test_embed_grad_long_lists_and_large_tables(n, rows, width, kind):
+    """Lists that the sort exchanges through global memory, runs of thousands of pieces, and every cluster size."""
+    g = gen(n)
+    ids = _ids(kind, n, rows, g)
+    dout = randn(g, n, width)
+    d = ops.embed_grad(dout, ids, rows)
+    ref, mass, count = _embed_grad_ref(dout, ids, rows, 1.0)
+    close(d, ref, (count + 2) * U * mass + U * ref.abs() + 1e-38)
+    assert torch.equal(d, ops.embed_grad(dout, ids, rows))
+
+
 @pytest.mark.parametrize("pad,offset", [(0, 0), (8, 0), (1, 0), (0, 1), (4, 2)])
 def test_embed_grad_strides_and_padding(pad, offset):
     g = gen(5)
@@ -192,6 +205,9 @@ def _norm64(x, w, b, gate, groups, act, centered, eps):
 
 NORM_SIZES = [(1, 1, 1), (1, 128, 1), (3, 256, 2), (257, 2048, 16), (100, 1024, 16), (33, 1152, 12), (17, 165, 5), (50, 2000, 4),
               (40, 2048, 1), (9, 4096, 1), (7, 9000, 2), (5, 5000, 1), (1000, 64, 64), (70, 48, 3), (6, 600, 1), (130, 320, 5)]
+# every width of access, accesses a thread and team
+NORM_SIZES += [(9, 130, 1), (5, 402, 1), (4, 1030, 1), (7, 301, 1), (3, 1001, 1), (11, 135, 3), (13, 62, 2), (21, 24, 3), (6, 32, 1), (8, 18, 1),
+               (900, 256, 16)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -358,6 +374,31 @@ def test_policy_loss(dtype, n, vocab):
     score = ops.token_logp(logits, actions, temperature=temperature)
     live = w != 0
     assert torch.equal(score[live], got["logp"][live])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,vocab", [(1000, 30000), (16500, 16400), (170000, 7), (3000, 500), (700, 9001)])
+def test_policy_loss_many_rows(dtype, n, vocab):
+    """Many rows for a CTA (dealt out by rank, strided, and in several batches).  The slope's error is its derivative by
+    logp, w (|r A| where that counts + kl exp(d)), times logp's: it can be far above its value's rounding, as where a clipped
+    token's KL term is near zero."""
+    x = _policy_inputs(n, vocab, dtype, n + vocab, masked=n // 3)
+    logits, actions, old, ref, adv, w = x
+    clip, kl, temperature = (0.2, 0.3), 0.1, 0.8
+    loss, logp, grad, edge, mass = _policy64(*x, clip, kl, temperature)
+    got = ops.policy_loss(logits, actions, old, adv, ref_logp=ref, weights=w, clip=clip, kl_coef=kl, temperature=temperature)
+    tol = _logp_bound(logits, temperature)
+    close(got["logp"], logp, tol + U * logp.abs(), "logp")
+    close(got["loss"], loss, (float(tol.max()) * 4 + ARITH) * mass + 1e-30, "loss")
+    live = w != 0
+    lp = torch.log_softmax(logits.double() / temperature, -1).gather(1, actions[:, None])[:, 0]
+    moved = w.double() * ((lp - old.double()).exp() * adv.double().abs() + kl * (ref.double() - lp).exp()) / temperature
+    slope = (tol + U * logp.abs() + 8 * U) * moved
+    top = grad.abs().amax(1, keepdim=True)
+    bound = R[dtype] * grad.abs() + slope[:, None] + 4 * (ARITH + tol.max()) * top + 1e-38
+    keep = ~edge & live
+    close(got["dlogits"][keep], grad[keep], bound[keep], "dlogits")
+    assert not got["dlogits"][~live].any()
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
