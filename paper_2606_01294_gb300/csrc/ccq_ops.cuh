@@ -180,6 +180,13 @@ __device__ __forceinline__ int64_t load_index(const void *p, int bytes, int64_t 
     return bytes == 8 ? static_cast<const int64_t *>(p)[i] : static_cast<const int32_t *>(p)[i];
 }
 
+// Wait until the shared-memory sources of all but the N most recently committed bulk-store groups have been read.
+template <int N> __device__ __forceinline__ void tma_store_wait_read_but() {
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+
+// Status code of an index outside its range (CCQ_ERR_INDEX), for the device status word.
+constexpr int kStatusIndex = 6;
 __device__ __forceinline__ void note_index(int *status) { atomicExch(status, kStatusIndex); }
 
 }  // namespace ccq

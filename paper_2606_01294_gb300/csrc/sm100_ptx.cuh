@@ -17,8 +17,6 @@ constexpr int kStatusTimeout = 4;
 // Status code a kernel writes when its inputs leave the range it can represent
 // (CCQ_ERR_RANGE); the kernel runs to completion, its outputs are not valid.
 constexpr int kStatusRange = 5;
-// Status code of an index outside its range (CCQ_ERR_INDEX).
-constexpr int kStatusIndex = 6;
 // A bounded wait gives up after this many SM clock cycles (about one second).
 constexpr long long kWaitLimitCycles = 2000000000LL;
 
@@ -198,12 +196,6 @@ __device__ __forceinline__ void tma_store_commit() {
 // Wait until the shared-memory source of every committed store has been read.
 __device__ __forceinline__ void tma_store_wait_read() {
     asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-}
-
-// Wait until the shared-memory sources of all but the N most recently committed store groups have been read.
-template <int N>
-__device__ __forceinline__ void tma_store_wait_read_but() {
-    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
 }
 
 // Wait until every committed store has completed.
