@@ -14,8 +14,8 @@
 //      longer ones every piece leaves its part in the workspace.
 //   3. embed_join_kernel: adds the parts of the runs over three pieces and more, in order.
 // 16384 x 2048 bf16 into 32000 fp32 rows (329 MB, 48.6 us at the copy rate): 70 us, of which the zeros beside the sort are
-// 38, the sums 23 (116 MB, 5 TB/s), the join 6 and the gaps between launches the rest.  With short lists the sort's
-// latency (16 to 30 us) is most of it.
+// about 38 (213 MB, 5.6 TB/s; a plain fill of that size runs at 3.9), the sums 23 (116 MB, 5 TB/s), the join 6 and the
+// gaps between launches the rest.  With short lists the sort's latency (16 to 30 us) is most of it.
 #include <algorithm>
 
 #include "ccq_ops.cuh"
@@ -543,8 +543,8 @@ int key_bits(int64_t rows) {  // keys 0 .. rows
     return b;
 }
 
-// CTAs of the sort's cluster.  More make it faster (16384 ids: about 30, 20 and 16 us with 4, 8 and 16) and leave fewer SMs
-// to write zeros beside it (148, 112, 96): few where the rows that surely have no entry are many, 16 (beyond the
+// CTAs of the sort's cluster.  More make it faster (16384 ids: 21 us with 8, 16 with 16) and leave fewer SMs to write
+// zeros beside it (140, 112, 96 with 4, 8, 16): few where the rows that surely have no entry are many, 16 (beyond the
 // portable size) where ids are.  16384 x 2048 into 32000 rows: 70, 74, 80 us; 60000 x 64 into 100000: 82, 53, 47.
 int sort_ctas(int64_t n, int64_t rows, size_t row_bytes) {
     if (n > 32768) return kMostCtas;
