@@ -533,7 +533,7 @@ template <typename T, typename O, int N> cudaError_t launch_sum(SumArgs a, cudaS
     const int per = kSumThreads / 32;
     cudaError_t e = launch_after(embed_sum_kernel<T, O, N>, static_cast<unsigned>((warps + per - 1) / per), kSumThreads,
                                  0, s, a);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || a.pieces < 3) return e;  // (no run spans three pieces)
     return launch_after(embed_join_kernel<O>, kJoinCtas, kJoinThreads, 0, s, a);
 }
 

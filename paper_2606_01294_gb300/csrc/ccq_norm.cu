@@ -649,6 +649,10 @@ template <typename T, int BWD> cudaError_t launch_norm(NormArgs a, const Shape &
     if constexpr (sizeof(T) == 2) {
         if (sh.n == 8)
             return sh.k == 1 ? launch_one<T, 8, 1, BWD>(a, sh, s) : launch_one<T, 8, 2, BWD>(a, sh, s);
+        if (sh.n == 4)
+            return sh.k == 1   ? launch_one<T, 4, 1, BWD>(a, sh, s)
+                   : sh.k == 2 ? launch_one<T, 4, 2, BWD>(a, sh, s)
+                               : launch_one<T, 4, 4, BWD>(a, sh, s);
         if (sh.n == 2)
             return sh.k == 1   ? launch_one<T, 2, 1, BWD>(a, sh, s)
                    : sh.k == 4 ? launch_one<T, 2, 4, BWD>(a, sh, s)
@@ -689,8 +693,8 @@ ccq_status check_operand(const char *name, const void *p, int64_t stride, int64_
     return op_pointer(name, p, es);
 }
 
-// The widest access with its kernels: 16 bytes, 4 bytes, or one element.
-int access_elems(int bytes, int es) { return bytes == 16 ? 16 / es : bytes >= 4 && es == 2 ? 2 : 1; }
+// Elements of the widest access with its kernels: 16 bytes, 8 or 4 of bf16, or one element.
+int access_elems(int bytes, int es) { return bytes == 16 ? 16 / es : es == 2 ? bytes / 2 : 1; }
 
 ccq_status check_param(const char *name, const void *p, ccq_dtype dt) {
     return p ? op_pointer(name, p, dtype_bytes(dt)) : CCQ_OK;
@@ -699,7 +703,7 @@ ccq_status check_param(const char *name, const void *p, ccq_dtype dt) {
 // The most slots any access width gives: bounds the partial sums.
 size_t bwd_workspace(int64_t tokens, int channels, int groups, int es) {
     int slots = 1;
-    for (int n : {16 / es, 2, 1})
+    for (int n : {16 / es, 4, 2, 1})
         if ((channels / groups) % n == 0) slots = std::max(slots, shape_of(tokens, channels, groups, n, 1).slots);
     return static_cast<size_t>(2) * slots * channels * sizeof(float);
 }
