@@ -43,7 +43,7 @@ CCQ_API ccq_status ccq_embed(const void *table, ccq_dtype dtype, int64_t table_s
  *   padding_id an id whose row gets no gradient (zero), or negative: none.  Its rows of
  *              dout are not read.
  *   dtable     [rows, width] in grad_dtype, row stride dtable_stride; written in full.
- *   workspace  ccq_embed_grad_workspace_size() bytes, 16-byte aligned.
+ *   workspace  ccq_embed_grad_workspace_size() bytes, 16-byte aligned (NULL where that is 0).
  * The ids are sorted (stably), then every run of equal ids is summed in fp32 in ascending
  * i within pieces whose bounds depend on the ids alone, and the pieces in a fixed order.  An id
  * outside [0, rows) contributes nothing and leaves CCQ_ERR_INDEX.

@@ -13,6 +13,7 @@
 //      run of equal ids ends.  A run that ends in the next piece is finished by the piece in which it begins; of
 //      longer ones every piece leaves its part in the workspace.
 //   3. embed_join_kernel: adds the parts of the runs over three pieces and more, in order.
+// (Few ids need none of it: embed_few_kernel.)
 // 16384 x 2048 bf16 into 32000 fp32 rows (329 MB, 48.6 us at the copy rate): 70 us, of which the zeros beside the sort are
 // about 38 (213 MB, 5.6 TB/s; a plain fill of that size runs at 3.9), the sums 23 (116 MB, 5 TB/s), the join 6 and the
 // gaps between launches the rest.  With short lists the sort's latency (16 to 30 us) is most of it.
@@ -533,9 +534,132 @@ template <typename T, typename O, int N> cudaError_t launch_sum(SumArgs a, cudaS
     const int per = kSumThreads / 32;
     cudaError_t e = launch_after(embed_sum_kernel<T, O, N>, static_cast<unsigned>((warps + per - 1) / per), kSumThreads,
                                  0, s, a);
-    if (e != cudaSuccess || a.pieces < 3) return e;  // (no run spans three pieces)
+    if (e != cudaSuccess) return e;
     return launch_after(embed_join_kernel<O>, kJoinCtas, kJoinThreads, 0, s, a);
 }
+
+// ---------------------------------------------------------------- few ids
+
+// Up to kFewIds ids need no sort: every warp holds them all, eight a lane, and for each row it writes asks by ballots which
+// are equal to it, and adds their entries in ascending order.  One launch, bound by the table's rows that it writes: 30 x 2048
+// into 300 rows 6.3 us (the sort and the sums took 17), 100 x 2048 into 30000 fp32 rows 41 us (45), 6.0 TB/s.  More ids than
+// these are better sorted: a frequent id's entries are one warp's here.
+constexpr int kFewIds = 256;
+constexpr int kFewThreads = 256;
+
+struct FewArgs {
+    const void *ids;
+    int id_bytes, n, rows, width, packs, parts;  // parts: warps that share a row
+    int64_t padding;
+    const void *dout;
+    int64_t dout_stride, dtable_stride;
+    void *dtable;
+    float scale;
+    int *status;
+};
+
+template <typename T, typename O, int N> __global__ void __launch_bounds__(kFewThreads) embed_few_kernel(FewArgs a) {
+    constexpr int K = N >= 8 ? 2 : 4;                 // accesses of a lane at once
+    constexpr int kFlight = N >= 4 ? 2 : 4;           // entries at once
+    __shared__ uint8_t lists[kFewThreads / 32][kFewIds];
+    uint8_t *list = lists[threadIdx.x >> 5];
+    const int lane = threadIdx.x & 31;
+    uint32_t id[kFewIds / 32];
+#pragma unroll
+    for (int j = 0; j < kFewIds / 32; ++j) {
+        const int i = j * 32 + lane;
+        id[j] = ~0u;
+        if (i >= a.n) continue;
+        const int64_t v = load_index(a.ids, a.id_bytes, i);
+        if (v < 0 || v >= a.rows) {
+            if (blockIdx.x == 0 && threadIdx.x < 32) note_index(a.status);
+        } else if (v != a.padding) {
+            id[j] = static_cast<uint32_t>(v);
+        }
+    }
+    const uint32_t jobs = static_cast<uint32_t>(a.rows) * static_cast<uint32_t>(a.parts), warps = gridDim.x * (kFewThreads / 32);
+    for (uint32_t job = blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5); job < jobs; job += warps) {
+        const uint32_t row = job / a.parts, part = job - row * a.parts;
+        // the row's entries, in ascending order
+        int count = 0;
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < kFewIds / 32; ++j) {
+            const bool mine = id[j] == row;
+            const uint32_t hit = __ballot_sync(~0u, mine);
+            if (mine) list[count + __popc(hit & ((1u << lane) - 1))] = static_cast<uint8_t>(j * 32 + lane);
+            count += __popc(hit);
+        }
+        __syncwarp();
+        O *out = static_cast<O *>(a.dtable) + static_cast<int64_t>(row) * a.dtable_stride;
+        for (int c0 = part * 32 * K; c0 < a.packs; c0 += a.parts * 32 * K) {
+            float acc[K][N];
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int e = 0; e < N; ++e) acc[k][e] = 0.f;
+            for (int q0 = 0; q0 < count; q0 += kFlight) {
+                Pack<T, N> x[kFlight][K];
+#pragma unroll
+                for (int q = 0; q < kFlight; ++q) {
+                    const T *from = static_cast<const T *>(a.dout) + list[min(q0 + q, count - 1)] * a.dout_stride;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) x[q][k] = load_stream<T, N>(from + static_cast<int64_t>(min(c0 + k * 32 + lane, a.packs - 1)) * N);
+                }
+#pragma unroll
+                for (int q = 0; q < kFlight; ++q) {
+                    if (q0 + q >= count) break;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        float f[N];
+                        unpack(x[q][k], f);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) acc[k][e] += f[e];
+                    }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int c = c0 + k * 32 + lane;
+                if (c >= a.packs) continue;
+                float f[N];
+                Pack<O, N> o;
+#pragma unroll
+                for (int e = 0; e < N; ++e) f[e] = acc[k][e] * a.scale;
+                pack(f, o);
+                store_stream<O, N>(out + static_cast<int64_t>(c) * N, o);
+            }
+        }
+    }
+}
+
+template <typename T, typename O, int N> cudaError_t launch_few(FewArgs a, cudaStream_t s) {
+    a.packs = a.width / N;
+    a.parts = std::min(256, (a.packs + 127) / 128);  // (rows and parts: below 2^31 jobs)
+    const int64_t jobs = static_cast<int64_t>(a.rows) * a.parts;
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>((jobs + kFewThreads / 32 - 1) / (kFewThreads / 32), sm_count_now() * 8));
+    embed_few_kernel<T, O, N><<<grid, kFewThreads, 0, s>>>(a);
+    return cudaGetLastError();
+}
+
+// launch(packs of N elements of T and O) with the widest packs that `b` elements allow.
+template <template <typename, typename, int> class Launch, typename A>
+cudaError_t by_types(ccq_dtype dtype, ccq_dtype grad_dtype, int b, const A &a, cudaStream_t s) {
+    using B = __nv_bfloat16;
+    if (dtype == CCQ_BF16 && grad_dtype == CCQ_BF16)
+        return b >= 8 ? Launch<B, B, 8>::go(a, s) : b >= 2 ? Launch<B, B, 2>::go(a, s) : Launch<B, B, 1>::go(a, s);
+    if (dtype == CCQ_BF16)
+        return b >= 4 ? Launch<B, float, 4>::go(a, s) : b >= 2 ? Launch<B, float, 2>::go(a, s) : Launch<B, float, 1>::go(a, s);
+    if (grad_dtype == CCQ_BF16)
+        return b >= 4 ? Launch<float, B, 4>::go(a, s) : b >= 2 ? Launch<float, B, 2>::go(a, s) : Launch<float, B, 1>::go(a, s);
+    return b >= 4 ? Launch<float, float, 4>::go(a, s) : b >= 2 ? Launch<float, float, 2>::go(a, s) : Launch<float, float, 1>::go(a, s);
+}
+template <typename T, typename O, int N> struct Few {
+    static cudaError_t go(const FewArgs &a, cudaStream_t s) { return launch_few<T, O, N>(a, s); }
+};
+template <typename T, typename O, int N> struct Sums {
+    static cudaError_t go(const SumArgs &a, cudaStream_t s) { return launch_sum<T, O, N>(a, s); }
+};
 
 int key_bits(int64_t rows) {  // keys 0 .. rows
     int b = 1;
@@ -581,6 +705,7 @@ int64_t piece_count(int64_t n) { return (n + kPiece - 1) / kPiece; }
 size_t round16(size_t x) { return (x + 15) & ~static_cast<size_t>(15); }
 
 size_t grad_workspace(int64_t n, int width) {
+    if (n <= kFewIds) return 0;
     const size_t pieces = static_cast<size_t>(piece_count(n));
     return 2 * round16(static_cast<size_t>(n) * 8) + 16 + round16(pieces * 8) + round16(pieces * 2 * width * sizeof(float));
 }
@@ -670,13 +795,33 @@ ccq_status ccq_embed_grad(const void *dout, ccq_dtype dtype, int64_t dout_stride
         return op_fail(CCQ_ERR_INVALID_ARG, "padding_id=%lld is outside the table of %lld rows",
                        static_cast<long long>(padding_id), static_cast<long long>(rows));
     const size_t need = grad_workspace(n, width);
-    if ((st = op_pointer("workspace", workspace, 16)) != CCQ_OK) return st;
+    if (need && (st = op_pointer("workspace", workspace, 16)) != CCQ_OK) return st;
     if (workspace_bytes < need)
         return op_fail(CCQ_ERR_INVALID_ARG, "workspace of %zu bytes, needs %zu", workspace_bytes, need);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    // elements an access may hold in both operands, at most 16 bytes of the wider type
+    const int es = dtype_bytes(dtype), eo = dtype_bytes(grad_dtype);
+    const int out_bytes = row_access(dtable, dtable_stride, eo, rows, access_bytes(static_cast<uintptr_t>(width) * eo));
+    int b = out_bytes / eo;
+    if (n > 0) b = std::min(b, row_access(dout, dout_stride, es, n, access_bytes(static_cast<uintptr_t>(width) * es)) / es);
+    if (n <= kFewIds) {
+        FewArgs f = {};
+        f.ids = ids;
+        f.id_bytes = id_bytes;
+        f.n = static_cast<int>(n);
+        f.rows = static_cast<int>(rows);
+        f.width = width;
+        f.padding = padding_id;
+        f.dout = dout;
+        f.dout_stride = dout_stride;
+        f.dtable = dtable;
+        f.dtable_stride = dtable_stride;
+        f.scale = scale;
+        f.status = device_status_word();
+        return op_cuda(by_types<Few>(dtype, grad_dtype, b, f, s), "embedding gradient launch");
+    }
     const size_t list = round16(static_cast<size_t>(n) * 8);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
-    const int eo = dtype_bytes(grad_dtype), out_bytes = row_access(dtable, dtable_stride, eo, rows, access_bytes(static_cast<uintptr_t>(width) * eo));
     SortArgs so = {};
     so.ids = ids;
     so.id_bytes = id_bytes;
@@ -709,7 +854,6 @@ ccq_status ccq_embed_grad(const void *dout, ccq_dtype dtype, int64_t dout_stride
     cfg.stream = s;
     e = cudaLaunchKernelEx(&cfg, embed_sort_kernel, so);
     if (e != cudaSuccess) return op_cuda(e, "sort launch");
-    if (n == 0) return CCQ_OK;
     SumArgs a = {};
     a.dout = dout;
     a.dout_stride = dout_stride;
@@ -724,19 +868,7 @@ ccq_status ccq_embed_grad(const void *dout, ccq_dtype dtype, int64_t dout_stride
     a.joins = reinterpret_cast<int2 *>(ws + 2 * list + 16);
     a.pieces = static_cast<int>(piece_count(n));
     a.part = reinterpret_cast<float *>(ws + 2 * list + 16 + round16(static_cast<size_t>(a.pieces) * 8));
-    const int es = dtype_bytes(dtype);
-    // elements an access may hold in both operands, at most 16 bytes of the wider type
-    const int b = std::min(out_bytes / eo, row_access(dout, dout_stride, es, n, access_bytes(static_cast<uintptr_t>(width) * es)) / es);
-    using B = __nv_bfloat16;
-    if (dtype == CCQ_BF16 && grad_dtype == CCQ_BF16)
-        e = b >= 8 ? launch_sum<B, B, 8>(a, s) : b >= 2 ? launch_sum<B, B, 2>(a, s) : launch_sum<B, B, 1>(a, s);
-    else if (dtype == CCQ_BF16)
-        e = b >= 4 ? launch_sum<B, float, 4>(a, s) : b >= 2 ? launch_sum<B, float, 2>(a, s) : launch_sum<B, float, 1>(a, s);
-    else if (grad_dtype == CCQ_BF16)
-        e = b >= 4 ? launch_sum<float, B, 4>(a, s) : b >= 2 ? launch_sum<float, B, 2>(a, s) : launch_sum<float, B, 1>(a, s);
-    else
-        e = b >= 4 ? launch_sum<float, float, 4>(a, s) : b >= 2 ? launch_sum<float, float, 2>(a, s)
-                                                               : launch_sum<float, float, 1>(a, s);
+    e = by_types<Sums>(dtype, grad_dtype, b, a, s);
     return op_cuda(e, "embedding gradient launch");
 }
 

@@ -83,6 +83,8 @@ def _size(fn, device, *args):
 
 
 def _workspace(workspace, need, device):
+    if workspace is None and not need:
+        return None, 0
     if workspace is None:
         return torch.empty(max(need, 16), dtype=torch.uint8, device=device), max(need, 16)
     _dense(workspace, "workspace", device)
@@ -196,7 +198,7 @@ def embed_grad(dout, ids, rows: int, *, scale: float = 1.0, padding_id: Optional
     workspace, nbytes = _workspace(workspace, _size("ccq_embed_grad_workspace_size", -1, n, rows, width), dev)
     _check(_library().ccq_embed_grad(dout.data_ptr(), _dtype_code(dout), ds, ids.data_ptr(), id_bytes, n, rows, width,
                                      scale, -1 if padding_id is None else padding_id, out.data_ptr(), _dtype_code(out),
-                                     os, workspace.data_ptr(), nbytes, _stream(dev, stream)))
+                                     os, _ptr(workspace), nbytes, _stream(dev, stream)))
     return out
 
 
@@ -264,7 +266,7 @@ def group_norm_bwd(x, weight, bias, gate, dout, *, groups: int, activation: str 
         x.data_ptr(), xs, _ptr(gate), gs, _ptr(weight), _ptr(bias), dout.data_ptr(), ds, _dtype_code(x), pdt,
         g["dx"].data_ptr(), strides["dx"], _ptr(g.get("dgate")), strides["dgate"], _ptr(g.get("dweight")),
         _ptr(g.get("dbias")), tokens, channels, groups, int(bool(centered)), eps, ACTIVATION[activation],
-        workspace.data_ptr(), nbytes, _stream(dev, stream)))
+        _ptr(workspace), nbytes, _stream(dev, stream)))
     return g
 
 
@@ -312,7 +314,7 @@ def policy_loss(logits, actions, old_logp, advantages, *, ref_logp=None, weights
     _check(_library().ccq_policy_loss(
         logits.data_ptr(), _dtype_code(logits), ls, actions.data_ptr(), id_bytes, old_logp.data_ptr(), _ptr(ref_logp),
         advantages.data_ptr(), _ptr(weights), n, vocab, ctypes.byref(p), loss.data_ptr(), logp.data_ptr(),
-        _ptr(dlogits), gs, workspace.data_ptr(), nbytes, _stream(dev, stream)))
+        _ptr(dlogits), gs, _ptr(workspace), nbytes, _stream(dev, stream)))
     return {"loss": loss, "logp": logp, "dlogits": dlogits} if grad else {"loss": loss, "logp": logp}
 
 

@@ -142,6 +142,21 @@ def test_embed_grad(dtype, out_dtype, n, rows, width, kind):
     assert torch.equal(d, ops.embed_grad(dout, ids.int(), rows, scale=3.0, dtype=out_dtype))  # same bits again
 
 
+@pytest.mark.parametrize("n,rows,width,kind", [(256, 40, 2048, "zipf"), (257, 40, 2048, "zipf"), (200, 20000, 1030, "even"), (256, 3, 40, "same"),
+                                               (64, 5000, 4100, "half"), (2, 70000, 7, "even")])
+@pytest.mark.parametrize("dtype,out_dtype", [(a, b) for a in DTYPES for b in DTYPES])
+def test_embed_grad_few_ids(dtype, out_dtype, n, rows, width, kind):
+    """On both sides of the count up to which no sort is made; some ids are padding."""
+    g = gen(n + width)
+    ids = _ids(kind, n, rows, g)
+    dout = randn(g, n, width, dtype=dtype)
+    pad = int(ids[n // 2]) if kind != "same" else 0
+    d = ops.embed_grad(dout, ids, rows, scale=0.5, padding_id=pad, dtype=out_dtype)
+    ref, mass, count = _embed_grad_ref(dout, ids, rows, 0.5, padding=pad)
+    close(d, ref, (count + 2) * U * mass + R[out_dtype] * ref.abs() + 1e-38)
+    assert not d[pad].any()
+
+
 @pytest.mark.parametrize("n,rows,width,kind", [(131072, 5000, 16, "zipf"), (200001, 3000, 8, "half"), (300000, 400000, 8, "zipf"),
                                                (150000, 100, 24, "same"), (3000, 300000, 64, "zipf"), (40000, 513, 40, "even")])
 def test_embed_grad_long_lists_and_large_tables(n, rows, width, kind):

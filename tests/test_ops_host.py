@@ -48,7 +48,7 @@ def test_embed_refusals(lib):
 
 
 def test_embed_grad_refusals(lib):
-    good = dict(dout=FAKE, dtype=0, ds=64, ids=FAKE, id_bytes=8, n=5, rows=10, width=64, scale=1.0, padding=-1, dtable=FAKE, od=1, os=64,
+    good = dict(dout=FAKE, dtype=0, ds=64, ids=FAKE, id_bytes=8, n=500, rows=10, width=64, scale=1.0, padding=-1, dtable=FAKE, od=1, os=64,
                 ws=FAKE, nbytes=1 << 30, stream=None)
     for text, ch in ((b"NULL", dict(dout=None)), (b"NULL", dict(dtable=None)), (b"NULL", dict(ws=None)), (b"aligned", dict(ws=FAKE + 8)),
                      (b"workspace", dict(nbytes=16)), (b"padding", dict(padding=10)), (b"stride", dict(ds=60)), (b"stride", dict(os=60)),
@@ -58,6 +58,8 @@ def test_embed_grad_refusals(lib):
     n = ctypes.c_size_t()
     assert lib.ccq_embed_grad_workspace_size(1000, 500, 64, ctypes.byref(n)) == 0 and n.value >= 16 * 1000
     assert lib.ccq_embed_grad_workspace_size(1000, 500, 64, None) == INVALID
+    assert lib.ccq_embed_grad_workspace_size(256, 500, 64, ctypes.byref(n)) == 0 and n.value == 0  # few ids need none
+    assert lib.ccq_embed_grad_workspace_size(257, 500, 64, ctypes.byref(n)) == 0 and n.value >= 16 * 257
 
 
 def test_group_norm_refusals(lib):
