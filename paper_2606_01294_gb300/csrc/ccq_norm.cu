@@ -554,7 +554,8 @@ template <typename T, int BWD> __global__ void __launch_bounds__(kThreads) norm_
     }
 }
 
-// dweight and dbias: 32 channels a CTA, the slots over 32 rows of threads, then those 32 in order.
+// dweight and dbias: 32 channels a CTA, the slots over 32 rows of threads (ten loads under way), then those 32 sums of
+// a channel by a warp.
 constexpr int kParamRows = 32;
 __global__ void __launch_bounds__(32 * kParamRows) norm_param_kernel(const float *part, int slots, int channels,
                                                                      void *dweight, void *dbias, int param_bf16) {
@@ -563,17 +564,24 @@ __global__ void __launch_bounds__(32 * kParamRows) norm_param_kernel(const float
     const int which = blockIdx.y, c = blockIdx.x * 32 + threadIdx.x;
     void *out = which ? dbias : dweight;
     if (!out) return;
-    const float *p = part + static_cast<int64_t>(which) * slots * channels;
+    const float *p = part + static_cast<int64_t>(which) * slots * channels + min(c, channels - 1);
     float s = 0.f;
-    if (c < channels)
-        for (int i = threadIdx.y; i < slots; i += kParamRows) s += p[static_cast<int64_t>(i) * channels + c];
+    for (int i0 = threadIdx.y; i0 < slots; i0 += 10 * kParamRows) {
+        float v[10];
+#pragma unroll
+        for (int q = 0; q < 10; ++q) v[q] = p[static_cast<int64_t>(min(i0 + q * kParamRows, slots - 1)) * channels];
+#pragma unroll
+        for (int q = 0; q < 10; ++q) s += i0 + q * kParamRows < slots ? v[q] : 0.f;
+    }
     sums[threadIdx.y][threadIdx.x] = s;
     __syncthreads();
-    if (threadIdx.y || c >= channels) return;
-    s = 0.f;
-    for (int r = 0; r < kParamRows; ++r) s += sums[r][threadIdx.x];
-    if (param_bf16) static_cast<__nv_bfloat16 *>(out)[c] = __float2bfloat16_rn(s);
-    else static_cast<float *>(out)[c] = s;
+    s = sums[threadIdx.x][threadIdx.y];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+    const int mine = blockIdx.x * 32 + threadIdx.y;
+    if (threadIdx.x || mine >= channels) return;
+    if (param_bf16) static_cast<__nv_bfloat16 *>(out)[mine] = __float2bfloat16_rn(s);
+    else static_cast<float *>(out)[mine] = s;
 }
 
 // How the groups are spread over threads, and how many slots of tokens there are.
