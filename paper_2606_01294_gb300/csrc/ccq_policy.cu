@@ -10,8 +10,8 @@
 // registers, until its sum is known, and the gradient leaves by the way the logits came.  Rows beyond what 16 CTAs
 // hold (vocabularies above 520 thousand in bf16, 260 thousand in fp32) go through policy_row_kernel, which reads them
 // twice.  policy_loss_kernel adds the rows' losses.
-// HBM bounds it: 8192 x 32000 bf16, a quarter masked (918 MB): 153 us, 6.0 TB/s, 88 % of the copy rate; 1500 x 128001 (rows on
-// no 16-byte boundary, 742 MB): 133 us, 82 %.  Short rows are bound by a row's chain of reductions (8192 x 3500: 61 %),
+// HBM bounds it: 8192 x 32000 bf16, a quarter masked (918 MB): 154 us, 6.0 TB/s, 88 % of the copy rate; 1500 x 128001 (rows on
+// no 16-byte boundary, 742 MB): 135 us, 81 %.  Short rows are bound by a row's chain of reductions (8192 x 3500: 58 %),
 // rows over several CTAs also by how many clusters fit the groups of SMs (512 x 200000 fp32: 67 %).
 #include <algorithm>
 
@@ -28,8 +28,9 @@ struct PolicyArgs {
     int id_bytes, vocab;
     const float *old_logp, *ref_logp, *advantages, *weights;
     ccq_policy_params p;
-    float scale;      // log2(e) / temperature
-    float grad_mul;   // grad_scale / temperature
+    float scale;        // log2(e) / temperature
+    float inv, inv_lo;  // 1 / temperature, as a sum
+    float grad_mul;     // grad_scale / temperature
     float *logp, *row_loss;
     void *dlogits;
     int score;  // 1: log-probabilities alone
@@ -66,17 +67,39 @@ __device__ __forceinline__ bool is_live(const PolicyArgs &a, int64_t i) {
     return w != 0.f && t >= 0 && t < a.vocab;
 }
 
+// The log-probability (chosen - m) / T - log z as the sum of two floats.  The loss needs its differences from the old and
+// reference ones to more than its own rounding: at logp = -8 that is 5e-7, which a KL term with d = 1e-3 sees 1000-fold.
+// (Knuth's exact difference; log z = e log 2 + log f with the high part of log 2 short enough for an exact product, after
+// Cody and Waite.)
+struct TwoFloats {
+    float hi, lo;
+};
+__device__ __forceinline__ TwoFloats exact_sum(float a, float b) {
+    const float s = a + b, t = s - a;
+    return {s, (a - (s - t)) + (b - t)};
+}
+__device__ __forceinline__ TwoFloats log_probability(float chosen, float m, float z, float inv, float inv_lo) {
+    const TwoFloats diff = exact_sum(chosen, -m);
+    if (!(fabsf(diff.hi) < INFINITY)) return {diff.hi - logf(z), 0.f};
+    const float q = diff.hi * inv, r = fmaf(diff.hi, inv_lo, fmaf(diff.lo, inv, fmaf(diff.hi, inv, -q)));
+    const int e = (static_cast<int>(__float_as_uint(z)) - 0x3f400000) >> 23;  // z = 2^e f, f in [0.75, 1.5)
+    const float f = __uint_as_float(__float_as_uint(z) - (static_cast<uint32_t>(e) << 23)), k = static_cast<float>(e);
+    const TwoFloats s = exact_sum(q, -k * 0.693115234375f);
+    const float rest = (r + s.lo) - fmaf(k, 3.19461849453e-05f, logf(f) + (z - z));  // (z - z: not a number stays one)
+    return exact_sum(s.hi, rest);
+}
+
 // The row's loss and c of the gradient, from its log-probability.
-__device__ __forceinline__ float row_loss(const PolicyArgs &a, const RowScalars &r, float logp, float &c) {
+__device__ __forceinline__ float row_loss(const PolicyArgs &a, const RowScalars &r, TwoFloats logp, float &c) {
     const float adv = r.adv;
-    const float ratio = expf(logp - r.old);
+    const float ratio = expf((logp.hi - r.old) + logp.lo);
     const float open = ratio * adv;
     const float held = fminf(fmaxf(ratio, 1.f - a.p.clip_low), 1.f + a.p.clip_high) * adv;
     // a ratio or advantage that is not a number stays one
     float loss = open <= held || !(held < open) ? -open : -held;
     float slope = open <= held || !(held < open) ? -open : 0.f;
     if (a.ref_logp && a.p.kl_coef != 0.f) {
-        const float d = r.ref - logp;
+        const float d = (r.ref - logp.hi) - logp.lo;
         const float em1 = expm1f(d);
         loss += a.p.kl_coef * (em1 - d);
         slope -= a.p.kl_coef * em1;
@@ -142,10 +165,10 @@ template <typename T, int N> __global__ void __launch_bounds__(kRowThreads) poli
         __syncthreads();
         if (tid == 0) {
             for (int w = 1; w < kRowThreads / 32; ++w) join(m, z, sm[w], sz[w], a.scale);
-            const float logp = (to_f32(x[row.action]) - m) / a.p.temperature - logf(z);
+            const TwoFloats logp = log_probability(to_f32(x[row.action]), m, z, a.inv, a.inv_lo);
             float c = 0.f;
             if (a.score) {
-                a.logp[i] = logp;
+                a.logp[i] = logp.hi;
             } else {
                 RowScalars r = {};
                 r.weight = row.weight;
@@ -153,7 +176,7 @@ template <typename T, int N> __global__ void __launch_bounds__(kRowThreads) poli
                 r.old = a.old_logp[i];
                 if (a.ref_logp) r.ref = a.ref_logp[i];
                 a.row_loss[i] = row_loss(a, r, logp, c);
-                if (a.logp) a.logp[i] = logp;
+                if (a.logp) a.logp[i] = logp.hi;
             }
             bc[0] = m;
             bc[1] = c;
@@ -556,11 +579,11 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
                 z = p.y;
                 join_warp(m, z, a.scale);
             }
-            const float logp = (sc.chosen - m) / a.p.temperature - logf(z);  // (divided: a rounded 1 / T would shift all rows)
+            const TwoFloats logp = log_probability(sc.chosen, m, z, a.inv, a.inv_lo);
             float c1 = 0.f, loss = 0.f;
             if (!a.score) loss = row_loss(a, sc, logp, c1);
             if (rank == 0 && tid == 0) {
-                if (a.logp) a.logp[i] = logp;
+                if (a.logp) a.logp[i] = logp.hi;
                 if (!a.score) a.row_loss[i] = loss;
             }
             if constexpr (GRAD) {
@@ -803,6 +826,12 @@ cudaError_t launch_policy(const PolicyArgs &a, ccq_dtype dtype, cudaStream_t s) 
     return b == 16 ? launch_rows<float, 4>(a, s) : launch_rows<float, 1>(a, s);
 }
 
+void set_inverse(PolicyArgs *a) {
+    const double inv = 1.0 / static_cast<double>(a->p.temperature);
+    a->inv = static_cast<float>(inv);
+    a->inv_lo = static_cast<float>(inv - static_cast<double>(a->inv));
+}
+
 ccq_status check_logits(const char *name, const void *p, int64_t stride, ccq_dtype dtype, int64_t n, int vocab) {
     if (n > 1 && stride < vocab)
         return op_fail(CCQ_ERR_INVALID_ARG, "%s: row stride %lld is below the vocabulary %d", name,
@@ -875,6 +904,7 @@ ccq_status ccq_policy_loss(const void *logits, ccq_dtype dtype, int64_t logits_s
     a.n = n; a.vocab = vocab;
     a.old_logp = old_logp; a.ref_logp = ref_logp; a.advantages = advantages; a.weights = weights;
     a.scale = kLog2e / a.p.temperature;
+    set_inverse(&a);
     a.grad_mul = a.p.grad_scale / a.p.temperature;
     a.logp = logp; a.row_loss = static_cast<float *>(workspace);
     a.dlogits = dlogits; a.dlogits_stride = dlogits_stride;
@@ -898,6 +928,7 @@ ccq_status ccq_token_logp(const void *logits, ccq_dtype dtype, int64_t logits_st
     a.n = n; a.vocab = vocab;
     a.p.temperature = temperature;
     a.scale = kLog2e / temperature;
+    set_inverse(&a);
     a.logp = logp;
     a.score = 1;
     a.status = device_status_word();
