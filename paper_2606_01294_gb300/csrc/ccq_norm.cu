@@ -13,9 +13,9 @@
 // adds them in a fixed order.  A team is at most a warp where K accesses each suffice, else the
 // whole CTA; groups beyond that (d > 4096) are walked in memory (norm_long_kernel).
 // Measured, bf16 with a gate and groups of 128: forward of 32768 x 2048 64 us (6.3 TB/s, 93 % of the copy rate; HBM bounds
-// it); backward of 16384 x 2048 62 us (5.4 TB/s, 80 %; 41 instructions an element, about half of them in the FMA pipes,
-// which packed pairs do not speed up, and 5 us for the parameters' gradients).  Groups of 33, one element an access: 31 and
-// 26 %.
+// it); backward of 16384 x 2048 62 us (5.4 TB/s, 80 %), of 65536 tokens 216 us (92 %): about 10 us of a call are its two
+// launches, first loads and the parameters' partial sums, the rest HBM with the issue slots 62 % busy (41 instructions an
+// element).  Groups of 33, one element an access: 31 and 26 %.
 #include <algorithm>
 
 #include "ccq_ops.cuh"

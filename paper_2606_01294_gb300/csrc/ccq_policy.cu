@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
     T *dlogits = static_cast<T *>(a.dlogits);
     const int first = rank * g.per;  // this slice's first granule
     // rows loaded (thread 0) and computed so far: their buffers and the barriers' phases
-    uint32_t load_at = 0, at = 0, phase = 0, rows = 0;
+    uint32_t load_at = 0, at = 0, phase = 0, rows = 0, issued = 0;
     const int lag = g.buffers > 3 ? 2 : 1;  // rows whose gradients may still be leaving
     const int ahead = g.buffers - lag;      // rows whose logits are under way or here
 
@@ -367,6 +367,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
             mbar_arrive(&full[b]);
         }
         load_at = load_at + 1 == static_cast<uint32_t>(g.buffers) ? 0 : load_at + 1;
+        ++issued;
     };
     // The last warp's lanes: the elements of the granules that row i shares with its neighbours, -inf in the others' places.
     // `cell` is where the value belongs in the row's buffer (-1: nowhere in this slice).
@@ -647,8 +648,13 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
         }
         __syncthreads();  // the batch's scalars may go
     }
-    if constexpr (GRAD) {
-        if (tid == 0) tma_store_wait_all();
+    if (tid == 0) {
+        if constexpr (GRAD) tma_store_wait_all();
+        // copies that a wait gave up on have landed too before the CTA leaves (all others have: no time)
+        const uint32_t buffers = static_cast<uint32_t>(g.buffers);
+        for (uint32_t b = 0; b < buffers; ++b)
+            if (const uint32_t uses = (issued + buffers - 1 - b) / buffers) mbar_drain(&full[b], (uses - 1) & 1);
+        if (g.cs > 1 && rows) mbar_drain(&heard[(rows - 1) & 1], ((rows - 1) >> 1) & 1);
     }
     if (g.cs > 1) cluster_barrier();  // no CTA leaves while others may still write to it
 }
