@@ -600,7 +600,7 @@ Shape shape_of(int64_t tokens, int channels, int groups, int n, int bwd) {
     while (s.k < kmax && 32 * s.k < packs) s.k = n == 1 || n == 2 ? s.k * 4 : s.k * 2;
     s.k = std::min(s.k, kmax);
     if (32 * s.k >= packs) {
-        s.team = s.k == 4 && n <= 2 ? (packs <= 32 ? 8 : packs <= 64 ? 16 : 32) : s.k > 1 ? 32 : packs <= 1 ? 1 : packs <= 4 ? 4 : packs <= 8 ? 8 : packs <= 16 ? 16 : 32;
+        s.team = s.k == 4 && n <= 2 ? (packs <= 64 ? 16 : 32) : s.k > 1 ? 32 : packs <= 1 ? 1 : packs <= 4 ? 4 : packs <= 8 ? 8 : packs <= 16 ? 16 : 32;
     } else if (kThreads * kmax >= packs) {
         s.k = kThreads >= packs ? 1 : kmax;
         s.team = kThreads;
@@ -639,10 +639,8 @@ template <typename T, int N, int K, int BWD> cudaError_t launch_one(const NormAr
             case 16: return launch_team<T, N, K, 16, BWD>(a, sh, s);
         }
     }
-    if constexpr (K == 4 && N <= 2) {
-        if (sh.team == 8) return launch_team<T, N, K, 8, BWD>(a, sh, s);
+    if constexpr (K == 4 && N <= 2)
         if (sh.team == 16) return launch_team<T, N, K, 16, BWD>(a, sh, s);
-    }
     if constexpr (K == 1 || N * K == kMaxElems)
         if (sh.team == kWide) return launch_team<T, N, K, kWide, BWD>(a, sh, s);
     return launch_team<T, N, K, 32, BWD>(a, sh, s);

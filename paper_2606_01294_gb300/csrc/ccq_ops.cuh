@@ -113,14 +113,13 @@ template <typename T, int N> __device__ __forceinline__ Pack<T, N> load_plain(co
 template <typename T, int N> __device__ __forceinline__ void store_stream(T *p, const Pack<T, N> &v) {
     __stcs(reinterpret_cast<typename Pack<T, N>::Mem *>(p), static_cast<typename Pack<T, N>::Mem>(v.raw));
 }
-template <typename T, int N> __device__ __forceinline__ void store_plain(T *p, const Pack<T, N> &v) {
-    *reinterpret_cast<typename Pack<T, N>::Mem *>(p) = static_cast<typename Pack<T, N>::Mem>(v.raw);
-}
 
 template <int W> __device__ __forceinline__ uint32_t word_of(const uint4 &r) {
     return W == 0 ? r.x : W == 1 ? r.y : W == 2 ? r.z : r.w;
 }
+
 template <int W> __device__ __forceinline__ uint32_t word_of(const uint2 &r) { return W == 0 ? r.x : r.y; }
+
 template <int W> __device__ __forceinline__ uint32_t word_of(uint32_t r) { return r; }
 template <int W> __device__ __forceinline__ void set_word(uint4 &r, uint32_t w) {
     (W == 0 ? r.x : W == 1 ? r.y : W == 2 ? r.z : r.w) = w;

@@ -216,8 +216,7 @@ constexpr int batch_rows(int threads) { return threads <= 128 ? 64 : 256; }
 constexpr int kMaxCluster = 16;
 constexpr int kRanked = 16384;
 constexpr int kGranules = 8;  // of a thread: their exponentials stay in registers until the row's sum is known
-constexpr size_t kMaxSlice = 512 * kGranules * 16;  // bytes of a buffer: three and the scalars fit an SM
-constexpr size_t kSmBytes = 206848;                      // of which an SM's CTAs share
+constexpr size_t kSmBytes = 206848;  // shared memory that the CTAs of an SM divide among them
 constexpr float kLowest = -3.402823466e38f;
 
 struct Staging {
