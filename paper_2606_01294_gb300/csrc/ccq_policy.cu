@@ -80,8 +80,10 @@ __device__ __forceinline__ TwoFloats exact_sum(float a, float b) {
 }
 __device__ __forceinline__ TwoFloats log_probability(float chosen, float m, float z, float inv, float inv_lo) {
     const TwoFloats diff = exact_sum(chosen, -m);
-    if (!(fabsf(diff.hi) < INFINITY)) return {diff.hi - logf(z), 0.f};
-    const float q = diff.hi * inv, r = fmaf(diff.hi, inv_lo, fmaf(diff.lo, inv, fmaf(diff.hi, inv, -q)));
+    const float q = diff.hi * inv;
+    // no digits below an infinity (a masked action, also one at the type's lowest value once the temperature has divided it)
+    if (!(fabsf(q) < INFINITY)) return {q - logf(z), 0.f};
+    const float r = fmaf(diff.hi, inv_lo, fmaf(diff.lo, inv, fmaf(diff.hi, inv, -q)));
     const int e = (static_cast<int>(__float_as_uint(z)) - 0x3f400000) >> 23;  // z = 2^e f, f in [0.75, 1.5)
     const float f = __uint_as_float(__float_as_uint(z) - (static_cast<uint32_t>(e) << 23)), k = static_cast<float>(e);
     const TwoFloats s = exact_sum(q, -k * 0.693115234375f);

@@ -475,6 +475,36 @@ def test_policy_loss_infinite_logits_and_bad_actions():
     assert torch.isnan(score[[2, 4]]).all() and torch.isfinite(score[[0, 1, 3, 5]]).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", [5000, 1000003])  # staged rows, and rows that are read twice
+@pytest.mark.parametrize("temperature", [0.8, 1.0, 1.5])
+def test_policy_loss_of_an_action_at_the_lowest_value(dtype, vocab, temperature):
+    """A mask of the type's lowest value on the action itself: divided by a temperature below 1 it is below every fp32
+    number, so its log-probability is -inf; the ratio is 0, the loss finite, and nothing of the row moves."""
+    logits, actions, old, ref, adv, w = _policy_inputs(6, vocab, dtype, 11)
+    masked = torch.tensor([0, 3, 4], device="cuda")
+    adv[0], adv[3] = 1.5, -0.7  # both sides of the smaller term
+    logits[masked, actions[masked]] = torch.finfo(dtype).min
+    clip = (0.2, 0.3)
+    loss, logp, grad, edge, mass = _policy64(logits, actions, old, None, adv, w, clip, 0, float(torch.tensor(temperature)))
+    got = ops.policy_loss(logits, actions, old, adv, weights=w, clip=clip, temperature=temperature)
+    live = torch.tensor([1, 2, 5], device="cuda")
+    live = live[~edge[live]]
+    # masked: lowest / temperature, a quotient, a sum and its rounding: 4 u of it, or beyond fp32: -inf
+    low = torch.where(logp.float().isinf(), float("-inf"), logp)[masked]
+    if temperature < 1:
+        assert torch.isneginf(low).all() and torch.equal(got["logp"][masked].double(), low)
+    else:
+        close(got["logp"][masked], low, 4 * U * low.abs(), "masked logp")
+    tol = 8 * U * (2 * 20 / temperature + math.log(vocab) + 1) + 1e-6  # |logits| below 20
+    close(got["logp"][live], logp[live], tol + U * logp[live].abs(), "logp")
+    close(got["loss"], loss, (4 * tol + ARITH) * mass + 1e-30, "loss")
+    assert not got["dlogits"][masked].any()
+    top = grad.abs().amax(1, keepdim=True)
+    close(got["dlogits"][live], grad[live], (R[dtype] * grad.abs() + (4 * tol + 2 * ARITH) * 4 * top + 1e-38)[live], "dlogits")
+    assert torch.equal(ops.token_logp(logits, actions, temperature=temperature), got["logp"])
+
+
 def test_policy_loss_nan_stays_in_its_row_and_empty():
     logits, actions, old, ref, adv, w = _policy_inputs(8, 40000, torch.bfloat16, 12)
     clean = ops.policy_loss(logits, actions, old, adv)
