@@ -103,7 +103,7 @@ __device__ __forceinline__ float row_loss(const PolicyArgs &a, const RowScalars 
     if (a.ref_logp && a.p.kl_coef != 0.f) {
         const float d = (r.ref - logp.hi) - logp.lo;
         const float em1 = expm1f(d);
-        loss += a.p.kl_coef * (em1 - d);
+        loss += a.p.kl_coef * (em1 < INFINITY ? em1 - d : em1);  // (infinite d: exp(d) outgrows it)
         slope -= a.p.kl_coef * em1;
     }
     c = r.weight * slope * a.grad_mul;

@@ -505,6 +505,20 @@ def test_policy_loss_of_an_action_at_the_lowest_value(dtype, vocab, temperature)
     assert torch.equal(ops.token_logp(logits, actions, temperature=temperature), got["logp"])
 
 
+@pytest.mark.parametrize("vocab", [5000, 300008])  # staged rows, and rows that are read twice
+def test_policy_loss_kl_term_of_a_masked_action(vocab):
+    """exp(d) - d - 1 for d = ref - logp without bounds (an action whose logit is -inf) is infinite, and not NaN."""
+    logits, actions, old, ref, adv, w = _policy_inputs(5, vocab, torch.float32, 13)
+    logits[2, actions[2]] = float("-inf")
+    got = ops.policy_loss(logits, actions, old, adv, ref_logp=ref, weights=w, kl_coef=0.1)
+    assert torch.isneginf(got["logp"][2]) and float(got["loss"]) == math.inf
+    ref[2] = float("-inf")  # d the other way: exp(d) = 0, -d infinite
+    logits[2, actions[2]] = 0.0
+    assert float(ops.policy_loss(logits, actions, old, adv, ref_logp=ref, weights=w, kl_coef=0.1)["loss"]) == math.inf
+    w[2] = 0
+    assert math.isfinite(float(ops.policy_loss(logits, actions, old, adv, ref_logp=ref, weights=w, kl_coef=0.1)["loss"]))
+
+
 def test_policy_loss_nan_stays_in_its_row_and_empty():
     logits, actions, old, ref, adv, w = _policy_inputs(8, 40000, torch.bfloat16, 12)
     clean = ops.policy_loss(logits, actions, old, adv)
