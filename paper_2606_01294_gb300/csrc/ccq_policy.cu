@@ -390,6 +390,14 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
         return v;
     };
 
+    // A later bulk copy writes over these cells when the buffer comes round, so the ordinary store is ordered before the copies
+    // that the next barrier lets thread 0 start.  (With a gradient the fence that every thread makes in the row itself does that.)
+    auto set_edge = [&](uint4 *buf, int cell, T v) {
+        if (cell < 0) return;
+        reinterpret_cast<T *>(buf)[cell] = v;
+        if constexpr (!GRAD) fence_proxy_async_smem();
+    };
+
     for (int64_t start = 0; start < a.n; start += g.span) {
         // this cluster's rows of the span: `live` ones to compute and `dead` (masked) ones to zero
         const int64_t span = a.n - start < g.span ? a.n - start : g.span;
@@ -507,7 +515,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
         if (count > 0) {
             int cell;
             const T v = edge_of(row_index(0), cell);
-            if (cell >= 0) reinterpret_cast<T *>(buffer(at))[cell] = v;
+            set_edge(buffer(at), cell, v);
         }
         if constexpr (GRAD) {
             // masked rows: zeros, while the first rows come in
@@ -628,7 +636,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS) policy_staged_kernel(P
                 }
                 fence_proxy_async_smem();
             }
-            if (edge_cell >= 0) reinterpret_cast<T *>(buffer(next))[edge_cell] = edge;
+            set_edge(buffer(next), edge_cell, edge);
             __syncthreads();
             if (tid == 0) {
                 if constexpr (GRAD) {

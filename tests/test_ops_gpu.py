@@ -417,6 +417,22 @@ def test_policy_loss_many_rows(dtype, n, vocab):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,vocab", [(9000, 1003), (5000, 8197), (2500, 33001), (700, 70001)])
+def test_token_logp_many_odd_rows(dtype, n, vocab):
+    """Rows of every alignment in turn through each buffer, without a gradient: a buffer's cells are written by bulk copies
+    in one row and by ordinary stores (a row's first and last elements) in another."""
+    g = gen(n)
+    logits, actions = randn(g, n, vocab).mul_(2).to(dtype), torch.randint(0, vocab, (n,), device="cuda", generator=g)
+    # half of the actions on a row's first and last elements
+    actions[::4], actions[1::4] = 0, vocab - 1
+    logp = torch.cat([torch.log_softmax(x.double() / 0.8, -1).gather(1, a[:, None])[:, 0]
+                      for x, a in zip(logits.split(500), actions.split(500))])
+    bound = _logp_bound(logits, 0.8) + U * logp.abs()
+    for _ in range(3):
+        close(ops.token_logp(logits, actions, temperature=0.8), logp, bound, "logp")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("pad,offset", [(0, 1), (1, 0), (8, 8), (3, 5), (2, 4), (16, 0)])
 @pytest.mark.parametrize("vocab", [3000, 40008, 70001])
 def test_policy_loss_strides(dtype, pad, offset, vocab):
