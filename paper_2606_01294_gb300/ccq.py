@@ -243,6 +243,27 @@ def _stream(device, stream):
     return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
 
 
+def _on_stream(stream, call, *args, **kw):
+    """``call`` as within ``torch.cuda.stream(stream)``: what it allocates belongs to that stream, so that the allocator
+    gives no workspace's memory to other work before the stream is through with it (and hands out none that other
+    streams still use).  What it returns is recorded on the caller's stream too, where it is used as a rule."""
+    caller = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        result = call(*args, **kw)
+    rest = [result]
+    while rest:
+        t = rest.pop()
+        if isinstance(t, torch.Tensor):
+            t.record_stream(caller)
+        elif isinstance(t, CCQState):
+            rest += [t.S, t.C, t.m, t.t]
+        elif isinstance(t, (tuple, list)):
+            rest += t
+        elif isinstance(t, dict):
+            rest += t.values()
+    return result
+
+
 @dataclass
 class CCQState:
     """Recurrent cache (Algorithm 2's triple plus the position): S^T [B,H,Dk,Dv],

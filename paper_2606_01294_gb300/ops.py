@@ -4,7 +4,9 @@ The embedding lookup and its gradient, the (gated) group norm after the mixer's 
 clipped policy loss with its gradient, the token log-probabilities, and the AdamW update of many tensors.  As in
 :mod:`.ccq`, this is argument marshalling only: tensors are CUDA tensors (there is no CPU path), outputs
 and workspaces are allocated with torch on the inputs' device, and every computation runs in the
-library's kernels on the current stream.
+library's kernels on the current stream.  ``stream=`` makes a call as within ``torch.cuda.stream(stream)``: what
+it allocates belongs to that stream, which waits for the inputs, and is waited for, as torch's streams do; what
+it returns may be used on the caller's stream after such a wait, and dropped there.
 
 Tensors of rows need contiguous rows; the rows themselves may lie apart (a slice of a wider projection), as
 long as one stride reaches them all.
@@ -21,7 +23,7 @@ from typing import List, Optional
 import torch
 
 from . import ccq
-from .ccq import _check, _dtype_code, _ptr, _stream
+from .ccq import _check, _dtype_code, _on_stream, _ptr, _stream
 
 ACTIVATION = {"none": 0, "silu": 1, "sigmoid": 2}
 ADAMW_BLOCK = 256
@@ -164,6 +166,8 @@ def embed(table, ids, *, scale: float = 1.0, out=None, stream=None):
     """``scale * table[ids]`` (ccq_embed): table [rows, width] bf16 or fp32, ids int64 or int32 of any
     shape; returns [*ids.shape, width].  An id outside the table gives a zero row and CCQ_ERR_INDEX
     from :func:`ccq.device_status`."""
+    if stream is not None:
+        return _on_stream(stream, embed, table, ids, scale=scale, out=out)
     ts = _rows(table, "table")
     if table.dim() != 2:
         raise ValueError("table must be [rows, width]")
@@ -175,7 +179,7 @@ def embed(table, ids, *, scale: float = 1.0, out=None, stream=None):
     else:
         os = _rows(out, "out", dev, table.dtype, ids.shape + (width,))
     _check(_library().ccq_embed(table.data_ptr(), _dtype_code(table), ts, ids.data_ptr(), id_bytes, ids.numel(), rows,
-                                width, scale, out.data_ptr(), os, _stream(dev, stream)))
+                                width, scale, out.data_ptr(), os, _stream(dev, None)))
     return out
 
 
@@ -184,6 +188,9 @@ def embed_grad(dout, ids, rows: int, *, scale: float = 1.0, padding_id: Optional
     """Gradient of :func:`embed`'s table (ccq_embed_grad): row r is ``scale`` times the sum of dout over
     the tokens with id r, summed in fp32 in a fixed order; rows without a token (and ``padding_id``'s) are zero.
     dout [*ids.shape, width]; returns [rows, width] in ``dtype`` (dout's when not given) or ``out``."""
+    if stream is not None:
+        return _on_stream(stream, embed_grad, dout, ids, rows, scale=scale, padding_id=padding_id, dtype=dtype, out=out,
+                          workspace=workspace)
     _rows(dout, "dout")
     dev = dout.device
     id_bytes = _ids(ids, "ids", dev)
@@ -198,7 +205,7 @@ def embed_grad(dout, ids, rows: int, *, scale: float = 1.0, padding_id: Optional
     workspace, nbytes = _workspace(workspace, _size("ccq_embed_grad_workspace_size", -1, n, rows, width), dev)
     _check(_library().ccq_embed_grad(dout.data_ptr(), _dtype_code(dout), ds, ids.data_ptr(), id_bytes, n, rows, width,
                                      scale, -1 if padding_id is None else padding_id, out.data_ptr(), _dtype_code(out),
-                                     os, _ptr(workspace), nbytes, _stream(dev, stream)))
+                                     os, _ptr(workspace), nbytes, _stream(dev, None)))
     return out
 
 
@@ -228,6 +235,9 @@ def group_norm(x, weight=None, bias=None, gate=None, *, groups: int, activation:
     follows the mixer's read.  x [..., channels] bf16 or fp32; weight, bias [channels] (None: 1 and
     0); ``u * act(gate)`` with a gate of x's shape, ``act(u)`` without.  ``centered=False`` leaves the mean in
     (a root-mean-square norm)."""
+    if stream is not None:
+        return _on_stream(stream, group_norm, x, weight, bias, gate, groups=groups, activation=activation,
+                          centered=centered, eps=eps, out=out)
     dev, xs, gs, channels, pdt, tokens = _norm_args(x, weight, bias, gate, groups, activation)
     if out is None:
         out, os = torch.empty(x.shape, dtype=x.dtype, device=dev), channels
@@ -235,7 +245,7 @@ def group_norm(x, weight=None, bias=None, gate=None, *, groups: int, activation:
         os = _rows(out, "out", dev, x.dtype, x.shape)
     _check(_library().ccq_group_norm(x.data_ptr(), xs, _ptr(gate), gs, _ptr(weight), _ptr(bias), _dtype_code(x), pdt,
                                      out.data_ptr(), os, tokens, channels, groups, int(bool(centered)), eps,
-                                     ACTIVATION[activation], _stream(dev, stream)))
+                                     ACTIVATION[activation], _stream(dev, None)))
     return out
 
 
@@ -244,6 +254,9 @@ def group_norm_bwd(x, weight, bias, gate, dout, *, groups: int, activation: str 
     """Gradients of :func:`group_norm` (ccq_group_norm_bwd): a dict of dx, dgate (where there is a gate), dweight
     and dbias (where there are those).  Only the forward's inputs are needed.  ``out`` may hold preallocated
     tensors under those names."""
+    if stream is not None:
+        return _on_stream(stream, group_norm_bwd, x, weight, bias, gate, dout, groups=groups, activation=activation,
+                          centered=centered, eps=eps, out=out, workspace=workspace)
     dev, xs, gs, channels, pdt, tokens = _norm_args(x, weight, bias, gate, groups, activation)
     ds = _rows(dout, "dout", dev, x.dtype, x.shape)
     g = dict(out or {})
@@ -266,7 +279,7 @@ def group_norm_bwd(x, weight, bias, gate, dout, *, groups: int, activation: str 
         x.data_ptr(), xs, _ptr(gate), gs, _ptr(weight), _ptr(bias), dout.data_ptr(), ds, _dtype_code(x), pdt,
         g["dx"].data_ptr(), strides["dx"], _ptr(g.get("dgate")), strides["dgate"], _ptr(g.get("dweight")),
         _ptr(g.get("dbias")), tokens, channels, groups, int(bool(centered)), eps, ACTIVATION[activation],
-        _ptr(workspace), nbytes, _stream(dev, stream)))
+        _ptr(workspace), nbytes, _stream(dev, None)))
     return g
 
 
@@ -290,6 +303,10 @@ def policy_loss(logits, actions, old_logp, advantages, *, ref_logp=None, weights
     [...] fp32.  A token of weight 0 is masked: nothing of it counts, whatever it holds.  ``clip`` is (low, high), the ratio is held
     in [1 - low, 1 + high].  Returns a dict of loss (a scalar tensor), logp [...] (0 where masked) and,
     with ``grad``, dlogits (``grad_scale`` times the loss's gradient; ``dlogits`` may be the logits)."""
+    if stream is not None:
+        return _on_stream(stream, policy_loss, logits, actions, old_logp, advantages, ref_logp=ref_logp, weights=weights,
+                          clip=clip, kl_coef=kl_coef, temperature=temperature, grad_scale=grad_scale, grad=grad,
+                          dlogits=dlogits, workspace=workspace)
     dev, ls, id_bytes = _tokens(logits, actions)
     shape, vocab = actions.shape, logits.shape[-1]
     _dense(old_logp, "old_logp", dev, torch.float32, shape)
@@ -314,13 +331,15 @@ def policy_loss(logits, actions, old_logp, advantages, *, ref_logp=None, weights
     _check(_library().ccq_policy_loss(
         logits.data_ptr(), _dtype_code(logits), ls, actions.data_ptr(), id_bytes, old_logp.data_ptr(), _ptr(ref_logp),
         advantages.data_ptr(), _ptr(weights), n, vocab, ctypes.byref(p), loss.data_ptr(), logp.data_ptr(),
-        _ptr(dlogits), gs, _ptr(workspace), nbytes, _stream(dev, stream)))
+        _ptr(dlogits), gs, _ptr(workspace), nbytes, _stream(dev, None)))
     return {"loss": loss, "logp": logp, "dlogits": dlogits} if grad else {"loss": loss, "logp": logp}
 
 
 def token_logp(logits, actions, *, temperature: float = 1.0, out=None, stream=None):
     """``log_softmax(logits / temperature)`` at the actions (ccq_token_logp), fp32 [...]: the old and reference
     log-probabilities of a policy loss."""
+    if stream is not None:
+        return _on_stream(stream, token_logp, logits, actions, temperature=temperature, out=out)
     dev, ls, id_bytes = _tokens(logits, actions)
     if out is None:
         out = torch.empty(actions.shape, dtype=torch.float32, device=dev)
@@ -328,7 +347,7 @@ def token_logp(logits, actions, *, temperature: float = 1.0, out=None, stream=No
         _dense(out, "out", dev, torch.float32, actions.shape)
     _check(_library().ccq_token_logp(logits.data_ptr(), _dtype_code(logits), ls, actions.data_ptr(), id_bytes,
                                      actions.numel(), logits.shape[-1], temperature, out.data_ptr(),
-                                     _stream(dev, stream)))
+                                     _stream(dev, None)))
     return out
 
 

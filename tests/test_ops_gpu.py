@@ -760,3 +760,46 @@ def test_operators_run_on_the_current_stream():
     torch.cuda.synchronize()
     for a, b in zip(want, held):
         assert torch.equal(a, b)
+
+
+def test_stream_argument(monkeypatch):
+    """A call with stream= behind a long wait on that stream: its workspace is not given to the current stream's next
+    tensors, and results are those of the current stream."""
+    g = gen(42)
+    n = 3000
+    ids = torch.randint(0, 500, (n,), device="cuda", generator=g)
+    x, gate, dy = (randn(g, n, 256, dtype=torch.bfloat16) for _ in range(3))
+    w, b = 1 + 0.1 * randn(g, 256), 0.1 * randn(g, 256)
+    table = randn(g, 500, 256)
+    logits, actions, old, ref, adv, weights = _policy_inputs(n, 700, torch.bfloat16, 43)
+
+    def all_of(**how):
+        d = ops.group_norm_bwd(x, w, b, gate, dy, groups=2, **how)
+        p = ops.policy_loss(logits, actions, old, adv, ref_logp=ref, weights=weights, kl_coef=0.1, **how)
+        return [ops.embed(table, ids, **how), ops.group_norm(x, w, b, gate, groups=2, **how), ops.token_logp(logits, actions, **how),
+                ops.embed_grad(dy, ids, 500, **how)] + [d[k] for k in sorted(d)] + [p[k] for k in sorted(p)]
+
+    want = all_of()
+    side, spaces, keep = torch.cuda.Stream(), [], ops._workspace
+
+    def workspace(*args):
+        made = keep(*args)
+        if made[0] is not None:
+            spaces.append((made[0].data_ptr(), made[1]))
+        return made
+
+    monkeypatch.setattr(ops, "_workspace", workspace)
+    torch.cuda.synchronize()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    got = all_of(stream=side)
+    assert len(spaces) == 3
+    # tensors of those sizes on the current stream, written while the other has yet to begin
+    fills = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for _, size in spaces for _ in range(8)]
+    assert not side.query()
+    for at, size in spaces:
+        assert all(f.data_ptr() + f.numel() <= at or at + size <= f.data_ptr() for f in fills)
+    torch.cuda.current_stream().wait_stream(side)
+    for a, c in zip(want, got):
+        assert torch.equal(a, c)

@@ -1,6 +1,7 @@
 """Host-side checks of the operators around the token mixer (ccq_ops.h): every bad argument is refused with a
 status before any CUDA call, sizes are answered without a GPU, and the binding refuses CPU tensors."""
 import ctypes
+import inspect
 
 import pytest
 import torch
@@ -149,3 +150,50 @@ def test_rows_strides(monkeypatch):
     assert ops._rows(torch.zeros(3, 4, 9)[..., 2:7], "t") == 9
     assert ops._rows(torch.zeros(3, 9)[1:2, :4], "t") == 4
     assert ops._rows(torch.zeros(6, 4, 9)[::2, 1:2, :5], "t") == 72
+
+
+@pytest.mark.parametrize("call", [ops.embed, ops.embed_grad, ops.group_norm, ops.group_norm_bwd, ops.policy_loss, ops.token_logp])
+def test_a_given_stream_is_entered_for_the_whole_call(call, monkeypatch):
+    """What a call allocates has to belong to the stream it runs on: with ``stream`` the whole call is made within it, with
+    every other argument as it came."""
+    seen = []
+    monkeypatch.setattr(ops, "_on_stream", lambda stream, fn, *args, **kw: seen.append((stream, fn, args, kw)) or "result")
+    given = {name: object() for name in inspect.signature(call).parameters}
+    assert call(**given) == "result"
+    (stream, fn, args, kw), = seen
+    assert stream is given.pop("stream") and fn is call
+    bound = inspect.signature(call).bind(*args, **kw).arguments
+    assert bound.keys() == given.keys() and all(bound[name] is given[name] for name in given)
+
+
+def test_on_stream_enters_and_records(monkeypatch):
+    """The call runs inside the stream's context and every tensor that it returns is recorded on the caller's."""
+    inside, recorded = [], []
+
+    class Context:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            inside.append(self.stream)
+
+        def __exit__(self, *error):
+            inside.pop()
+
+    class Stream:
+        device = "cuda:0"
+
+    stream = Stream()
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: ("caller", device))
+    monkeypatch.setattr(torch.cuda, "stream", Context)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: recorded.append((t.numel(), s)))
+    made = [torch.zeros(k) for k in range(1, 8)]
+    state = ccq.CCQState(*made[3:])
+
+    def call(a, b=None):
+        assert inside == [stream] and (a, b) == (1, 2)
+        return made[0], None, {"x": made[1], "y": [made[2], state]}
+
+    result = ccq._on_stream(stream, call, 1, b=2)
+    assert not inside and result[2]["y"][1] is state
+    assert sorted(recorded) == [(k, ("caller", "cuda:0")) for k in range(1, 8)]
