@@ -4,7 +4,8 @@ Every step of the CCQ computation runs in the library's CUDA kernels; this
 module checks tensor placement/dtype/layout, allocates outputs with torch on
 the input's device, and passes raw device pointers plus the current CUDA
 stream through ctypes.  There is no CPU path: if the library is missing, or a
-tensor is not on a CUDA device, the call raises.
+tensor is not on a CUDA device, the call raises.  ``stream=`` makes a call as within
+``torch.cuda.stream(stream)``, what it allocates included.
 """
 from __future__ import annotations
 
@@ -309,6 +310,9 @@ def gla_fwd(q, k, v, gk, lam, state: Optional[CCQState] = None, *, out=None,
     is allocated on the fly when needed and not given.  Keyword arguments go to
     :func:`params`.
     """
+    if stream is not None:
+        return _on_stream(stream, gla_fwd, q, k, v, gk, lam, state, out=out, final_state=final_state, return_state=return_state,
+                          workspace=workspace, **kw)
     dev = q.device
     B, T, H, Dk = q.shape
     Dv = v.shape[-1]
@@ -335,7 +339,7 @@ def gla_fwd(q, k, v, gk, lam, state: Optional[CCQState] = None, *, out=None,
         _ptr(S0), _ptr(C0), _ptr(m0), _ptr(t0), _ptr(o),
         _ptr(fs.S if fs else None), _ptr(fs.C if fs else None), _ptr(fs.m if fs else None),
         _ptr(fs.t if fs else None), B, T, H, Dk, Dv, _ptr(workspace), ws_bytes,
-        pref, _stream(dev, stream))
+        pref, _stream(dev, None))
     _check(st)
     return (o, fs) if return_state else o
 
@@ -353,6 +357,9 @@ def gla_fwd_save(q, k, v, gk, lam, state: Optional[CCQState] = None, *, ckpt=Non
     """:func:`gla_fwd` that also writes the chunk-start states the backward
     needs into ``ckpt`` (a CUDA uint8 tensor of :func:`gla_ckpt_size` bytes,
     allocated when not given).  Returns (o, final_state, ckpt)."""
+    if stream is not None:
+        return _on_stream(stream, gla_fwd_save, q, k, v, gk, lam, state, ckpt=ckpt, out=out, final_state=final_state,
+                          return_state=return_state, workspace=workspace, **kw)
     dev = q.device
     B, T, H, Dk = q.shape
     Dv = v.shape[-1]
@@ -382,7 +389,7 @@ def gla_fwd_save(q, k, v, gk, lam, state: Optional[CCQState] = None, *, ckpt=Non
         _ptr(S0), _ptr(C0), _ptr(m0), _ptr(t0), _ptr(o),
         _ptr(fs.S if fs else None), _ptr(fs.C if fs else None), _ptr(fs.m if fs else None),
         _ptr(fs.t if fs else None), B, T, H, Dk, Dv, _ptr(workspace), ws_bytes,
-        _ptr(ckpt), ckpt.numel(), pref, _stream(dev, stream))
+        _ptr(ckpt), ckpt.numel(), pref, _stream(dev, None))
     _check(st)
     return o, fs, ckpt
 
@@ -401,6 +408,9 @@ def gla_bwd(q, k, v, gk, lam, dout, state: Optional[CCQState] = None, *, dST=Non
     the gradients of the final states (None = 0); ``ckpt`` the checkpoints of
     :func:`gla_fwd_save` on the same inputs (None = recompute them).  ``out``
     may hold preallocated tensors under those names."""
+    if stream is not None:
+        return _on_stream(stream, gla_bwd, q, k, v, gk, lam, dout, state, dST=dST, dCT=dCT, dmT=dmT, ckpt=ckpt, out=out,
+                          workspace=workspace, **kw)
     dev = q.device
     B, T, H, Dk = q.shape
     Dv = v.shape[-1]
@@ -439,7 +449,7 @@ def gla_bwd(q, k, v, gk, lam, dout, state: Optional[CCQState] = None, *, dST=Non
         _ptr(S0), _ptr(C0), _ptr(m0), _ptr(t0), _ptr(dout), _ptr(dST), _ptr(dCT), _ptr(dmT),
         _ptr(ckpt), _ptr(g["dq"]), _ptr(g["dk"]), _ptr(g["dv"]), _ptr(g["dgk"]),
         _ptr(g["dlambda"]), _ptr(g["dS0"]), _ptr(g["dC0"]), _ptr(g["dm0"]),
-        B, T, H, Dk, Dv, _ptr(workspace), ws_bytes, pref, _stream(dev, stream))
+        B, T, H, Dk, Dv, _ptr(workspace), ws_bytes, pref, _stream(dev, None))
     _check(st)
     return g
 
@@ -450,6 +460,9 @@ def gdn_fwd(q, k, v, g, beta, lam, state: Optional[CCQState] = None, *, out=None
     """CCQ-Gated-DeltaNet forward.  g (log decay) and beta are [B,T,H] fp32.
     ``workspace`` (a CUDA byte tensor of at least ccq_gdn_workspace_size bytes)
     is allocated on the fly when not given."""
+    if stream is not None:
+        return _on_stream(stream, gdn_fwd, q, k, v, g, beta, lam, state, out=out, final_state=final_state,
+                          return_state=return_state, workspace=workspace, **kw)
     dev = q.device
     B, T, H, Dk = q.shape
     Dv = v.shape[-1]
@@ -476,7 +489,7 @@ def gdn_fwd(q, k, v, g, beta, lam, state: Optional[CCQState] = None, *, out=None
         _ptr(S0), _ptr(C0), _ptr(m0), _ptr(t0), _ptr(o),
         _ptr(fs.S if fs else None), _ptr(fs.C if fs else None), _ptr(fs.m if fs else None),
         _ptr(fs.t if fs else None), B, T, H, Dk, Dv, _ptr(workspace), ws_bytes,
-        pref, _stream(dev, stream))
+        pref, _stream(dev, None))
     _check(st)
     return (o, fs) if return_state else o
 
@@ -488,6 +501,9 @@ def gdn_bwd(q, k, v, g, beta, lam, dout, state: Optional[CCQState] = None, *, dS
     gradients of the final states (None = 0).  ``out`` may hold preallocated tensors under
     those names; ``workspace`` (a CUDA byte tensor of at least
     ccq_gdn_bwd_workspace_size bytes) is allocated on the fly when not given."""
+    if stream is not None:
+        return _on_stream(stream, gdn_bwd, q, k, v, g, beta, lam, dout, state, dST=dST, dCT=dCT, dmT=dmT, out=out,
+                          workspace=workspace, **kw)
     dev = q.device
     B, T, H, Dk = q.shape
     Dv = v.shape[-1]
@@ -527,7 +543,7 @@ def gdn_bwd(q, k, v, g, beta, lam, dout, state: Optional[CCQState] = None, *, dS
         _ptr(grads["dq"]), _ptr(grads["dk"]), _ptr(grads["dv"]), _ptr(grads["dg"]),
         _ptr(grads["dbeta"]), _ptr(grads["dlambda"]), _ptr(grads["dS0"]), _ptr(grads["dC0"]),
         _ptr(grads["dm0"]), B, T, H, Dk, Dv, _ptr(workspace), ws_bytes, pref,
-        _stream(dev, stream))
+        _stream(dev, None))
     _check(st)
     return grads
 
@@ -545,6 +561,9 @@ def gdn_fwd_decayed(q, k, v, g, beta, lam, *, S0=None, C0=None, m0=None, n0=None
     "resolvent" ((I + lambda Sigma)^{-1}) or "exponential" (exp(-lambda Sigma)).
     S0 [B,H,Dk,Dv], C0 [B,H,Dk,Dk], m0 [B,H,Dk], n0 [B,H] fp32 (None = zero).  Returns o, or
     (o, dict S, C, m, n of final states) when ``return_state``."""
+    if stream is not None:
+        return _on_stream(stream, gdn_fwd_decayed, q, k, v, g, beta, lam, S0=S0, C0=C0, m0=m0, n0=n0, out=out,
+                          return_state=return_state, workspace=workspace, contraction=contraction, decayed=decayed, **kw)
     dev = q.device
     B, T, H, Dk = q.shape
     Dv = v.shape[-1]
@@ -576,7 +595,7 @@ def gdn_fwd_decayed(q, k, v, g, beta, lam, *, S0=None, C0=None, m0=None, n0=None
         _ptr(S0), _ptr(C0), _ptr(m0), _ptr(n0), _ptr(o),
         _ptr(fs["S"] if fs else None), _ptr(fs["C"] if fs else None), _ptr(fs["m"] if fs else None),
         _ptr(fs["n"] if fs else None), B, T, H, Dk, Dv, CONTRACTION[contraction], int(bool(decayed)),
-        _ptr(workspace), ws_bytes, pref, _stream(dev, stream))
+        _ptr(workspace), ws_bytes, pref, _stream(dev, None))
     _check(st)
     return (o, fs) if return_state else o
 
@@ -601,6 +620,9 @@ def fwd_varlen(backbone, q, k, v, gate, lam, cu_seqlens, *, beta=None, state: Op
     [total,H]; ``cu_seqlens`` the num_seqs + 1 offsets (a list or CPU integer tensor; it stays on
     the host).  ``state`` / the returned CCQState hold one row per sequence.  Returns o
     [total,H,Dv] and (optionally) the final CCQState."""
+    if stream is not None:
+        return _on_stream(stream, fwd_varlen, backbone, q, k, v, gate, lam, cu_seqlens, beta=beta, state=state, out=out,
+                          final_state=final_state, return_state=return_state, workspace=workspace, **kw)
     dev = q.device
     total, H, Dk = q.shape
     Dv = v.shape[-1]
@@ -640,7 +662,7 @@ def fwd_varlen(backbone, q, k, v, gate, lam, cu_seqlens, *, beta=None, state: Op
         int(backbone), _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(beta), _ptr(lam), _dtype_code(q),
         _dtype_code(gate), ctypes.cast(cu_arr, _VP), ns, _ptr(S0), _ptr(C0), _ptr(m0), _ptr(t0), _ptr(o),
         _ptr(fs.S if fs else None), _ptr(fs.C if fs else None), _ptr(fs.m if fs else None),
-        _ptr(fs.t if fs else None), H, Dk, Dv, _ptr(workspace), ws_bytes, pref, _stream(dev, stream))
+        _ptr(fs.t if fs else None), H, Dk, Dv, _ptr(workspace), ws_bytes, pref, _stream(dev, None))
     _check(st)
     return (o, fs) if return_state else o
 
@@ -671,6 +693,8 @@ def decode_step(backbone: int, q, k, v, gate, lam, state: CCQState, beta=None, *
     """One recurrent token (Algorithm 2): q, k [B,H,Dk], v [B,H,Dv]; gate
     [B,H,Dk] (GLA, bf16/fp32) or [B,H] fp32 (GDN); lam (and beta) [B,H] fp32.
     Updates ``state`` in place and returns o [B,H,Dv]."""
+    if stream is not None:
+        return _on_stream(stream, decode_step, backbone, q, k, v, gate, lam, state, beta, out=out, **kw)
     dev = q.device
     B, H, Dk = q.shape
     Dv = v.shape[-1]
@@ -688,7 +712,7 @@ def decode_step(backbone: int, q, k, v, gate, lam, state: CCQState, beta=None, *
     st = load_library().ccq_decode_step(
         int(backbone), _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(beta), _ptr(lam),
         _dtype_code(q), _dtype_code(gate), _ptr(S), _ptr(C), _ptr(m), _ptr(t), _ptr(o),
-        B, H, Dk, Dv, pref, _stream(dev, stream))
+        B, H, Dk, Dv, pref, _stream(dev, None))
     _check(st)
     return o
 

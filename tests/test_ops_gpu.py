@@ -15,7 +15,7 @@ import math
 import pytest
 import torch
 
-from paper_2606_01294_gb300 import ccq, ops
+from paper_2606_01294_gb300 import ccq, inputs, ops
 
 pytestmark = pytest.mark.gpu
 
@@ -803,3 +803,35 @@ def test_stream_argument(monkeypatch):
     torch.cuda.current_stream().wait_stream(side)
     for a, c in zip(want, got):
         assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("backbone", [ccq.GLA, ccq.GDN])
+def test_stream_argument_of_the_mixer(backbone):
+    """As above, for the mixer's forward (split sequences, which need a workspace) and the decode step."""
+    P = inputs.make_inputs(backbone, 1, 4096, 2, 128, 128, dtype=torch.bfloat16, seed=5)
+    D = {n: (None if x is None else x.cuda()) for n, x in P.items()}
+    token = {n: (None if x is None else x[:, -1].clone()) for n, x in D.items()}
+    gates = (D["gate"],) if backbone == ccq.GLA else (D["gate"], D["beta"])
+    fwd = ccq.gla_fwd if backbone == ccq.GLA else ccq.gdn_fwd
+    made = (ccq.gla_workspace if backbone == ccq.GLA else ccq.gdn_workspace)(1, 4096, 2, 128, 128, "cuda")
+    assert made is not None
+    size = made.numel()
+    del made
+
+    def both(**how):
+        o, state = fwd(D["q"], D["k"], D["v"], *gates, D["lam"], **how)
+        y = ccq.decode_step(backbone, token["q"], token["k"], token["v"], token["gate"], token["lam"], state, token["beta"], **how)
+        return [o, y, state.S, state.C, state.m, state.t]
+
+    want, side = both(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    got = both(stream=side)
+    fills = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    assert not side.query()
+    torch.cuda.current_stream().wait_stream(side)
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+    assert all(bool((f == 255).all()) for f in fills)

@@ -152,17 +152,24 @@ def test_rows_strides(monkeypatch):
     assert ops._rows(torch.zeros(6, 4, 9)[::2, 1:2, :5], "t") == 72
 
 
-@pytest.mark.parametrize("call", [ops.embed, ops.embed_grad, ops.group_norm, ops.group_norm_bwd, ops.policy_loss, ops.token_logp])
+STREAMED = [ops.embed, ops.embed_grad, ops.group_norm, ops.group_norm_bwd, ops.policy_loss, ops.token_logp, ccq.gla_fwd, ccq.gla_fwd_save,
+            ccq.gla_bwd, ccq.gdn_fwd, ccq.gdn_bwd, ccq.gdn_fwd_decayed, ccq.fwd_varlen, ccq.decode_step]
+
+
+@pytest.mark.parametrize("call", STREAMED, ids=lambda f: f.__name__)
 def test_a_given_stream_is_entered_for_the_whole_call(call, monkeypatch):
     """What a call allocates has to belong to the stream it runs on: with ``stream`` the whole call is made within it, with
     every other argument as it came."""
     seen = []
-    monkeypatch.setattr(ops, "_on_stream", lambda stream, fn, *args, **kw: seen.append((stream, fn, args, kw)) or "result")
-    given = {name: object() for name in inspect.signature(call).parameters}
-    assert call(**given) == "result"
+    for module in (ops, ccq):
+        monkeypatch.setattr(module, "_on_stream", lambda stream, fn, *args, **kw: seen.append((stream, fn, args, kw)) or "result")
+    given = {name: object() for name, p in inspect.signature(call).parameters.items() if p.kind != p.VAR_KEYWORD}
+    more = {"l2norm": object(), "seq_split": object()} if len(given) < len(inspect.signature(call).parameters) else {}
+    assert call(**given, **more) == "result"
     (stream, fn, args, kw), = seen
     assert stream is given.pop("stream") and fn is call
-    bound = inspect.signature(call).bind(*args, **kw).arguments
+    bound = dict(inspect.signature(call).bind(*args, **kw).arguments)
+    assert bound.pop("kw", {}) == more
     assert bound.keys() == given.keys() and all(bound[name] is given[name] for name in given)
 
 
