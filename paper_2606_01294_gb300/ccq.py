@@ -236,9 +236,15 @@ def _req(t, name, device, dtype=None, shape=None):
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(device, stream):
+    """The raw stream a call runs on.  The library launches on the current device and asks that one for its SMs, its
+    occupancy and its status word, so tensors of another are refused."""
+    if device.index is not None and device.index != _current_device():
+        raise ValueError(f"the tensors are on {device}, the current device is cuda:{_current_device()}: "
+                         "make the call within torch.cuda.device()")
     if stream is None and _raw_stream is not None and device.index is not None:
         return _raw_stream(device.index)
     return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream

@@ -259,6 +259,7 @@ def group_norm_bwd(x, weight, bias, gate, dout, *, groups: int, activation: str 
                           centered=centered, eps=eps, out=out, workspace=workspace)
     dev, xs, gs, channels, pdt, tokens = _norm_args(x, weight, bias, gate, groups, activation)
     ds = _rows(dout, "dout", dev, x.dtype, x.shape)
+    raw = _stream(dev, None)  # (before the workspace's size is asked for: a function of the current device's SMs)
     g = dict(out or {})
     strides = {"dgate": 0}
     for name, like in (("dx", x), ("dgate", gate)):
@@ -279,7 +280,7 @@ def group_norm_bwd(x, weight, bias, gate, dout, *, groups: int, activation: str 
         x.data_ptr(), xs, _ptr(gate), gs, _ptr(weight), _ptr(bias), dout.data_ptr(), ds, _dtype_code(x), pdt,
         g["dx"].data_ptr(), strides["dx"], _ptr(g.get("dgate")), strides["dgate"], _ptr(g.get("dweight")),
         _ptr(g.get("dbias")), tokens, channels, groups, int(bool(centered)), eps, ACTIVATION[activation],
-        _ptr(workspace), nbytes, _stream(dev, None)))
+        _ptr(workspace), nbytes, raw))
     return g
 
 

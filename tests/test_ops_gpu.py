@@ -835,3 +835,20 @@ def test_stream_argument_of_the_mixer(backbone):
     for a, b in zip(want, got):
         assert torch.equal(a, b)
     assert all(bool((f == 255).all()) for f in fills)
+
+
+def test_tensors_of_a_device_that_is_not_current_are_refused(monkeypatch):
+    """(The other device is the host's fiction: nothing is launched, and no workspace's size is asked for.)"""
+    x, ids = torch.ones(4, 64, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    monkeypatch.setattr(ccq, "_current_device", lambda: 1)
+    sizes = ops._size.cache_info().currsize
+    for call in (lambda: ops.embed(x, ids), lambda: ops.group_norm(x, groups=1), lambda: ops.token_logp(x, ids),
+                 lambda: ops.group_norm_bwd(x, x[0], None, None, x, groups=1), lambda: ops.embed_grad(x, ids, 5),
+                 lambda: ops.policy_loss(x, ids, x[:, 0].contiguous(), x[:, 0].contiguous()),
+                 lambda: ops.adamw_step([x], [x], ops.adamw_state([x]), 1, lr=1e-3), lambda: ccq.device_status(device=x.device)):
+        with pytest.raises(ValueError, match="current device is cuda:1"):
+            call()
+    # (those of the embedding's gradient and of the policy loss are the same on every device)
+    assert ops._size.cache_info().currsize <= sizes + 2
+    monkeypatch.undo()
+    assert torch.equal(ops.embed(x, ids), x[ids])

@@ -204,3 +204,11 @@ def test_on_stream_enters_and_records(monkeypatch):
     result = ccq._on_stream(stream, call, 1, b=2)
     assert not inside and result[2]["y"][1] is state
     assert sorted(recorded) == [(k, ("caller", "cuda:0")) for k in range(1, 8)]
+
+
+def test_tensors_of_a_device_that_is_not_current_are_refused(monkeypatch):
+    monkeypatch.setattr(ccq, "_current_device", lambda: 0, raising=False)
+    monkeypatch.setattr(ccq, "_raw_stream", lambda index: 100 + index)
+    assert ccq._stream(torch.device("cuda:0"), None) == 100
+    with pytest.raises(ValueError, match="cuda:1.*current device is cuda:0"):
+        ccq._stream(torch.device("cuda:1"), None)
