@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kLookupThreads) embed_kernel(const T *__restri
 
 template <typename T, int N>
 cudaError_t launch_embed(const void *table, int64_t table_stride, const void *ids, int id_bytes, int64_t n,
-                         int64_t rows, int width, float scale, void *out, int64_t out_stride, cudaStream_t s) {
+                         int64_t rows, int width, float scale, void *out, int64_t out_stride, int *status, cudaStream_t s) {
     const int packs = width / N;
     int tx = 32;
     while (tx < kLookupThreads && tx < packs) tx *= 2;
@@ -89,7 +89,7 @@ cudaError_t launch_embed(const void *table, int64_t table_stride, const void *id
     const unsigned grid = static_cast<unsigned>((n + ty * kLookupRows - 1) / (ty * kLookupRows));
     embed_kernel<T, N><<<grid, dim3(tx, ty), 0, s>>>(
         static_cast<const T *>(table), table_stride, ids, id_bytes, n, rows, packs, scale, static_cast<T *>(out),
-        out_stride, device_status_word());
+        out_stride, status);
     return cudaGetLastError();
 }
 
@@ -756,12 +756,14 @@ ccq_status ccq_embed(const void *table, ccq_dtype dtype, int64_t table_stride, c
     if (n == 0) return CCQ_OK;
     if ((st = check_ids(ids, id_bytes)) != CCQ_OK) return st;
     if ((st = check_rows("out", out, dtype, out_stride, n, width)) != CCQ_OK) return st;
+    int *status = nullptr;
+    if ((st = op_status_word(&status)) != CCQ_OK) return st;
     const int es = dtype_bytes(dtype);
     int b = access_bytes(static_cast<uintptr_t>(width) * es);
     b = row_access(table, table_stride, es, rows, b);
     b = row_access(out, out_stride, es, n, b);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    auto go = [&](auto fn) { return fn(table, table_stride, ids, id_bytes, n, rows, width, scale, out, out_stride, s); };
+    auto go = [&](auto fn) { return fn(table, table_stride, ids, id_bytes, n, rows, width, scale, out, out_stride, status, s); };
     cudaError_t e;
     if (dtype == CCQ_BF16)
         e = b == 16  ? go(launch_embed<__nv_bfloat16, 8>)
@@ -798,6 +800,8 @@ ccq_status ccq_embed_grad(const void *dout, ccq_dtype dtype, int64_t dout_stride
     if (need && (st = op_pointer("workspace", workspace, 16)) != CCQ_OK) return st;
     if (workspace_bytes < need)
         return op_fail(CCQ_ERR_INVALID_ARG, "workspace of %zu bytes, needs %zu", workspace_bytes, need);
+    int *status = nullptr;
+    if ((st = op_status_word(&status)) != CCQ_OK) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     // elements an access may hold in both operands, at most 16 bytes of the wider type
     const int es = dtype_bytes(dtype), eo = dtype_bytes(grad_dtype);
@@ -817,7 +821,7 @@ ccq_status ccq_embed_grad(const void *dout, ccq_dtype dtype, int64_t dout_stride
         f.dtable = dtable;
         f.dtable_stride = dtable_stride;
         f.scale = scale;
-        f.status = device_status_word();
+        f.status = status;
         return op_cuda(by_types<Few>(dtype, grad_dtype, b, f, s), "embedding gradient launch");
     }
     const size_t list = round16(static_cast<size_t>(n) * 8);
@@ -833,7 +837,7 @@ ccq_status ccq_embed_grad(const void *dout, ccq_dtype dtype, int64_t dout_stride
     so.digit = std::max(2, (bits + so.passes - 1) / so.passes);  // (bins are told four at a time)
     for (int k = 0; k < 2; ++k) so.list[k] = reinterpret_cast<uint2 *>(ws + k * list);
     so.joins = reinterpret_cast<int *>(ws + 2 * list);
-    so.status = device_status_word();
+    so.status = status;
     so.ctas = sort_ctas(n, rows, static_cast<size_t>(width) * eo);
     const bool held = sort_holds(so.n, so.ctas);
     cudaLaunchConfig_t cfg;

@@ -41,6 +41,12 @@ inline ccq_status op_pointer(const char *name, const void *p, uintptr_t least) {
     return CCQ_OK;
 }
 
+// The device status word that a call's kernels write.
+inline ccq_status op_status_word(int **word) {
+    *word = device_status_word();
+    return *word ? CCQ_OK : op_fail(CCQ_ERR_CUDA, "cannot resolve the device status word");
+}
+
 // The largest of 16, 8, 4, 2 bytes that divides a base address or row stride, `bytes`.
 inline int access_bytes(uintptr_t bytes, int most = 16) {
     while (most > 2 && bytes % most) most >>= 1;

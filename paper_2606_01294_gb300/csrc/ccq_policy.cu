@@ -915,6 +915,7 @@ ccq_status ccq_policy_loss(const void *logits, ccq_dtype dtype, int64_t logits_s
     if ((st = op_pointer("workspace", workspace, 16)) != CCQ_OK) return st;
     if (workspace_bytes < need)
         return op_fail(CCQ_ERR_INVALID_ARG, "workspace of %zu bytes, needs %zu", workspace_bytes, need);
+    if ((st = op_status_word(&a.status)) != CCQ_OK) return st;
     a.logits = logits; a.logits_stride = logits_stride; a.actions = actions; a.id_bytes = id_bytes;
     a.n = n; a.vocab = vocab;
     a.old_logp = old_logp; a.ref_logp = ref_logp; a.advantages = advantages; a.weights = weights;
@@ -923,7 +924,6 @@ ccq_status ccq_policy_loss(const void *logits, ccq_dtype dtype, int64_t logits_s
     a.grad_mul = a.p.grad_scale / a.p.temperature;
     a.logp = logp; a.row_loss = static_cast<float *>(workspace);
     a.dlogits = dlogits; a.dlogits_stride = dlogits_stride;
-    a.status = device_status_word();
     cudaError_t e = launch_policy(a, dtype, s);
     if (e != cudaSuccess) return op_cuda(e, "policy loss launch");
     e = launch_after(policy_loss_kernel, 1, kLossThreads, 0, s, static_cast<const float *>(a.row_loss), n, loss);
@@ -939,6 +939,7 @@ ccq_status ccq_token_logp(const void *logits, ccq_dtype dtype, int64_t logits_st
     if ((st = op_pointer("actions", actions, id_bytes)) != CCQ_OK) return st;
     if ((st = op_pointer("logp", logp, 4)) != CCQ_OK) return st;
     PolicyArgs a = {};
+    if ((st = op_status_word(&a.status)) != CCQ_OK) return st;
     a.logits = logits; a.logits_stride = logits_stride; a.actions = actions; a.id_bytes = id_bytes;
     a.n = n; a.vocab = vocab;
     a.p.temperature = temperature;
@@ -946,7 +947,6 @@ ccq_status ccq_token_logp(const void *logits, ccq_dtype dtype, int64_t logits_st
     set_inverse(&a);
     a.logp = logp;
     a.score = 1;
-    a.status = device_status_word();
     return op_cuda(launch_policy(a, dtype, static_cast<cudaStream_t>(stream)), "token log-probability launch");
 }
 

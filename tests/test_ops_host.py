@@ -212,3 +212,22 @@ def test_tensors_of_a_device_that_is_not_current_are_refused(monkeypatch):
     assert ccq._stream(torch.device("cuda:0"), None) == 100
     with pytest.raises(ValueError, match="cuda:1.*current device is cuda:0"):
         ccq._stream(torch.device("cuda:1"), None)
+
+
+def test_a_status_word_that_cannot_be_resolved_is_an_error(lib):
+    """Kernels write to the status word, so no call passes on one that is missing, as it is without a device.  (With a device
+    the same calls, on its memory, pass.)"""
+    gpu = torch.cuda.is_available()
+    held = [torch.zeros(1 << 16, dtype=torch.uint8, device="cuda") for _ in range(8)] if gpu else []
+    at = [t.data_ptr() for t in held] or [FAKE] * 8
+    p = ops._PolicyParams(0.2, 0.2, 0.0, 1.0, 1.0)
+    for got in (lib.ccq_embed(at[0], 1, 8, at[1], 8, 4, 10, 8, 1.0, at[2], 8, None),
+                lib.ccq_embed_grad(at[0], 1, 8, at[1], 8, 4, 10, 8, 1.0, -1, at[2], 1, 8, None, 0, None),
+                lib.ccq_embed_grad(at[0], 1, 8, at[1], 8, 300, 10, 8, 1.0, -1, at[2], 1, 8, at[3], 1 << 16, None),
+                lib.ccq_policy_loss(at[0], 1, 100, at[1], 8, at[2], None, at[3], None, 3, 100, ctypes.byref(p), at[4], None, at[5], 100, at[6],
+                                    1 << 16, None),
+                lib.ccq_token_logp(at[0], 1, 100, at[1], 8, 3, 100, 1.0, at[2], None)):
+        assert got == (ccq.CCQ_OK if gpu else ccq.CCQ_ERR_CUDA)
+        assert gpu or b"status word" in lib.ccq_last_error()
+    if gpu:
+        torch.cuda.synchronize()
