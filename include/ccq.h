@@ -417,9 +417,9 @@ CCQ_API ccq_status ccq_gla_fwd_fixed_scratch(const void *q, const void *k, const
 /*
  * Synchronise `stream`, then read and clear the device status word that the
  * kernels write.  Returns CCQ_OK, CCQ_ERR_RANGE (a chunkwise CCQ-GLA kernel met
- * gates stronger than its factored decays can represent: see ccq_gla_fwd), CCQ_ERR_INDEX (an operator of
- * ccq_ops.h met an index outside its range), CCQ_ERR_TIMEOUT (a kernel gave up waiting; its outputs are not
- * valid) or CCQ_ERR_CUDA.
+ * gates stronger than its factored decays can represent: see ccq_gla_fwd), CCQ_ERR_TIMEOUT (a kernel gave up
+ * waiting; its outputs are not valid), CCQ_ERR_INDEX (an operator of ccq_ops.h met an index outside its
+ * range; where kernels left RANGE or TIMEOUT too, that one is returned) or CCQ_ERR_CUDA.
  */
 CCQ_API ccq_status ccq_device_status(void *stream);
 

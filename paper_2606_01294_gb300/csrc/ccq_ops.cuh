@@ -190,8 +190,9 @@ template <int N> __device__ __forceinline__ void tma_store_wait_read_but() {
     asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
 }
 
-// Status code of an index outside its range (CCQ_ERR_INDEX), for the device status word.
+// Status code of an index outside its range (CCQ_ERR_INDEX), for the device status word.  It concerns a row, the other codes
+// say that outputs are not valid, so it is left in a clear word alone (and the others replace it).
 constexpr int kStatusIndex = 6;
-__device__ __forceinline__ void note_index(int *status) { atomicExch(status, kStatusIndex); }
+__device__ __forceinline__ void note_index(int *status) { atomicCAS(status, 0, kStatusIndex); }
 
 }  // namespace ccq

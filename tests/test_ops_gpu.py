@@ -10,6 +10,7 @@ its type: r = 2^-8 of its value in bf16 (8 significant bits), u in fp32.
   policy loss  log-probabilities: (|z| + |log Z|) 8 u, sums of V terms in trees; gradients ARITH of the row's largest, + r.
   AdamW        8 operations: 1e-6 of each term's magnitude; 8-bit codes are equal to the fp32 operations' codes.
 """
+import ctypes
 import math
 
 import pytest
@@ -92,6 +93,21 @@ def test_embed_reports_ids_outside_the_table():
     with pytest.raises(ccq.CCQError):
         ccq.device_status()
     assert torch.equal(d.sum(1).nonzero()[:, 0], torch.tensor([3, 9], device="cuda"))
+
+
+@pytest.mark.parametrize("first", ["index", "timeout"])
+def test_an_index_does_not_hide_a_timeout(first):
+    """One word reports for all kernels: outputs that are not valid come before an id that made a zero row."""
+    lib = ccq.load_library()
+    lib.ccq_diag_wait_timeout.argtypes = [ctypes.c_void_p]
+    lib.ccq_diag_wait_timeout.restype = ctypes.c_int
+    steps = [lambda: ops.embed(torch.ones(4, 64, device="cuda"), torch.tensor([0, 9], device="cuda")),
+             lambda: lib.ccq_diag_wait_timeout(torch.cuda.current_stream().cuda_stream)]
+    for step in steps if first == "index" else steps[::-1]:
+        step()
+    with pytest.raises(ccq.CCQError) as e:
+        ccq.device_status()
+    assert e.value.status == ccq.CCQ_ERR_TIMEOUT
 
 
 def test_embed_offsets_past_32_bits():
