@@ -105,7 +105,7 @@ CCQ_API ccq_status ccq_group_norm_bwd_workspace_size(int64_t tokens, int channel
 typedef struct {
     float clip_low, clip_high; /* the ratio is held in [1 - clip_low, 1 + clip_high]      */
     float kl_coef;             /* weight of the KL term; 0 or no reference: none            */
-    float temperature;         /* the logits are divided by it                              */
+    float temperature;         /* the logits are divided by it; 4.3e-39 to 1e30             */
     float grad_scale;          /* factor of dlogits (not of the loss)                       */
 } ccq_policy_params;
 

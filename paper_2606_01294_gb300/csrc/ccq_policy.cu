@@ -858,8 +858,10 @@ ccq_status check_policy(int64_t n, int vocab, ccq_dtype dtype, float temperature
     if (n < 0 || vocab < 1 || vocab > (1 << 30))
         return op_fail(CCQ_ERR_INVALID_ARG, "bad sizes n=%lld vocab=%d", static_cast<long long>(n), vocab);
     if (!valid_dtype(dtype)) return op_fail(CCQ_ERR_INVALID_ARG, "unknown dtype %d", dtype);
-    if (!(temperature > 0.f) || temperature > 1e30f)
-        return op_fail(CCQ_ERR_INVALID_ARG, "temperature=%g must be positive and finite", static_cast<double>(temperature));
+    // (below 4.3e-39 log2(e) / temperature is infinite, and every row's largest logit 0 times that)
+    if (!(temperature > 0.f) || temperature > 1e30f || !(kLog2e / temperature < INFINITY))
+        return op_fail(CCQ_ERR_INVALID_ARG, "temperature=%g must be positive and finite, its reciprocal too",
+                       static_cast<double>(temperature));
     if (id_bytes != 4 && id_bytes != 8) return op_fail(CCQ_ERR_INVALID_ARG, "id_bytes=%d: 4 or 8", id_bytes);
     return CCQ_OK;
 }

@@ -231,3 +231,12 @@ def test_a_status_word_that_cannot_be_resolved_is_an_error(lib):
         assert gpu or b"status word" in lib.ccq_last_error()
     if gpu:
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("temperature", [1e-45, 1e-39, 4.2e-39])
+def test_a_temperature_without_a_finite_reciprocal_is_refused(lib, temperature):
+    """n = 0: a call that passes its checks launches nothing.  log2(e) / 4.3e-39 = 3.36e38 is a number in fp32, / 4.2e-39 is not."""
+    n0 = (FAKE, 0, 100, FAKE, 8)
+    score = lambda t: lib.ccq_token_logp(*n0, 0, 100, t, FAKE, None)  # noqa: E731
+    assert score(temperature) == INVALID and b"temperature" in lib.ccq_last_error()
+    assert score(4.3e-39) == 0 and score(1e30) == 0 and score(2e30) == INVALID
