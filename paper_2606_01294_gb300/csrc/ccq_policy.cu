@@ -70,23 +70,24 @@ __device__ __forceinline__ bool is_live(const PolicyArgs &a, int64_t i) {
 // The log-probability (chosen - m) / T - log z as the sum of two floats.  The loss needs its differences from the old and
 // reference ones to more than its own rounding: at logp = -8 that is 5e-7, which a KL term with d = 1e-3 sees 1000-fold.
 // (Knuth's exact difference; log z = e log 2 + log f with the high part of log 2 short enough for an exact product, after
-// Cody and Waite.)
+// Cody and Waite.  Each of these roundings is an operation of its own: a product fused into the sum behind it would leave
+// in the low part what r has already.)
 struct TwoFloats {
     float hi, lo;
 };
 __device__ __forceinline__ TwoFloats exact_sum(float a, float b) {
-    const float s = a + b, t = s - a;
-    return {s, (a - (s - t)) + (b - t)};
+    const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+    return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
 }
 __device__ __forceinline__ TwoFloats log_probability(float chosen, float m, float z, float inv, float inv_lo) {
     const TwoFloats diff = exact_sum(chosen, -m);
-    const float q = diff.hi * inv;
+    const float q = __fmul_rn(diff.hi, inv);
     // no digits below an infinity (a masked action, also one at the type's lowest value once the temperature has divided it)
     if (!(fabsf(q) < INFINITY)) return {q - logf(z), 0.f};
     const float r = fmaf(diff.hi, inv_lo, fmaf(diff.lo, inv, fmaf(diff.hi, inv, -q)));
     const int e = (static_cast<int>(__float_as_uint(z)) - 0x3f400000) >> 23;  // z = 2^e f, f in [0.75, 1.5)
     const float f = __uint_as_float(__float_as_uint(z) - (static_cast<uint32_t>(e) << 23)), k = static_cast<float>(e);
-    const TwoFloats s = exact_sum(q, -k * 0.693115234375f);
+    const TwoFloats s = exact_sum(q, __fmul_rn(-k, 0.693115234375f));
     const float rest = (r + s.lo) - fmaf(k, 3.19461849453e-05f, logf(f) + (z - z));  // (z - z: not a number stays one)
     return exact_sum(s.hi, rest);
 }

@@ -579,6 +579,34 @@ def test_policy_loss_offsets_past_32_bits():
     assert abs(float(got["dlogits"][n - 1, vocab - 1]) * n + float(1 - p)) < 0.02
 
 
+@pytest.mark.parametrize("n,vocab", [(4096, 4096), (64, 300000)])  # staged rows, and rows that are read twice
+@pytest.mark.parametrize("temperature", [1.0, 0.9, 0.8, 1.3])
+@pytest.mark.parametrize("reach", [10.0, 90.0])
+def test_policy_loss_near_the_reference(n, vocab, temperature, reach):
+    """KL term alone, |ref - logp| about 1e-3: the gradient follows logp's error 1000-fold, and logp in one float would have
+    half steps of up to 2^-18 (64 u) at logp = -100.  Rows of zeros but for the action at -c: the exponentials are 1 (exactly)
+    and e^(-c/T), so Z is off by half a step a level of its sum at most, and relative to Z by 4 u (the e^(-c/T) counts in
+    a few partial sums that double from one to the next).  logp: those, log f (|log f| < 0.41: one step and its sum, 1 u), the low
+    parts' own roundings (1 u); d = ref - logp: u |d|.  The slope -expm1(d) / T (1 - p): 8 u of itself."""
+    g = gen(51)
+    actions = torch.randint(0, vocab, (n,), device="cuda", generator=g)
+    c = reach * (0.5 + torch.rand(n, device="cuda", generator=g))
+    logits = torch.zeros(n, vocab, device="cuda").scatter_(1, actions[:, None], -c[:, None])
+    T = float(torch.tensor(temperature, dtype=torch.float32))
+    z = -c.double() / T
+    logp = z - torch.log(vocab - 1 + z.exp())
+    ref = (logp + 1e-3 * torch.randn(n, device="cuda", generator=g)).float()
+    zeros = torch.zeros(n, device="cuda")
+    got = ops.policy_loss(logits, actions, logp.float(), zeros, ref_logp=ref, weights=torch.ones_like(zeros), kl_coef=1.0,
+                          temperature=temperature)
+    d = ref.double() - logp
+    slope = -torch.expm1(d) / T * (1 - logp.exp())
+    close(got["dlogits"].gather(1, actions[:, None])[:, 0], slope, 6 * U * d.exp() / T + 8 * U * slope.abs(), "dlogits")
+    # the loss: expm1(d) - d, each rounded (2 u |d|), its slope by logp, and the rows' sum
+    each = torch.expm1(d) - d
+    close(got["loss"], each.sum(), (6 * U * torch.expm1(d).abs() + 4 * U * d.abs()).sum() + 12 * U * each.sum(), "loss")
+
+
 def test_policy_gradient_by_differences():
     logits, actions, old, ref, adv, w = _policy_inputs(12, 50, torch.float32, 14)
     how = dict(ref_logp=ref, weights=w, clip=(5.0, 5.0), kl_coef=0.3, temperature=1.3)
