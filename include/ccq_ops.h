@@ -175,7 +175,7 @@ typedef struct {
  *   g = grad * (grad_scale ? *grad_scale : 1)      (a device scalar, e.g. from gradient clipping)
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * in fp32.  With a master copy p is the master, and param receives its rounded value; master is
+ * in fp32; eps is 0 or at least 2^-126.  With a master copy p is the master, and param receives its rounded value; master is
  * NULL for all tensors or for none, and needs param_dtype BF16.
  * state_bits 32: m and v are fp32.
  * state_bits 8: per element one e4m3 byte for m and one for sqrt(v), over a power-of-two scale

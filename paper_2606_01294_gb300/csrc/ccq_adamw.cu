@@ -14,6 +14,7 @@
 // (Tried and taken back: the next block's operands by asynchronous copies while one is computed, 748 us.)
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -335,6 +336,9 @@ extern "C" ccq_status ccq_adamw_step(const ccq_adamw_tensor *tensors, int count,
     if (!(p->beta1 >= 0 && p->beta1 < 1) || !(p->beta2 >= 0 && p->beta2 < 1))
         return op_fail(CCQ_ERR_INVALID_ARG, "betas must be in [0, 1)");
     if (!(p->eps >= 0)) return op_fail(CCQ_ERR_INVALID_ARG, "eps must be >= 0");
+    // (a smaller one is 0 to the approximate reciprocal, and 0 / eps not a number)
+    if (p->eps > 0 && p->eps < FLT_MIN)
+        return op_fail(CCQ_ERR_INVALID_ARG, "eps=%g: 0, or at least fp32's smallest normal number %g", p->eps, static_cast<double>(FLT_MIN));
     if (grad_scale && reinterpret_cast<uintptr_t>(grad_scale) % 4)
         return op_fail(CCQ_ERR_INVALID_ARG, "grad_scale is not aligned to 4 bytes");
     const int pe = dtype_bytes(param_dtype), ge = dtype_bytes(grad_dtype);

@@ -756,6 +756,17 @@ def test_adamw_8bit_non_finite_gradient_stays_in_its_element():
     assert torch.equal(torch.isnan(state.master[0]), bad)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_smallest_eps(bits):
+    """No gradient so far and the smallest eps: 0 / eps is 0, and the parameters decay alone."""
+    params, _ = _tensors([(1000,)], torch.float32, torch.float32, 31)
+    start, state = params[0].double(), ops.adamw_state(params, bits=bits)
+    ops.adamw_step(params, [torch.zeros(1000, device="cuda")], state, 1, lr=1e-2, eps=2.0 ** -126, weight_decay=0.1)
+    close(params[0], start * (1 - 1e-3), 2 * U * start.abs())
+    with pytest.raises(ccq.CCQError, match="eps"):
+        ops.adamw_step(params, [torch.zeros(1000, device="cuda")], state, 2, lr=1e-2, eps=1e-39)
+
+
 def test_adamw_tensor_past_32_bits():
     n = 2 ** 31 + 4097
     p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")

@@ -240,3 +240,10 @@ def test_a_temperature_without_a_finite_reciprocal_is_refused(lib, temperature):
     score = lambda t: lib.ccq_token_logp(*n0, 0, 100, t, FAKE, None)  # noqa: E731
     assert score(temperature) == INVALID and b"temperature" in lib.ccq_last_error()
     assert score(4.3e-39) == 0 and score(1e30) == 0 and score(2e30) == INVALID
+
+
+def test_an_eps_below_the_normal_numbers_is_refused(lib):
+    for eps in (1e-60, 1e-45, 1e-39, 1.17e-38):
+        assert _adamw(lib, [], eps=eps) == INVALID and b"eps" in lib.ccq_last_error(), eps
+    for eps in (0.0, 1.18e-38, 1e-8):
+        assert _adamw(lib, [], eps=eps) == 0, eps
