@@ -259,6 +259,9 @@ def group_norm_bwd(x, weight, bias, gate, dout, *, groups: int, activation: str 
                           centered=centered, eps=eps, out=out, workspace=workspace)
     dev, xs, gs, channels, pdt, tokens = _norm_args(x, weight, bias, gate, groups, activation)
     ds = _rows(dout, "dout", dev, x.dtype, x.shape)
+    for name, like in (("dgate", gate), ("dweight", weight), ("dbias", bias)):
+        if like is None and out and out.get(name) is not None:
+            raise ValueError(f"out has {name}, but there is no {name[1:]}")
     raw = _stream(dev, None)  # (before the workspace's size is asked for: a function of the current device's SMs)
     g = dict(out or {})
     strides = {"dgate": 0}

@@ -327,6 +327,19 @@ def test_group_norm_without_parameters_and_empty():
     assert ops.group_norm(x[:0], groups=2).shape == (0, 64)
 
 
+def test_group_norm_gradients_into_given_tensors():
+    x, dy = (randn(gen(7), 30, 96) for _ in range(2))
+    w = torch.ones(96, device="cuda")
+    want = ops.group_norm_bwd(x, w, None, None, dy, groups=3)
+    out = {"dx": torch.empty_like(x), "dweight": torch.empty_like(w), "dbias": None}
+    got = ops.group_norm_bwd(x, w, None, None, dy, groups=3, out=out)
+    for name in ("dx", "dweight"):
+        assert got[name] is out[name] and torch.equal(got[name], want[name])
+    for name, t in (("dbias", torch.empty(1, device="cuda")), ("dgate", torch.empty(1, device="cuda"))):
+        with pytest.raises(ValueError, match=name):
+            ops.group_norm_bwd(x, w, None, None, dy, groups=3, out={name: t})
+
+
 def test_group_norm_gradients_by_differences():
     g = gen(8)
     x, gate, dy = randn(g, 6, 96), randn(g, 6, 96), randn(g, 6, 96)

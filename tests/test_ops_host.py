@@ -247,3 +247,14 @@ def test_an_eps_below_the_normal_numbers_is_refused(lib):
         assert _adamw(lib, [], eps=eps) == INVALID and b"eps" in lib.ccq_last_error(), eps
     for eps in (0.0, 1.18e-38, 1e-8):
         assert _adamw(lib, [], eps=eps) == 0, eps
+
+
+@pytest.mark.parametrize("name", ["dgate", "dweight", "dbias"])
+def test_group_norm_gradients_that_nothing_belongs_to_are_refused(name, monkeypatch):
+    """A tensor under the name of an operand that is not there has no type or size that it could be checked for."""
+    monkeypatch.setattr(ops, "_cuda", lambda t, name, device=None: t)
+    x = torch.zeros(4, 64)
+    operands = dict(zip(("dweight", "dbias", "dgate"), (x[0], x[0], x)))
+    operands[name] = None
+    with pytest.raises(ValueError, match=f"out has {name}, but there is no {name[1:]}"):
+        ops.group_norm_bwd(x, operands["dweight"], operands["dbias"], operands["dgate"], x, groups=1, out={name: torch.zeros(1)})
