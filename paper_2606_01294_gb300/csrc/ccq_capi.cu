@@ -11,6 +11,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <initializer_list>
 
 #include "../../include/ccq.h"
@@ -25,15 +26,17 @@ __device__ int g_status = 0;
 
 int *device_status_word() {
     // one slot per device ordinal; filled on first use with that device current
-    static int *addr[64] = {};
+    static std::atomic<int *> addr[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
-    if (!addr[dev]) {
+    int *word = addr[dev].load(std::memory_order_relaxed);
+    if (!word) {
         void *p = nullptr;
         if (cudaGetSymbolAddress(&p, g_status) != cudaSuccess) return nullptr;
-        addr[dev] = static_cast<int *>(p);
+        word = static_cast<int *>(p);
+        addr[dev].store(word, std::memory_order_relaxed);
     }
-    return addr[dev];
+    return word;
 }
 
 namespace {

@@ -60,15 +60,15 @@ inline int row_access(const void *p, int64_t stride, int elem, int64_t rows, int
 }
 
 inline int sm_count_now() {
-    static int counts[64] = {};
+    static std::atomic<int> counts[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 152;
-    if (!counts[dev]) {
-        int n = 0;
+    int n = counts[dev].load(std::memory_order_relaxed);
+    if (!n) {
         if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 152;
-        counts[dev] = n;
+        counts[dev].store(n, std::memory_order_relaxed);
     }
-    return counts[dev];
+    return n;
 }
 
 // Opts a kernel into `bytes` of dynamic shared memory, once for a kernel and device.

@@ -12,6 +12,7 @@ its type: r = 2^-8 of its value in bf16 (8 significant bits), u in fp32.
 """
 import ctypes
 import math
+import threading
 
 import pytest
 import torch
@@ -920,3 +921,46 @@ def test_tensors_of_a_device_that_is_not_current_are_refused(monkeypatch):
     assert ops._size.cache_info().currsize <= sizes + 2
     monkeypatch.undo()
     assert torch.equal(ops.embed(x, ids), x[ids])
+
+
+def test_two_threads_at_once():
+    """Each thread has its own plan, argument block and stream; what they share is the library's memory of the device."""
+    g = gen(44)
+    jobs = []
+    for vocab, tokens in ((700, 2000), (4096, 900)):
+        x = _policy_inputs(tokens, vocab, torch.bfloat16, vocab)
+        params, grads = _tensors([(300,), (64, 100), (5000,)], torch.float32, torch.float32, vocab)
+        ids = torch.randint(0, vocab, (tokens,), device="cuda", generator=g)
+        rows, w = randn(g, tokens, 256), 1 + 0.1 * randn(g, 256)
+
+        def job(x=x, params=params, grads=grads, ids=ids, rows=rows, w=w, vocab=vocab):
+            logits, actions, old, ref, adv, weights = x
+            p = [t.clone() for t in params]
+            ops.adamw_step(p, grads, ops.adamw_state(p, bits=8), 1, lr=1e-2)
+            loss = ops.policy_loss(logits, actions, old, adv, ref_logp=ref, weights=weights, kl_coef=0.1)
+            d = ops.group_norm_bwd(rows, w, None, None, rows, groups=2)
+            return p + [loss["loss"], loss["dlogits"], d["dx"], d["dweight"], ops.embed_grad(rows, ids, vocab), ops.embed(rows, ids % 100)]
+
+        jobs.append(job)
+    want = [job() for job in jobs]
+    torch.cuda.synchronize()
+    wrong, start = [], threading.Barrier(2)
+
+    def run(k):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                start.wait()
+                for _ in range(20):
+                    got = jobs[k]()
+                    torch.cuda.current_stream().synchronize()
+                    if not all(torch.equal(a, b) for a, b in zip(want[k], got)):
+                        wrong.append(k)
+        except Exception as e:  # (an error in a thread is not the test's by itself)
+            wrong.append(e)
+
+    threads = [threading.Thread(target=run, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
