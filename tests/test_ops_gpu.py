@@ -355,6 +355,35 @@ def test_group_norm_gradients_by_differences():
     assert abs((f(1) - f(-1)) / (2 * h) - slope) < 576 * (h * h + 1e-6 / h)
 
 
+def test_group_norm_offsets_past_32_bits():
+    """More than 2^31 elements, then rows that lie more than 2^31 elements apart: a token's result is that of a call on it alone."""
+    tokens, channels = 1_100_000, 2048  # 2.25e9 elements
+    g = gen(9)
+    x = torch.zeros(tokens, channels, dtype=torch.bfloat16, device="cuda")
+    rows = torch.tensor([0, 1_048_575, 1_048_576, tokens - 2, tokens - 1], device="cuda")
+    some, dsome = randn(g, 5, channels, dtype=torch.bfloat16), randn(g, 5, channels, dtype=torch.bfloat16)
+    x[rows] = some
+    w, b = 1 + 0.1 * randn(g, channels), 0.1 * randn(g, channels)
+    how = dict(groups=16, activation="silu")
+    y = ops.group_norm(x, w, b, x, **how)
+    assert torch.equal(y[rows], ops.group_norm(some, w, b, some, **how))
+    dy = y.zero_()
+    dy[rows] = dsome
+    got = ops.group_norm_bwd(x, w, None, None, dy, out={"dx": dy}, **how)
+    want = ops.group_norm_bwd(some, w, None, None, dsome, **how)
+    assert torch.equal(got["dx"][rows], want["dx"])
+    # five tokens' terms in the sums, in another order, and zeros
+    close(got["dweight"], want["dweight"].double(), 10 * U * (dsome.double().abs() * 1.1 * math.sqrt(128)).sum(0))
+    assert int((got["dx"].view(tokens, -1) != 0).any(1).sum()) == 5
+    del x, y, dy, got
+    stride = 1_200_000_000
+    far = torch.zeros(2 * stride + 256, dtype=torch.bfloat16, device="cuda").as_strided((3, 256), (stride, 1))
+    far.copy_(some[:3, :256])
+    assert torch.equal(ops.group_norm(far, groups=2), ops.group_norm(some[:3, :256], groups=2))
+    p = ops.group_norm_bwd(far, None, None, None, far, groups=2)["dx"]
+    assert torch.equal(p, ops.group_norm_bwd(far.contiguous(), None, None, None, far.contiguous(), groups=2)["dx"])
+
+
 # ---------------------------------------------------------------- policy loss
 
 
@@ -964,3 +993,36 @@ def test_two_threads_at_once():
     for t in threads:
         t.join()
     assert not wrong
+
+
+def test_a_graph_replayed_on_other_inputs():
+    """A captured step computes from what its inputs hold at the replay: ids, masks and values."""
+    g = gen(45)
+    n = 700
+    ids = torch.randint(0, 90, (n,), device="cuda", generator=g)
+    rows, gate, w = randn(g, n, 256), randn(g, n, 256), 1 + 0.1 * randn(g, 256)
+    x = list(_policy_inputs(n, 801, torch.bfloat16, 46, masked=200))
+
+    def step():
+        logits, actions, old, ref, adv, weights = x
+        d = ops.group_norm_bwd(rows, w, None, gate, rows, groups=2)
+        loss = ops.policy_loss(logits, actions, old, adv, ref_logp=ref, weights=weights, kl_coef=0.1)
+        few = ops.embed_grad(rows[:100], ids[:100], 90, padding_id=3)
+        return [ops.embed(rows, ids), ops.group_norm(rows, w, None, gate, groups=2), d["dx"], d["dgate"], d["dweight"], loss["loss"],
+                loss["logp"], loss["dlogits"], ops.embed_grad(rows, ids, 90, padding_id=3), few, ops.token_logp(logits, actions)]
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in (47, 48):
+        h = gen(seed)
+        ids.copy_(_ids("zipf", n, 90, h))
+        rows.copy_(randn(h, n, 256))
+        gate.copy_(randn(h, n, 256))
+        for old, new in zip(x, _policy_inputs(n, 801, torch.bfloat16, seed, masked=40 * (seed - 46))):
+            old.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, step()):
+            assert torch.equal(a, b)
