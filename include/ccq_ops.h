@@ -72,6 +72,7 @@ typedef enum { CCQ_ACT_NONE = 0, CCQ_ACT_SILU = 1, CCQ_ACT_SIGMOID = 2 } ccq_act
  *   y    = u * act(gate)  with a gate,   act(u)  without.
  *   x, gate, y     [tokens, channels] in dtype, with row strides (gate may be NULL).
  *   weight, bias   [channels] in param_dtype (each may be NULL: 1 and 0).
+ * tokens and row strides below 2^31, channels up to 2^24.
  */
 CCQ_API ccq_status ccq_group_norm(const void *x, int64_t x_stride, const void *gate, int64_t gate_stride,
                                   const void *weight, const void *bias, ccq_dtype dtype,
@@ -188,6 +189,9 @@ typedef struct {
  * eighth apart, which rounding to nearest would lose for good.  A v > 0 is never stored as 0.
  * Moments that are not finite are stored as NaN in their own element.
  * A tensor with n = 0 is skipped.  Any number of tensors; 482 share a launch.
+ * `params` is read by the call: a call captured in a graph keeps its lr and step, and with the step the bias
+ * corrections and the thresholds of the 8-bit rounding, at every replay (grad_scale, a device
+ * scalar, is read anew).  A training step's graph ends before this call.
  */
 CCQ_API ccq_status ccq_adamw_step(const ccq_adamw_tensor *tensors, int count, ccq_dtype param_dtype,
                                   ccq_dtype grad_dtype, int state_bits, const ccq_adamw_params *p,

@@ -72,14 +72,11 @@ __device__ __forceinline__ uint32_t code_bits(float y) {
 // The code, rounded up where the fraction between neighbours reaches 2^20 - turn.
 __device__ __forceinline__ uint32_t encode(float y, uint32_t turn) { return ((code_bits(y) + turn) >> 20) - (120u << 3); }
 
+// Within two units in the last place, as fast_rcp is: of an update's step, which is a small part of the parameter, in both
+// forms of the state (the stored 8-bit roots are corrected below; the 32-bit moments take neither).
 __device__ __forceinline__ float approx_sqrt(float x) {
     float y;
     asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float fast_rcp(float x) {
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 

@@ -176,8 +176,8 @@ __device__ __forceinline__ void zero_absent_rows(const SortArgs &a, uint32_t par
 // the warps before it and over the CTAs before that keep equal digits in order.  Invalid and padding ids get the
 // key `rows`, behind every row.  All passes run in one launch.  Its time is latency: n = 16384 takes two passes of about
 // five barriers each.  A lane finds the others with its digit by a ballot for each bit (match.any takes a time that grows with
-// the number of different digits, 2000 cycles a step for 32 warps of random ones), and up to 65536 entries pass from CTA to
-// CTA in shared memory (through global memory a pass took 6000 cycles for its stores and loads alone).
+// the number of different digits, 2000 cycles a step for 32 warps of random ones), and up to 8192 entries a CTA (131072 with
+// 16) pass from CTA to CTA in shared memory (through global memory a pass took 6000 cycles for its stores and loads alone).
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortArgs a) {
     extern __shared__ __align__(16) uint32_t smem[];
     const int ctas = a.ctas;

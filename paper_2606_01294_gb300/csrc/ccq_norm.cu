@@ -43,11 +43,6 @@ __device__ __forceinline__ float param_at(const void *p, int bf16, int i, float 
     return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]) : static_cast<const float *>(p)[i];
 }
 
-__device__ __forceinline__ float fast_rcp(float x) {
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ float sigmoid(float u) { return fast_rcp(1.f + fast_exp2(-1.4426950408889634f * u)); }
 
 // act(u) and, where asked for, its derivative.
@@ -287,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, resident(N * K, BWD)) norm_kernel(No
     constexpr int E = N * K;
     __shared__ float red[kThreads / 32];
     constexpr int kTeams = kThreads / TEAM;
-    // the grid is at most a few CTAs an SM, or a CTA for each kTeams groups: below 2^31 teams
+    // the grid is at most a few CTAs an SM, or `unit` (of shape_of()) of them, at most one a group: below 2^24 x kThreads teams
     const uint32_t gt = blockIdx.x * kTeams + threadIdx.x / TEAM;
     const int l = threadIdx.x % TEAM;
     const int group = static_cast<int>(gt % static_cast<uint32_t>(a.groups));
@@ -608,9 +603,11 @@ Shape shape_of(int64_t tokens, int channels, int groups, int n, int bwd) {
     const int teams = s.team ? kThreads / s.team : 1;  // a CTA's teams
     // a CTA count that is a multiple of `unit` gives every group the same number of teams
     const int unit = groups / gcd(groups, teams);
-    // the forward takes four times the CTAs that fit at once, so that SMs that finish early take more (32768 x 2048
+    // The forward takes four times the CTAs that fit at once, so that SMs that finish early take more (32768 x 2048
     // bf16, gated: 1 x 69.3, 2 x 66.7, 4 x 63.6, 8 x 67.6 us); the backward one wave, its slots' partial sums cost more
-    // (16384 x 2048: 1 x 63.0, 2 x 67.9 us)
+    // (16384 x 2048: 1 x 63.0, 2 x 67.9 us).  That is by the long walks: where a slot has few tokens four waves cost a
+    // first fetch each (gated bf16 after an L2 flush, 1 and 4 waves: 4096 x 16 x 128 17.1 and 21.2 us, 20000 x 1 x 2048 49.8 and
+    // 56.0, 65536 x 4 x 64 25.2 and 27.3, 32768 x 16 x 128 76.4 and 70.3).
     const int64_t most = static_cast<int64_t>(sm_count_now()) * (s.team ? resident(n * s.k, bwd) * (bwd ? 1 : 4) : 4);
     const int64_t want = std::min<int64_t>(most, (tokens * groups + teams - 1) / teams);
     const int64_t grid = std::max<int64_t>(1, want / unit) * unit;

@@ -405,7 +405,9 @@ def adamw_step(params, grads, state: AdamWState, step: int, *, lr: float, betas=
                weight_decay: float = 0.01, grad_scale: Optional[torch.Tensor] = None, stream=None):
     """One AdamW update of all ``params`` (ccq_adamw_step), in place, with the moments of ``state``; ``step`` counts
     from 1.  params and grads: lists of contiguous bf16 or fp32 tensors (one type for all params, one for all
-    grads).  ``grad_scale``: a CUDA fp32 scalar that multiplies the gradients (as from clipping their norm)."""
+    grads).  ``grad_scale``: a CUDA fp32 scalar that multiplies the gradients (as from clipping their norm).  ``step``
+    and ``lr`` are the host's: a CUDA graph that has captured the call keeps them (and what follows from the step) at
+    every replay, so it is made outside of one."""
     if not params:
         return
     first = _cuda(params[0], "params[0]")
