@@ -242,11 +242,12 @@ _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device
 def _stream(device, stream):
     """The raw stream a call runs on.  The library launches on the current device and asks that one for its SMs, its
     occupancy and its status word, so tensors of another are refused."""
-    if device.index is not None and device.index != _current_device():
+    index = device.index
+    if index is not None and index != _current_device():
         raise ValueError(f"the tensors are on {device}, the current device is cuda:{_current_device()}: "
                          "make the call within torch.cuda.device()")
-    if stream is None and _raw_stream is not None and device.index is not None:
-        return _raw_stream(device.index)
+    if stream is None and _raw_stream is not None and index is not None:
+        return _raw_stream(index)
     return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
 
 
