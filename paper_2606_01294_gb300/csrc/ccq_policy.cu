@@ -11,7 +11,7 @@
 // hold (vocabularies above 520 thousand in bf16, 260 thousand in fp32) go through policy_row_kernel, which reads them
 // twice.  policy_loss_kernel adds the rows' losses.
 // HBM bounds it: 8192 x 32000 bf16, a quarter masked (918 MB): 154 us, 6.0 TB/s, 88 % of the copy rate; 1500 x 128001 (rows on
-// no 16-byte boundary, 742 MB): 135 us, 81 %.  Short rows are bound by a row's chain of reductions (8192 x 3500: 58 %),
+// no 16-byte boundary, 742 MB): 135 to 137 us, 80 %.  Short rows are bound by a row's chain of reductions (8192 x 3500: 58 %),
 // rows over several CTAs also by how many clusters fit the groups of SMs (512 x 200000 fp32: 67 %).
 #include <algorithm>
 
