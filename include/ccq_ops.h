@@ -1,8 +1,9 @@
 /*
  * ccq_ops.h -- C ABI of the operators around the CCQ token mixer: the embedding
- * lookup that feeds a stack of mixers, the gated group norm after the mixer's
- * read, the clipped policy loss at the end of the stack, and the AdamW update of
- * its weights.  Same library and conventions as ccq.h:
+ * lookup that feeds a stack of mixers, the rotation of queries and keys by their
+ * positions, linear attention with a constant decay for each head (the mixer without the
+ * correction), the gated group norm after the mixer's read, the clipped policy loss at the
+ * end of the stack, and the AdamW update of its weights.  Same library and conventions as ccq.h:
  *   - pointers are DEVICE pointers owned by the caller (host arrays are named so),
  *     nothing is allocated, calls are asynchronous on `stream`, argument errors
  *     are reported through the return value and ccq_last_error();
@@ -57,6 +58,105 @@ CCQ_API ccq_status ccq_embed_grad(const void *dout, ccq_dtype dtype, int64_t dou
 
 /* Workspace bytes ccq_embed_grad needs.  Host-only. */
 CCQ_API ccq_status ccq_embed_grad_workspace_size(int64_t n, int64_t rows, int width, size_t *bytes);
+
+/* ---------------------------------------------------------------------- heads */
+
+/*
+ * Heads of tokens: channel c of head h of token (b, t) is p[b * batch + t * token + h * head + c].
+ * Strides are in elements, 0 <= stride < 2^40 (those of extents of one are not looked at).  An input may
+ * repeat itself (a stride of 0); an output's channels lie apart.  Tensors whose addresses and strides are
+ * multiples of 16 bytes are faster.
+ */
+typedef struct {
+    void *p;
+    int64_t batch, token, head;
+    int64_t heads;
+} ccq_heads;
+
+/* ------------------------------------------------------------ rotary positions */
+
+/*
+ * Rotation of the first `part` channels of every head by the token's position, for one or two tensors (queries,
+ * keys) in one launch:
+ *   theta = positions[b, t] freqs[i],  0 <= i < part / 2,
+ *   (y_a, y_b) = amplitude (x_a cos theta - x_b sin theta, x_a sin theta + x_b cos theta)
+ * for the pairs (a, b) = (i, i + part / 2), or (2 i, 2 i + 1) with interleaved = 1.  The channels from `part` on are
+ * copied.  inverse = 1 turns by -theta: with it, the call on the outputs' gradients gives the inputs'.
+ *   x, y       arrays (HOST) of `count` tensors of [B, T, heads, width] in dtype; y[i] may be x[i] itself, or lies
+ *              apart from it.
+ *   positions  [B, T], position_bytes 4 (int32) or 8 (int64); any values.
+ *   freqs      [part / 2] radians a position, fp64 (any finite values).
+ * An angle is formed to 2^-31 of a turn, whatever the position; products and sums are fp32, rounded once.
+ */
+CCQ_API ccq_status ccq_rotary(const ccq_heads *x, const ccq_heads *y, int count, ccq_dtype dtype, int64_t B,
+                              int64_t T, int width, int part, const void *positions, int position_bytes,
+                              const double *freqs, float amplitude, int interleaved, int inverse,
+                              void *stream);
+
+/* ------------------------------------------ linear attention, a decay for each head */
+
+/*
+ * With g_h = exp(log_decay[h]) and, for every sequence and head, a state S of [d, d]:
+ *   S_t = g S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t.
+ *   q, k, v    [B, T, heads, d] in dtype, d 64 or 128; each may have fewer heads than H, a divisor of it: head h then
+ *              reads head h / (H / heads).
+ *   log_decay  [H] fp32, <= 0 (-inf: nothing is kept); a constant of the layer, without a gradient.
+ *   S0         [num_seqs, H, d, d] fp32, or NULL (0): the states before the first tokens.
+ *   o          [B, T, H, d] in dtype, apart from the inputs.
+ *   ST         [num_seqs, H, d, d] fp32, or NULL: the states after the last tokens.  May be S0.
+ *   cu         NULL: B sequences of T tokens (num_seqs = B).  Else B = 1 and sequence s is the tokens cu[s] to
+ *              cu[s + 1] (a device array of num_seqs + 1, cu_bytes 4 or 8; 0 <= cu[s] <= cu[s + 1] <= T).
+ *              Tokens of no sequence are left as they are in o.  An offset outside its range is held to it
+ *              and leaves CCQ_ERR_INDEX.
+ *   workspace  ccq_decay_attention_workspace_size() bytes, 16-byte aligned (NULL where that is 0).
+ * fp32 inputs, and bf16 ones whose addresses or strides are not multiples of 16 bytes, are computed in fp32.  Other
+ * bf16 inputs run on the tensor cores in chunks of 128 tokens: the products of a chunk's queries and keys and the state
+ * that its queries read are rounded to bf16, the state itself is carried to 2^-17 of its terms.  There a value that is not finite
+ * also reaches the outputs of the other tokens of its chunk.
+ */
+CCQ_API ccq_status ccq_decay_attention(const ccq_heads *q, const ccq_heads *k, const ccq_heads *v,
+                                       ccq_dtype dtype, const float *log_decay, float scale,
+                                       const float *S0, const ccq_heads *o, float *ST, int64_t B, int64_t T,
+                                       int H, int d, const void *cu, int cu_bytes, int64_t num_seqs,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradients of ccq_decay_attention for a given dout [B, T, H, d] and, where it is not NULL, dST [num_seqs, H, d, d].
+ * Nothing is kept from the forward.
+ *   dq, dk, dv [B, T, heads, d] in dtype with the heads of q, k and v, apart from the inputs: a head that
+ *              several read gets their sum (formed in fp32, in ascending order).
+ *   dS0        [num_seqs, H, d, d] fp32, or NULL.  Apart from dST.
+ *   workspace  ccq_decay_attention_bwd_workspace_size() bytes, 16-byte aligned (NULL where that is 0).
+ */
+CCQ_API ccq_status ccq_decay_attention_bwd(const ccq_heads *q, const ccq_heads *k, const ccq_heads *v,
+                                           ccq_dtype dtype, const float *log_decay, float scale,
+                                           const float *S0, const ccq_heads *dout, const float *dST,
+                                           const ccq_heads *dq, const ccq_heads *dk, const ccq_heads *dv,
+                                           float *dS0, int64_t B, int64_t T, int H, int d, const void *cu,
+                                           int cu_bytes, int64_t num_seqs, void *workspace,
+                                           size_t workspace_bytes, void *stream);
+
+/* Workspace bytes of the two calls (q_heads, k_heads, v_heads: those of q, k and v).  Host-only. */
+CCQ_API ccq_status ccq_decay_attention_workspace_size(int64_t B, int64_t T, int H, int d, int64_t num_seqs,
+                                                      ccq_dtype dtype, size_t *bytes);
+CCQ_API ccq_status ccq_decay_attention_bwd_workspace_size(int64_t B, int64_t T, int H, int q_heads,
+                                                          int k_heads, int v_heads, int d,
+                                                          int64_t num_seqs, ccq_dtype dtype,
+                                                          size_t *bytes);
+
+/*
+ * One token of every sequence of a batch, in place: state = g state + k v^T, o = scale state^T q, in fp32.
+ *   q, k, v    [B, heads, d] in dtype (the token stride is not looked at), heads as above.
+ *   state      [rows, H, d, d] fp32.
+ *   slots      NULL (row b's state is b; rows >= B), or [B] with slot_bytes 4 or 8: the row of `state` of each.  A
+ *              negative one is a batch row without a sequence: its o is 0.  One that is not below `rows`, or
+ *              that an earlier batch row has, gives a zero row, changes no state and leaves CCQ_ERR_INDEX.
+ *   o          [B, H, d] in dtype.
+ */
+CCQ_API ccq_status ccq_decay_attention_step(const ccq_heads *q, const ccq_heads *k, const ccq_heads *v,
+                                            ccq_dtype dtype, const float *log_decay, float scale,
+                                            float *state, int64_t rows, const void *slots, int slot_bytes,
+                                            const ccq_heads *o, int64_t B, int H, int d, void *stream);
 
 /* ------------------------------------------------------- group norm, activation */
 

@@ -1,0 +1,599 @@
+// ccq_decay.cu -- linear attention with a decay for each head in fp32 arithmetic, for any type and alignment, and the
+// entry points (ccq_ops.h).  ccq_decay.cuh says how one pass serves the forward and the gradients.
+//
+// decay_block_kernel: a CTA walks the tokens of one (sequence, head, segment) in blocks of 32 with a slice of 32 columns of
+// the state, in fp32 on the CUDA cores:
+//   P = Q K^T (32 x 32), masked and times g^|i - j|;  O = P V + diag(g^..) Q S;  S = g^n S + K^T diag(g^..) V.
+// 32 tokens cost 32 d (16 + 2 * 32) + 16 * 32 * 32 multiply-adds a CTA, of which P, formed again by each slice, is a fifth.
+// Bound by the CUDA cores' fp32 rate and by the latency of a block's steps where the CTAs do not fill the GPU.
+#include <algorithm>
+#include <cmath>
+
+#include "ccq_decay.cuh"
+
+namespace ccq {
+namespace {
+
+constexpr int kC = 32;        // tokens of a block
+constexpr int kN = 32;        // columns of a CTA
+constexpr int kThreads = 128;
+constexpr int kPad = 4;
+
+template <int D> struct BlockShared {
+    float q[kC][D + kPad], k[kC][D + kPad], v[kC][kN + kPad], p[kC][kN + kPad], s[D][kN + kPad];
+    float power[kC + 1];  // g^n
+};
+
+// Rows begin .. begin + n of a head (of `width` channels from column c0) to shared memory, zeros up to kC.
+template <typename T, int W, int STRIDE>
+__device__ __forceinline__ void load_rows(float (*dst)[STRIDE], const DecayView &x, int64_t b, int64_t begin, int n, int h,
+                                          int c0, bool vec) {
+    const T *src = static_cast<const T *>(x.p) + b * x.batch + begin * x.token + (h / x.share) * x.head + c0;
+    if (vec) {
+        constexpr int N = 16 / sizeof(T);
+        for (int j = threadIdx.x; j < kC * W / N; j += kThreads) {
+            const int r = j / (W / N), c = (j % (W / N)) * N;
+            float f[N];
+            if (r < n) {
+                const Pack<T, N> p = load_plain<T, N>(src + r * x.token + c);
+                unpack(p, f);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) f[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < N; e += 4)
+                *reinterpret_cast<float4 *>(&dst[r][c + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+        }
+    } else {
+        for (int j = threadIdx.x; j < kC * W; j += kThreads) {
+            const int r = j / W, c = j % W;
+            dst[r][c] = r < n ? to_f32(src[r * x.token + c]) : 0.f;
+        }
+    }
+}
+
+template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a) {
+    extern __shared__ float4 shared_raw[];
+    BlockShared<D> &sh = *reinterpret_cast<BlockShared<D> *>(shared_raw);
+    constexpr int kSlices = D / kN;
+    constexpr int R = D / 16;  // state rows of a thread: R x 4 of its slice
+    int64_t x = blockIdx.x;
+    const int slice = static_cast<int>(x % kSlices);
+    x /= kSlices;
+    const int nseg = a.parts_only ? a.segments - 1 : a.segments;
+    const int segment = static_cast<int>(x % nseg);
+    x /= nseg;
+    const int h = static_cast<int>(x % a.H);
+    x /= a.H;
+    const int sequence = static_cast<int>(x % a.sequences);
+    const DecayPass &ps = a.pass[x / a.sequences];
+    const int tid = threadIdx.x, tx = tid % 8, ty = tid / 8;
+    const int c0 = slice * kN;
+    const bool down = ps.descending != 0;
+
+    const DecaySpan span = decay_span(a, sequence);
+    const int64_t blocks = (span.length + kC - 1) / kC, per = (blocks + a.segments - 1) / a.segments;
+    const int64_t first = min(per * segment, blocks), last = min(first + per, blocks);
+    const float l2 = decay_log2(a.log_decay, h);
+    if (tid <= kC) sh.power[tid] = exp2f(l2 * tid);
+
+    // tokens of block j in the pass's order: the ragged block is the sequence's last
+    auto block_begin = [&](int64_t j) { return (down ? blocks - 1 - j : j) * kC; };
+
+    // ---- the state at the segment's start; this thread's rows R ty .. and columns 4 tx ..
+    float S[R][4];
+    {
+        const int64_t at = (static_cast<int64_t>(sequence) * a.H + h) * D * D;
+        auto add = [&](const float *m, bool transposed, float keep) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int row = R * ty + r, col = c0 + 4 * tx + c;
+                    const float f = m[transposed ? col * D + row : row * D + col];
+                    S[r][c] = keep == 0.f ? f : S[r][c] * keep + f;
+                }
+            }
+        };
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) S[r][c] = 0.f;
+        if (a.segments == 1 || (a.parts_only && segment == 0)) {
+            if (ps.state_in) add(ps.state_in + at, ps.transposed, 0.f);
+            if (a.parts_only) {
+                float *to = a.parts + decay_part(a, ps.kind, sequence, h, 0);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    *reinterpret_cast<float4 *>(to + (R * ty + r) * D + c0 + 4 * tx) =
+                        make_float4(S[r][0], S[r][1], S[r][2], S[r][3]);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) S[r][c] = 0.f;
+            }
+        } else if (!a.parts_only) {
+            for (int g = 0; g <= segment; ++g) {
+                // tokens of segment g - 1
+                const int64_t lo = min(per * (g - 1), blocks), hi = min(per * g, blocks);
+                int64_t n = 0;
+                if (g > 0 && hi > lo) n = (hi - lo) * kC - ((down ? lo == 0 : hi == blocks) ? blocks * kC - span.length : 0);
+                add(a.parts + decay_part(a, ps.kind, sequence, h, g), ps.parts_transposed,
+                    g == 0 ? 0.f : exp2f(l2 * static_cast<float>(n)));
+            }
+        }
+    }
+
+    for (int64_t j = first; j < last; ++j) {
+        const int64_t begin = block_begin(j);
+        const int n = static_cast<int>(min(static_cast<int64_t>(kC), span.length - begin));
+        __syncthreads();  // the last block's readers
+        load_rows<T, D>(sh.k, ps.k, span.b, span.begin + begin, n, h, 0, a.vec);
+        load_rows<T, kN>(sh.v, ps.v, span.b, span.begin + begin, n, h, c0, a.vec);
+        if (!a.parts_only) {
+            load_rows<T, D>(sh.q, ps.q, span.b, span.begin + begin, n, h, 0, a.vec);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                *reinterpret_cast<float4 *>(&sh.s[R * ty + r][4 * tx]) = make_float4(S[r][0], S[r][1], S[r][2], S[r][3]);
+        }
+        __syncthreads();
+        if (!a.parts_only) {
+            // P: rows 2 ty, 2 ty + 1, columns tx + 8 c
+            float p[2][4] = {};
+            for (int e = 0; e < D; e += 4) {
+                float4 qv[2], kv[4];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) qv[r] = *reinterpret_cast<const float4 *>(&sh.q[2 * ty + r][e]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) kv[c] = *reinterpret_cast<const float4 *>(&sh.k[tx + 8 * c][e]);
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        p[r][c] += qv[r].x * kv[c].x + qv[r].y * kv[c].y + qv[r].z * kv[c].z + qv[r].w * kv[c].w;
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int i = 2 * ty + r, jj = tx + 8 * c, gap = down ? jj - i : i - jj;
+                    sh.p[i][jj] = gap >= 0 ? p[r][c] * (sh.power[gap] * ps.p_scale) : 0.f;
+                }
+            }
+            __syncthreads();
+            // O: rows 2 ty, 2 ty + 1, columns 4 tx .. 4 tx + 3
+            float o[2][4] = {};
+            for (int e = 0; e < D; e += 4) {
+                float4 qv[2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) qv[r] = *reinterpret_cast<const float4 *>(&sh.q[2 * ty + r][e]);
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                    const float4 sv = *reinterpret_cast<const float4 *>(&sh.s[e + f][4 * tx]);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const float w = f == 0 ? qv[r].x : f == 1 ? qv[r].y : f == 2 ? qv[r].z : qv[r].w;
+                        o[r][0] += w * sv.x;
+                        o[r][1] += w * sv.y;
+                        o[r][2] += w * sv.z;
+                        o[r][3] += w * sv.w;
+                    }
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int i = 2 * ty + r, m = down ? n - 1 - i : i + 1;
+                const float f = m >= 0 ? sh.power[m] * ps.s_scale : 0.f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) o[r][c] *= f;
+            }
+            // (a value that is not finite does not reach the rows before it: the sums end at the row)
+            const int from = down ? 2 * ty : 0, to = down ? n : min(n, 2 * ty + 2);
+            for (int jj = from; jj < to; ++jj) {
+                const float4 vv = *reinterpret_cast<const float4 *>(&sh.v[jj][4 * tx]);
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    if (down ? jj < 2 * ty + r : jj > 2 * ty + r) continue;
+                    const float w = sh.p[2 * ty + r][jj];
+                    o[r][0] += w * vv.x;
+                    o[r][1] += w * vv.y;
+                    o[r][2] += w * vv.z;
+                    o[r][3] += w * vv.w;
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int i = 2 * ty + r;
+                if (i >= n) continue;
+                const int64_t at = span.b * ps.o_batch + (span.begin + begin + i) * ps.o_token + h * ps.o_head + c0 + 4 * tx;
+                if (ps.o_fp32) {
+                    float *to_p = static_cast<float *>(ps.o) + at;
+                    *reinterpret_cast<float4 *>(to_p) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
+                } else {
+                    T *to_p = static_cast<T *>(ps.o) + at;
+                    if (a.vec) {
+                        Pack<T, 4> u;
+                        pack(o[r], u);
+                        store_stream<T, 4>(to_p, u);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) to_p[c] = from_f32<T>(o[r][c]);
+                    }
+                }
+            }
+        }
+        // S = g^n S + K^T diag(k_scale g^..) V, rows R ty .., columns 4 tx ..
+        const float keep = sh.power[n];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) S[r][c] *= keep;
+        for (int jj = 0; jj < n; ++jj) {
+            const float u = sh.power[down ? jj + 1 : n - 1 - jj] * ps.k_scale;
+            float4 vv = *reinterpret_cast<const float4 *>(&sh.v[jj][4 * tx]);
+            vv.x *= u;
+            vv.y *= u;
+            vv.z *= u;
+            vv.w *= u;
+#pragma unroll
+            for (int r = 0; r < R; r += 4) {
+                const float4 kv = *reinterpret_cast<const float4 *>(&sh.k[jj][R * ty + r]);
+                const float kk[4] = {kv.x, kv.y, kv.z, kv.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    S[r + e][0] += kk[e] * vv.x;
+                    S[r + e][1] += kk[e] * vv.y;
+                    S[r + e][2] += kk[e] * vv.z;
+                    S[r + e][3] += kk[e] * vv.w;
+                }
+            }
+        }
+    }
+    float *to = nullptr;
+    if (a.parts_only)
+        to = a.parts + decay_part(a, ps.kind, sequence, h, segment + 1);
+    else if (ps.state_out && segment == a.segments - 1)
+        to = ps.state_out + (static_cast<int64_t>(sequence) * a.H + h) * D * D;
+    if (to) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            *reinterpret_cast<float4 *>(to + (R * ty + r) * D + c0 + 4 * tx) = make_float4(S[r][0], S[r][1], S[r][2], S[r][3]);
+    }
+}
+
+template <typename T, int D> cudaError_t launch_blocks(const DecayArgs &a, cudaStream_t s) {
+    constexpr int kBytes = sizeof(BlockShared<D>);
+    cudaError_t e = allow_shared<decay_block_kernel<T, D>>(kBytes);
+    if (e != cudaSuccess) return e;
+    const int64_t grid = static_cast<int64_t>(D / kN) * (a.parts_only ? a.segments - 1 : a.segments) * a.H * a.sequences * a.passes;
+    if (grid > 0x7fffffff) return cudaErrorInvalidValue;
+    decay_block_kernel<T, D><<<static_cast<unsigned>(grid), kThreads, kBytes, s>>>(a);
+    return cudaGetLastError();
+}
+
+// ---------------------------------------------------------------- gradients of shared heads
+
+struct SumArgs {
+    const float *part;  // [rows][H][d]
+    void *out[3];
+    int64_t token[3], batch[3], head[3];
+    const float *parts[3];
+    int share[3];
+    int count;
+    int H, d;
+    int64_t rows, T;
+};
+
+// out[row, head, c] = sum over the heads that read it, in ascending order; one thread four channels.
+template <typename T> __global__ void __launch_bounds__(256) decay_sum_kernel(const SumArgs a, int vec) {
+    const int which = blockIdx.y;
+    const int share = a.share[which], heads = a.H / share, quads = a.d / 4;
+    const int64_t total = a.rows * heads * quads;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+        const int c = static_cast<int>(i % quads) * 4;
+        const int64_t r = i / quads;
+        const int h = static_cast<int>(r % heads);
+        const int64_t row = r / heads, b = row / a.T, t = row - b * a.T;
+        const float *src = a.parts[which] + (row * a.H + static_cast<int64_t>(h) * share) * a.d + c;
+        float f[4] = {};
+        for (int g = 0; g < share; ++g) {
+            const float4 u = __ldcs(reinterpret_cast<const float4 *>(src + static_cast<int64_t>(g) * a.d));
+            f[0] += u.x;
+            f[1] += u.y;
+            f[2] += u.z;
+            f[3] += u.w;
+        }
+        T *to = static_cast<T *>(a.out[which]) + b * a.batch[which] + t * a.token[which] + h * a.head[which] + c;
+        if (vec) {
+            Pack<T, 4> p;
+            pack(f, p);
+            store_stream<T, 4>(to, p);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) to[e] = from_f32<T>(f[e]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- the calls
+
+// Segments of each sequence: as many as fill the GPU with one CTA an SM (tensor cores) or a few (fp32), of at least
+// `least` tokens each.  Forming the states before them reads two of a pass's four operands once more.
+int segments_for(int64_t sequences, int64_t T, int64_t ctas, int64_t slots, int64_t least) {
+    if (sequences < 1 || ctas < 1) return 1;
+    const int64_t fill = slots / ctas, most = T / sequences / least;
+    return static_cast<int>(std::max<int64_t>(1, std::min(fill, most)));
+}
+
+int plan_segments(int64_t B, int64_t T, int H, int d, int64_t num_seqs, ccq_dtype dtype, int passes) {
+    const int64_t total = B * T;
+    return segments_for(num_seqs, total, num_seqs * H * passes * (d / kN), 4 * sm_count_now(), 4 * kC);
+}
+
+size_t parts_bytes(int64_t num_seqs, int H, int d, int segments, int kinds) {
+    return segments > 1 ? static_cast<size_t>(kinds) * num_seqs * H * segments * d * d * 4 : 0;
+}
+
+ccq_status check_sizes(int64_t B, int64_t T, int H, int d, int64_t num_seqs) {
+    ccq_status st = check_tokens(B, T);
+    if (st != CCQ_OK) return st;
+    if (H < 1 || H > (1 << 20)) return op_fail(CCQ_ERR_INVALID_ARG, "bad sizes: H=%d", H);
+    if (d != 64 && d != 128) return op_fail(CCQ_ERR_UNSUPPORTED, "d=%d: 64 or 128", d);
+    if (num_seqs < 0 || num_seqs > (1 << 24) || num_seqs * H > (1 << 24))
+        return op_fail(CCQ_ERR_UNSUPPORTED, "%lld sequences of %d heads: at most 2^24 of both",
+                       static_cast<long long>(num_seqs), H);
+    return CCQ_OK;
+}
+
+ccq_status check_shared(const char *name, const ccq_heads &x, ccq_dtype dtype, int64_t B, int64_t T, int H, int d, bool apart) {
+    ccq_status st = check_heads(name, x, dtype, B, T, d, apart);
+    if (st != CCQ_OK) return st;
+    if (x.heads > H || H % x.heads)
+        return op_fail(CCQ_ERR_INVALID_ARG, "%s has %lld heads, no divisor of %d", name, static_cast<long long>(x.heads), H);
+    return CCQ_OK;
+}
+
+ccq_status check_common(ccq_dtype dtype, const float *log_decay, float scale, int64_t B, int64_t T, int H, int d,
+                        const void *cu, int cu_bytes, int64_t num_seqs) {
+    if (!valid_dtype(dtype)) return op_fail(CCQ_ERR_INVALID_ARG, "unknown dtype %d", static_cast<int>(dtype));
+    ccq_status st = check_sizes(B, T, H, d, num_seqs);
+    if (st != CCQ_OK) return st;
+    if (!std::isfinite(scale)) return op_fail(CCQ_ERR_INVALID_ARG, "scale is not finite");
+    if ((st = op_pointer("log_decay", log_decay, 4)) != CCQ_OK) return st;
+    if (!cu) {
+        if (num_seqs != B) return op_fail(CCQ_ERR_INVALID_ARG, "num_seqs=%lld without cu, B=%lld",
+                                          static_cast<long long>(num_seqs), static_cast<long long>(B));
+        return CCQ_OK;
+    }
+    if (B != 1) return op_fail(CCQ_ERR_INVALID_ARG, "cu with B=%lld: packed sequences have B = 1", static_cast<long long>(B));
+    if (cu_bytes != 4 && cu_bytes != 8) return op_fail(CCQ_ERR_INVALID_ARG, "cu_bytes=%d: 4 or 8", cu_bytes);
+    return op_pointer("cu", cu, cu_bytes);
+}
+
+ccq_status check_state(const char *name, const float *p) {
+    return p ? op_pointer(name, p, 16) : CCQ_OK;
+}
+
+DecayView view_of(const ccq_heads &x, int H) {
+    return {x.p, x.batch, x.token, x.head, static_cast<int>(H / x.heads)};
+}
+
+ccq_status run_passes(DecayArgs &a, ccq_dtype dtype, unsigned parts_mask, cudaStream_t s) {
+    cudaError_t e = cudaSuccess;
+    if (a.segments > 1) {
+        DecayArgs p = a;
+        p.parts_only = 1;
+        p.passes = 0;
+        for (int i = 0; i < a.passes; ++i)
+            if (parts_mask >> i & 1) p.pass[p.passes++] = a.pass[i];
+        e = launch_decay_blocks(p, dtype, s);
+    }
+    if (e == cudaSuccess) e = launch_decay_blocks(a, dtype, s);
+    return op_cuda(e, "decayed attention launch");
+}
+
+}  // namespace
+
+cudaError_t launch_decay_blocks(const DecayArgs &a, ccq_dtype dtype, cudaStream_t s) {
+    if (dtype == CCQ_BF16)
+        return a.d == 128 ? launch_blocks<__nv_bfloat16, 128>(a, s) : launch_blocks<__nv_bfloat16, 64>(a, s);
+    return a.d == 128 ? launch_blocks<float, 128>(a, s) : launch_blocks<float, 64>(a, s);
+}
+
+}  // namespace ccq
+
+using namespace ccq;
+
+extern "C" {
+
+ccq_status ccq_decay_attention_workspace_size(int64_t B, int64_t T, int H, int d, int64_t num_seqs, ccq_dtype dtype,
+                                              size_t *bytes) {
+    if (!valid_dtype(dtype)) return op_fail(CCQ_ERR_INVALID_ARG, "unknown dtype %d", static_cast<int>(dtype));
+    ccq_status st = check_sizes(B, T, H, d, num_seqs);
+    if (st != CCQ_OK) return st;
+    if (!bytes) return op_fail(CCQ_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = parts_bytes(num_seqs, H, d, plan_segments(B, T, H, d, num_seqs, dtype, 1), 1);
+    return CCQ_OK;
+}
+
+ccq_status ccq_decay_attention(const ccq_heads *q, const ccq_heads *k, const ccq_heads *v, ccq_dtype dtype,
+                               const float *log_decay, float scale, const float *S0, const ccq_heads *o, float *ST, int64_t B,
+                               int64_t T, int H, int d, const void *cu, int cu_bytes, int64_t num_seqs, void *workspace,
+                               size_t workspace_bytes, void *stream) {
+    if (!q || !k || !v || !o) return op_fail(CCQ_ERR_INVALID_ARG, "q, k, v or o is NULL");
+    ccq_status st = check_common(dtype, log_decay, scale, B, T, H, d, cu, cu_bytes, num_seqs);
+    if (st != CCQ_OK) return st;
+    const ccq_heads *in[3] = {q, k, v};
+    const char *names[3] = {"q", "k", "v"};
+    int access = 16;
+    for (int i = 0; i < 3; ++i) {
+        if ((st = check_shared(names[i], *in[i], dtype, B, T, H, d, false)) != CCQ_OK) return st;
+        access = heads_access(*in[i], dtype_bytes(dtype), B, T, access);
+    }
+    if ((st = check_shared("o", *o, dtype, B, T, H, d, true)) != CCQ_OK) return st;
+    if (o->heads != H) return op_fail(CCQ_ERR_INVALID_ARG, "o has %lld heads, expected %d", static_cast<long long>(o->heads), H);
+    for (int i = 0; i < 3 && B * T; ++i)
+        if (in[i]->p == o->p) return op_fail(CCQ_ERR_INVALID_ARG, "o is %s: other tokens still read it", names[i]);
+    access = heads_access(*o, dtype_bytes(dtype), B, T, access);
+    if ((st = check_state("S0", S0)) != CCQ_OK) return st;
+    if ((st = check_state("ST", ST)) != CCQ_OK) return st;
+    DecayArgs a = {};
+    a.segments = plan_segments(B, T, H, d, num_seqs, dtype, 1);
+    const size_t need = parts_bytes(num_seqs, H, d, a.segments, 1);
+    if (need && (st = op_pointer("workspace", workspace, 16)) != CCQ_OK) return st;
+    if (workspace_bytes < need)
+        return op_fail(CCQ_ERR_INVALID_ARG, "workspace of %zu bytes, needs %zu", workspace_bytes, need);
+    if (num_seqs == 0) return CCQ_OK;
+    if ((st = op_status_word(&a.status)) != CCQ_OK) return st;
+    a.passes = 1;
+    DecayPass &p = a.pass[0];
+    p.q = view_of(*q, H);
+    p.k = view_of(*k, H);
+    p.v = view_of(*v, H);
+    p.o = o->p;
+    p.o_batch = o->batch;
+    p.o_token = o->token;
+    p.o_head = o->head;
+    p.state_in = S0;
+    p.state_out = ST;
+    p.p_scale = p.s_scale = scale;
+    p.k_scale = 1.f;
+    a.H = H;
+    a.d = d;
+    a.T = T;
+    a.sequences = static_cast<int>(num_seqs);
+    a.log_decay = log_decay;
+    a.cu = cu;
+    a.cu_bytes = cu_bytes;
+    a.parts = static_cast<float *>(workspace);
+    a.vec = access == 16;
+    return run_passes(a, dtype, 1u, static_cast<cudaStream_t>(stream));
+}
+
+ccq_status ccq_decay_attention_bwd_workspace_size(int64_t B, int64_t T, int H, int q_heads, int k_heads, int v_heads, int d,
+                                                  int64_t num_seqs, ccq_dtype dtype, size_t *bytes) {
+    if (!valid_dtype(dtype)) return op_fail(CCQ_ERR_INVALID_ARG, "unknown dtype %d", static_cast<int>(dtype));
+    ccq_status st = check_sizes(B, T, H, d, num_seqs);
+    if (st != CCQ_OK) return st;
+    size_t shared = 0;
+    for (int heads : {q_heads, k_heads, v_heads}) {
+        if (heads < 1 || heads > H || H % heads) return op_fail(CCQ_ERR_INVALID_ARG, "%d heads, no divisor of %d", heads, H);
+        shared += heads < H;
+    }
+    if (!bytes) return op_fail(CCQ_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = parts_bytes(num_seqs, H, d, plan_segments(B, T, H, d, num_seqs, dtype, 3), 2) +
+             shared * static_cast<size_t>(B * T) * H * d * 4;
+    return CCQ_OK;
+}
+
+ccq_status ccq_decay_attention_bwd(const ccq_heads *q, const ccq_heads *k, const ccq_heads *v, ccq_dtype dtype,
+                                   const float *log_decay, float scale, const float *S0, const ccq_heads *dout,
+                                   const float *dST, const ccq_heads *dq, const ccq_heads *dk, const ccq_heads *dv, float *dS0,
+                                   int64_t B, int64_t T, int H, int d, const void *cu, int cu_bytes, int64_t num_seqs,
+                                   void *workspace, size_t workspace_bytes, void *stream) {
+    if (!q || !k || !v || !dout || !dq || !dk || !dv) return op_fail(CCQ_ERR_INVALID_ARG, "a tensor of heads is NULL");
+    ccq_status st = check_common(dtype, log_decay, scale, B, T, H, d, cu, cu_bytes, num_seqs);
+    if (st != CCQ_OK) return st;
+    const ccq_heads *in[4] = {q, k, v, dout}, *out[3] = {dq, dk, dv};
+    const char *names[4] = {"q", "k", "v", "dout"}, *outs[3] = {"dq", "dk", "dv"};
+    int access = 16, access_out = 16;
+    size_t shared = 0;
+    for (int i = 0; i < 4; ++i) {
+        if ((st = check_shared(names[i], *in[i], dtype, B, T, H, d, false)) != CCQ_OK) return st;
+        access = heads_access(*in[i], dtype_bytes(dtype), B, T, access);
+    }
+    if (dout->heads != H)
+        return op_fail(CCQ_ERR_INVALID_ARG, "dout has %lld heads, expected %d", static_cast<long long>(dout->heads), H);
+    for (int i = 0; i < 3; ++i) {
+        if ((st = check_shared(outs[i], *out[i], dtype, B, T, H, d, true)) != CCQ_OK) return st;
+        if (out[i]->heads != in[i]->heads)
+            return op_fail(CCQ_ERR_INVALID_ARG, "%s has %lld heads, %s %lld", outs[i], static_cast<long long>(out[i]->heads),
+                           names[i], static_cast<long long>(in[i]->heads));
+        for (int j = 0; j < 4 && B * T; ++j)
+            if (in[j]->p == out[i]->p) return op_fail(CCQ_ERR_INVALID_ARG, "%s is %s: other passes still read it", outs[i], names[j]);
+        access_out = heads_access(*out[i], dtype_bytes(dtype), B, T, access_out);
+        shared += out[i]->heads < H;
+    }
+    if ((st = check_state("S0", S0)) != CCQ_OK) return st;
+    if ((st = check_state("dST", dST)) != CCQ_OK) return st;
+    if ((st = check_state("dS0", dS0)) != CCQ_OK) return st;
+    if (dS0 && dS0 == dST) return op_fail(CCQ_ERR_INVALID_ARG, "dS0 is dST: both are in use at once");
+    DecayArgs a = {};
+    a.segments = plan_segments(B, T, H, d, num_seqs, dtype, 3);
+    const size_t states = parts_bytes(num_seqs, H, d, a.segments, 2);
+    const size_t rows = static_cast<size_t>(B * T) * H * d * 4, need = states + shared * rows;
+    if (need && (st = op_pointer("workspace", workspace, 16)) != CCQ_OK) return st;
+    if (workspace_bytes < need)
+        return op_fail(CCQ_ERR_INVALID_ARG, "workspace of %zu bytes, needs %zu", workspace_bytes, need);
+    if (num_seqs == 0) return CCQ_OK;
+    if ((st = op_status_word(&a.status)) != CCQ_OK) return st;
+    a.passes = 3;
+    const DecayView Q = view_of(*q, H), K = view_of(*k, H), V = view_of(*v, H), O = view_of(*dout, H);
+    a.pass[0].q = O;
+    a.pass[0].k = V;
+    a.pass[0].v = K;
+    a.pass[1].q = V;
+    a.pass[1].k = O;
+    a.pass[1].v = Q;
+    a.pass[2].q = K;
+    a.pass[2].k = Q;
+    a.pass[2].v = O;
+    uint8_t *part = static_cast<uint8_t *>(workspace) + states;
+    SumArgs sum = {};
+    for (int i = 0; i < 3; ++i) {
+        DecayPass &p = a.pass[i];
+        p.p_scale = scale;
+        p.k_scale = i ? scale : 1.f;
+        p.s_scale = i ? 1.f : scale;
+        p.descending = i > 0;
+        p.state_in = i ? dST : S0;
+        p.state_out = i == 2 ? dS0 : nullptr;
+        p.transposed = i < 2;
+        p.kind = i > 0;
+        p.parts_transposed = i == 1;
+        if (out[i]->heads < H) {
+            p.o = part;
+            p.o_fp32 = 1;
+            p.o_head = d;
+            p.o_token = static_cast<int64_t>(H) * d;
+            p.o_batch = p.o_token * T;
+            const int n = sum.count++;
+            sum.parts[n] = reinterpret_cast<const float *>(part);
+            sum.out[n] = out[i]->p;
+            sum.batch[n] = out[i]->batch;
+            sum.token[n] = out[i]->token;
+            sum.head[n] = out[i]->head;
+            sum.share[n] = static_cast<int>(H / out[i]->heads);
+            part += rows;
+        } else {
+            p.o = out[i]->p;
+            p.o_batch = out[i]->batch;
+            p.o_token = out[i]->token;
+            p.o_head = out[i]->head;
+        }
+    }
+    a.H = H;
+    a.d = d;
+    a.T = T;
+    a.sequences = static_cast<int>(num_seqs);
+    a.log_decay = log_decay;
+    a.cu = cu;
+    a.cu_bytes = cu_bytes;
+    a.parts = static_cast<float *>(workspace);
+    a.vec = access == 16 && access_out == 16;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if ((st = run_passes(a, dtype, 5u, s)) != CCQ_OK || !sum.count || !(B * T)) return st;
+    sum.H = H;
+    sum.d = d;
+    sum.rows = B * T;
+    sum.T = T;
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>((sum.rows * H * d / 4 + 255) / 256, 16 * sm_count_now())), sum.count);
+    if (dtype == CCQ_BF16)
+        decay_sum_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(sum, access_out == 16);
+    else
+        decay_sum_kernel<float><<<grid, 256, 0, s>>>(sum, access_out == 16);
+    return op_cuda(cudaGetLastError(), "shared heads' sum launch");
+}
+
+}  // extern "C"

@@ -1,0 +1,96 @@
+// ccq_decay.cuh -- what the kernels of linear attention with a decay for each head share (ccq_ops.h).
+//
+// One pass over the tokens of a sequence, in ascending or descending order, serves the forward and all of the backward.
+// With factors g^n, a pass over (q, k, v) gives
+//   o_i = p_scale sum over j up to i of g^|i - j| (q_i . k_j) v_j + s_scale g^(..) S^T q_i,
+// S being the state that the tokens before the block have left, and
+//   forward   (q, k, v) ascending                 -> o,  S_T
+//   dq        (dout, v, k) ascending, S transposed -> dq
+//   dk        (v, dout, q) descending, dS transposed -> dk
+//   dv        (k, q, dout) descending              -> dv, dS_0
+// Descending, S is g times the gradient of the state after the token to the right (dS_T at the last), so that a block of n
+// tokens, m tokens passed, reads it with g^m where the ascending pass has g^(m + 1), and adds a token to it with
+// k_scale g^(n - m) where that one has g^(n - 1 - m).
+#pragma once
+
+#include "ccq_ops.cuh"
+
+namespace ccq {
+
+struct DecayView {
+    const void *p;
+    int64_t batch, token, head;
+    int share;  // heads of the call that read a head of this one
+};
+
+struct DecayPass {
+    DecayView q, k, v;
+    void *o;
+    int64_t o_batch, o_token, o_head;
+    int o_fp32;           // partial gradients of shared heads: fp32 in the workspace
+    const float *state_in;  // [sequences][H][d][d] or NULL
+    float *state_out;       // or NULL
+    int transposed;         // state_in, and the parts of segments, are read transposed
+    int descending;
+    float p_scale, k_scale, s_scale;
+    int kind, parts_transposed;  // whose segments' states it starts from, and how it reads them
+};
+
+struct DecayArgs {
+    DecayPass pass[3];
+    int passes;
+    int H, d;
+    int64_t T;          // of a sequence, or of all packed ones
+    int sequences;
+    const float *log_decay;
+    const void *cu;
+    int cu_bytes;
+    int *status;
+    // Segments of a sequence, in the order of a pass.  With more than one, a launch with parts_only = 1 leaves in
+    // parts[kind][sequence][H][segments][d][d] first the pass's state_in, then what each segment but the last adds to a
+    // state from zero, and the segments of the second launch start from these (state_out may be state_in for that reason).
+    int segments;
+    float *parts;
+    int parts_only;
+    int vec;            // every address and stride is a multiple of 16 bytes
+};
+
+// The tokens of a sequence: rows begin .. begin + length of batch row b.
+struct DecaySpan {
+    int64_t b, begin;
+    int64_t length;
+};
+
+__device__ __forceinline__ DecaySpan decay_span(const DecayArgs &a, int sequence) {
+    DecaySpan s;
+    if (!a.cu) {
+        s.b = sequence;
+        s.begin = 0;
+        s.length = a.T;
+        return s;
+    }
+    const int64_t from = load_index(a.cu, a.cu_bytes, sequence), to = load_index(a.cu, a.cu_bytes, sequence + 1);
+    s.b = 0;
+    s.begin = min(max(from, static_cast<int64_t>(0)), a.T);
+    const int64_t end = min(max(to, s.begin), a.T);
+    s.length = end - s.begin;
+    if ((s.begin != from || end != to) && threadIdx.x == 0) note_index(a.status);
+    return s;
+}
+
+// log2 of a head's decay g.  One below 2^-200 keeps nothing in fp32 either way (and -inf would give NaN as g^0).
+// g^n is exp2f(n log2 g): within |n log2 g| 2^-24 + 2^-22 of itself, 2e-6 where g^n is still 2^-24.
+__device__ __forceinline__ float decay_log2(const float *log_decay, int h) {
+    const float l = log_decay[h] * 1.4426950408889634f;
+    return l < -200.f ? -200.f : l;
+}
+
+// Where the state of (sequence, head, segment) lies among the parts.
+__device__ __forceinline__ int64_t decay_part(const DecayArgs &a, int kind, int sequence, int h, int segment) {
+    return (((static_cast<int64_t>(kind) * a.sequences + sequence) * a.H + h) * a.segments + segment) * a.d * a.d;
+}
+
+cudaError_t launch_decay_chunks(const DecayArgs &a, cudaStream_t s);  // bf16 on the tensor cores
+cudaError_t launch_decay_blocks(const DecayArgs &a, ccq_dtype dtype, cudaStream_t s);
+
+}  // namespace ccq

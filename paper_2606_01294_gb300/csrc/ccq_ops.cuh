@@ -59,6 +59,56 @@ inline int row_access(const void *p, int64_t stride, int elem, int64_t rows, int
     return rows > 1 ? access_bytes(static_cast<uintptr_t>(stride) * elem, most) : most;
 }
 
+// ---------------------------------------------------------------- heads of tokens
+
+// B and T, and their product, where offsets and grids stay within their types.
+inline ccq_status check_tokens(int64_t B, int64_t T) {
+    constexpr int64_t most = (1LL << 31) - 1;
+    if (B < 0 || T < 0) return op_fail(CCQ_ERR_INVALID_ARG, "bad sizes: B=%lld T=%lld", static_cast<long long>(B),
+                                       static_cast<long long>(T));
+    if (B > most || T > most || (T && B > most / T))
+        return op_fail(CCQ_ERR_UNSUPPORTED, "B=%lld T=%lld: fewer than 2^31 tokens", static_cast<long long>(B),
+                       static_cast<long long>(T));
+    return CCQ_OK;
+}
+
+// [B, T, heads, width]; `apart`: an output, none of whose elements may share an address.
+inline ccq_status check_heads(const char *name, const ccq_heads &x, ccq_dtype dtype, int64_t B, int64_t T, int64_t width,
+                              bool apart) {
+    if (x.heads < 1 || x.heads > (1 << 20))
+        return op_fail(CCQ_ERR_INVALID_ARG, "%s has %lld heads", name, static_cast<long long>(x.heads));
+    if (B * T == 0) return CCQ_OK;
+    ccq_status st = op_pointer(name, x.p, dtype_bytes(dtype));
+    if (st != CCQ_OK) return st;
+    int64_t extent[3] = {x.heads, T, B}, stride[3] = {x.head, x.token, x.batch};
+    for (int i = 0; i < 3; ++i)
+        if (extent[i] > 1 && (stride[i] < 0 || stride[i] >= (1LL << 40)))
+            return op_fail(CCQ_ERR_INVALID_ARG, "%s has a stride of %lld", name, static_cast<long long>(stride[i]));
+    if (!apart) return CCQ_OK;
+    // each dimension, in the order of their strides, steps over all that those before it reach
+    int64_t reach = width;
+    for (int left = 3; left > 0; --left) {
+        int at = -1;
+        for (int i = 0; i < 3; ++i)
+            if (extent[i] > 1 && (at < 0 || stride[i] < stride[at])) at = i;
+        if (at < 0) break;
+        if (stride[at] < reach) return op_fail(CCQ_ERR_INVALID_ARG, "%s: its elements overlap (stride %lld)", name,
+                                               static_cast<long long>(stride[at]));
+        reach += stride[at] * (extent[at] - 1);
+        extent[at] = 1;
+    }
+    return CCQ_OK;
+}
+
+// The largest access, at most `most` bytes, that a tensor of heads takes.
+inline int heads_access(const ccq_heads &x, int elem, int64_t B, int64_t T, int most) {
+    most = access_bytes(reinterpret_cast<uintptr_t>(x.p), most);
+    if (B > 1) most = access_bytes(static_cast<uintptr_t>(x.batch) * elem, most);
+    if (T > 1) most = access_bytes(static_cast<uintptr_t>(x.token) * elem, most);
+    if (x.heads > 1) most = access_bytes(static_cast<uintptr_t>(x.head) * elem, most);
+    return most;
+}
+
 inline int sm_count_now() {
     static std::atomic<int> counts[64];
     int dev = 0;

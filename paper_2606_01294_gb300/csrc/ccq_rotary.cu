@@ -1,0 +1,234 @@
+// ccq_rotary.cu -- rotation of the heads of queries and keys by their positions (ccq_ops.h).
+//
+// The pair (a, b) of a token at position p turns by p f_i radians: a' = m (a cos - b sin), b' = m (a sin + b cos).
+// Angles are kept as 64-bit fractions of a turn: F_i = f_i 2^64 / (2 pi) mod 2^64 and p F_i mod 2^64 in integers,
+// exact whatever p (F_i is within 2 units of 2^-64 turns for f_i < 1, so 2^-33 turns at p = 2^30); the top 32 bits become
+// the argument of sincospif.  (The same in 64-bit floating point, at this GPU's rate for it, would take a fifth of the
+// prefill's time.)  A CTA computes the cosines and sines of its tokens once for all heads.
+// Bound by HBM: every element read once and written once.
+#include <algorithm>
+
+#include "ccq_ops.cuh"
+
+namespace ccq {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMostAngles = 2048;  // of a CTA: 16 KB of shared memory
+
+struct RotaryTensor {
+    const void *x;
+    void *y;
+    int64_t xb, xt, xh, yb, yt, yh;
+    int heads;
+};
+
+struct RotaryArgs {
+    RotaryTensor t[2];
+    int heads;             // of both tensors
+    int64_t tokens, T;     // B * T, T
+    int width, part;
+    const void *positions;
+    int position_bytes;
+    const double *freqs;
+    float amplitude;
+    int inverse;
+    int tile;              // tokens of a CTA
+    int turned, items;     // a head's rotated items, and with those that are copied
+};
+
+// f 2^64 / (2 pi) mod 2^64, from the bits of f.
+__device__ __forceinline__ uint64_t turns_of(double f) {
+    constexpr uint64_t kInvTwoPi = 2935890503282001226ull;  // 2^64 / (2 pi)
+    const uint64_t bits = static_cast<uint64_t>(__double_as_longlong(f));
+    const int e = static_cast<int>((bits >> 52) & 0x7ff);
+    uint64_t m = bits & 0xfffffffffffffull;
+    m = e ? m | (1ull << 52) : 0;  // (a subnormal frequency turns by nothing)
+    const uint64_t hi = __umul64hi(m << 11, kInvTwoPi);  // f = (m << 11) 2^(e - 1086): F = hi 2^(e - 1022)
+    const int s = e - 1022;
+    const uint64_t F = s >= 64 || s <= -64 ? 0 : s >= 0 ? hi << s : hi >> -s;
+    return bits >> 63 ? 0 - F : F;
+}
+
+// N elements an access; PAIR: the two halves of N pairs as an access each (N = 1 interleaved: its two elements), else an
+// access holds N / 2 pairs side by side.
+template <typename T, int N, bool PAIR, bool INTER>
+__global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryArgs a) {
+    extern __shared__ float2 turn[];  // [tile][part / 2]: cos, sin
+    const int half = a.part / 2;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * a.tile;
+    const int tokens = static_cast<int>(min(static_cast<int64_t>(a.tile), a.tokens - first));
+    for (int j = threadIdx.x; j < tokens * half; j += kThreads) {
+        const int t = j / half, i = j - t * half;
+        const double f = a.freqs[i];
+        const uint64_t p = static_cast<uint64_t>(load_index(a.positions, a.position_bytes, first + t));
+        const int32_t top = static_cast<int32_t>((p * turns_of(f)) >> 32);
+        float s, c;
+        sincospif(static_cast<float>(top) * 0x1p-31f, &s, &c);
+        if (!isfinite(f)) s = c = __int_as_float(0x7fffffff);
+        turn[j] = make_float2(c * a.amplitude, (a.inverse ? -s : s) * a.amplitude);
+    }
+    __syncthreads();
+    const int per_token = a.heads * a.items;
+    constexpr int K = N * sizeof(T) <= 4 ? 4 : 2;  // items at once
+    const int total = tokens * per_token;
+    for (int j0 = threadIdx.x; j0 < total; j0 += K * kThreads) {
+        Pack<T, N> u[K], w[K];
+        T *out[K];
+        int angle[K], second[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int j = min(j0 + k * kThreads, total - 1);  // (without conditions, so that all loads stay under way)
+            const int t = j / per_token, r = j - t * per_token;
+            int h = r / a.items;
+            const int c = r - h * a.items;
+            const bool key = h >= a.t[0].heads;
+            const RotaryTensor &x = a.t[key];
+            if (key) h -= a.t[0].heads;
+            const int64_t row = first + t, b = row / a.T, at = row - b * a.T;
+            int64_t from = b * x.xb + at * x.xt + h * x.xh, to = b * x.yb + at * x.yt + h * x.yh;
+            int lo;
+            second[k] = 0;
+            if (c < a.turned) {
+                lo = PAIR && INTER ? 2 * c : c * N;
+                if (PAIR) second[k] = INTER ? 1 : half;
+                angle[k] = t * half + (PAIR ? c * N : c * N / 2);
+            } else {
+                lo = a.part + (c - a.turned) * N;
+                angle[k] = -1;
+            }
+            const T *src = static_cast<const T *>(x.x) + from + lo;
+            u[k] = load_stream<T, N>(src);
+            if (PAIR) w[k] = load_stream<T, N>(src + second[k]);
+            out[k] = static_cast<T *>(x.y) + to + lo;
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (j0 + k * kThreads >= total) continue;
+            if (angle[k] < 0) {
+                store_stream<T, N>(out[k], u[k]);
+                continue;
+            }
+            float p[N], q[N];
+            unpack(u[k], p);
+            if constexpr (PAIR) {
+                unpack(w[k], q);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float2 cs = turn[angle[k] + e];
+                    const float x = p[e] * cs.x - q[e] * cs.y, y = p[e] * cs.y + q[e] * cs.x;
+                    p[e] = x;
+                    q[e] = y;
+                }
+                pack(q, w[k]);
+                store_stream<T, N>(out[k] + second[k], w[k]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; e += 2) {
+                    const float2 cs = turn[angle[k] + e / 2];
+                    const float x = p[e] * cs.x - p[e + 1] * cs.y, y = p[e] * cs.y + p[e + 1] * cs.x;
+                    p[e] = x;
+                    p[e + 1] = y;
+                }
+            }
+            pack(p, u[k]);
+            store_stream<T, N>(out[k], u[k]);
+        }
+    }
+}
+
+template <typename T, int N, bool PAIR, bool INTER>
+cudaError_t launch(RotaryArgs &a, bool in_place, cudaStream_t s) {
+    a.turned = PAIR ? a.part / 2 / N : a.part / N;
+    a.items = a.turned + (in_place ? 0 : (a.width - a.part) / N);
+    const int half = a.part / 2;
+    // tokens of a CTA: a few accesses a thread where the tokens fill the GPU, one token (latency) where they do not
+    const int per_token = a.heads * a.items;
+    const int64_t fill = a.tokens / (8 * sm_count_now());
+    const int want = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(fill, (6 * kThreads) / per_token)));
+    a.tile = std::max(1, std::min(want, kMostAngles / half));
+    const int64_t grid = (a.tokens + a.tile - 1) / a.tile;
+    rotary_kernel<T, N, PAIR, INTER><<<static_cast<unsigned>(grid), kThreads, a.tile * half * sizeof(float2), s>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename T> cudaError_t by_access(RotaryArgs &a, int bytes, bool interleaved, bool in_place, cudaStream_t s) {
+    const int n = bytes / static_cast<int>(sizeof(T));
+    constexpr int N16 = 16 / sizeof(T), N8 = 8 / sizeof(T), N4 = 4 / sizeof(T);
+    if (interleaved) {
+        if (n >= N16) return launch<T, N16, false, true>(a, in_place, s);
+        if (n >= 2 && n >= N8) return launch<T, N8, false, true>(a, in_place, s);
+        if constexpr (N4 >= 2)
+            if (n >= N4) return launch<T, N4, false, true>(a, in_place, s);
+        return launch<T, 1, true, true>(a, in_place, s);
+    }
+    if (n >= N16) return launch<T, N16, true, false>(a, in_place, s);
+    if (n >= N8) return launch<T, N8, true, false>(a, in_place, s);
+    if constexpr (N4 >= 2)
+        if (n >= N4) return launch<T, N4, true, false>(a, in_place, s);
+    return launch<T, 1, true, false>(a, in_place, s);
+}
+
+}  // namespace
+}  // namespace ccq
+
+using namespace ccq;
+
+extern "C" {
+
+ccq_status ccq_rotary(const ccq_heads *x, const ccq_heads *y, int count, ccq_dtype dtype, int64_t B, int64_t T, int width,
+                      int part, const void *positions, int position_bytes, const double *freqs, float amplitude,
+                      int interleaved, int inverse, void *stream) {
+    if (count < 1 || count > 2) return op_fail(CCQ_ERR_INVALID_ARG, "count=%d: one or two tensors", count);
+    if (!x || !y) return op_fail(CCQ_ERR_INVALID_ARG, "x or y is NULL");
+    if (!valid_dtype(dtype)) return op_fail(CCQ_ERR_INVALID_ARG, "unknown dtype %d", static_cast<int>(dtype));
+    ccq_status st = check_tokens(B, T);
+    if (st != CCQ_OK) return st;
+    if (width < 2 || width > 65536 || part < 2 || part > width || part % 2)
+        return op_fail(CCQ_ERR_INVALID_ARG, "head width %d with %d rotated: an even part from 2 to the width (at most 65536)",
+                       width, part);
+    if (part / 2 > kMostAngles) return op_fail(CCQ_ERR_UNSUPPORTED, "at most %d rotated channels a head", 2 * kMostAngles);
+    if (position_bytes != 4 && position_bytes != 8)
+        return op_fail(CCQ_ERR_INVALID_ARG, "position_bytes=%d: 4 or 8", position_bytes);
+    if (!isfinite(amplitude)) return op_fail(CCQ_ERR_INVALID_ARG, "amplitude is not finite");
+    const int elem = dtype_bytes(dtype);
+    RotaryArgs a = {};
+    // elements of an access: what the pairs' places, the strides and the addresses of all tensors divide by
+    int bytes = access_bytes(static_cast<uintptr_t>(width) * elem);
+    bytes = access_bytes(static_cast<uintptr_t>(interleaved ? part : part / 2) * elem, bytes);
+    bytes = access_bytes(static_cast<uintptr_t>(width - part) * elem, bytes);
+    bool in_place = true;
+    int64_t heads = 0;
+    for (int i = 0; i < count; ++i) {
+        const char *names[2][2] = {{"x[0]", "y[0]"}, {"x[1]", "y[1]"}};
+        if ((st = check_heads(names[i][0], x[i], dtype, B, T, width, false)) != CCQ_OK) return st;
+        if ((st = check_heads(names[i][1], y[i], dtype, B, T, width, true)) != CCQ_OK) return st;
+        if (x[i].heads != y[i].heads) return op_fail(CCQ_ERR_INVALID_ARG, "x[%d] and y[%d] differ in heads", i, i);
+        bytes = heads_access(x[i], elem, B, T, heads_access(y[i], elem, B, T, bytes));
+        a.t[i] = {x[i].p, y[i].p, x[i].batch, x[i].token, x[i].head, y[i].batch, y[i].token, y[i].head,
+                  static_cast<int>(x[i].heads)};
+        in_place = in_place && x[i].p == y[i].p && (B <= 1 || x[i].batch == y[i].batch) &&
+                   (T <= 1 || x[i].token == y[i].token) && (x[i].heads <= 1 || x[i].head == y[i].head);
+        heads += x[i].heads;
+    }
+    if (heads * width > (1 << 24)) return op_fail(CCQ_ERR_UNSUPPORTED, "at most 2^24 channels a token");
+    if (B * T == 0) return CCQ_OK;
+    if ((st = op_pointer("positions", positions, position_bytes)) != CCQ_OK) return st;
+    if ((st = op_pointer("freqs", freqs, 8)) != CCQ_OK) return st;
+    a.heads = static_cast<int>(heads);
+    a.tokens = B * T;
+    a.T = T;
+    a.width = width;
+    a.part = part;
+    a.positions = positions;
+    a.position_bytes = position_bytes;
+    a.freqs = freqs;
+    a.amplitude = amplitude;
+    a.inverse = inverse != 0;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return op_cuda(dtype == CCQ_BF16 ? by_access<__nv_bfloat16>(a, bytes, interleaved != 0, in_place, s)
+                                     : by_access<float>(a, bytes, interleaved != 0, in_place, s),
+                   "rotary launch");
+}
+
+}  // extern "C"

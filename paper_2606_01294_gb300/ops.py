@@ -1,7 +1,8 @@
 """Python binding of include/ccq_ops.h: the operators around the CCQ token mixer.
 
-The embedding lookup and its gradient, the (gated) group norm after the mixer's read and its gradient, the
-clipped policy loss with its gradient, the token log-probabilities, and the AdamW update of many tensors.  As in
+The embedding lookup and its gradient, the rotation of queries and keys by their positions, linear attention with a
+decay for each head (prompts, their gradients, single tokens), the (gated) group norm after the mixer's read and its
+gradient, the clipped policy loss with its gradient, the token log-probabilities, and the AdamW update of many tensors.  As in
 :mod:`.ccq`, this is argument marshalling only: tensors are CUDA tensors (there is no CPU path), outputs
 and workspaces are allocated with torch on the inputs' device, and every computation runs in the
 library's kernels on the current stream.  ``stream=`` makes a call as within ``torch.cuda.stream(stream)``: what
@@ -15,6 +16,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import struct
 from dataclasses import dataclass
 from itertools import chain
@@ -67,6 +69,18 @@ def _library() -> ctypes.CDLL:
                                 _VP, _VP, _L, _VP, _Z, _VP],
             "ccq_policy_loss_workspace_size": [_L, size],
             "ccq_token_logp": [_VP, _I, _L, _VP, _I, _L, _I, _F, _VP, _VP],
+            # x, y (arrays), count, dtype | B, T, width, part | positions, bytes | freqs, amplitude, interleaved, inverse | stream
+            "ccq_rotary": [_VP, _VP, _I, _I, _L, _L, _I, _I, _VP, _I, _VP, _F, _I, _I, _VP],
+            # q, k, v, dtype | log_decay, scale, S0 | o, ST | B, T, H, d | cu, cu_bytes, num_seqs | ws | stream
+            "ccq_decay_attention": [_VP, _VP, _VP, _I, _VP, _F, _VP, _VP, _VP, _L, _L, _I, _I, _VP, _I, _L, _VP, _Z, _VP],
+            # q, k, v, dtype | log_decay, scale, S0 | dout, dST | dq, dk, dv, dS0 | B, T, H, d | cu, cu_bytes, num_seqs | ws
+            # | stream
+            "ccq_decay_attention_bwd": [_VP, _VP, _VP, _I, _VP, _F, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _L, _L, _I, _I, _VP, _I,
+                                        _L, _VP, _Z, _VP],
+            "ccq_decay_attention_workspace_size": [_L, _L, _I, _I, _L, _I, size],
+            "ccq_decay_attention_bwd_workspace_size": [_L, _L, _I, _I, _I, _I, _I, _L, _I, size],
+            # q, k, v, dtype | log_decay, scale, state, rows, slots, slot_bytes | o | B, H, d | stream
+            "ccq_decay_attention_step": [_VP, _VP, _VP, _I, _VP, _F, _VP, _L, _VP, _I, _VP, _L, _I, _I, _VP],
             "ccq_adamw_step": [_VP, _I, _I, _I, _I, ctypes.POINTER(_AdamWParams), _VP, _VP]}.items():
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, _I
@@ -206,6 +220,236 @@ def embed_grad(dout, ids, rows: int, *, scale: float = 1.0, padding_id: Optional
     _check(_library().ccq_embed_grad(dout.data_ptr(), _dtype_code(dout), ds, ids.data_ptr(), id_bytes, n, rows, width,
                                      scale, -1 if padding_id is None else padding_id, out.data_ptr(), _dtype_code(out),
                                      os, _ptr(workspace), nbytes, _stream(dev, None)))
+    return out
+
+
+# ---------------------------------------------------------------- heads of tokens
+
+
+def _heads(t, name, device=None, dtype=None, shape=None, heads=None):
+    """A ccq_heads of a [batch, tokens, heads, width] tensor (or [rows, heads, width]: one batch row of tokens, a batch
+    of one token for the step).  Any strides but the channels', which are contiguous."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and (device is None or t.device == device)):
+        _cuda(t, name, device)
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if heads is not None and (t.shape[-2] < 1 or heads % t.shape[-2]):
+        raise ValueError(f"{name} has {t.shape[-2]} heads, no divisor of {heads}")
+    strides = t.stride()
+    if strides[-1] != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name} must have contiguous channels (its last dimension)")
+    if len(strides) == 4:
+        return struct.pack("5q", t.data_ptr(), strides[0], strides[1], strides[2], t.shape[2])
+    return struct.pack("5q", t.data_ptr(), strides[0], strides[0], strides[1], t.shape[1])
+
+
+def rotary_frequencies(part: int, *, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                       original_length: int = 4096, fast: float = 32.0, slow: float = 1.0, device="cuda"):
+    """Frequencies for :func:`rotary`, fp64 [part / 2] radians a position, and the amplitude that goes with them.
+    ``base ** (-2 i / part)``, for contexts ``factor`` times as long by ``scaling``: "linear" divides positions by the
+    factor; "ntk" raises the base so that the slowest pair is stretched by it and the fastest is kept; "yarn" stretches the
+    pairs that turn fewer than ``slow`` times in the ``original_length``, keeps those that turn more than ``fast`` times,
+    blends those between, and raises the amplitude to ``0.1 log(factor) + 1``."""
+    if part < 2 or part % 2:
+        raise ValueError(f"part={part}: an even number of channels")
+    if not (base > 1 and factor >= 1 and math.isfinite(base) and math.isfinite(factor)):
+        raise ValueError(f"base={base}, factor={factor}: a base above 1 and a factor from 1 on")
+    if scaling not in ("none", "linear", "ntk", "yarn"):
+        raise ValueError(f"unknown scaling {scaling!r}: none, linear, ntk or yarn")
+    if scaling == "none" and factor != 1:
+        raise ValueError(f"factor={factor} without a scaling")
+    if scaling == "ntk" and part > 2:
+        base *= factor ** (part / (part - 2))
+    freqs = base ** (-torch.arange(0, part, 2, dtype=torch.float64) / part)
+    if scaling == "linear":
+        freqs = freqs / factor
+    if scaling != "yarn":
+        return freqs.to(device), 1.0
+    if not (original_length > 0 and fast >= slow > 0):
+        raise ValueError(f"original_length={original_length}, fast={fast}, slow={slow}: positive, and fast >= slow")
+    # the pair that turns so many times in the original length, as a fraction of an index
+    lo, hi = (part * math.log(original_length / (2 * math.pi * turns)) / (2 * math.log(base)) for turns in (fast, slow))
+    lo, hi = max(math.floor(lo), 0), min(math.ceil(hi), part - 1)
+    stretched = ((torch.arange(part // 2, dtype=torch.float64) - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
+    return (freqs * (1 - stretched) + freqs / factor * stretched).to(device), 0.1 * math.log(factor) + 1.0
+
+
+def _rotary(q, k, positions, freqs, interleaved, amplitude, inverse, out):
+    if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4):
+        raise ValueError("q must be a CUDA tensor of [batch, tokens, heads, width] or [tokens, heads, width]")
+    x = _heads(q, "q")
+    dev, shape, width = q.device, q.shape, q.shape[-1]
+    B, T = shape[:2] if q.dim() == 4 else (1, shape[0])
+    outs = []
+    y = b""
+    for i, t in enumerate((q, k)):
+        if t is None:
+            break
+        name = "qk"[i]
+        if i:
+            if not isinstance(t, torch.Tensor) or t.dim() != q.dim():
+                raise ValueError(f"k must be a CUDA tensor of {q.dim()} dimensions, as q is")
+            x += _heads(t, name, dev, q.dtype, shape[:-2] + (t.shape[-2], width))
+        o = None if out is None else out[i]
+        if o is None:
+            o = torch.empty(t.shape, dtype=t.dtype, device=dev)
+        y += _heads(o, "out", dev, t.dtype, t.shape)
+        outs.append(o)
+    _dense(freqs, "freqs", dev, torch.float64)
+    bytes_ = _ids(positions, "positions", dev)
+    if positions.shape != shape[:-2]:
+        raise ValueError(f"positions have shape {tuple(positions.shape)}, expected {tuple(shape[:-2])}")
+    _check(_library().ccq_rotary(x, y, len(outs), _dtype_code(q), B, T, width, 2 * freqs.numel(), positions.data_ptr(), bytes_,
+                                 freqs.data_ptr(), amplitude, interleaved, inverse, _stream(dev, None)))
+    return (outs[0], outs[1]) if k is not None else outs[0]
+
+
+def rotary(q, k, positions, freqs, *, interleaved: bool = False, amplitude: float = 1.0, out=None, stream=None):
+    """Rotation of queries and keys by their positions (ccq_rotary).  q [batch, tokens, heads, width] (or [tokens, heads,
+    width]) and k, with heads of its own, bf16 or fp32 with any strides (slices of one projection); k may be None.
+    positions int64 or int32 of the tokens' shape; freqs fp64 [part / 2] radians a position, as from
+    :func:`rotary_frequencies`: the first ``part`` channels of a head turn, in pairs (i, i + part / 2) or
+    (2 i, 2 i + 1) with ``interleaved``, the rest is copied.  Returns new (q, k), or q without k; ``out`` (a pair) may hold
+    their tensors, the inputs themselves among them."""
+    if stream is not None:
+        return _on_stream(stream, rotary, q, k, positions, freqs, interleaved=interleaved, amplitude=amplitude, out=out)
+    return _rotary(q, k, positions, freqs, bool(interleaved), amplitude, 0, out)
+
+
+def rotary_bwd(dq, dk, positions, freqs, *, interleaved: bool = False, amplitude: float = 1.0, out=None, stream=None):
+    """Gradients of :func:`rotary`'s q and k, of those of what it returned: the same rotation, the other way."""
+    if stream is not None:
+        return _on_stream(stream, rotary_bwd, dq, dk, positions, freqs, interleaved=interleaved, amplitude=amplitude, out=out)
+    return _rotary(dq, dk, positions, freqs, bool(interleaved), amplitude, 1, out)
+
+
+# ---------------------------------------------------------------- linear attention, a decay for each head
+
+
+def _decay_args(q, k, v, log_decay, scale, cu_seqlens):
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be a CUDA tensor of [batch, tokens, heads, d]")
+    B, T, _, d = q.shape
+    dev = _cuda(q, "q").device
+    _dense(log_decay, "log_decay", dev, torch.float32)
+    if log_decay.dim() != 1:
+        raise ValueError("log_decay must be [heads]")
+    H = log_decay.shape[0]
+    packed = [_heads(q, "q", heads=H)]
+    for name, t in (("k", k), ("v", v)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 4:
+            raise ValueError(f"{name} must be a CUDA tensor of [batch, tokens, heads, d]")
+        packed.append(_heads(t, name, dev, q.dtype, (B, T, t.shape[2], d), H))
+    cu, cu_bytes, seqs = None, 8, B
+    if cu_seqlens is not None:
+        cu_bytes = _ids(cu_seqlens, "cu_seqlens", dev)
+        if B != 1 or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
+            raise ValueError("cu_seqlens must be [sequences + 1] offsets into a batch of one row of packed tokens")
+        cu, seqs = cu_seqlens.data_ptr(), cu_seqlens.shape[0] - 1
+    return dev, B, T, H, d, packed, (cu, cu_bytes, seqs), d ** -0.5 if scale is None else scale
+
+
+def decay_attention(q, k, v, log_decay, *, scale: Optional[float] = None, state=None, cu_seqlens=None, out=None,
+                    final_state=None, return_state: bool = True, workspace=None, stream=None):
+    """Linear attention with a constant decay for each head (ccq_decay_attention): with S = exp(log_decay) S + k v^T token by
+    token, o = scale S^T q.  q, k, v [B, T, heads, d], d 64 or 128, bf16 or fp32 with any strides; fewer heads
+    than log_decay's (fp32 [H], <= 0, a constant of the layer) are shared by consecutive ones.  ``scale``: d ** -0.5.
+    ``cu_seqlens``: CUDA offsets [N + 1] of sequences packed in one row (tokens of none are left as they are in ``out``).
+    ``state`` [B or N, H, d, d] fp32: the states before the first tokens.  Returns (o [B, T, H, d], the states after the
+    last tokens; None without ``return_state``); ``final_state`` may be ``state``."""
+    if stream is not None:
+        return _on_stream(stream, decay_attention, q, k, v, log_decay, scale=scale, state=state, cu_seqlens=cu_seqlens, out=out,
+                          final_state=final_state, return_state=return_state, workspace=workspace)
+    dev, B, T, H, d, (hq, hk, hv), cu, scale = _decay_args(q, k, v, log_decay, scale, cu_seqlens)
+    shape = (cu[2], H, d, d)
+    if state is not None:
+        _dense(state, "state", dev, torch.float32, shape)
+    if final_state is not None:
+        _dense(final_state, "final_state", dev, torch.float32, shape)
+    elif return_state:
+        final_state = torch.empty(shape, dtype=torch.float32, device=dev)
+    if out is None:
+        out = torch.empty((B, T, H, d), dtype=q.dtype, device=dev)
+    raw = _stream(dev, None)  # (before the workspace's size is asked for: a function of the current device's SMs)
+    code = _dtype_code(q)
+    workspace, nbytes = _workspace(workspace, _size("ccq_decay_attention_workspace_size", dev.index, B, T, H, d, cu[2], code),
+                                   dev)
+    _check(_library().ccq_decay_attention(hq, hk, hv, code, log_decay.data_ptr(), scale, _ptr(state),
+                                          _heads(out, "out", dev, q.dtype, (B, T, H, d)), _ptr(final_state), B, T, H, d, *cu,
+                                          _ptr(workspace), nbytes, raw))
+    return out, final_state
+
+
+def decay_attention_bwd(q, k, v, log_decay, dout, *, scale: Optional[float] = None, state=None, dfinal_state=None,
+                        cu_seqlens=None, out: Optional[dict] = None, workspace=None, stream=None):
+    """Gradients of :func:`decay_attention` (ccq_decay_attention_bwd): a dict of dq, dk, dv (with q's, k's and v's heads) and,
+    with ``state`` or ``dfinal_state`` (the gradient of the states that the forward returned), dstate.  Only the
+    forward's inputs are needed.  ``out`` may hold preallocated tensors under those names."""
+    if stream is not None:
+        return _on_stream(stream, decay_attention_bwd, q, k, v, log_decay, dout, scale=scale, state=state,
+                          dfinal_state=dfinal_state, cu_seqlens=cu_seqlens, out=out, workspace=workspace)
+    dev, B, T, H, d, (hq, hk, hv), cu, scale = _decay_args(q, k, v, log_decay, scale, cu_seqlens)
+    shape = (cu[2], H, d, d)
+    ho = _heads(dout, "dout", dev, q.dtype, (B, T, H, d))
+    g = dict(out or {})
+    if state is not None:
+        _dense(state, "state", dev, torch.float32, shape)
+    if dfinal_state is not None:
+        _dense(dfinal_state, "dfinal_state", dev, torch.float32, shape)
+    if g.get("dstate") is not None:
+        _dense(g["dstate"], "dstate", dev, torch.float32, shape)
+    elif state is not None or dfinal_state is not None:
+        g["dstate"] = torch.empty(shape, dtype=torch.float32, device=dev)
+    heads = []
+    for name, like in (("dq", q), ("dk", k), ("dv", v)):
+        if g.get(name) is None:
+            g[name] = torch.empty(like.shape, dtype=like.dtype, device=dev)
+        heads.append(_heads(g[name], name, dev, like.dtype, like.shape))
+    raw = _stream(dev, None)
+    code = _dtype_code(q)
+    workspace, nbytes = _workspace(workspace, _size("ccq_decay_attention_bwd_workspace_size", dev.index, B, T, H, q.shape[2],
+                                                    k.shape[2], v.shape[2], d, cu[2], code), dev)
+    _check(_library().ccq_decay_attention_bwd(hq, hk, hv, code, log_decay.data_ptr(), scale, _ptr(state), ho,
+                                              _ptr(dfinal_state), *heads, _ptr(g.get("dstate")), B, T, H, d, *cu,
+                                              _ptr(workspace), nbytes, raw))
+    return g
+
+
+def decay_attention_step(q, k, v, log_decay, state, *, scale: Optional[float] = None, slots=None, out=None, stream=None):
+    """One token of every sequence (ccq_decay_attention_step): q, k, v [B, heads, d] as for :func:`decay_attention`; ``state``
+    fp32 [B, H, d, d], or [rows, H, d, d] with ``slots`` (int32 or int64 [B]: the row of each; negative: none, a zero
+    output), is updated in place.  Returns o [B, H, d].  A slot outside the rows, or that an earlier row of the
+    batch has, gives a zero output, changes nothing and leaves CCQ_ERR_INDEX for :func:`ccq.device_status`."""
+    if stream is not None:
+        return _on_stream(stream, decay_attention_step, q, k, v, log_decay, state, scale=scale, slots=slots, out=out)
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a CUDA tensor of [batch, heads, d]")
+    B, _, d = q.shape
+    dev = _cuda(q, "q").device
+    _dense(log_decay, "log_decay", dev, torch.float32)
+    if log_decay.dim() != 1:
+        raise ValueError("log_decay must be [heads]")
+    H = log_decay.shape[0]
+    packed = [_heads(q, "q", heads=H)]
+    for name, t in (("k", k), ("v", v)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 3:
+            raise ValueError(f"{name} must be a CUDA tensor of [batch, heads, d]")
+        packed.append(_heads(t, name, dev, q.dtype, (B, t.shape[1], d), H))
+    _dense(state, "state", dev, torch.float32)
+    if state.dim() != 4 or state.shape[1:] != (H, d, d) or (slots is None and state.shape[0] != B):
+        raise ValueError(f"state has shape {tuple(state.shape)}, expected {(B if slots is None else 'rows', H, d, d)}")
+    slot_bytes = 4
+    if slots is not None:
+        slot_bytes = _ids(slots, "slots", dev)
+        if slots.shape != (B,):
+            raise ValueError(f"slots have shape {tuple(slots.shape)}, expected {(B,)}")
+    if out is None:
+        out = torch.empty((B, H, d), dtype=q.dtype, device=dev)
+    _check(_library().ccq_decay_attention_step(*packed, _dtype_code(q), log_decay.data_ptr(), d ** -0.5 if scale is None else scale,
+                                               state.data_ptr(), state.shape[0], _ptr(slots), slot_bytes,
+                                               _heads(out, "out", dev, q.dtype, (B, H, d)), B, H, d, _stream(dev, None)))
     return out
 
 
