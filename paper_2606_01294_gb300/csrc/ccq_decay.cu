@@ -22,6 +22,7 @@ constexpr int kPad = 4;
 template <int D> struct BlockShared {
     float q[kC][D + kPad], k[kC][D + kPad], v[kC][kN + kPad], p[kC][kN + kPad], s[D][kN + kPad];
     float power[kC + 1];  // g^n
+    float2 keep[2];       // g^32 and g^n of the ragged block, as two floats
 };
 
 // Rows begin .. begin + n of a head (of `width` channels from column c0) to shared memory, zeros up to kC.
@@ -75,8 +76,10 @@ template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_b
     const DecaySpan span = decay_span(a, sequence);
     const int64_t blocks = (span.length + kC - 1) / kC, per = (blocks + a.segments - 1) / a.segments;
     const int64_t first = min(per * segment, blocks), last = min(first + per, blocks);
-    const float l2 = decay_log2(a.log_decay, h);
-    if (tid <= kC) sh.power[tid] = exp2f(l2 * tid);
+    const DecayLog l2 = decay_log2(a.log_decay, h);
+    const int ragged = static_cast<int>(span.length - (blocks - 1) * kC);  // tokens of the sequence's last block
+    if (tid <= kC) sh.power[tid] = decay_power(l2, tid);
+    if (tid >= kThreads - 2) sh.keep[tid - (kThreads - 2)] = decay_keep(l2, tid == kThreads - 2 ? kC : ragged);
 
     // tokens of block j in the pass's order: the ragged block is the sequence's last
     auto block_begin = [&](int64_t j) { return (down ? blocks - 1 - j : j) * kC; };
@@ -120,7 +123,7 @@ template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_b
                 int64_t n = 0;
                 if (g > 0 && hi > lo) n = (hi - lo) * kC - ((down ? lo == 0 : hi == blocks) ? blocks * kC - span.length : 0);
                 add(a.parts + decay_part(a, ps.kind, sequence, h, g), ps.parts_transposed,
-                    g == 0 ? 0.f : exp2f(l2 * static_cast<float>(n)));
+                    g == 0 ? 0.f : decay_power(l2, static_cast<int>(n)));
             }
         }
     }
@@ -224,11 +227,11 @@ template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_b
             }
         }
         // S = g^n S + K^T diag(k_scale g^..) V, rows R ty .., columns 4 tx ..
-        const float keep = sh.power[n];
+        const float2 keep = sh.keep[n < kC];
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) S[r][c] *= keep;
+            for (int c = 0; c < 4; ++c) S[r][c] = fmaf(S[r][c], keep.x, S[r][c] * keep.y);
         for (int jj = 0; jj < n; ++jj) {
             const float u = sh.power[down ? jj + 1 : n - 1 - jj] * ps.k_scale;
             float4 vv = *reinterpret_cast<const float4 *>(&sh.v[jj][4 * tx]);
@@ -318,17 +321,34 @@ template <typename T> __global__ void __launch_bounds__(256) decay_sum_kernel(co
 
 // ---------------------------------------------------------------- the calls
 
-// Segments of each sequence: as many as fill the GPU with one CTA an SM (tensor cores) or a few (fp32), of at least
-// `least` tokens each.  Forming the states before them reads two of a pass's four operands once more.
-int segments_for(int64_t sequences, int64_t T, int64_t ctas, int64_t slots, int64_t least) {
-    if (sequences < 1 || ctas < 1) return 1;
-    const int64_t fill = slots / ctas, most = T / sequences / least;
-    return static_cast<int>(std::max<int64_t>(1, std::min(fill, most)));
-}
+// Segments of each sequence, by a count of what a launch takes: rounds of resident CTAs times the blocks of a CTA, for the
+// passes and, with more than one segment, for the states before them (`kinds`, all segments but the last).
+struct Cost {
+    int block;           // tokens
+    double main, parts;  // microseconds a block
+    double launch;
+    int resident;        // CTAs the GPU holds
+};
 
 int plan_segments(int64_t B, int64_t T, int H, int d, int64_t num_seqs, ccq_dtype dtype, int passes) {
-    const int64_t total = B * T;
-    return segments_for(num_seqs, total, num_seqs * H * passes * (d / kN), 4 * sm_count_now(), 4 * kC);
+    if (num_seqs < 1 || B * T < 1) return 1;
+    const bool cores = dtype == CCQ_BF16;
+    const Cost c = cores ? Cost{128, 2.5, 1.6, 5.0, sm_count_now()}
+                         : Cost{kC, d == 128 ? 6.0 : 3.5, d == 128 ? 3.0 : 2.0, 5.0, 3 * sm_count_now()};
+    const int64_t ctas = num_seqs * H * (cores ? 1 : d / kN), blocks = (B * T / num_seqs + c.block - 1) / c.block;
+    const int64_t kinds = passes > 1 ? 2 : 1;
+    auto rounds = [&](int64_t n) { return static_cast<double>((n + c.resident - 1) / c.resident); };
+    int best = 1;
+    double least = rounds(ctas * passes) * static_cast<double>(blocks) * c.main;
+    for (int s = 2; s <= 64 && s <= blocks / 2; ++s) {
+        const double per = static_cast<double>((blocks + s - 1) / s);
+        const double t = rounds(ctas * passes * s) * per * c.main + rounds(ctas * kinds * (s - 1)) * per * c.parts + c.launch;
+        if (t < least) {
+            least = t;
+            best = s;
+        }
+    }
+    return best;
 }
 
 size_t parts_bytes(int64_t num_seqs, int H, int d, int segments, int kinds) {
@@ -375,21 +395,26 @@ ccq_status check_state(const char *name, const float *p) {
     return p ? op_pointer(name, p, 16) : CCQ_OK;
 }
 
+// (one head's values as all heads, by a stride of 0, are one shared head)
 DecayView view_of(const ccq_heads &x, int H) {
-    return {x.p, x.batch, x.token, x.head, static_cast<int>(H / x.heads)};
+    return {x.p, x.batch, x.token, x.head, static_cast<int>(x.head == 0 ? H : H / x.heads)};
 }
 
-ccq_status run_passes(DecayArgs &a, ccq_dtype dtype, unsigned parts_mask, cudaStream_t s) {
+// Whether a tensor can be loaded in tiles: no dimension of more than one steps by nothing.
+bool steps(const ccq_heads &x, int64_t B, int64_t T) { return (B <= 1 || x.batch > 0) && (T <= 1 || x.token > 0); }
+
+ccq_status run_passes(DecayArgs &a, ccq_dtype dtype, bool cores, int64_t B, unsigned parts_mask, cudaStream_t s) {
     cudaError_t e = cudaSuccess;
+    auto run = [&](const DecayArgs &x) { return cores ? launch_decay_chunks(x, B, s) : launch_decay_blocks(x, dtype, s); };
     if (a.segments > 1) {
         DecayArgs p = a;
         p.parts_only = 1;
         p.passes = 0;
         for (int i = 0; i < a.passes; ++i)
             if (parts_mask >> i & 1) p.pass[p.passes++] = a.pass[i];
-        e = launch_decay_blocks(p, dtype, s);
+        e = run(p);
     }
-    if (e == cudaSuccess) e = launch_decay_blocks(a, dtype, s);
+    if (e == cudaSuccess) e = run(a);
     return op_cuda(e, "decayed attention launch");
 }
 
@@ -468,7 +493,8 @@ ccq_status ccq_decay_attention(const ccq_heads *q, const ccq_heads *k, const ccq
     a.cu_bytes = cu_bytes;
     a.parts = static_cast<float *>(workspace);
     a.vec = access == 16;
-    return run_passes(a, dtype, 1u, static_cast<cudaStream_t>(stream));
+    const bool cores = dtype == CCQ_BF16 && a.vec && B * T > 0 && steps(*q, B, T) && steps(*k, B, T) && steps(*v, B, T);
+    return run_passes(a, dtype, cores, B, 1u, static_cast<cudaStream_t>(stream));
 }
 
 ccq_status ccq_decay_attention_bwd_workspace_size(int64_t B, int64_t T, int H, int q_heads, int k_heads, int v_heads, int d,
@@ -583,7 +609,9 @@ ccq_status ccq_decay_attention_bwd(const ccq_heads *q, const ccq_heads *k, const
     a.parts = static_cast<float *>(workspace);
     a.vec = access == 16 && access_out == 16;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if ((st = run_passes(a, dtype, 5u, s)) != CCQ_OK || !sum.count || !(B * T)) return st;
+    bool cores = dtype == CCQ_BF16 && a.vec && B * T > 0;
+    for (int i = 0; i < 4; ++i) cores = cores && steps(*in[i], B, T);
+    if ((st = run_passes(a, dtype, cores, B, 5u, s)) != CCQ_OK || !sum.count || !(B * T)) return st;
     sum.H = H;
     sum.d = d;
     sum.rows = B * T;

@@ -78,11 +78,32 @@ __device__ __forceinline__ DecaySpan decay_span(const DecayArgs &a, int sequence
     return s;
 }
 
-// log2 of a head's decay g.  One below 2^-200 keeps nothing in fp32 either way (and -inf would give NaN as g^0).
-// g^n is exp2f(n log2 g): within |n log2 g| 2^-24 + 2^-22 of itself, 2e-6 where g^n is still 2^-24.
-__device__ __forceinline__ float decay_log2(const float *log_decay, int h) {
-    const float l = log_decay[h] * 1.4426950408889634f;
-    return l < -200.f ? -200.f : l;
+// The logarithm of a head's decay g, and log2 g as two floats.  A decay below 2^-200 keeps nothing in fp32 either way (and
+// -inf would give NaN as g^0).
+struct DecayLog {
+    float natural, hi, lo;
+};
+__device__ __forceinline__ DecayLog decay_log2(const float *log_decay, int h) {
+    constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.9259629911266175e-8f;
+    DecayLog l;
+    l.natural = log_decay[h] < -138.f ? -138.f : log_decay[h];
+    l.hi = l.natural * kLog2e;
+    l.lo = fmaf(l.natural, kLog2e, -l.hi) + l.natural * kLog2eLow;
+    return l;
+}
+
+// g^n within 2^-22 of itself: the exponent's rounding is put back as a factor.
+__device__ __forceinline__ float decay_power(const DecayLog &l, int n) {
+    const float x = l.hi * n, rest = fmaf(l.hi, static_cast<float>(n), -x) + l.lo * n;
+    const float p = exp2f(x);
+    return fmaf(p, rest * 0.6931471805599453f, p);
+}
+
+// g^n as two floats: the factor of the state at every block, whose error would add up over a sequence.
+__device__ __forceinline__ float2 decay_keep(const DecayLog &l, int n) {
+    const double p = exp(static_cast<double>(l.natural) * n);
+    const float hi = static_cast<float>(p);
+    return make_float2(hi, static_cast<float>(p - hi));
 }
 
 // Where the state of (sequence, head, segment) lies among the parts.
@@ -90,7 +111,7 @@ __device__ __forceinline__ int64_t decay_part(const DecayArgs &a, int kind, int 
     return (((static_cast<int64_t>(kind) * a.sequences + sequence) * a.H + h) * a.segments + segment) * a.d * a.d;
 }
 
-cudaError_t launch_decay_chunks(const DecayArgs &a, cudaStream_t s);  // bf16 on the tensor cores
+cudaError_t launch_decay_chunks(const DecayArgs &a, int64_t B, cudaStream_t s);  // bf16 on the tensor cores
 cudaError_t launch_decay_blocks(const DecayArgs &a, ccq_dtype dtype, cudaStream_t s);
 
 }  // namespace ccq

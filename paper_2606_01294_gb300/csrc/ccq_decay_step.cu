@@ -61,7 +61,7 @@ template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_s
         for (int i = tid; i < b; i += kThreads) taken |= load_index(a.slots, a.slot_bytes, i) == row;
     if (__syncthreads_or(taken)) live = false;
     if (!live && a.slots && row >= 0 && tid == 0) note_index(a.status);
-    const float g = exp2f(decay_log2(a.log_decay, h));
+    const float g = decay_power(decay_log2(a.log_decay, h), 1);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     if (live) {
         const float4 vv = *reinterpret_cast<const float4 *>(&vs[4 * tx]);
