@@ -21,6 +21,9 @@ struct DecayView {
     const void *p;
     int64_t batch, token, head;
     int share;  // heads of the call that read a head of this one
+    bool operator==(const DecayView &x) const {
+        return p == x.p && batch == x.batch && token == x.token && head == x.head && share == x.share;
+    }
 };
 
 struct DecayPass {
