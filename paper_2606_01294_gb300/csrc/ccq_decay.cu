@@ -5,6 +5,7 @@
 // the state, in fp32 on the CUDA cores:
 //   P = Q K^T (32 x 32), masked and times g^|i - j|;  O = P V + diag(g^..) Q S;  S = g^n S + K^T diag(g^..) V.
 // 32 tokens cost 32 d (16 + 2 * 32) + 16 * 32 * 32 multiply-adds a CTA, of which P, formed again by each slice, is a fifth.
+// Aligned fp32 operands of the next block are copied while this one is computed.
 // Bound by the CUDA cores' fp32 rate and by the latency of a block's steps where the CTAs do not fill the GPU.
 #include <algorithm>
 #include <cmath>
@@ -19,8 +20,11 @@ constexpr int kN = 32;        // columns of a CTA
 constexpr int kThreads = 128;
 constexpr int kPad = 4;
 
-template <int D> struct BlockShared {
-    float q[kC][D + kPad], k[kC][D + kPad], v[kC][kN + kPad], p[kC][kN + kPad], s[D][kN + kPad];
+template <int D, int BUFFERS> struct BlockShared {
+    struct {
+        float q[kC][D + kPad], k[kC][D + kPad], v[kC][kN + kPad];
+    } in[BUFFERS];
+    float p[kC][kN + kPad], s[D][kN + kPad];
     float power[kC + 1];  // g^n
     float2 keep[2];       // g^32 and g^n of the ragged block, as two floats
 };
@@ -54,9 +58,26 @@ __device__ __forceinline__ void load_rows(float (*dst)[STRIDE], const DecayView 
     }
 }
 
-template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a) {
+// The same by asynchronous copies (aligned fp32).
+template <int W, int STRIDE>
+__device__ __forceinline__ void copy_rows(float (*dst)[STRIDE], const DecayView &x, int64_t b, int64_t begin, int n, int h,
+                                          int c0) {
+    const float *src = static_cast<const float *>(x.p) + b * x.batch + begin * x.token + (h / x.share) * x.head + c0;
+    for (int j = threadIdx.x; j < kC * W / 4; j += kThreads) {
+        const int r = j / (W / 4), c = (j % (W / 4)) * 4;
+        if (r < n)
+            copy_async<16>(&dst[r][c], src + r * x.token + c);
+        else
+            *reinterpret_cast<float4 *>(&dst[r][c]) = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+}
+
+// ASYNC: fp32 operands on 16-byte boundaries, copied a block ahead.
+template <typename T, int D, bool ASYNC>
+__global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a) {
+    constexpr int kBuffers = ASYNC ? 2 : 1;
     extern __shared__ float4 shared_raw[];
-    BlockShared<D> &sh = *reinterpret_cast<BlockShared<D> *>(shared_raw);
+    BlockShared<D, kBuffers> &sh = *reinterpret_cast<BlockShared<D, kBuffers> *>(shared_raw);
     constexpr int kSlices = D / kN;
     constexpr int R = D / 16;  // state rows of a thread: R x 4 of its slice
     int64_t x = blockIdx.x;
@@ -128,14 +149,37 @@ template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_b
         }
     }
 
+    auto tokens_of = [&](int64_t begin) { return static_cast<int>(min(static_cast<int64_t>(kC), span.length - begin)); };
+    auto copy = [&](int64_t j) {
+        if constexpr (ASYNC) {
+            const int64_t begin = block_begin(j);
+            const int n = tokens_of(begin);
+            auto &to = sh.in[j & 1];
+            copy_rows<D>(to.k, ps.k, span.b, span.begin + begin, n, h, 0);
+            copy_rows<kN>(to.v, ps.v, span.b, span.begin + begin, n, h, c0);
+            if (!a.parts_only) copy_rows<D>(to.q, ps.q, span.b, span.begin + begin, n, h, 0);
+            copy_commit();
+        }
+    };
+    if (first < last) copy(first);
     for (int64_t j = first; j < last; ++j) {
         const int64_t begin = block_begin(j);
-        const int n = static_cast<int>(min(static_cast<int64_t>(kC), span.length - begin));
+        const int n = tokens_of(begin);
+        auto &in = sh.in[ASYNC ? j & 1 : 0];
         __syncthreads();  // the last block's readers
-        load_rows<T, D>(sh.k, ps.k, span.b, span.begin + begin, n, h, 0, a.vec);
-        load_rows<T, kN>(sh.v, ps.v, span.b, span.begin + begin, n, h, c0, a.vec);
+        if constexpr (ASYNC) {
+            if (j + 1 < last) {
+                copy(j + 1);
+                copy_wait<1>();
+            } else {
+                copy_wait<0>();
+            }
+        } else {
+            load_rows<T, D>(in.k, ps.k, span.b, span.begin + begin, n, h, 0, a.vec);
+            load_rows<T, kN>(in.v, ps.v, span.b, span.begin + begin, n, h, c0, a.vec);
+            if (!a.parts_only) load_rows<T, D>(in.q, ps.q, span.b, span.begin + begin, n, h, 0, a.vec);
+        }
         if (!a.parts_only) {
-            load_rows<T, D>(sh.q, ps.q, span.b, span.begin + begin, n, h, 0, a.vec);
 #pragma unroll
             for (int r = 0; r < R; ++r)
                 *reinterpret_cast<float4 *>(&sh.s[R * ty + r][4 * tx]) = make_float4(S[r][0], S[r][1], S[r][2], S[r][3]);
@@ -147,9 +191,9 @@ template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_b
             for (int e = 0; e < D; e += 4) {
                 float4 qv[2], kv[4];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) qv[r] = *reinterpret_cast<const float4 *>(&sh.q[2 * ty + r][e]);
+                for (int r = 0; r < 2; ++r) qv[r] = *reinterpret_cast<const float4 *>(&in.q[2 * ty + r][e]);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) kv[c] = *reinterpret_cast<const float4 *>(&sh.k[tx + 8 * c][e]);
+                for (int c = 0; c < 4; ++c) kv[c] = *reinterpret_cast<const float4 *>(&in.k[tx + 8 * c][e]);
 #pragma unroll
                 for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -170,7 +214,7 @@ template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_b
             for (int e = 0; e < D; e += 4) {
                 float4 qv[2];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) qv[r] = *reinterpret_cast<const float4 *>(&sh.q[2 * ty + r][e]);
+                for (int r = 0; r < 2; ++r) qv[r] = *reinterpret_cast<const float4 *>(&in.q[2 * ty + r][e]);
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
                     const float4 sv = *reinterpret_cast<const float4 *>(&sh.s[e + f][4 * tx]);
@@ -194,7 +238,7 @@ template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_b
             // (a value that is not finite does not reach the rows before it: the sums end at the row)
             const int from = down ? 2 * ty : 0, to = down ? n : min(n, 2 * ty + 2);
             for (int jj = from; jj < to; ++jj) {
-                const float4 vv = *reinterpret_cast<const float4 *>(&sh.v[jj][4 * tx]);
+                const float4 vv = *reinterpret_cast<const float4 *>(&in.v[jj][4 * tx]);
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     if (down ? jj < 2 * ty + r : jj > 2 * ty + r) continue;
@@ -234,14 +278,14 @@ template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_b
             for (int c = 0; c < 4; ++c) S[r][c] = fmaf(S[r][c], keep.x, S[r][c] * keep.y);
         for (int jj = 0; jj < n; ++jj) {
             const float u = sh.power[down ? jj + 1 : n - 1 - jj] * ps.k_scale;
-            float4 vv = *reinterpret_cast<const float4 *>(&sh.v[jj][4 * tx]);
+            float4 vv = *reinterpret_cast<const float4 *>(&in.v[jj][4 * tx]);
             vv.x *= u;
             vv.y *= u;
             vv.z *= u;
             vv.w *= u;
 #pragma unroll
             for (int r = 0; r < R; r += 4) {
-                const float4 kv = *reinterpret_cast<const float4 *>(&sh.k[jj][R * ty + r]);
+                const float4 kv = *reinterpret_cast<const float4 *>(&in.k[jj][R * ty + r]);
                 const float kk[4] = {kv.x, kv.y, kv.z, kv.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -265,13 +309,13 @@ template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_b
     }
 }
 
-template <typename T, int D> cudaError_t launch_blocks(const DecayArgs &a, cudaStream_t s) {
-    constexpr int kBytes = sizeof(BlockShared<D>);
-    cudaError_t e = allow_shared<decay_block_kernel<T, D>>(kBytes);
+template <typename T, int D, bool ASYNC> cudaError_t launch_blocks(const DecayArgs &a, cudaStream_t s) {
+    constexpr int kBytes = sizeof(BlockShared<D, ASYNC ? 2 : 1>);
+    cudaError_t e = allow_shared<decay_block_kernel<T, D, ASYNC>>(kBytes);
     if (e != cudaSuccess) return e;
     const int64_t grid = static_cast<int64_t>(D / kN) * (a.parts_only ? a.segments - 1 : a.segments) * a.H * a.sequences * a.passes;
     if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-    decay_block_kernel<T, D><<<static_cast<unsigned>(grid), kThreads, kBytes, s>>>(a);
+    decay_block_kernel<T, D, ASYNC><<<static_cast<unsigned>(grid), kThreads, kBytes, s>>>(a);
     return cudaGetLastError();
 }
 
@@ -333,7 +377,7 @@ struct Cost {
 int plan_segments(int64_t B, int64_t T, int H, int d, int64_t num_seqs, ccq_dtype dtype, int passes) {
     if (num_seqs < 1 || B * T < 1) return 1;
     const bool cores = dtype == CCQ_BF16;
-    const Cost c = cores ? Cost{128, 2.5, 1.6, 5.0, sm_count_now()}
+    const Cost c = cores ? Cost{128, d == 128 ? 3.45 : 2.4, d == 128 ? 4.0 : 2.8, 6.0, sm_count_now()}
                          : Cost{kC, d == 128 ? 6.0 : 3.5, d == 128 ? 3.0 : 2.0, 5.0, 3 * sm_count_now()};
     const int64_t ctas = num_seqs * H * (cores ? 1 : d / kN), blocks = (B * T / num_seqs + c.block - 1) / c.block;
     const int64_t kinds = passes > 1 ? 2 : 1;
@@ -422,8 +466,9 @@ ccq_status run_passes(DecayArgs &a, ccq_dtype dtype, bool cores, int64_t B, unsi
 
 cudaError_t launch_decay_blocks(const DecayArgs &a, ccq_dtype dtype, cudaStream_t s) {
     if (dtype == CCQ_BF16)
-        return a.d == 128 ? launch_blocks<__nv_bfloat16, 128>(a, s) : launch_blocks<__nv_bfloat16, 64>(a, s);
-    return a.d == 128 ? launch_blocks<float, 128>(a, s) : launch_blocks<float, 64>(a, s);
+        return a.d == 128 ? launch_blocks<__nv_bfloat16, 128, false>(a, s) : launch_blocks<__nv_bfloat16, 64, false>(a, s);
+    if (!a.vec) return a.d == 128 ? launch_blocks<float, 128, false>(a, s) : launch_blocks<float, 64, false>(a, s);
+    return a.d == 128 ? launch_blocks<float, 128, true>(a, s) : launch_blocks<float, 64, true>(a, s);
 }
 
 }  // namespace ccq

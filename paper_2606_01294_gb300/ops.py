@@ -226,6 +226,9 @@ def embed_grad(dout, ids, rows: int, *, scale: float = 1.0, padding_id: Optional
 # ---------------------------------------------------------------- heads of tokens
 
 
+_FIVE = struct.Struct("5q").pack
+
+
 def _heads(t, name, device=None, dtype=None, shape=None, heads=None):
     """A ccq_heads of a [batch, tokens, heads, width] tensor (or [rows, heads, width]: one batch row of tokens, a batch
     of one token for the step).  Any strides but the channels', which are contiguous."""
@@ -241,8 +244,8 @@ def _heads(t, name, device=None, dtype=None, shape=None, heads=None):
     if strides[-1] != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name} must have contiguous channels (its last dimension)")
     if len(strides) == 4:
-        return struct.pack("5q", t.data_ptr(), strides[0], strides[1], strides[2], t.shape[2])
-    return struct.pack("5q", t.data_ptr(), strides[0], strides[0], strides[1], t.shape[1])
+        return _FIVE(t.data_ptr(), strides[0], strides[1], strides[2], t.shape[2])
+    return _FIVE(t.data_ptr(), strides[0], strides[0], strides[1], t.shape[1])
 
 
 def rotary_frequencies(part: int, *, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -294,8 +297,11 @@ def _rotary(q, k, positions, freqs, interleaved, amplitude, inverse, out):
             x += _heads(t, name, dev, q.dtype, shape[:-2] + (t.shape[-2], width))
         o = None if out is None else out[i]
         if o is None:
-            o = torch.empty(t.shape, dtype=t.dtype, device=dev)
-        y += _heads(o, "out", dev, t.dtype, t.shape)
+            n = t.shape[-2]
+            o = t.new_empty(t.shape)
+            y += _FIVE(o.data_ptr(), T * n * width, n * width, width, n)
+        else:
+            y += _heads(o, "out", dev, t.dtype, t.shape)
         outs.append(o)
     _dense(freqs, "freqs", dev, torch.float64)
     bytes_ = _ids(positions, "positions", dev)
@@ -372,12 +378,15 @@ def decay_attention(q, k, v, log_decay, *, scale: Optional[float] = None, state=
         final_state = torch.empty(shape, dtype=torch.float32, device=dev)
     if out is None:
         out = torch.empty((B, T, H, d), dtype=q.dtype, device=dev)
+        ho = _FIVE(out.data_ptr(), T * H * d, H * d, d, H)
+    else:
+        ho = _heads(out, "out", dev, q.dtype, (B, T, H, d))
     raw = _stream(dev, None)  # (before the workspace's size is asked for: a function of the current device's SMs)
     code = _dtype_code(q)
     workspace, nbytes = _workspace(workspace, _size("ccq_decay_attention_workspace_size", dev.index, B, T, H, d, cu[2], code),
                                    dev)
     _check(_library().ccq_decay_attention(hq, hk, hv, code, log_decay.data_ptr(), scale, _ptr(state),
-                                          _heads(out, "out", dev, q.dtype, (B, T, H, d)), _ptr(final_state), B, T, H, d, *cu,
+                                          ho, _ptr(final_state), B, T, H, d, *cu,
                                           _ptr(workspace), nbytes, raw))
     return out, final_state
 
@@ -405,8 +414,11 @@ def decay_attention_bwd(q, k, v, log_decay, dout, *, scale: Optional[float] = No
     heads = []
     for name, like in (("dq", q), ("dk", k), ("dv", v)):
         if g.get(name) is None:
-            g[name] = torch.empty(like.shape, dtype=like.dtype, device=dev)
-        heads.append(_heads(g[name], name, dev, like.dtype, like.shape))
+            n = like.shape[2]
+            g[name] = like.new_empty(like.shape)
+            heads.append(_FIVE(g[name].data_ptr(), T * n * d, n * d, d, n))
+        else:
+            heads.append(_heads(g[name], name, dev, like.dtype, like.shape))
     raw = _stream(dev, None)
     code = _dtype_code(q)
     workspace, nbytes = _workspace(workspace, _size("ccq_decay_attention_bwd_workspace_size", dev.index, B, T, H, q.shape[2],
@@ -447,9 +459,12 @@ def decay_attention_step(q, k, v, log_decay, state, *, scale: Optional[float] = 
             raise ValueError(f"slots have shape {tuple(slots.shape)}, expected {(B,)}")
     if out is None:
         out = torch.empty((B, H, d), dtype=q.dtype, device=dev)
+        ho = _FIVE(out.data_ptr(), H * d, d, d, H)
+    else:
+        ho = _heads(out, "out", dev, q.dtype, (B, H, d))
     _check(_library().ccq_decay_attention_step(*packed, _dtype_code(q), log_decay.data_ptr(), d ** -0.5 if scale is None else scale,
                                                state.data_ptr(), state.shape[0], _ptr(slots), slot_bytes,
-                                               _heads(out, "out", dev, q.dtype, (B, H, d)), B, H, d, _stream(dev, None)))
+                                               ho, B, H, d, _stream(dev, None)))
     return out
 
 
