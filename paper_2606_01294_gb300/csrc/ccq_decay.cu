@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
     x /= nseg;
     const int h = static_cast<int>(x % a.H);
     x /= a.H;
-    const int sequence = static_cast<int>(x % a.sequences);
+    const int sequence = decay_longest_first(a, static_cast<int>(x % a.sequences), reinterpret_cast<int *>(shared_raw));
     const DecayPass &ps = a.pass[x / a.sequences];
     const int tid = threadIdx.x, tx = tid % 8, ty = tid / 8;
     const int c0 = slice * kN;
@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
     if (tid <= kC) sh.power[tid] = decay_power(l2, tid);
     if (tid >= kThreads - 2) sh.keep[tid - (kThreads - 2)] = decay_keep(l2, tid == kThreads - 2 ? kC : ragged);
 
+    if (a.cu) __syncthreads();  // (the ranks' place becomes the first block's)
     // tokens of block j in the pass's order: the ragged block is the sequence's last
     auto block_begin = [&](int64_t j) { return (down ? blocks - 1 - j : j) * kC; };
 
@@ -188,6 +189,7 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
         if (!a.parts_only) {
             // P: rows 2 ty, 2 ty + 1, columns tx + 8 c
             float p[2][4] = {};
+#pragma unroll 2
             for (int e = 0; e < D; e += 4) {
                 float4 qv[2], kv[4];
 #pragma unroll
@@ -211,6 +213,7 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
             __syncthreads();
             // O: rows 2 ty, 2 ty + 1, columns 4 tx .. 4 tx + 3
             float o[2][4] = {};
+#pragma unroll 2
             for (int e = 0; e < D; e += 4) {
                 float4 qv[2];
 #pragma unroll
@@ -276,6 +279,7 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int c = 0; c < 4; ++c) S[r][c] = fmaf(S[r][c], keep.x, S[r][c] * keep.y);
+#pragma unroll 2
         for (int jj = 0; jj < n; ++jj) {
             const float u = sh.power[down ? jj + 1 : n - 1 - jj] * ps.k_scale;
             float4 vv = *reinterpret_cast<const float4 *>(&in.v[jj][4 * tx]);
@@ -366,7 +370,9 @@ template <typename T> __global__ void __launch_bounds__(256) decay_sum_kernel(co
 // ---------------------------------------------------------------- the calls
 
 // Segments of each sequence, by a count of what a launch takes: rounds of resident CTAs times the blocks of a CTA, for the
-// passes and, with more than one segment, for the states before them (`kinds`, all segments but the last).
+// passes and, with more than one segment, for the states before them (`kinds`, all segments but the last).  A block's times
+// are those measured with the GPU full.  1 x 16 x 20480 x 128 bf16: 482 us whole, 125 in 9 segments; the gradients of
+// 4 x 16 x 4096 x 128: 214 whole, 249 in 2; 1 x 8 x 4000 x 128 fp32: 1112 whole, 298 in 9.
 struct Cost {
     int block;           // tokens
     double main, parts;  // microseconds a block
@@ -378,7 +384,7 @@ int plan_segments(int64_t B, int64_t T, int H, int d, int64_t num_seqs, ccq_dtyp
     if (num_seqs < 1 || B * T < 1) return 1;
     const bool cores = dtype == CCQ_BF16;
     const Cost c = cores ? Cost{128, d == 128 ? 3.45 : 2.4, d == 128 ? 4.0 : 2.8, 6.0, sm_count_now()}
-                         : Cost{kC, d == 128 ? 6.0 : 3.5, d == 128 ? 3.0 : 2.0, 5.0, 3 * sm_count_now()};
+                         : Cost{kC, d == 128 ? 12.0 : 8.5, d == 128 ? 5.0 : 3.5, 6.0, 2 * sm_count_now()};
     const int64_t ctas = num_seqs * H * (cores ? 1 : d / kN), blocks = (B * T / num_seqs + c.block - 1) / c.block;
     const int64_t kinds = passes > 1 ? 2 : 1;
     auto rounds = [&](int64_t n) { return static_cast<double>((n + c.resident - 1) / c.resident); };

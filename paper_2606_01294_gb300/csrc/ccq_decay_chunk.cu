@@ -176,7 +176,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
     const int nseg = PARTS ? a.segments - 1 : a.segments;
     const int segment = x % nseg;
     x /= nseg;
-    const int h = x % a.H, sequence = x / a.H;
+    const int h = x % a.H, sequence = decay_longest_first(a, x / a.H, reinterpret_cast<int *>(table));
     const DecayPass &ps = a.pass[pi];
     const ChunkMapsOf &mp = maps.pass[pi];
     const bool down = ps.descending != 0;
@@ -207,6 +207,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
     }
     if (warp == 0) tmem_alloc(tmem_slot, kTmemCols);
     grid_wait();  // (the segments' parts)
+    if (a.cu) __syncthreads();  // (the ranks' place becomes the table's)
     if (!PARTS && tid < 256) table[tid] = tid < 127 ? 0.f : ps.p_scale * decay_power(l2, tid - 127);
     if (tid >= 256 && tid <= 256 + kC) powers[tid - 256] = ps.k_scale * decay_power(l2, tid - 256);
     if (tid >= 512 && tid < 544) reinterpret_cast<float *>(sm + M::kColumn)[tid - 512] = decay_power(l2, down ? tid - 512 : 543 - tid);
