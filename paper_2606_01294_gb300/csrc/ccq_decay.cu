@@ -450,8 +450,12 @@ DecayView view_of(const ccq_heads &x, int H) {
     return {x.p, x.batch, x.token, x.head, static_cast<int>(x.head == 0 ? H : H / x.heads)};
 }
 
-// Whether a tensor can be loaded in tiles: no dimension of more than one steps by nothing.
-bool steps(const ccq_heads &x, int64_t B, int64_t T) { return (B <= 1 || x.batch > 0) && (T <= 1 || x.token > 0); }
+// Whether a tensor can be loaded in tiles: its batch rows and tokens do not step by nothing, and no step has 2^40 bytes.
+bool steps(const ccq_heads &x, int64_t B, int64_t T) {
+    constexpr int64_t most = (1LL << 39) - 1;
+    return (B <= 1 || (x.batch > 0 && x.batch <= most)) && (T <= 1 || (x.token > 0 && x.token <= most)) &&
+           (x.heads <= 1 || x.head <= most);
+}
 
 ccq_status run_passes(DecayArgs &a, ccq_dtype dtype, bool cores, int64_t B, unsigned parts_mask, cudaStream_t s) {
     cudaError_t e = cudaSuccess;
@@ -544,7 +548,8 @@ ccq_status ccq_decay_attention(const ccq_heads *q, const ccq_heads *k, const ccq
     a.cu_bytes = cu_bytes;
     a.parts = static_cast<float *>(workspace);
     a.vec = access == 16;
-    const bool cores = dtype == CCQ_BF16 && a.vec && B * T > 0 && steps(*q, B, T) && steps(*k, B, T) && steps(*v, B, T);
+    const bool cores = dtype == CCQ_BF16 && a.vec && B * T > 0 && steps(*q, B, T) && steps(*k, B, T) && steps(*v, B, T) &&
+                       steps(*o, B, T);
     return run_passes(a, dtype, cores, B, 1u, static_cast<cudaStream_t>(stream));
 }
 
@@ -661,7 +666,7 @@ ccq_status ccq_decay_attention_bwd(const ccq_heads *q, const ccq_heads *k, const
     a.vec = access == 16 && access_out == 16;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     bool cores = dtype == CCQ_BF16 && a.vec && B * T > 0;
-    for (int i = 0; i < 4; ++i) cores = cores && steps(*in[i], B, T);
+    for (int i = 0; i < 4; ++i) cores = cores && steps(*in[i], B, T) && (i > 2 || steps(*out[i], B, T));
     if ((st = run_passes(a, dtype, cores, B, 5u, s)) != CCQ_OK || !sum.count || !(B * T)) return st;
     sum.H = H;
     sum.d = d;

@@ -30,14 +30,16 @@ constexpr int kAhead = 1;  // chunks
 constexpr int kWarps = 8;  // SP's and W's
 constexpr int kOWarps = 4;
 constexpr int kWWarp0 = kWarps, kOWarp0 = 2 * kWarps, kIssueWarp = kOWarp0 + kOWarps, kLoadWarp = kIssueWarp + 1,
-              kIssueWWarp = kIssueWarp + 2;
-constexpr int kThreads = 32 * 24;  // six warpgroups, the last warp idle
+              kIssueWWarp = kIssueWarp + 2, kKeepWarp = kIssueWarp + 3;
+constexpr int kThreads = 32 * 24;  // six warpgroups
 // Registers a thread: 80 at launch, then as the warps' work wants them, 480 for the six warpgroups together.
 constexpr int kSpRegs = 120, kWRegs = 56, kORegs = 72, kOtherRegs = 56;
 constexpr int kLaunchRegs = 80;
 static_assert(2 * kSpRegs + 2 * kWRegs + kORegs + kOtherRegs <= 6 * kLaunchRegs, "more registers than the launch has");
 static_assert(kSpRegs >= kLaunchRegs && kWRegs <= kLaunchRegs && kORegs <= kLaunchRegs && kOtherRegs <= kLaunchRegs,
               "one kind of warps takes registers, the others give them");
+
+enum { kOutBar = 1, kKeepBar = 2 };  // named barriers
 
 template <int D> struct Map {
     static constexpr uint32_t kBlocks = D / 64;                 // T64 tiles side by side
@@ -211,9 +213,6 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
     if (!PARTS && tid < 256) table[tid] = tid < 127 ? 0.f : ps.p_scale * decay_power(l2, tid - 127);
     if (tid >= 256 && tid <= 256 + kC) powers[tid - 256] = ps.k_scale * decay_power(l2, tid - 256);
     if (tid >= 512 && tid < 544) reinterpret_cast<float *>(sm + M::kColumn)[tid - 512] = decay_power(l2, down ? tid - 512 : 543 - tid);
-    if (tid >= kThreads - 2) {
-        keeps[tid - (kThreads - 2)] = decay_keep(l2, tid == kThreads - 2 ? kC : ragged);
-    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -266,6 +265,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
         auto advance = [&](int r) {  // S past chunk r
             wait_for(&bar[BAR_D], r & 1, abort_flag, status);
             tc_fence_after();
+            if (r == 0) named_bar(kKeepBar, 32 * (kWarps + 1));
             const float2 keep = keeps[chunk_at(r) == chunks - 1];
             const uint64_t kx = f2_make(keep.x, keep.x), ky = f2_make(keep.y, keep.y);
 #pragma unroll
@@ -437,7 +437,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
             const bool by_rows = ps.o_fp32 || others_in(r);
             if (!by_rows) {
                 if (storer) tma_store_wait_read();
-                named_bar(1, 32 * kOWarps);  // the tile has been read
+                named_bar(kOutBar, 32 * kOWarps);  // the tile has been read
             }
             wait_for(&bar[BAR_O1], r & 1, abort_flag, status);
             wait_for(&bar[BAR_O2], r & 1, abort_flag, status);
@@ -478,7 +478,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
             }
             if (!by_rows) {
                 fence_proxy_async_smem();
-                named_bar(1, 32 * kOWarps);
+                named_bar(kOutBar, 32 * kOWarps);
                 if (storer) {
 #pragma unroll
                     for (uint32_t c = 0; c < M::kBlocks; ++c)
@@ -615,6 +615,11 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
                 for (int j = 0; j < 2; ++j) mbar_drain(&bar[BAR_V + j], last);
                 for (int half = max(0, 2 * count - 3); half < 2 * count; ++half) mbar_drain(&bar[BAR_K + half % 3], (half / 3) & 1);
             }
+        } else if (warp == kKeepWarp && count > 0) {
+            // ======================================================== the powers in 64 bits, a microsecond that SP needs not wait for
+            if (lane < 2) keeps[lane] = decay_keep(l2, lane ? ragged : kC);
+            __syncwarp();
+            named_bar_arrive(kKeepBar, 32 * (kWarps + 1));
         }
     }
     tc_fence_before();

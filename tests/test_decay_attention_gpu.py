@@ -218,6 +218,65 @@ def test_packed(dtype, d, lengths):
 
 
 @pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("n", [200, 256, 257, 700])
+def test_many_packed_sequences(dtype, n):
+    """Up to 256 run by their lengths, more as they lie: a token's result is that of its sequence by itself either way."""
+    H, d = 2, 64
+    lengths = torch.randint(0, 60, (n,), device="cuda", generator=gen(n))
+    lengths[n // 2] = 300
+    cu = torch.cat([lengths.new_zeros(1), lengths.cumsum(0)])
+    total = int(cu[-1])
+    q, k, v, ld, _ = make(1, total, H, H, H, H, d, dtype, n, False)
+    S0 = torch.randn(n, H, d, d, device="cuda", generator=gen(n + 1))
+    o, ST = ops.decay_attention(q, k, v, ld, state=S0, cu_seqlens=cu)
+    g = ops.decay_attention_bwd(q, k, v, ld, v, state=S0, dfinal_state=S0, cu_seqlens=cu)
+    # in a batch of rows of the longest's length, with zeros past each end: they add nothing to o; one sequence at a time for states
+    at = torch.arange(300, device="cuda")
+    held = at < lengths[:, None]
+    rows = torch.where(held, cu[:-1, None] + at, 0)
+    pad = lambda x: x[0][rows] * held[..., None, None]  # noqa: E731
+    padded, _ = ops.decay_attention(pad(q), pad(k), pad(v), ld, state=S0)
+    assert torch.equal(o[0], padded[held])
+    for s in (0, n // 2, n - 1):
+        cut = slice(int(cu[s]), int(cu[s + 1]))
+        if cut.start == cut.stop:
+            assert torch.equal(ST[s], S0[s])
+            continue
+        args = q[:, cut], k[:, cut], v[:, cut], ld, S0[s:s + 1], d ** -0.5
+        check_forward(o[:, cut], ST[s:s + 1], *args, dtype == BF16)
+        mine = {x: g[x][:, cut] for x in ("dq", "dk", "dv")} | {"dstate": g["dstate"][s:s + 1]}
+        check_backward(mine, *args, v[:, cut], S0[s:s + 1], dtype == BF16)
+
+
+def test_offsets_that_go_back():
+    """An offset below the one before it makes an empty sequence, and is reported; nothing is read or written out of range."""
+    q, k, v, ld, _ = make(1, 300, 2, 2, 2, 2, 64, BF16, 8, False)
+    cu = torch.tensor([0, 200, 100, 300], device="cuda")
+    o, ST = ops.decay_attention(q, k, v, ld, cu_seqlens=cu)
+    with pytest.raises(ccq.CCQError) as e:
+        ccq.device_status()
+    assert e.value.status == 6 and not ST[1].any()
+    check_forward(o[:, :100], None, q[:, :200][:, :100], k[:, :100], v[:, :100], ld, None, 64 ** -0.5, True)
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("given", ["state", "gradient"])
+@pytest.mark.parametrize("T", [100, 1600])
+def test_backward_with_one_state(dtype, given, T):
+    """A state before without a gradient behind, and the other way round: the missing one is zero."""
+    B, H, d = 1, 2, 64
+    q, k, v, _, S = make(B, T, H, H, H, H, d, dtype, T + 3)
+    ld = torch.tensor([-0.01, -0.2], device="cuda")
+    dout = torch.randn(B, T, H, d, device="cuda", generator=gen(T)).to(dtype)
+    zero = torch.zeros_like(S)
+    S0, dST = (S, None) if given == "state" else (None, S)
+    g = ops.decay_attention_bwd(q, k, v, ld, dout, state=S0, dfinal_state=dST)
+    check_backward(g, q, k, v, ld, zero if S0 is None else S0, d ** -0.5, dout, zero if dST is None else dST, dtype == BF16)
+    both = ops.decay_attention_bwd(q, k, v, ld, dout, state=zero if S0 is None else S0, dfinal_state=zero if dST is None else dST)
+    assert all(torch.equal(g[x], both[x]) for x in both)
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("B,T,H", [(1, 3000, 2), (1, 1537, 1), (3, 1025, 1)])
 def test_long_sequences_in_segments(dtype, d, B, T, H):
