@@ -459,6 +459,7 @@ bool steps(const ccq_heads &x, int64_t B, int64_t T) {
 
 ccq_status run_passes(DecayArgs &a, ccq_dtype dtype, bool cores, int64_t B, unsigned parts_mask, cudaStream_t s) {
     cudaError_t e = cudaSuccess;
+    for (int i = 0; i < a.passes; ++i) a.exact_state |= a.pass[i].state_out != nullptr;
     auto run = [&](const DecayArgs &x) { return cores ? launch_decay_chunks(x, B, s) : launch_decay_blocks(x, dtype, s); };
     if (a.segments > 1) {
         DecayArgs p = a;

@@ -55,6 +55,7 @@ struct DecayArgs {
     int segments;
     float *parts;
     int parts_only;
+    int exact_state;    // a pass hands its states out
     int vec;            // every address and stride is a multiple of 16 bytes
 };
 

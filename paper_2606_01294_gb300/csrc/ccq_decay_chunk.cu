@@ -150,16 +150,18 @@ struct DecayMaps {
 };
 
 // Two values in three bf16 terms each, the bits of 24 from the top: cutting off leaves differences that are exact.
-__device__ __forceinline__ void split3(uint64_t x, uint32_t &hi, uint32_t &mid, uint32_t &lo) {
+// In two terms they are rounded, the second within 2^-17 of the value.
+template <int TERMS> __device__ __forceinline__ void split(uint64_t x, uint32_t &hi, uint32_t &mid, uint32_t &lo) {
     const uint64_t minus = f2_make(-1.f, -1.f);
     auto top = [](uint64_t v) { return __byte_perm(static_cast<uint32_t>(v), static_cast<uint32_t>(v >> 32), 0x7632); };
-    hi = top(x);
+    hi = TERMS == 2 ? bf16x2_from_f2(x) : top(x);
     x = f2_fma(f2_from_bf16x2(hi), minus, x);
-    mid = top(x);
-    lo = top(f2_fma(f2_from_bf16x2(mid), minus, x));
+    mid = TERMS == 2 ? bf16x2_from_f2(x) : top(x);
+    if (TERMS == 3) lo = top(f2_fma(f2_from_bf16x2(mid), minus, x));
 }
 
-template <int D, bool PARTS>
+// TERMS: of W.  Three where a state is handed out, two where the state serves the outputs alone, which read it rounded to bf16.
+template <int D, bool PARTS, int TERMS>
 __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constant__ DecayMaps maps, const __grid_constant__ DecayArgs a) {
     using M = Map<D>;
     extern __shared__ uint8_t smem_raw[];
@@ -395,15 +397,15 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
                     if (t < n) {
                         const float w = powers[down ? t + 1 : n - 1 - t];
                         const uint64_t ww = f2_make(w, w);
-                        split3(f2_mul(f2_from_bf16x2(u.x), ww), hi.x, mid.x, lo.x);
-                        split3(f2_mul(f2_from_bf16x2(u.y), ww), hi.y, mid.y, lo.y);
-                        split3(f2_mul(f2_from_bf16x2(u.z), ww), hi.z, mid.z, lo.z);
-                        split3(f2_mul(f2_from_bf16x2(u.w), ww), hi.w, mid.w, lo.w);
+                        split<TERMS>(f2_mul(f2_from_bf16x2(u.x), ww), hi.x, mid.x, lo.x);
+                        split<TERMS>(f2_mul(f2_from_bf16x2(u.y), ww), hi.y, mid.y, lo.y);
+                        split<TERMS>(f2_mul(f2_from_bf16x2(u.z), ww), hi.z, mid.z, lo.z);
+                        split<TERMS>(f2_mul(f2_from_bf16x2(u.w), ww), hi.w, mid.w, lo.w);
                     }
                     uint8_t *to = w_to + kRows * 128 * k;
                     *reinterpret_cast<uint4 *>(to) = hi;
                     *reinterpret_cast<uint4 *>(to + M::kWTerm) = mid;
-                    *reinterpret_cast<uint4 *>(to + 2 * M::kWTerm) = lo;
+                    if (TERMS == 3) *reinterpret_cast<uint4 *>(to + 2 * M::kWTerm) = lo;
                 }
                 if (q == 0 && others_in(r)) {  // zeros in V
                     for (int j = 0; j < 2; ++j) {
@@ -557,9 +559,9 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
 #pragma unroll
                     for (int k = 0; k < 2; ++k)
 #pragma unroll
-                        for (int t = 2; t >= 0; --t)  // the small terms first
+                        for (int t = TERMS - 1; t >= 0; --t)  // the small terms first
                             mma_bf16(tbase + TM_D, desc_mnmajor(v, M::kHBlock, 2 * slot + k),
-                                     desc_mnmajor(w + t * M::kWTerm, M::kWBlock, k), kWV, q > 0 || k > 0 || t < 2);
+                                     desc_mnmajor(w + t * M::kWTerm, M::kWBlock, k), kWV, q > 0 || k > 0 || t < TERMS - 1);
                     mma_commit(&bar[BAR_WFREE + slot]);
                     if (slot) mma_commit(&bar[BAR_VFREE + half]);
                 }
@@ -628,16 +630,20 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
     if (warp == 0) tmem_dealloc(tbase, kTmemCols);
 }
 
-template <int D, bool PARTS> cudaError_t launch(const DecayMaps &m, const DecayArgs &a, cudaStream_t s) {
+template <int D, bool PARTS, int TERMS> cudaError_t launch(const DecayMaps &m, const DecayArgs &a, cudaStream_t s) {
     constexpr int kBytes = Map<D>::kBytes;
-    cudaError_t e = allow_shared<decay_chunk_kernel<D, PARTS>>(kBytes);
+    cudaError_t e = allow_shared<decay_chunk_kernel<D, PARTS, TERMS>>(kBytes);
     if (e != cudaSuccess) return e;
     const int64_t grid = static_cast<int64_t>(PARTS ? a.segments - 1 : a.segments) * a.H * a.sequences * a.passes;
     if (grid > 0x7fffffff) return cudaErrorInvalidValue;
     if (!PARTS && a.segments > 1)
-        return launch_after(decay_chunk_kernel<D, PARTS>, static_cast<unsigned>(grid), kThreads, kBytes, s, m, a);
-    decay_chunk_kernel<D, PARTS><<<static_cast<unsigned>(grid), kThreads, kBytes, s>>>(m, a);
+        return launch_after(decay_chunk_kernel<D, PARTS, TERMS>, static_cast<unsigned>(grid), kThreads, kBytes, s, m, a);
+    decay_chunk_kernel<D, PARTS, TERMS><<<static_cast<unsigned>(grid), kThreads, kBytes, s>>>(m, a);
     return cudaGetLastError();
+}
+
+template <int D, int TERMS> cudaError_t launch_any(const DecayMaps &m, const DecayArgs &a, cudaStream_t s) {
+    return a.parts_only ? launch<D, true, TERMS>(m, a, s) : launch<D, false, TERMS>(m, a, s);
 }
 
 }  // namespace
@@ -672,8 +678,8 @@ cudaError_t launch_decay_chunks(const DecayArgs &a, int64_t B, cudaStream_t s) {
         else if (!make_heads_map(&m.pass[i].o, ps.o, B, a.T, a.H, a.d, ps.o_batch, ps.o_token, ps.o_head, kC))
             return cudaErrorInvalidValue;
     }
-    if (a.parts_only) return a.d == 128 ? launch<128, true>(m, a, s) : launch<64, true>(m, a, s);
-    return a.d == 128 ? launch<128, false>(m, a, s) : launch<64, false>(m, a, s);
+    if (a.exact_state) return a.d == 128 ? launch_any<128, 3>(m, a, s) : launch_any<64, 3>(m, a, s);
+    return a.d == 128 ? launch_any<128, 2>(m, a, s) : launch_any<64, 2>(m, a, s);
 }
 
 }  // namespace ccq
