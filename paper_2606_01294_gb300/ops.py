@@ -29,6 +29,7 @@ from .ccq import _check, _dtype_code, _on_stream, _ptr, _stream
 
 ACTIVATION = {"none": 0, "silu": 1, "sigmoid": 2}
 ADAMW_BLOCK = 256
+_CODE = {torch.bfloat16: ccq.BF16, torch.float32: ccq.FP32}
 
 _VP, _I, _L, _F, _D, _Z = (ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_double,
                            ctypes.c_size_t)
@@ -226,7 +227,107 @@ def embed_grad(dout, ids, rows: int, *, scale: float = 1.0, padding_id: Optional
 # ---------------------------------------------------------------- heads of tokens
 
 
+# A call on small tensors costs the host more than the GPU, so what follows from shapes, strides and types alone is formed once
+# for each combination of them (bounded caches of plain values).  A plan is None where a check fails: the call then goes the way
+# that makes the checks one by one and says what is wrong.
 _FIVE = struct.Struct("5q").pack
+_INDEX = {torch.int64: 8, torch.int32: 4}
+
+
+def _strides(shape, stride):
+    """(batch, token, head stride, heads) of [batch, tokens, heads, width] or [rows, heads, width]; None: not contiguous channels."""
+    if stride[-1] != 1 and shape[-1] > 1:
+        return None
+    return (*stride[:3], shape[2]) if len(shape) == 4 else (stride[0], stride[0], stride[1], shape[1])
+
+
+def _dense_strides(shape):
+    B, T, n, width = shape if len(shape) == 4 else (1, *shape)
+    return T * n * width, n * width, width, n
+
+
+def _is_dense(shape, stride):
+    step = 1
+    for n, s in zip(reversed(shape), reversed(stride)):
+        if n != 1 and s != step:
+            return 0 in shape
+        step *= n
+    return True
+
+
+@functools.lru_cache(maxsize=512)
+def _rotary_plan(q, k, positions, freqs):
+    (dtype, shape, _), (kdtype, kshape, _) = q, k
+    xq, xk = _strides(*q[1:]), _strides(*k[1:])
+    if (len(shape) not in (3, 4) or len(kshape) != len(shape) or kdtype != dtype or dtype not in _CODE or not xq or not xk
+            or kshape[:-2] != shape[:-2] or kshape[-1] != shape[-1] or positions[0] not in _INDEX or positions[1] != shape[:-2]
+            or not _is_dense(*positions[1:]) or freqs[0] is not torch.float64 or not _is_dense(*freqs[1:])):
+        return None
+    B, T = shape[:2] if len(shape) == 4 else (1, shape[0])
+    return xq, xk, _dense_strides(shape), _dense_strides(kshape), (2, _CODE[dtype], B, T, shape[-1], 2 * math.prod(freqs[1])), _INDEX[positions[0]]
+
+
+@functools.lru_cache(maxsize=512)
+def _decay_plan(q, k, v, log_decay, cu, states, index, dout=None):
+    """Of decay_attention (dout None) and its gradients: (strides of q, k, v[, dout]), of o, its shape, the states' shape, the
+    arguments from B on, type code and workspace bytes.  ``states``: shapes, strides and types of the states that are given."""
+    dtype, shape, _ = q
+    if dtype not in _CODE or len(shape) != 4 or log_decay[0] is not torch.float32 or len(log_decay[1]) != 1 or not _is_dense(*log_decay[1:]):
+        return None
+    B, T, _, d = shape
+    H = log_decay[1][0]
+    out = (B, T, H, d)
+    tails = []
+    for t in (q, k, v) + ((dout,) if dout else ()):
+        x = _strides(*t[1:]) if len(t[1]) == 4 else None
+        if t[0] != dtype or not x or tuple(t[1][:2]) != (B, T) or t[1][3] != d or t[1][2] < 1 or H % t[1][2] or (t is dout and t[1][2] != H):
+            return None
+        tails.append(x)
+    seqs, cu_bytes = B, 8
+    if cu is not None:
+        if cu[0] not in _INDEX or len(cu[1]) != 1 or cu[1][0] < 1 or not _is_dense(*cu[1:]) or B != 1:
+            return None
+        seqs, cu_bytes = cu[1][0] - 1, _INDEX[cu[0]]
+    state = (seqs, H, d, d)
+    if any(t[0] is not torch.float32 or tuple(t[1]) != state or not _is_dense(*t[1:]) for t in states):
+        return None
+    code = _CODE[dtype]
+    if dout:
+        need = _size("ccq_decay_attention_bwd_workspace_size", index, B, T, H, shape[2], k[1][2], v[1][2], d, seqs, code)
+    else:
+        need = _size("ccq_decay_attention_workspace_size", index, B, T, H, d, seqs, code)
+    return tails, _dense_strides(out), out, state, (B, T, H, d), (cu_bytes, seqs), code, need, d ** -0.5
+
+
+@functools.lru_cache(maxsize=512)
+def _step_plan(q, k, v, log_decay, state, slots):
+    dtype, shape, _ = q
+    if dtype not in _CODE or len(shape) != 3 or log_decay[0] is not torch.float32 or len(log_decay[1]) != 1 or not _is_dense(*log_decay[1:]):
+        return None
+    B, _, d = shape
+    H = log_decay[1][0]
+    tails = []
+    for t in (q, k, v):
+        x = _strides(*t[1:]) if len(t[1]) == 3 else None
+        if t[0] != dtype or not x or t[1][0] != B or t[1][2] != d or t[1][1] < 1 or H % t[1][1]:
+            return None
+        tails.append(x)
+    if state[0] is not torch.float32 or len(state[1]) != 4 or tuple(state[1][1:]) != (H, d, d) or not _is_dense(*state[1:]):
+        return None
+    if slots is None:
+        if state[1][0] != B:
+            return None
+    elif slots[0] not in _INDEX or tuple(slots[1]) != (B,) or not _is_dense(*slots[1:]):
+        return None
+    return tails, (H * d, d, d, H), (B, H, d), _CODE[dtype], state[1][0], 4 if slots is None else _INDEX[slots[0]], d ** -0.5
+
+
+def _like(t):
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
+def _meta(t):
+    return None if t is None else (t.dtype, t.shape, t.stride())
 
 
 def _heads(t, name, device=None, dtype=None, shape=None, heads=None):
@@ -280,6 +381,16 @@ def rotary_frequencies(part: int, *, base: float = 10000.0, scaling: str = "none
 
 
 def _rotary(q, k, positions, freqs, interleaved, amplitude, inverse, out):
+    if out is None and all(isinstance(t, torch.Tensor) and t.is_cuda for t in (q, k, positions, freqs)):
+        dev = q.device
+        plan = _rotary_plan((q.dtype, q.shape, q.stride()), (k.dtype, k.shape, k.stride()), _meta(positions), _meta(freqs))
+        if plan is not None and k.device == dev and positions.device == dev and freqs.device == dev:
+            xq, xk, yq, yk, sizes, index = plan
+            a, b = _like(q), _like(k)
+            _check(_library().ccq_rotary(_FIVE(q.data_ptr(), *xq) + _FIVE(k.data_ptr(), *xk),
+                                         _FIVE(a.data_ptr(), *yq) + _FIVE(b.data_ptr(), *yk), *sizes, positions.data_ptr(), index,
+                                         freqs.data_ptr(), amplitude, interleaved, inverse, _stream(dev, None)))
+            return a, b
     if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4):
         raise ValueError("q must be a CUDA tensor of [batch, tokens, heads, width] or [tokens, heads, width]")
     x = _heads(q, "q")
@@ -298,7 +409,7 @@ def _rotary(q, k, positions, freqs, interleaved, amplitude, inverse, out):
         o = None if out is None else out[i]
         if o is None:
             n = t.shape[-2]
-            o = t.new_empty(t.shape)
+            o = _like(t)
             y += _FIVE(o.data_ptr(), T * n * width, n * width, width, n)
         else:
             y += _heads(o, "out", dev, t.dtype, t.shape)
@@ -368,6 +479,25 @@ def decay_attention(q, k, v, log_decay, *, scale: Optional[float] = None, state=
     if stream is not None:
         return _on_stream(stream, decay_attention, q, k, v, log_decay, scale=scale, state=state, cu_seqlens=cu_seqlens, out=out,
                           final_state=final_state, return_state=return_state, workspace=workspace)
+    given = [t for t in (state, final_state) if t is not None]
+    if out is None and all(isinstance(t, torch.Tensor) and t.is_cuda for t in (q, k, v, log_decay, *given)) and (
+            cu_seqlens is None or (isinstance(cu_seqlens, torch.Tensor) and cu_seqlens.is_cuda)):
+        dev = q.device
+        raw = _stream(dev, None)
+        plan = _decay_plan((q.dtype, q.shape, q.stride()), (k.dtype, k.shape, k.stride()), (v.dtype, v.shape, v.stride()),
+                           _meta(log_decay), _meta(cu_seqlens), tuple(map(_meta, given)), dev.index)
+        if plan is not None and k.device == dev and v.device == dev and log_decay.device == dev and all(
+                t.device == dev for t in given) and (cu_seqlens is None or cu_seqlens.device == dev):
+            (xq, xk, xv), xo, shape, state_shape, sizes, (cu_bytes, seqs), code, need, root = plan
+            out = _like(q) if q.shape == shape else torch.empty(shape, dtype=q.dtype, device=dev)
+            if final_state is None and return_state:
+                final_state = torch.empty(state_shape, dtype=torch.float32, device=dev)
+            workspace, nbytes = _workspace(workspace, need, dev)
+            _check(_library().ccq_decay_attention(
+                _FIVE(q.data_ptr(), *xq), _FIVE(k.data_ptr(), *xk), _FIVE(v.data_ptr(), *xv), code, log_decay.data_ptr(),
+                root if scale is None else scale, _ptr(state), _FIVE(out.data_ptr(), *xo), _ptr(final_state), *sizes,
+                _ptr(cu_seqlens), cu_bytes, seqs, _ptr(workspace), nbytes, raw))
+            return out, final_state
     dev, B, T, H, d, (hq, hk, hv), cu, scale = _decay_args(q, k, v, log_decay, scale, cu_seqlens)
     shape = (cu[2], H, d, d)
     if state is not None:
@@ -399,6 +529,27 @@ def decay_attention_bwd(q, k, v, log_decay, dout, *, scale: Optional[float] = No
     if stream is not None:
         return _on_stream(stream, decay_attention_bwd, q, k, v, log_decay, dout, scale=scale, state=state,
                           dfinal_state=dfinal_state, cu_seqlens=cu_seqlens, out=out, workspace=workspace)
+    given = [t for t in (state, dfinal_state) if t is not None]
+    if not out and all(isinstance(t, torch.Tensor) and t.is_cuda for t in (q, k, v, log_decay, dout, *given)) and (
+            cu_seqlens is None or (isinstance(cu_seqlens, torch.Tensor) and cu_seqlens.is_cuda)):
+        dev = q.device
+        raw = _stream(dev, None)
+        plan = _decay_plan((q.dtype, q.shape, q.stride()), (k.dtype, k.shape, k.stride()), (v.dtype, v.shape, v.stride()),
+                           _meta(log_decay), _meta(cu_seqlens), tuple(map(_meta, given)), dev.index, _meta(dout))
+        if plan is not None and all(t.device == dev for t in (k, v, log_decay, dout, *given)) and (
+                cu_seqlens is None or cu_seqlens.device == dev):
+            (xq, xk, xv, xo), _, _, state_shape, sizes, (cu_bytes, seqs), code, need, root = plan
+            dq, dk, dv = _like(q), _like(k), _like(v)
+            g = {"dq": dq, "dk": dk, "dv": dv}
+            if given:
+                g["dstate"] = torch.empty(state_shape, dtype=torch.float32, device=dev)
+            workspace, nbytes = _workspace(workspace, need, dev)
+            _check(_library().ccq_decay_attention_bwd(
+                _FIVE(q.data_ptr(), *xq), _FIVE(k.data_ptr(), *xk), _FIVE(v.data_ptr(), *xv), code, log_decay.data_ptr(),
+                root if scale is None else scale, _ptr(state), _FIVE(dout.data_ptr(), *xo), _ptr(dfinal_state),
+                *(_FIVE(t.data_ptr(), *_dense_strides(t.shape)) for t in (dq, dk, dv)), _ptr(g.get("dstate")), *sizes,
+                _ptr(cu_seqlens), cu_bytes, seqs, _ptr(workspace), nbytes, raw))
+            return g
     dev, B, T, H, d, (hq, hk, hv), cu, scale = _decay_args(q, k, v, log_decay, scale, cu_seqlens)
     shape = (cu[2], H, d, d)
     ho = _heads(dout, "dout", dev, q.dtype, (B, T, H, d))
@@ -415,7 +566,7 @@ def decay_attention_bwd(q, k, v, log_decay, dout, *, scale: Optional[float] = No
     for name, like in (("dq", q), ("dk", k), ("dv", v)):
         if g.get(name) is None:
             n = like.shape[2]
-            g[name] = like.new_empty(like.shape)
+            g[name] = _like(like)
             heads.append(_FIVE(g[name].data_ptr(), T * n * d, n * d, d, n))
         else:
             heads.append(_heads(g[name], name, dev, like.dtype, like.shape))
@@ -436,6 +587,20 @@ def decay_attention_step(q, k, v, log_decay, state, *, scale: Optional[float] = 
     batch has, gives a zero output, changes nothing and leaves CCQ_ERR_INDEX for :func:`ccq.device_status`."""
     if stream is not None:
         return _on_stream(stream, decay_attention_step, q, k, v, log_decay, state, scale=scale, slots=slots, out=out)
+    if out is None and all(isinstance(t, torch.Tensor) and t.is_cuda for t in (q, k, v, log_decay, state)) and (
+            slots is None or (isinstance(slots, torch.Tensor) and slots.is_cuda)):
+        dev = q.device
+        plan = _step_plan((q.dtype, q.shape, q.stride()), (k.dtype, k.shape, k.stride()), (v.dtype, v.shape, v.stride()),
+                          _meta(log_decay), _meta(state), _meta(slots))
+        if plan is not None and k.device == dev and v.device == dev and log_decay.device == dev and state.device == dev and (
+                slots is None or slots.device == dev):
+            (xq, xk, xv), xo, shape, code, rows, slot_bytes, root = plan
+            out = _like(q) if q.shape == shape else torch.empty(shape, dtype=q.dtype, device=dev)
+            _check(_library().ccq_decay_attention_step(
+                _FIVE(q.data_ptr(), *xq), _FIVE(k.data_ptr(), *xk), _FIVE(v.data_ptr(), *xv), code, log_decay.data_ptr(),
+                root if scale is None else scale, state.data_ptr(), rows, _ptr(slots), slot_bytes, _FIVE(out.data_ptr(), *xo),
+                *shape, _stream(dev, None)))
+            return out
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a CUDA tensor of [batch, heads, d]")
     B, _, d = q.shape
