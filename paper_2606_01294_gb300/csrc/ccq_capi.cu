@@ -168,22 +168,20 @@ bool make_token_map(CUtensorMap *map, const void *base, int elem_bytes, int B, i
     return r == CUDA_SUCCESS;
 }
 
-bool make_heads_map(CUtensorMap *map, const void *base, long long B, long long T, long long heads, int D, long long batch,
-                    long long token, long long head, int box_tokens) {
+bool make_heads_map(CUtensorMap *map, const void *base, int elem_bytes, long long B, long long T, long long heads, int D,
+                    long long batch, long long token, long long head, int box_tokens) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[4] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(T),
                                 static_cast<cuuint64_t>(B)};
     // (the stride of an extent of one is not looked at, but has to be a valid one)
-    const cuuint64_t row = 2 * static_cast<cuuint64_t>(D);
-    const cuuint64_t strides[3] = {heads > 1 ? 2 * static_cast<cuuint64_t>(head) : row,
-                                   T > 1 ? 2 * static_cast<cuuint64_t>(token) : row,
-                                   B > 1 ? 2 * static_cast<cuuint64_t>(batch) : row};
-    const cuuint32_t box[4] = {64, 1, static_cast<cuuint32_t>(box_tokens), 1};
+    const cuuint64_t eb = static_cast<cuuint64_t>(elem_bytes), row = eb * D;
+    const cuuint64_t strides[3] = {heads > 1 ? eb * head : row, T > 1 ? eb * token : row, B > 1 ? eb * batch : row};
+    const cuuint32_t box[4] = {static_cast<cuuint32_t>(128 / elem_bytes), 1, static_cast<cuuint32_t>(box_tokens), 1};
     const cuuint32_t estr[4] = {1, 1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn(map, elem_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4,
+              const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool make_f32_rows_map(CUtensorMap *map, const void *base, long long rows, int cols, int box_cols, int box_rows) {

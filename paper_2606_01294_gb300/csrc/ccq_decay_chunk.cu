@@ -47,9 +47,9 @@ template <int D> struct Map {
     static constexpr uint32_t kTile = kBlock * kBlocks;         // [128 tokens][D]
     static constexpr uint32_t kHBlock = 64 * 128, kHalf = kHBlock * kBlocks;  // of 64 tokens
     static constexpr uint32_t kWBlock = 32 * 128, kWTerm = kWBlock * kBlocks, kWSlot = 3 * kWTerm;
-    static constexpr uint32_t kQ = 0, kO = kTile;
-    static constexpr uint32_t kV = 2 * kTile;                   // two halves
-    static constexpr uint32_t kK = 3 * kTile;                   // three halves, [d / 64][half][64 tokens]
+    static constexpr uint32_t kQ = 0, kO = kTile;               // o: two blocks, of 64 columns in bf16, 32 in fp32
+    static constexpr uint32_t kV = kO + 2 * kBlock;             // two halves
+    static constexpr uint32_t kK = kV + kTile;                  // three halves, [d / 64][half][64 tokens]
     static constexpr uint32_t kKBlock = 3 * kHBlock;
     static constexpr uint32_t kW = kK + 3 * kHalf;              // two slots of 32 tokens, three terms each
     static constexpr uint32_t kS = kW + 2 * kWSlot;             // [D][D]
@@ -161,7 +161,8 @@ template <int TERMS> __device__ __forceinline__ void split(uint64_t x, uint32_t 
 }
 
 // TERMS: of W.  Three where a state is handed out, two where the state serves the outputs alone, which read it rounded to bf16.
-template <int D, bool PARTS, int TERMS>
+// SUMS: some passes leave parts of shared heads' gradients, in fp32 (without their code the others run 4 % faster).
+template <int D, bool PARTS, int TERMS, bool SUMS>
 __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constant__ DecayMaps maps, const __grid_constant__ DecayArgs a) {
     using M = Map<D>;
     extern __shared__ uint8_t smem_raw[];
@@ -429,23 +430,35 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
         // ============================================================ O
         fewer_registers<kORegs>();
         const int i = 32 * (warp & 3) + lane;
-        const bool storer = tid == 32 * kOWarp0;
+        const bool storer = tid == 32 * kOWarp0, fp32 = SUMS && ps.o_fp32;
         const float near = decay_power(l2, i + 1) * ps.s_scale;  // ascending, or a full chunk's mirror image below
         const float far = decay_power(l2, kC - 1 - i) * ps.s_scale;
         for (int r = 0; r < (PARTS ? 0 : count); ++r) {
             const int n = tokens_of(r);
             const float fac = down ? (n == kC ? far : i < n ? decay_power(l2, n - 1 - i) * ps.s_scale : 0.f) : near;
             const int64_t at = span.b * ps.o_batch + (span.begin + begin_of(r) + i) * ps.o_token + h * ps.o_head;
-            const bool by_rows = ps.o_fp32 || others_in(r);
-            if (!by_rows) {
+            const bool by_rows = others_in(r);
+            auto wait_tile = [&]() {  // the tile has been read
                 if (storer) tma_store_wait_read();
-                named_bar(kOutBar, 32 * kOWarps);  // the tile has been read
-            }
+                named_bar(kOutBar, 32 * kOWarps);
+            };
+            auto store_tile = [&](int column, int columns) {
+                fence_proxy_async_smem();
+                named_bar(kOutBar, 32 * kOWarps);
+                if (storer) {
+                    for (int c = 0; c < columns; c += 128 / (fp32 ? 4 : 2))
+                        tma_store_4d(&mp.o, sm + M::kO + c * (fp32 ? M::kBlock / 32 : M::kBlock / 64), column + c, h,
+                                     static_cast<int>(span.begin) + begin_of(r), static_cast<int>(span.b));
+                    tma_store_commit();
+                }
+            };
+            if (!by_rows) wait_tile();
             wait_for(&bar[BAR_O1], r & 1, abort_flag, status);
             wait_for(&bar[BAR_O2], r & 1, abort_flag, status);
             tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < D / 16; ++c) {
+                if (!by_rows && fp32 && c && !(c & 3)) wait_tile();  // (in fp32 64 columns at a time)
                 float u[16], w[16];
                 tmem_ld16_two(tq + TM_O1 + 16 * c, tq + TM_O2 + 16 * c, u, w);
                 if (c == D / 16 - 1) {
@@ -459,13 +472,17 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
                     u[e] = f.x;
                     u[e + 1] = f.y;
                 }
-                if (ps.o_fp32) {
-                    float *to = static_cast<float *>(ps.o) + at + 16 * c;
-                    if (i < n) {
+                if (fp32) {
 #pragma unroll
-                        for (int e = 0; e < 16; e += 4)
-                            *reinterpret_cast<float4 *>(to + e) = make_float4(u[e], u[e + 1], u[e + 2], u[e + 3]);
+                    for (int e = 0; e < 16; e += 4) {
+                        const float4 four = make_float4(u[e], u[e + 1], u[e + 2], u[e + 3]);
+                        if (!by_rows)
+                            *reinterpret_cast<float4 *>(sm + M::kO + ((c >> 1) & 1) * M::kBlock +
+                                                        t64_chunk(i, 4 * (c & 1) + e / 4)) = four;
+                        else if (i < n)
+                            *reinterpret_cast<float4 *>(static_cast<float *>(ps.o) + at + 16 * c + e) = four;
                     }
+                    if (!by_rows && (c & 3) == 3) store_tile(16 * (c - 3), 64);
                     continue;
                 }
 #pragma unroll
@@ -478,17 +495,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
                         *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(ps.o) + at + 16 * c + e) = packed;
                 }
             }
-            if (!by_rows) {
-                fence_proxy_async_smem();
-                named_bar(kOutBar, 32 * kOWarps);
-                if (storer) {
-#pragma unroll
-                    for (uint32_t c = 0; c < M::kBlocks; ++c)
-                        tma_store_4d(&mp.o, sm + M::kO + c * M::kBlock, 64 * c, h, static_cast<int>(span.begin) + begin_of(r),
-                                     static_cast<int>(span.b));
-                    tma_store_commit();
-                }
-            }
+            if (!by_rows && !fp32) store_tile(0, D);
         }
         if (storer) tma_store_wait_all();
     } else {
@@ -630,20 +637,23 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
     if (warp == 0) tmem_dealloc(tbase, kTmemCols);
 }
 
-template <int D, bool PARTS, int TERMS> cudaError_t launch(const DecayMaps &m, const DecayArgs &a, cudaStream_t s) {
+template <int D, bool PARTS, int TERMS, bool SUMS> cudaError_t launch(const DecayMaps &m, const DecayArgs &a, cudaStream_t s) {
     constexpr int kBytes = Map<D>::kBytes;
-    cudaError_t e = allow_shared<decay_chunk_kernel<D, PARTS, TERMS>>(kBytes);
+    cudaError_t e = allow_shared<decay_chunk_kernel<D, PARTS, TERMS, SUMS>>(kBytes);
     if (e != cudaSuccess) return e;
     const int64_t grid = static_cast<int64_t>(PARTS ? a.segments - 1 : a.segments) * a.H * a.sequences * a.passes;
     if (grid > 0x7fffffff) return cudaErrorInvalidValue;
     if (!PARTS && a.segments > 1)
-        return launch_after(decay_chunk_kernel<D, PARTS, TERMS>, static_cast<unsigned>(grid), kThreads, kBytes, s, m, a);
-    decay_chunk_kernel<D, PARTS, TERMS><<<static_cast<unsigned>(grid), kThreads, kBytes, s>>>(m, a);
+        return launch_after(decay_chunk_kernel<D, PARTS, TERMS, SUMS>, static_cast<unsigned>(grid), kThreads, kBytes, s, m, a);
+    decay_chunk_kernel<D, PARTS, TERMS, SUMS><<<static_cast<unsigned>(grid), kThreads, kBytes, s>>>(m, a);
     return cudaGetLastError();
 }
 
 template <int D, int TERMS> cudaError_t launch_any(const DecayMaps &m, const DecayArgs &a, cudaStream_t s) {
-    return a.parts_only ? launch<D, true, TERMS>(m, a, s) : launch<D, false, TERMS>(m, a, s);
+    if (a.parts_only) return launch<D, true, TERMS, false>(m, a, s);
+    for (int i = 0; i < a.passes; ++i)
+        if (a.pass[i].o_fp32) return launch<D, false, TERMS, true>(m, a, s);
+    return launch<D, false, TERMS, false>(m, a, s);
 }
 
 }  // namespace
@@ -666,16 +676,16 @@ cudaError_t launch_decay_chunks(const DecayArgs &a, int64_t B, cudaStream_t s) {
                 *to[j] = *made[k];
                 continue;
             }
-            if (!make_heads_map(to[j], x.p, B, a.T, a.H / x.share, a.d, x.batch, x.token, x.head, box))
+            if (!make_heads_map(to[j], x.p, 2, B, a.T, a.H / x.share, a.d, x.batch, x.token, x.head, box))
                 return cudaErrorInvalidValue;
             seen[count] = &x;
             tokens[count] = box;
             made[count++] = to[j];
         }
         const DecayPass &ps = a.pass[i];
-        if (a.parts_only || ps.o_fp32)
+        if (a.parts_only)
             m.pass[i].o = m.pass[i].q;  // (not used)
-        else if (!make_heads_map(&m.pass[i].o, ps.o, B, a.T, a.H, a.d, ps.o_batch, ps.o_token, ps.o_head, kC))
+        else if (!make_heads_map(&m.pass[i].o, ps.o, ps.o_fp32 ? 4 : 2, B, a.T, a.H, a.d, ps.o_batch, ps.o_token, ps.o_head, kC))
             return cudaErrorInvalidValue;
     }
     if (a.exact_state) return a.d == 128 ? launch_any<128, 3>(m, a, s) : launch_any<64, 3>(m, a, s);

@@ -226,9 +226,9 @@ cudaError_t launch_gla_bwd(const BwdArgs &a, const BwdMaps &m, cudaStream_t s);
 // (128-byte swizzle).
 bool make_rows_map(CUtensorMap *map, const void *base, long long rows, int cols = 128);
 
-// Encode the tensor map of bf16 heads of tokens [B][T][heads][D] with strides in elements (multiples of 8) and 64 x 1 x
-// box_tokens x 1 boxes, 128-byte swizzled.
-bool make_heads_map(CUtensorMap *map, const void *base, long long B, long long T, long long heads, int D, long long batch,
+// Encode the tensor map of bf16 or fp32 heads of tokens [B][T][heads][D] with strides in elements (multiples of 16 bytes) and boxes of
+// 128 bytes x 1 x box_tokens x 1, 128-byte swizzled.
+bool make_heads_map(CUtensorMap *map, const void *base, int elem_bytes, long long B, long long T, long long heads, int D, long long batch,
                     long long token, long long head, int box_tokens);
 
 // Encode the tensor map of a [B][T][H][D] tensor with a (box_inner x 1 x 64 x 1)
