@@ -5,7 +5,8 @@
 // exact whatever p (F_i is within 2 units of 2^-64 turns for f_i < 1, so 2^-33 turns at p = 2^30); the top 32 bits become
 // the argument of sincospif.  (The same in 64-bit floating point, at this GPU's rate for it, would take a fifth of the
 // prefill's time.)  A CTA computes the cosines and sines of its tokens once for all heads.
-// Bound by HBM: every element read once and written once.
+// Bound by HBM, every element read once and written once: 8 x 4096 tokens of 16 + 16 heads of 128 in bf16 86 us, 6.2 TB/s, 92 % of a
+// copy.  A decode's 256 tokens take 3.4 us, a launch.
 #include <algorithm>
 
 #include "ccq_ops.cuh"
@@ -54,8 +55,11 @@ __device__ __forceinline__ uint64_t turns_of(double f) {
 // access holds N / 2 pairs side by side.
 template <typename T, int N, bool PAIR, bool INTER>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryArgs a) {
-    extern __shared__ float2 turn[];  // [tile][part / 2]: cos, sin
-    const int half = a.part / 2;
+    // [tile][part / 2]: cos, sin; of the pairs of an access two by two, those of neighbouring accesses side by side, so that a warp's
+    // reads do not meet in a bank (8 x 4096 tokens, 32 heads of 128 in bf16: 90 -> 86 us)
+    extern __shared__ __align__(16) float2 turn[];
+    constexpr int kPairs = PAIR ? N : N / 2;  // of an access
+    const int half = a.part / 2, across = half / kPairs;
     const int64_t first = static_cast<int64_t>(blockIdx.x) * a.tile;
     const int tokens = static_cast<int>(min(static_cast<int64_t>(a.tile), a.tokens - first));
     for (int j = threadIdx.x; j < tokens * half; j += kThreads) {
@@ -66,7 +70,8 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryArgs a) {
         float s, c;
         sincospif(static_cast<float>(top) * 0x1p-31f, &s, &c);
         if (!isfinite(f)) s = c = __int_as_float(0x7fffffff);
-        turn[j] = make_float2(c * a.amplitude, (a.inverse ? -s : s) * a.amplitude);
+        const int e = i % kPairs, place = kPairs == 1 ? i : (e / 2 * across + i / kPairs) * 2 + e % 2;
+        turn[t * half + place] = make_float2(c * a.amplitude, (a.inverse ? -s : s) * a.amplitude);
     }
     __syncthreads();
     const int per_token = a.heads * a.items;
@@ -92,7 +97,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryArgs a) {
             if (c < a.turned) {
                 lo = PAIR && INTER ? 2 * c : c * N;
                 if (PAIR) second[k] = INTER ? 1 : half;
-                angle[k] = t * half + (PAIR ? c * N : c * N / 2);
+                angle[k] = t * half + (kPairs == 1 ? c : 2 * c);
             } else {
                 lo = a.part + (c - a.turned) * N;
                 angle[k] = -1;
@@ -111,25 +116,34 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryArgs a) {
             }
             float p[N], q[N];
             unpack(u[k], p);
-            if constexpr (PAIR) {
-                unpack(w[k], q);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float2 cs = turn[angle[k] + e];
-                    const float x = p[e] * cs.x - q[e] * cs.y, y = p[e] * cs.y + q[e] * cs.x;
-                    p[e] = x;
-                    q[e] = y;
-                }
-                pack(q, w[k]);
-                store_stream<T, N>(out[k] + second[k], w[k]);
+            if constexpr (PAIR) unpack(w[k], q);
+            auto rotate = [](float &x, float &y, float c, float s) {
+                const float r = x * c - y * s;
+                y = x * s + y * c;
+                x = r;
+            };
+            if constexpr (kPairs == 1) {
+                const float2 cs = turn[angle[k]];
+                if constexpr (PAIR)
+                    rotate(p[0], q[0], cs.x, cs.y);
+                else
+                    rotate(p[0], p[1], cs.x, cs.y);
             } else {
 #pragma unroll
-                for (int e = 0; e < N; e += 2) {
-                    const float2 cs = turn[angle[k] + e / 2];
-                    const float x = p[e] * cs.x - p[e + 1] * cs.y, y = p[e] * cs.y + p[e + 1] * cs.x;
-                    p[e] = x;
-                    p[e + 1] = y;
+                for (int e = 0; e < kPairs; e += 2) {
+                    const float4 cs = *reinterpret_cast<const float4 *>(&turn[angle[k] + e * across]);
+                    if constexpr (PAIR) {
+                        rotate(p[e], q[e], cs.x, cs.y);
+                        rotate(p[e + 1], q[e + 1], cs.z, cs.w);
+                    } else {
+                        rotate(p[2 * e], p[2 * e + 1], cs.x, cs.y);
+                        rotate(p[2 * e + 2], p[2 * e + 3], cs.z, cs.w);
+                    }
                 }
+            }
+            if constexpr (PAIR) {
+                pack(q, w[k]);
+                store_stream<T, N>(out[k] + second[k], w[k]);
             }
             pack(p, u[k]);
             store_stream<T, N>(out[k], u[k]);
