@@ -82,8 +82,8 @@ typedef struct {
  *   (y_a, y_b) = amplitude (x_a cos theta - x_b sin theta, x_a sin theta + x_b cos theta)
  * for the pairs (a, b) = (i, i + part / 2), or (2 i, 2 i + 1) with interleaved = 1.  The channels from `part` on are
  * copied.  inverse = 1 turns by -theta: with it, the call on the outputs' gradients gives the inputs'.
- *   x, y       arrays (HOST) of `count` tensors of [B, T, heads, width] in dtype; y[i] may be x[i] itself, or lies
- *              apart from it.
+ *   x, y       arrays (HOST) of `count` tensors of [B, T, heads, width] in dtype; y[i] may be x[i] itself (with its
+ *              strides), else it lies apart from x and the other y.
  *   positions  [B, T], position_bytes 4 (int32) or 8 (int64); any values.
  *   freqs      [part / 2] radians a position, fp64 (any finite values).
  * An angle is formed to 2^-31 of a turn, whatever the position; products and sums are fp32, rounded once.
@@ -101,9 +101,9 @@ CCQ_API ccq_status ccq_rotary(const ccq_heads *x, const ccq_heads *y, int count,
  *   q, k, v    [B, T, heads, d] in dtype, d 64 or 128; each may have fewer heads than H, a divisor of it: head h then
  *              reads head h / (H / heads).
  *   log_decay  [H] fp32, <= 0 (-inf: nothing is kept); a constant of the layer, without a gradient.
- *   S0         [num_seqs, H, d, d] fp32, or NULL (0): the states before the first tokens.
+ *   S0         [num_seqs, H, d, d] fp32, 16-byte aligned as all states, or NULL (0): the states before the first tokens.
  *   o          [B, T, H, d] in dtype, apart from the inputs.
- *   ST         [num_seqs, H, d, d] fp32, or NULL: the states after the last tokens.  May be S0.
+ *   ST         [num_seqs, H, d, d] fp32, or NULL: the states after the last tokens.  May be S0, else apart from it.
  *   cu         NULL: B sequences of T tokens (num_seqs = B).  Else B = 1 and sequence s is the tokens cu[s] to
  *              cu[s + 1] (a device array of num_seqs + 1, cu_bytes 4 or 8; 0 <= cu[s] <= cu[s + 1] <= T).
  *              Tokens of no sequence are left as they are in o.  An offset outside its range is held to it
@@ -111,8 +111,9 @@ CCQ_API ccq_status ccq_rotary(const ccq_heads *x, const ccq_heads *y, int count,
  *   workspace  ccq_decay_attention_workspace_size() bytes, 16-byte aligned (NULL where that is 0).
  * fp32 inputs, and bf16 ones whose addresses or strides are not multiples of 16 bytes, are computed in fp32.  Other
  * bf16 inputs run on the tensor cores in chunks of 128 tokens: the products of a chunk's queries and keys and the state
- * that its queries read are rounded to bf16, the state itself is carried to 2^-17 of its terms.  There a value that is not finite
- * also reaches the outputs of the other tokens of its chunk.
+ * that its queries read are rounded to bf16.  The state itself is summed in fp32, of terms in 24 bits where a state is handed
+ * out (ST, dS0), else within 2^-17 of them.  There a value that is not finite also reaches the outputs of the other tokens of
+ * its chunk.
  */
 CCQ_API ccq_status ccq_decay_attention(const ccq_heads *q, const ccq_heads *k, const ccq_heads *v,
                                        ccq_dtype dtype, const float *log_decay, float scale,
@@ -123,9 +124,9 @@ CCQ_API ccq_status ccq_decay_attention(const ccq_heads *q, const ccq_heads *k, c
 /*
  * Gradients of ccq_decay_attention for a given dout [B, T, H, d] and, where it is not NULL, dST [num_seqs, H, d, d].
  * Nothing is kept from the forward.
- *   dq, dk, dv [B, T, heads, d] in dtype with the heads of q, k and v, apart from the inputs: a head that
- *              several read gets their sum (formed in fp32, in ascending order).
- *   dS0        [num_seqs, H, d, d] fp32, or NULL.  Apart from dST.
+ *   dq, dk, dv [B, T, heads, d] in dtype with the heads of q, k and v, apart from the inputs and each other: a head
+ *              that several read gets their sum (formed in fp32, in ascending order).
+ *   dS0        [num_seqs, H, d, d] fp32, or NULL.  Apart from S0 and dST.
  *   workspace  ccq_decay_attention_bwd_workspace_size() bytes, 16-byte aligned (NULL where that is 0).
  */
 CCQ_API ccq_status ccq_decay_attention_bwd(const ccq_heads *q, const ccq_heads *k, const ccq_heads *v,
@@ -147,11 +148,11 @@ CCQ_API ccq_status ccq_decay_attention_bwd_workspace_size(int64_t B, int64_t T, 
 /*
  * One token of every sequence of a batch, in place: state = g state + k v^T, o = scale state^T q, in fp32.
  *   q, k, v    [B, heads, d] in dtype (the token stride is not looked at), heads as above.
- *   state      [rows, H, d, d] fp32.
+ *   state      [rows, H, d, d] fp32, 16-byte aligned.
  *   slots      NULL (row b's state is b; rows >= B), or [B] with slot_bytes 4 or 8: the row of `state` of each.  A
  *              negative one is a batch row without a sequence: its o is 0.  One that is not below `rows`, or
  *              that an earlier batch row has, gives a zero row, changes no state and leaves CCQ_ERR_INDEX.
- *   o          [B, H, d] in dtype.
+ *   o          [B, H, d] in dtype, apart from the inputs.
  */
 CCQ_API ccq_status ccq_decay_attention_step(const ccq_heads *q, const ccq_heads *k, const ccq_heads *v,
                                             ccq_dtype dtype, const float *log_decay, float scale,

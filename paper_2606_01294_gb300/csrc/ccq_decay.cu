@@ -441,6 +441,13 @@ ccq_status check_common(ccq_dtype dtype, const float *log_decay, float scale, in
     return op_pointer("cu", cu, cu_bytes);
 }
 
+// States that a call reads while it writes others: apart, or (with `same`) the same ones.
+ccq_status check_states_apart(const char *in, const float *read, const char *out, const float *written, size_t bytes, bool same) {
+    if (!read || !written || !bytes || (same && read == written)) return CCQ_OK;
+    const uintptr_t r = reinterpret_cast<uintptr_t>(read), w = reinterpret_cast<uintptr_t>(written);
+    return (r < w ? w - r : r - w) < bytes ? op_fail(CCQ_ERR_INVALID_ARG, "%s overlaps %s", out, in) : CCQ_OK;
+}
+
 ccq_status check_state(const char *name, const float *p) {
     return p ? op_pointer(name, p, 16) : CCQ_OK;
 }
@@ -525,6 +532,8 @@ ccq_status ccq_decay_attention(const ccq_heads *q, const ccq_heads *k, const ccq
     if (need && (st = op_pointer("workspace", workspace, 16)) != CCQ_OK) return st;
     if (workspace_bytes < need)
         return op_fail(CCQ_ERR_INVALID_ARG, "workspace of %zu bytes, needs %zu", workspace_bytes, need);
+    const size_t state_bytes = static_cast<size_t>(num_seqs) * H * d * d * 4;
+    if ((st = check_states_apart("S0", S0, "ST", ST, state_bytes, true)) != CCQ_OK) return st;
     if (num_seqs == 0) return CCQ_OK;
     if ((st = op_status_word(&a.status)) != CCQ_OK) return st;
     a.passes = 1;
@@ -609,6 +618,12 @@ ccq_status ccq_decay_attention_bwd(const ccq_heads *q, const ccq_heads *k, const
     if (need && (st = op_pointer("workspace", workspace, 16)) != CCQ_OK) return st;
     if (workspace_bytes < need)
         return op_fail(CCQ_ERR_INVALID_ARG, "workspace of %zu bytes, needs %zu", workspace_bytes, need);
+    for (int i = 0; i < 3 && B * T; ++i)
+        if (out[i]->p == out[(i + 1) % 3]->p)
+            return op_fail(CCQ_ERR_INVALID_ARG, "%s is %s", outs[(i + 1) % 3], outs[i]);
+    const size_t state_bytes = static_cast<size_t>(num_seqs) * H * d * d * 4;
+    if ((st = check_states_apart("S0", S0, "dS0", dS0, state_bytes, false)) != CCQ_OK) return st;
+    if ((st = check_states_apart("dST", dST, "dS0", dS0, state_bytes, false)) != CCQ_OK) return st;
     if (num_seqs == 0) return CCQ_OK;
     if ((st = op_status_word(&a.status)) != CCQ_OK) return st;
     a.passes = 3;

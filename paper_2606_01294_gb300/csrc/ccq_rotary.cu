@@ -229,6 +229,13 @@ ccq_status ccq_rotary(const ccq_heads *x, const ccq_heads *y, int count, ccq_dty
     if (B * T == 0) return CCQ_OK;
     if ((st = op_pointer("positions", positions, position_bytes)) != CCQ_OK) return st;
     if ((st = op_pointer("freqs", freqs, 8)) != CCQ_OK) return st;
+    for (int i = 0; i < count; ++i) {
+        if (x[i].p == y[i].p && ((B > 1 && x[i].batch != y[i].batch) || (T > 1 && x[i].token != y[i].token) ||
+                                 (x[i].heads > 1 && x[i].head != y[i].head)))
+            return op_fail(CCQ_ERR_INVALID_ARG, "y[%d] is x[%d] with other strides", i, i);
+        if (count == 2 && (y[i].p == x[1 - i].p || y[0].p == y[1].p))
+            return op_fail(CCQ_ERR_INVALID_ARG, "y[%d] is %s[%d]", i, y[i].p == x[1 - i].p ? "x" : "y", 1 - i);
+    }
     a.heads = static_cast<int>(heads);
     a.tokens = B * T;
     a.T = T;

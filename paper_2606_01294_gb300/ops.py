@@ -258,8 +258,10 @@ def _is_dense(shape, stride):
 @functools.lru_cache(maxsize=512)
 def _rotary_plan(q, k, positions, freqs):
     (dtype, shape, _), (kdtype, kshape, _) = q, k
+    if len(shape) not in (3, 4) or len(kshape) != len(shape):
+        return None
     xq, xk = _strides(*q[1:]), _strides(*k[1:])
-    if (len(shape) not in (3, 4) or len(kshape) != len(shape) or kdtype != dtype or dtype not in _CODE or not xq or not xk
+    if (kdtype != dtype or dtype not in _CODE or not xq or not xk
             or kshape[:-2] != shape[:-2] or kshape[-1] != shape[-1] or positions[0] not in _INDEX or positions[1] != shape[:-2]
             or not _is_dense(*positions[1:]) or freqs[0] is not torch.float64 or not _is_dense(*freqs[1:])):
         return None

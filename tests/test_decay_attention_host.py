@@ -128,7 +128,7 @@ def test_status_word_is_required(lib):
         pytest.skip("a device resolves the status word")
     a = attention()
     assert lib.ccq_decay_attention(*a.values()) == ccq.CCQ_ERR_CUDA and b"status word" in lib.ccq_last_error()
-    step = (heads(), heads(), heads(), 1, FAKE, 0.1, FAKE, 9, None, 8, heads(), 5, 4, 64, None)
+    step = (heads(), heads(), heads(), 1, FAKE, 0.1, FAKE, 9, None, 8, heads(FAKE * 2), 5, 4, 64, None)
     assert lib.ccq_decay_attention_step(*step) == ccq.CCQ_ERR_CUDA and b"status word" in lib.ccq_last_error()
 
 
@@ -199,3 +199,37 @@ def test_frequencies():
                 dict(part=8, factor=2.0, scaling="yarn", fast=1.0, slow=2.0), dict(part=8, factor=math.inf, scaling="linear")):
         with pytest.raises(ValueError):
             ops.rotary_frequencies(bad.pop("part"), device="cpu", **bad)
+
+
+def test_outputs_that_another_block_still_reads_are_refused(lib):
+    """Outputs on top of inputs or each other, where blocks that run at the same time would read what others have written."""
+    big = 2 * 4 * 128 * 128 * 4  # bytes of the states
+    good = dict(attention(), S0=FAKE * 16)
+    for off in (16, -16, big - 16, 16 - big):
+        refused(lib, lib.ccq_decay_attention, good, INVALID, b"ST overlaps S0", ST=FAKE * 16 + off)
+    a = attention()
+    good = dict(q=a["q"], k=a["k"], v=a["v"], dtype=0, ld=FAKE, scale=0.1, S0=FAKE * 32, do=heads(), dST=FAKE * 64, dq=heads(FAKE * 2),
+                dk=heads(FAKE * 3), dv=heads(FAKE * 4, n=2), dS0=FAKE * 128, B=2, T=32, H=4, d=128, cu=None, cb=8, n=2, ws=FAKE,
+                nbytes=1 << 30, stream=None)
+    for text, ch in ((b"dS0 overlaps S0", dict(dS0=FAKE * 32)), (b"dS0 overlaps S0", dict(dS0=FAKE * 32 + big - 16)),
+                     (b"dS0 overlaps dST", dict(dS0=FAKE * 64 + 16)), (b"dk is dq", dict(dk=heads(FAKE * 2))),
+                     (b"dv is dk", dict(dv=heads(FAKE * 3, n=2))), (b"dq is dv", dict(dq=heads(FAKE * 4)))):
+        refused(lib, lib.ccq_decay_attention_bwd, good, INVALID, text, **ch)
+    step = dict(q=heads(), k=heads(FAKE * 2), v=heads(FAKE * 3, n=1), dtype=1, ld=FAKE, scale=0.1, state=FAKE, rows=9, slots=FAKE, sb=8,
+                o=heads(), B=5, H=4, d=64, stream=None)
+    for name, at in (("q", 1), ("k", 2), ("v", 3)):
+        refused(lib, lib.ccq_decay_attention_step, step, INVALID, b"o is " + name.encode(), o=heads(FAKE * at))
+    rotary = dict(x=heads() + heads(FAKE * 2), y=heads() + heads(FAKE * 2), count=2, dtype=0, B=2, T=32, width=128, part=64, positions=FAKE,
+                  pb=8, freqs=FAKE, amplitude=1.0, inter=0, inverse=0, stream=None)
+    for text, y in ((b"other strides", heads(token=1024, batch=1 << 15) + heads(FAKE * 2)), (b"is x[1]", heads(FAKE * 2) + heads(FAKE * 3)),
+                    (b"is x[0]", heads(FAKE * 3) + heads()), (b"is y[1]", heads(FAKE * 3) + heads(FAKE * 3))):
+        refused(lib, lib.ccq_rotary, rotary, INVALID, text, y=y)
+
+
+def test_plans_of_tensors_without_heads_are_none():
+    """(the call then goes the way that says what is wrong with them)"""
+    one, two = (torch.bfloat16, torch.Size([4]), (1,)), (torch.bfloat16, torch.Size([4, 2, 64]), (128, 64, 1))
+    pos, freqs = (torch.int64, torch.Size([4]), (1,)), (torch.float64, torch.Size([32]), (1,))
+    assert ops._rotary_plan(two, two, pos, freqs) is not None
+    for q, k in ((one, one), (one, two), (two, one)):
+        assert ops._rotary_plan(q, k, pos, freqs) is None
