@@ -103,7 +103,7 @@ __device__ __forceinline__ int decay_longest_first(const DecayArgs &a, int rank,
     return scratch[kRanked];
 }
 
-// The logarithm of a head's decay g, and log2 g as two floats.  A decay below 2^-200 keeps nothing in fp32 either way (and
+// The logarithm of a head's decay g, and log2 g as two floats.  A decay below 2^-199 keeps nothing in fp32 either way (and
 // -inf would give NaN as g^0).
 struct DecayLog {
     float natural, hi, lo;
