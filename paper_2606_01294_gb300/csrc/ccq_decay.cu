@@ -383,29 +383,46 @@ struct Cost {
     int resident;        // CTAs the GPU holds
 };
 
-int plan_segments(int64_t B, int64_t T, int H, int d, int64_t num_seqs, ccq_dtype dtype, int passes) {
-    if (num_seqs < 1 || B * T < 1) return 1;
+struct Plan {
+    int segments = 1, pairs = 0, pass = 0;  // DecayArgs' segments, split_pairs and split_pass
+};
+
+Plan plan_segments(int64_t B, int64_t T, int H, int d, int64_t num_seqs, ccq_dtype dtype, int passes) {
+    Plan best;
+    if (num_seqs < 1 || B * T < 1) return best;
     const bool cores = dtype == CCQ_BF16;
     const Cost c = cores ? Cost{128, d == 128 ? 3.45 : 2.4, d == 128 ? 4.0 : 2.8, 6.0, sm_count_now()}
                          : Cost{kC, d == 128 ? 12.0 : 8.5, d == 128 ? 5.0 : 3.5, 6.0, 2 * sm_count_now()};
     const int64_t ctas = num_seqs * H * (cores ? 1 : d / kN), blocks = (B * T / num_seqs + c.block - 1) / c.block;
     const int64_t kinds = passes > 1 ? 2 : 1;
     auto rounds = [&](int64_t n) { return static_cast<double>((n + c.resident - 1) / c.resident); };
-    int best = 1;
     double least = rounds(ctas * passes) * static_cast<double>(blocks) * c.main;
     for (int s = 2; s <= 64 && s <= blocks / 2; ++s) {
         const double per = static_cast<double>((blocks + s - 1) / s);
         const double t = rounds(ctas * passes * s) * per * c.main + rounds(ctas * kinds * (s - 1)) * per * c.parts + c.launch;
         if (t < least) {
             least = t;
-            best = s;
+            best = {s, static_cast<int>(num_seqs * H), 0};
         }
     }
+    // Full rounds of whole passes, and of what is left over (of the gradients dk and dv, which start from the same states) segments
+    // that fit beside their parts' launch into the last one.  Packed sequences are not of one length, and their short ones come last.
+    const int64_t all = ctas * passes, full = all / c.resident, rest = all % c.resident;
+    const int64_t split = passes > 1 ? passes - 1 : 1, pairs = (rest + split - 1) / split;
+    if (cores && num_seqs == B && full && rest)
+        for (int s = 2; s <= 64 && s <= blocks / 2 && pairs * (split * s + s - 1) <= c.resident; ++s) {
+            const double per = static_cast<double>((blocks + s - 1) / s);
+            const double t = static_cast<double>(full * blocks) * c.main + per * std::max(c.main, c.parts) + c.launch;
+            if (t < least) {
+                least = t;
+                best = {s, static_cast<int>(pairs), static_cast<int>(passes - split)};
+            }
+        }
     return best;
 }
 
-size_t parts_bytes(int64_t num_seqs, int H, int d, int segments, int kinds) {
-    return segments > 1 ? static_cast<size_t>(kinds) * num_seqs * H * segments * d * d * 4 : 0;
+size_t parts_bytes(const Plan &p, int d, int kinds) {
+    return p.segments > 1 ? static_cast<size_t>(kinds) * p.pairs * p.segments * d * d * 4 : 0;
 }
 
 ccq_status check_sizes(int64_t B, int64_t T, int H, int d, int64_t num_seqs) {
@@ -467,8 +484,15 @@ bool steps(const ccq_heads &x, int64_t B, int64_t T) {
            (x.heads <= 1 || x.head <= most);
 }
 
-ccq_status run_passes(DecayArgs &a, ccq_dtype dtype, bool cores, int64_t B, unsigned parts_mask, cudaStream_t s) {
+// parts_mask: the passes whose states the segments start from.
+ccq_status run_passes(DecayArgs &a, const Plan &plan, ccq_dtype dtype, bool cores, int64_t B, unsigned parts_mask, cudaStream_t s) {
     cudaError_t e = cudaSuccess;
+    a.segments = 1;
+    if (cores || plan.pairs == a.sequences * a.H) {  // (decay_block_kernel splits all or nothing)
+        a.segments = plan.segments;
+        a.split_pairs = plan.pairs;
+        a.split_pass = plan.pass;
+    }
     for (int i = 0; i < a.passes; ++i) a.exact_state |= a.pass[i].state_out != nullptr;
     auto run = [&](const DecayArgs &x) { return cores ? launch_decay_chunks(x, B, s) : launch_decay_blocks(x, dtype, s); };
     if (a.segments > 1) {
@@ -476,7 +500,7 @@ ccq_status run_passes(DecayArgs &a, ccq_dtype dtype, bool cores, int64_t B, unsi
         p.parts_only = 1;
         p.passes = 0;
         for (int i = 0; i < a.passes; ++i)
-            if (parts_mask >> i & 1) p.pass[p.passes++] = a.pass[i];
+            if (parts_mask >> i & 1 && i >= a.split_pass) p.pass[p.passes++] = a.pass[i];
         e = run(p);
     }
     if (e == cudaSuccess) e = run(a);
@@ -504,7 +528,7 @@ ccq_status ccq_decay_attention_workspace_size(int64_t B, int64_t T, int H, int d
     ccq_status st = check_sizes(B, T, H, d, num_seqs);
     if (st != CCQ_OK) return st;
     if (!bytes) return op_fail(CCQ_ERR_INVALID_ARG, "bytes is NULL");
-    *bytes = parts_bytes(num_seqs, H, d, plan_segments(B, T, H, d, num_seqs, dtype, 1), 1);
+    *bytes = parts_bytes(plan_segments(B, T, H, d, num_seqs, dtype, 1), d, 1);
     return CCQ_OK;
 }
 
@@ -530,8 +554,8 @@ ccq_status ccq_decay_attention(const ccq_heads *q, const ccq_heads *k, const ccq
     if ((st = check_state("S0", S0)) != CCQ_OK) return st;
     if ((st = check_state("ST", ST)) != CCQ_OK) return st;
     DecayArgs a = {};
-    a.segments = plan_segments(B, T, H, d, num_seqs, dtype, 1);
-    const size_t need = parts_bytes(num_seqs, H, d, a.segments, 1);
+    const Plan plan = plan_segments(B, T, H, d, num_seqs, dtype, 1);
+    const size_t need = parts_bytes(plan, d, 1);
     if (need && (st = op_pointer("workspace", workspace, 16)) != CCQ_OK) return st;
     if (workspace_bytes < need)
         return op_fail(CCQ_ERR_INVALID_ARG, "workspace of %zu bytes, needs %zu", workspace_bytes, need);
@@ -563,7 +587,7 @@ ccq_status ccq_decay_attention(const ccq_heads *q, const ccq_heads *k, const ccq
     a.vec = access == 16;
     const bool cores = dtype == CCQ_BF16 && a.vec && B * T > 0 && steps(*q, B, T) && steps(*k, B, T) && steps(*v, B, T) &&
                        steps(*o, B, T);
-    return run_passes(a, dtype, cores, B, 1u, static_cast<cudaStream_t>(stream));
+    return run_passes(a, plan, dtype, cores, B, 1u, static_cast<cudaStream_t>(stream));
 }
 
 ccq_status ccq_decay_attention_bwd_workspace_size(int64_t B, int64_t T, int H, int q_heads, int k_heads, int v_heads, int d,
@@ -577,7 +601,7 @@ ccq_status ccq_decay_attention_bwd_workspace_size(int64_t B, int64_t T, int H, i
         shared += heads < H;
     }
     if (!bytes) return op_fail(CCQ_ERR_INVALID_ARG, "bytes is NULL");
-    *bytes = parts_bytes(num_seqs, H, d, plan_segments(B, T, H, d, num_seqs, dtype, 3), 2) +
+    *bytes = parts_bytes(plan_segments(B, T, H, d, num_seqs, dtype, 3), d, 2) +
              shared * static_cast<size_t>(B * T) * H * d * 4;
     return CCQ_OK;
 }
@@ -615,8 +639,8 @@ ccq_status ccq_decay_attention_bwd(const ccq_heads *q, const ccq_heads *k, const
     if ((st = check_state("dS0", dS0)) != CCQ_OK) return st;
     if (dS0 && dS0 == dST) return op_fail(CCQ_ERR_INVALID_ARG, "dS0 is dST: both are in use at once");
     DecayArgs a = {};
-    a.segments = plan_segments(B, T, H, d, num_seqs, dtype, 3);
-    const size_t states = parts_bytes(num_seqs, H, d, a.segments, 2);
+    const Plan plan = plan_segments(B, T, H, d, num_seqs, dtype, 3);
+    const size_t states = parts_bytes(plan, d, 2);
     const size_t rows = static_cast<size_t>(B * T) * H * d * 4, need = states + shared * rows;
     if (need && (st = op_pointer("workspace", workspace, 16)) != CCQ_OK) return st;
     if (workspace_bytes < need)
@@ -686,7 +710,7 @@ ccq_status ccq_decay_attention_bwd(const ccq_heads *q, const ccq_heads *k, const
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     bool cores = dtype == CCQ_BF16 && a.vec && B * T > 0;
     for (int i = 0; i < 4; ++i) cores = cores && steps(*in[i], B, T) && (i > 2 || steps(*out[i], B, T));
-    if ((st = run_passes(a, dtype, cores, B, 5u, s)) != CCQ_OK || !sum.count || !(B * T)) return st;
+    if ((st = run_passes(a, plan, dtype, cores, B, 5u, s)) != CCQ_OK || !sum.count || !(B * T)) return st;
     sum.H = H;
     sum.d = d;
     sum.rows = B * T;

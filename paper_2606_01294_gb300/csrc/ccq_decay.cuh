@@ -52,7 +52,10 @@ struct DecayArgs {
     // Segments of a sequence, in the order of a pass.  With more than one, a launch with parts_only = 1 leaves in
     // parts[kind][sequence][H][segments][d][d] first the pass's state_in, then what each segment but the last adds to a
     // state from zero, and the segments of the second launch start from these (state_out may be state_in for that reason).
+    // Passes from split_pass on of the last split_pairs (sequence, head) pairs run in segments, everything else whole; parts are
+    // those of these pairs.
     int segments;
+    int split_pairs, split_pass;
     float *parts;
     int parts_only;
     int exact_state;    // a pass hands its states out
@@ -133,7 +136,8 @@ __device__ __forceinline__ float2 decay_keep(const DecayLog &l, int n) {
 
 // Where the state of (sequence, head, segment) lies among the parts.
 __device__ __forceinline__ int64_t decay_part(const DecayArgs &a, int kind, int sequence, int h, int segment) {
-    return (((static_cast<int64_t>(kind) * a.sequences + sequence) * a.H + h) * a.segments + segment) * a.d * a.d;
+    const int64_t pair = static_cast<int64_t>(sequence) * a.H + h - (static_cast<int64_t>(a.sequences) * a.H - a.split_pairs);
+    return ((static_cast<int64_t>(kind) * a.split_pairs + pair) * a.segments + segment) * a.d * a.d;
 }
 
 cudaError_t launch_decay_chunks(const DecayArgs &a, int64_t B, cudaStream_t s);  // bf16 on the tensor cores

@@ -137,6 +137,17 @@ template <int N> __device__ __forceinline__ void more_registers() {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
 }
 
+// One thread of a warp that runs together.  (The compiler then knows of one thread and keeps what it issues in uniform registers:
+// gradients of 3 x 4096 tokens, 16 heads of 64 90 us with `lane == 0`, 79 so.)
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p;
+}
+
+// Lets the launch after this one start where SMs are free.
+__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // The place of the next half of K in its ring of three.
 struct Ring {
     int slot = 0;
@@ -181,20 +192,25 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
     float2 *keeps = reinterpret_cast<float2 *>(sm + M::kMisc + 8);  // g^128 and g^n of the ragged chunk, as two floats
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    unsigned x = blockIdx.x;
-    const int pi = x % a.passes;
-    x /= a.passes;
-    const int nseg = PARTS ? a.segments - 1 : a.segments;
-    const int segment = x % nseg;
-    x /= nseg;
-    const int h = x % a.H, sequence = decay_longest_first(a, x / a.H, reinterpret_cast<int *>(table));
+    // What this CTA walks: a pass over a whole sequence, or a segment of one (these come last, and wait for their parts alone).
+    const unsigned whole_pairs = static_cast<unsigned>(a.sequences) * a.H - a.split_pairs, whole = whole_pairs * a.passes,
+                   whole_too = whole + static_cast<unsigned>(a.split_pairs) * a.split_pass;
+    const bool all = !PARTS && blockIdx.x < whole, cut = PARTS || blockIdx.x >= whole_too;
+    const int segments = cut ? a.segments : 1;
+    const unsigned first_pass = !PARTS && cut ? a.split_pass : 0,
+                   passes = cut ? a.passes - first_pass : all ? a.passes : a.split_pass;
+    const unsigned x = blockIdx.x - (PARTS || all ? 0 : cut ? whole_too : whole), y = x / passes;
+    const unsigned nseg = PARTS ? segments - 1 : segments;
+    const unsigned pi = first_pass + x % passes, segment = y % nseg, pair = y / nseg + (all ? 0 : whole_pairs);
+    if (PARTS) grid_release();  // (the launch after this one has work beside it)
+    const int h = pair % a.H, sequence = decay_longest_first(a, pair / a.H, reinterpret_cast<int *>(table));
     const DecayPass &ps = a.pass[pi];
     const ChunkMapsOf &mp = maps.pass[pi];
     const bool down = ps.descending != 0;
     const DecaySpan span = decay_span(a, sequence);
     const int length = static_cast<int>(span.length);
-    const int chunks = (length + kC - 1) / kC, per = (chunks + a.segments - 1) / a.segments;
-    const int first = min(per * segment, chunks), count = min(first + per, chunks) - first;
+    const int chunks = (length + kC - 1) / kC, per = (chunks + segments - 1) / segments;
+    const int first = min(per * static_cast<int>(segment), chunks), count = min(first + per, chunks) - first;
     const int ragged = length - (chunks - 1) * kC;  // tokens of the sequence's last chunk
     const DecayLog l2 = decay_log2(a.log_decay, h);
     // chunk r of the segment: its first token within the sequence, its tokens
@@ -217,7 +233,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
         fence_barrier_init();
     }
     if (warp == 0) tmem_alloc(tmem_slot, kTmemCols);
-    grid_wait();  // (the segments' parts)
+    if (segments > 1) grid_wait();  // (the segments' parts)
     if (a.cu) __syncthreads();  // (the ranks' place becomes the table's)
     if (!PARTS && tid < 256) table[tid] = tid < 127 ? 0.f : ps.p_scale * decay_power(l2, tid - 127);
     if (tid >= 256 && tid <= 256 + kC) powers[tid - 256] = ps.k_scale * decay_power(l2, tid - 256);
@@ -299,7 +315,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
 #pragma unroll
         for (int c = 0; c < kCols / 2; ++c) S[c] = 0;
         const int64_t matrix = (static_cast<int64_t>(sequence) * a.H + h) * D * D;
-        if (a.segments == 1 || (PARTS && segment == 0)) {
+        if (segments == 1 || (PARTS && segment == 0)) {
             if (ps.state_in) add(ps.state_in + matrix, ps.transposed, 0.f);
             if (PARTS) {
                 put(a.parts + decay_part(a, ps.kind, sequence, h, 0));
@@ -307,7 +323,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
                 for (int c = 0; c < kCols / 2; ++c) S[c] = 0;
             }
         } else if (!PARTS) {
-            for (int g = 0; g <= segment; ++g) {
+            for (int g = 0; g <= static_cast<int>(segment); ++g) {
                 const int lo = min(per * (g - 1), chunks), hi = min(per * g, chunks);  // segment g - 1
                 int n = 0;
                 if (g > 0 && hi > lo) n = (hi - lo) * kC - ((down ? lo == 0 : hi == chunks) ? kC - ragged : 0);
@@ -374,7 +390,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
         if (count) advance(count - 1);
         if (PARTS)
             put(a.parts + decay_part(a, ps.kind, sequence, h, segment + 1));
-        else if (ps.state_out && segment == a.segments - 1)
+        else if (ps.state_out && static_cast<int>(segment) == segments - 1)
             put(ps.state_out + matrix);
     } else if (warp < kOWarp0) {
         // ============================================================ W
@@ -506,7 +522,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
         if (storer) tma_store_wait_all();
     } else {
         fewer_registers<kOtherRegs>();
-        if (warp == kIssueWarp && lane == 0) {
+        if (warp == kIssueWarp && elect_one()) {
             // ======================================================== ISSUE: Q K^T, Q S, P V
             constexpr uint32_t kQK = make_idesc(kC, kC, 0, 0), kQKHalf = make_idesc(kC, 64, 0, 0), kQS = make_idesc(kC, D, 0, 0),
                                kPV = make_idesc(kC, D, 0, 1);
@@ -556,7 +572,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
                 mma_commit(&bar[BAR_O2]);
                 for (int j = 0; j < 2; ++j) mma_commit(&bar[BAR_VFREE + j]);
             }
-        } else if (warp == kIssueWWarp && lane == 0) {
+        } else if (warp == kIssueWWarp && elect_one()) {
             // ======================================================== ISSUE: V^T W, beside the other products
             constexpr uint32_t kWV = make_idesc(D, D, 1, 1);
             for (int r = 0; r < count; ++r) {
@@ -580,7 +596,7 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
                 }
                 mma_commit(&bar[BAR_D]);
             }
-        } else if (warp == kLoadWarp && lane == 0) {
+        } else if (warp == kLoadWarp && elect_one()) {
             // ======================================================== LOAD
             const int hq = h / ps.q.share, hk = h / ps.k.share, hv = h / ps.v.share, b = static_cast<int>(span.b);
             auto load = [&](const CUtensorMap *map, uint32_t to, uint32_t block, uint32_t apart, uint64_t *full, int head, int token) {
@@ -647,9 +663,11 @@ template <int D, bool PARTS, int TERMS, bool SUMS> cudaError_t launch(const Deca
     constexpr int kBytes = Map<D>::kBytes;
     cudaError_t e = allow_shared<decay_chunk_kernel<D, PARTS, TERMS, SUMS>>(kBytes);
     if (e != cudaSuccess) return e;
-    const int64_t grid = static_cast<int64_t>(PARTS ? a.segments - 1 : a.segments) * a.H * a.sequences * a.passes;
+    const int64_t pairs = static_cast<int64_t>(a.H) * a.sequences, split = a.split_pairs;
+    const int64_t grid = PARTS ? split * (a.segments - 1) * a.passes
+                               : (pairs - split) * a.passes + split * (a.split_pass + (a.passes - a.split_pass) * a.segments);
     if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-    if (!PARTS && a.segments > 1)
+    if (!PARTS && split)
         return launch_after(decay_chunk_kernel<D, PARTS, TERMS, SUMS>, static_cast<unsigned>(grid), kThreads, kBytes, s, m, a);
     decay_chunk_kernel<D, PARTS, TERMS, SUMS><<<static_cast<unsigned>(grid), kThreads, kBytes, s>>>(m, a);
     return cudaGetLastError();
