@@ -78,6 +78,7 @@ __device__ __forceinline__ void copy_rows(float (*dst)[STRIDE], const DecayView 
 template <typename T, int D, bool ASYNC>
 __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a) {
     constexpr int kBuffers = ASYNC ? 2 : 1;
+    if (a.parts_only) grid_release();  // (the launch after this one forms its tables and loads its first blocks meanwhile)
     extern __shared__ float4 shared_raw[];
     BlockShared<D, kBuffers> &sh = *reinterpret_cast<BlockShared<D, kBuffers> *>(shared_raw);
     constexpr int kSlices = D / kN;
@@ -107,6 +108,21 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
     if (a.cu) __syncthreads();  // (the ranks' place becomes the first block's)
     // tokens of block j in the pass's order: the ragged block is the sequence's last
     auto block_begin = [&](int64_t j) { return (down ? blocks - 1 - j : j) * kC; };
+
+    auto tokens_of = [&](int64_t begin) { return static_cast<int>(min(static_cast<int64_t>(kC), span.length - begin)); };
+    auto copy = [&](int64_t j) {
+        if constexpr (ASYNC) {
+            const int64_t begin = block_begin(j);
+            const int n = tokens_of(begin);
+            auto &to = sh.in[j & 1];
+            copy_rows<D>(to.k, ps.k, span.b, span.begin + begin, n, h, 0);
+            copy_rows<kN>(to.v, ps.v, span.b, span.begin + begin, n, h, c0);
+            if (!a.parts_only) copy_rows<D>(to.q, ps.q, span.b, span.begin + begin, n, h, 0);
+            copy_commit();
+        }
+    };
+    if (first < last) copy(first);
+    if (a.segments > 1 && !a.parts_only) grid_wait();  // (the segments' parts)
 
     // ---- the state at the segment's start; this thread's rows R ty .. and columns 4 tx ..
     float S[R][4];
@@ -152,19 +168,6 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
         }
     }
 
-    auto tokens_of = [&](int64_t begin) { return static_cast<int>(min(static_cast<int64_t>(kC), span.length - begin)); };
-    auto copy = [&](int64_t j) {
-        if constexpr (ASYNC) {
-            const int64_t begin = block_begin(j);
-            const int n = tokens_of(begin);
-            auto &to = sh.in[j & 1];
-            copy_rows<D>(to.k, ps.k, span.b, span.begin + begin, n, h, 0);
-            copy_rows<kN>(to.v, ps.v, span.b, span.begin + begin, n, h, c0);
-            if (!a.parts_only) copy_rows<D>(to.q, ps.q, span.b, span.begin + begin, n, h, 0);
-            copy_commit();
-        }
-    };
-    if (first < last) copy(first);
     for (int64_t j = first; j < last; ++j) {
         const int64_t begin = block_begin(j);
         const int n = tokens_of(begin);
@@ -191,7 +194,7 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
         if (!a.parts_only) {
             // P: rows 2 ty, 2 ty + 1, columns tx + 8 c
             float p[2][4] = {};
-#pragma unroll 2
+#pragma unroll 4
             for (int e = 0; e < D; e += 4) {
                 float4 qv[2], kv[4];
 #pragma unroll
@@ -215,7 +218,7 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
             __syncthreads();
             // O: rows 2 ty, 2 ty + 1, columns 4 tx .. 4 tx + 3
             float o[2][4] = {};
-#pragma unroll 2
+#pragma unroll 4
             for (int e = 0; e < D; e += 4) {
                 float4 qv[2];
 #pragma unroll
@@ -281,7 +284,7 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int c = 0; c < 4; ++c) S[r][c] = fmaf(S[r][c], keep.x, S[r][c] * keep.y);
-#pragma unroll 2
+#pragma unroll 4
         for (int jj = 0; jj < n; ++jj) {
             const float u = sh.power[down ? jj + 1 : n - 1 - jj] * ps.k_scale;
             float4 vv = *reinterpret_cast<const float4 *>(&in.v[jj][4 * tx]);
@@ -321,6 +324,8 @@ template <typename T, int D, bool ASYNC> cudaError_t launch_blocks(const DecayAr
     if (e != cudaSuccess) return e;
     const int64_t grid = static_cast<int64_t>(D / kN) * (a.parts_only ? a.segments - 1 : a.segments) * a.H * a.sequences * a.passes;
     if (grid > 0x7fffffff) return cudaErrorInvalidValue;
+    if (a.segments > 1 && !a.parts_only)
+        return launch_after(decay_block_kernel<T, D, ASYNC>, static_cast<unsigned>(grid), kThreads, kBytes, s, a);
     decay_block_kernel<T, D, ASYNC><<<static_cast<unsigned>(grid), kThreads, kBytes, s>>>(a);
     return cudaGetLastError();
 }
@@ -341,10 +346,12 @@ struct SumArgs {
 // out[row, head, c] = sum over the heads that read it, in ascending order; one thread four channels.  Bound by HBM and L2: parts of
 // 3 x 1501 tokens, 16 heads of 64 twice (37 MB) 11 us.
 template <typename T> __global__ void __launch_bounds__(256) decay_sum_kernel(const SumArgs a, int vec) {
-    const int which = blockIdx.y;
+    const int which = blockIdx.x % a.count;
+    grid_wait();  // (the passes' parts)
     const int share = a.share[which], heads = a.H / share, quads = a.d / 4;
     const int64_t total = a.rows * heads * quads;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+    const int64_t step = gridDim.x / a.count * 256ll;
+    for (int64_t i = blockIdx.x / a.count * 256ll + threadIdx.x; i < total; i += step) {
         const int c = static_cast<int>(i % quads) * 4;
         const int64_t r = i / quads;
         const int h = static_cast<int>(r % heads);
@@ -715,12 +722,10 @@ ccq_status ccq_decay_attention_bwd(const ccq_heads *q, const ccq_heads *k, const
     sum.d = d;
     sum.rows = B * T;
     sum.T = T;
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>((sum.rows * H * d / 4 + 255) / 256, 16 * sm_count_now())), sum.count);
-    if (dtype == CCQ_BF16)
-        decay_sum_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(sum, access_out == 16);
-    else
-        decay_sum_kernel<float><<<grid, 256, 0, s>>>(sum, access_out == 16);
-    return op_cuda(cudaGetLastError(), "shared heads' sum launch");
+    const unsigned grid = sum.count * static_cast<unsigned>(std::min<int64_t>((sum.rows * H * d / 4 + 255) / 256, 16 * sm_count_now()));
+    return op_cuda(dtype == CCQ_BF16 ? launch_after(decay_sum_kernel<__nv_bfloat16>, grid, 256, 0, s, sum, access_out == 16)
+                                     : launch_after(decay_sum_kernel<float>, grid, 256, 0, s, sum, access_out == 16),
+                   "shared heads' sum launch");
 }
 
 }  // extern "C"

@@ -134,6 +134,9 @@ __device__ __forceinline__ float2 decay_keep(const DecayLog &l, int n) {
     return make_float2(hi, static_cast<float>(p - hi));
 }
 
+// Lets the launch after this one start where SMs are free.
+__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Where the state of (sequence, head, segment) lies among the parts.
 __device__ __forceinline__ int64_t decay_part(const DecayArgs &a, int kind, int sequence, int h, int segment) {
     const int64_t pair = static_cast<int64_t>(sequence) * a.H + h - (static_cast<int64_t>(a.sequences) * a.H - a.split_pairs);

@@ -145,9 +145,6 @@ __device__ __forceinline__ bool elect_one() {
     return p;
 }
 
-// Lets the launch after this one start where SMs are free.
-__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
 // The place of the next half of K in its ring of three.
 struct Ring {
     int slot = 0;
