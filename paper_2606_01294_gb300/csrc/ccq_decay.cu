@@ -19,14 +19,14 @@ namespace {
 
 constexpr int kC = 32;        // tokens of a block
 constexpr int kN = 32;        // columns of a CTA
-constexpr int kThreads = 128;
+constexpr int kThreads = 256;
 constexpr int kPad = 4;
 
 template <int D, int BUFFERS> struct BlockShared {
     struct {
         float q[kC][D + kPad], k[kC][D + kPad], v[kC][kN + kPad];
     } in[BUFFERS];
-    float p[kC][kN + kPad], s[D][kN + kPad];
+    float p[kC][kN + kPad], o[kC][kN + kPad], s[D][kN + kPad];
     float power[kC + 1];  // g^n
     float2 keep[2];       // g^32 and g^n of the ragged block, as two floats
 };
@@ -74,26 +74,32 @@ __device__ __forceinline__ void copy_rows(float (*dst)[STRIDE], const DecayView 
     }
 }
 
-// ASYNC: fp32 operands on 16-byte boundaries, copied a block ahead.
-template <typename T, int D, bool ASYNC>
-__global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a) {
+// ASYNC: fp32 operands on 16-byte boundaries, copied a block ahead.  CTAS an SM: for d = 64 three where the launch has more than two
+// for each SM (gradients of 16 x 2000 tokens, 16 heads 2.33 ms, 2.90 with two), else two, with the registers of the third (4 x 777
+// tokens of 4 heads 43 us, 47 with three).
+template <typename T, int D, bool ASYNC, int CTAS, bool PARTS>
+__global__ void __launch_bounds__(kThreads, CTAS) decay_block_kernel(const DecayArgs a) {
     constexpr int kBuffers = ASYNC ? 2 : 1;
-    if (a.parts_only) grid_release();  // (the launch after this one forms its tables and loads its first blocks meanwhile)
+    // (the launch after this one forms its tables and loads its first blocks meanwhile; with three CTAs an SM it would crowd some SMs)
+    if (PARTS && CTAS == 2) grid_release();
     extern __shared__ float4 shared_raw[];
     BlockShared<D, kBuffers> &sh = *reinterpret_cast<BlockShared<D, kBuffers> *>(shared_raw);
     constexpr int kSlices = D / kN;
-    constexpr int R = D / 16;  // state rows of a thread: R x 4 of its slice
+    constexpr int R = PARTS ? D / 32 : D / 16;  // state rows of a thread: R x 4 of its slice
+    constexpr int kWide = R % 4 ? 2 : 4;
     int64_t x = blockIdx.x;
     const int slice = static_cast<int>(x % kSlices);
     x /= kSlices;
-    const int nseg = a.parts_only ? a.segments - 1 : a.segments;
+    const int nseg = PARTS ? a.segments - 1 : a.segments;
     const int segment = static_cast<int>(x % nseg);
     x /= nseg;
     const int h = static_cast<int>(x % a.H);
     x /= a.H;
     const int sequence = decay_longest_first(a, static_cast<int>(x % a.sequences), reinterpret_cast<int *>(shared_raw));
     const DecayPass &ps = a.pass[x / a.sequences];
-    const int tid = threadIdx.x, tx = tid % 8, ty = tid / 8;
+    const int tid = threadIdx.x, tx = tid % 8;
+    const bool states = PARTS || tid >= kThreads / 2;  // these threads have the state and what is read from it, the others P and O
+    const int ty = (PARTS ? tid : tid % (kThreads / 2)) / 8;
     const int c0 = slice * kN;
     const bool down = ps.descending != 0;
 
@@ -117,12 +123,12 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
             auto &to = sh.in[j & 1];
             copy_rows<D>(to.k, ps.k, span.b, span.begin + begin, n, h, 0);
             copy_rows<kN>(to.v, ps.v, span.b, span.begin + begin, n, h, c0);
-            if (!a.parts_only) copy_rows<D>(to.q, ps.q, span.b, span.begin + begin, n, h, 0);
+            if (!PARTS) copy_rows<D>(to.q, ps.q, span.b, span.begin + begin, n, h, 0);
             copy_commit();
         }
     };
     if (first < last) copy(first);
-    if (a.segments > 1 && !a.parts_only) grid_wait();  // (the segments' parts)
+    if (a.segments > 1 && !PARTS) grid_wait();  // (the segments' parts)
 
     // ---- the state at the segment's start; this thread's rows R ty .. and columns 4 tx ..
     float S[R][4];
@@ -143,9 +149,10 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int c = 0; c < 4; ++c) S[r][c] = 0.f;
-        if (a.segments == 1 || (a.parts_only && segment == 0)) {
+        if (!states) {
+        } else if (a.segments == 1 || (PARTS && segment == 0)) {
             if (ps.state_in) add(ps.state_in + at, ps.transposed, 0.f);
-            if (a.parts_only) {
+            if (PARTS) {
                 float *to = a.parts + decay_part(a, ps.kind, sequence, h, 0);
 #pragma unroll
                 for (int r = 0; r < R; ++r)
@@ -156,7 +163,7 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
 #pragma unroll
                     for (int c = 0; c < 4; ++c) S[r][c] = 0.f;
             }
-        } else if (!a.parts_only) {
+        } else if (!PARTS) {
             for (int g = 0; g <= segment; ++g) {
                 // tokens of segment g - 1
                 const int64_t lo = min(per * (g - 1), blocks), hi = min(per * g, blocks);
@@ -172,7 +179,7 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
         const int64_t begin = block_begin(j);
         const int n = tokens_of(begin);
         auto &in = sh.in[ASYNC ? j & 1 : 0];
-        __syncthreads();  // the last block's readers
+        // (all have read the last block: the barrier at its end, or no block was)
         if constexpr (ASYNC) {
             if (j + 1 < last) {
                 copy(j + 1);
@@ -183,18 +190,75 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
         } else {
             load_rows<T, D>(in.k, ps.k, span.b, span.begin + begin, n, h, 0, a.vec);
             load_rows<T, kN>(in.v, ps.v, span.b, span.begin + begin, n, h, c0, a.vec);
-            if (!a.parts_only) load_rows<T, D>(in.q, ps.q, span.b, span.begin + begin, n, h, 0, a.vec);
+            if (!PARTS) load_rows<T, D>(in.q, ps.q, span.b, span.begin + begin, n, h, 0, a.vec);
         }
-        if (!a.parts_only) {
+        if (!PARTS && states) {
 #pragma unroll
             for (int r = 0; r < R; ++r)
                 *reinterpret_cast<float4 *>(&sh.s[R * ty + r][4 * tx]) = make_float4(S[r][0], S[r][1], S[r][2], S[r][3]);
         }
         __syncthreads();
-        if (!a.parts_only) {
+        float o[2][4] = {};  // rows 2 ty, 2 ty + 1, columns 4 tx .. 4 tx + 3
+        if (states) {
+            if constexpr (!PARTS) {
+                // diag(g^..) Q S
+#pragma unroll 2
+                for (int e = 0; e < D; e += 4) {
+                    float4 qv[2];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) qv[r] = *reinterpret_cast<const float4 *>(&in.q[2 * ty + r][e]);
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) {
+                        const float4 sv = *reinterpret_cast<const float4 *>(&sh.s[e + f][4 * tx]);
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const float w = f == 0 ? qv[r].x : f == 1 ? qv[r].y : f == 2 ? qv[r].z : qv[r].w;
+                            o[r][0] += w * sv.x;
+                            o[r][1] += w * sv.y;
+                            o[r][2] += w * sv.z;
+                            o[r][3] += w * sv.w;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const int i = 2 * ty + r, m = down ? n - 1 - i : i + 1;
+                    const float f = m >= 0 ? sh.power[m] * ps.s_scale : 0.f;
+                    *reinterpret_cast<float4 *>(&sh.o[i][4 * tx]) = make_float4(o[r][0] * f, o[r][1] * f, o[r][2] * f, o[r][3] * f);
+                }
+            }
+            // S = g^n S + K^T diag(k_scale g^..) V, rows R ty .., columns 4 tx ..
+            const float2 keep = sh.keep[n < kC];
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) S[r][c] = fmaf(S[r][c], keep.x, S[r][c] * keep.y);
+#pragma unroll 2
+            for (int jj = 0; jj < n; ++jj) {
+                const float u = sh.power[down ? jj + 1 : n - 1 - jj] * ps.k_scale;
+                float4 vv = *reinterpret_cast<const float4 *>(&in.v[jj][4 * tx]);
+                vv.x *= u;
+                vv.y *= u;
+                vv.z *= u;
+                vv.w *= u;
+#pragma unroll
+                for (int r = 0; r < R; r += kWide) {
+                    const Pack<float, kWide> kv = load_plain<float, kWide>(&in.k[jj][R * ty + r]);
+                    float kk[kWide];
+                    unpack(kv, kk);
+#pragma unroll
+                    for (int e = 0; e < kWide; ++e) {
+                        S[r + e][0] += kk[e] * vv.x;
+                        S[r + e][1] += kk[e] * vv.y;
+                        S[r + e][2] += kk[e] * vv.z;
+                        S[r + e][3] += kk[e] * vv.w;
+                    }
+                }
+            }
+        } else if constexpr (!PARTS) {
             // P: rows 2 ty, 2 ty + 1, columns tx + 8 c
             float p[2][4] = {};
-#pragma unroll 4
+#pragma unroll 2
             for (int e = 0; e < D; e += 4) {
                 float4 qv[2], kv[4];
 #pragma unroll
@@ -215,34 +279,7 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
                     sh.p[i][jj] = gap >= 0 ? p[r][c] * (sh.power[gap] * ps.p_scale) : 0.f;
                 }
             }
-            __syncthreads();
-            // O: rows 2 ty, 2 ty + 1, columns 4 tx .. 4 tx + 3
-            float o[2][4] = {};
-#pragma unroll 4
-            for (int e = 0; e < D; e += 4) {
-                float4 qv[2];
-#pragma unroll
-                for (int r = 0; r < 2; ++r) qv[r] = *reinterpret_cast<const float4 *>(&in.q[2 * ty + r][e]);
-#pragma unroll
-                for (int f = 0; f < 4; ++f) {
-                    const float4 sv = *reinterpret_cast<const float4 *>(&sh.s[e + f][4 * tx]);
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const float w = f == 0 ? qv[r].x : f == 1 ? qv[r].y : f == 2 ? qv[r].z : qv[r].w;
-                        o[r][0] += w * sv.x;
-                        o[r][1] += w * sv.y;
-                        o[r][2] += w * sv.z;
-                        o[r][3] += w * sv.w;
-                    }
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int i = 2 * ty + r, m = down ? n - 1 - i : i + 1;
-                const float f = m >= 0 ? sh.power[m] * ps.s_scale : 0.f;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) o[r][c] *= f;
-            }
+            __syncwarp();  // (a warp reads the rows that it has written)
             // (a value that is not finite does not reach the rows before it: the sums end at the row)
             const int from = down ? 2 * ty : 0, to = down ? n : min(n, 2 * ty + 2);
             for (int jj = from; jj < to; ++jj) {
@@ -257,10 +294,19 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
                     o[r][3] += w * vv.w;
                 }
             }
+        }
+        __syncthreads();
+        if constexpr (!PARTS) {
+            if (states) continue;
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const int i = 2 * ty + r;
                 if (i >= n) continue;
+                const float4 f = *reinterpret_cast<const float4 *>(&sh.o[i][4 * tx]);
+                o[r][0] += f.x;
+                o[r][1] += f.y;
+                o[r][2] += f.z;
+                o[r][3] += f.w;
                 const int64_t at = span.b * ps.o_batch + (span.begin + begin + i) * ps.o_token + h * ps.o_head + c0 + 4 * tx;
                 if (ps.o_fp32) {
                     float *to_p = static_cast<float *>(ps.o) + at;
@@ -278,56 +324,40 @@ __global__ void __launch_bounds__(kThreads) decay_block_kernel(const DecayArgs a
                 }
             }
         }
-        // S = g^n S + K^T diag(k_scale g^..) V, rows R ty .., columns 4 tx ..
-        const float2 keep = sh.keep[n < kC];
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) S[r][c] = fmaf(S[r][c], keep.x, S[r][c] * keep.y);
-#pragma unroll 4
-        for (int jj = 0; jj < n; ++jj) {
-            const float u = sh.power[down ? jj + 1 : n - 1 - jj] * ps.k_scale;
-            float4 vv = *reinterpret_cast<const float4 *>(&in.v[jj][4 * tx]);
-            vv.x *= u;
-            vv.y *= u;
-            vv.z *= u;
-            vv.w *= u;
-#pragma unroll
-            for (int r = 0; r < R; r += 4) {
-                const float4 kv = *reinterpret_cast<const float4 *>(&in.k[jj][R * ty + r]);
-                const float kk[4] = {kv.x, kv.y, kv.z, kv.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    S[r + e][0] += kk[e] * vv.x;
-                    S[r + e][1] += kk[e] * vv.y;
-                    S[r + e][2] += kk[e] * vv.z;
-                    S[r + e][3] += kk[e] * vv.w;
-                }
-            }
-        }
     }
     float *to = nullptr;
-    if (a.parts_only)
+    if (PARTS)
         to = a.parts + decay_part(a, ps.kind, sequence, h, segment + 1);
     else if (ps.state_out && segment == a.segments - 1)
         to = ps.state_out + (static_cast<int64_t>(sequence) * a.H + h) * D * D;
-    if (to) {
+    if (to && states) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
             *reinterpret_cast<float4 *>(to + (R * ty + r) * D + c0 + 4 * tx) = make_float4(S[r][0], S[r][1], S[r][2], S[r][3]);
     }
 }
 
-template <typename T, int D, bool ASYNC> cudaError_t launch_blocks(const DecayArgs &a, cudaStream_t s) {
+template <typename T, int D, bool ASYNC, int CTAS> cudaError_t launch_blocks(const DecayArgs &a, int64_t grid, cudaStream_t s) {
     constexpr int kBytes = sizeof(BlockShared<D, ASYNC ? 2 : 1>);
-    cudaError_t e = allow_shared<decay_block_kernel<T, D, ASYNC>>(kBytes);
-    if (e != cudaSuccess) return e;
-    const int64_t grid = static_cast<int64_t>(D / kN) * (a.parts_only ? a.segments - 1 : a.segments) * a.H * a.sequences * a.passes;
-    if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-    if (a.segments > 1 && !a.parts_only)
-        return launch_after(decay_block_kernel<T, D, ASYNC>, static_cast<unsigned>(grid), kThreads, kBytes, s, a);
-    decay_block_kernel<T, D, ASYNC><<<static_cast<unsigned>(grid), kThreads, kBytes, s>>>(a);
+    const unsigned ctas = static_cast<unsigned>(grid);
+    cudaError_t e;
+    if (a.parts_only) {
+        if ((e = allow_shared<decay_block_kernel<T, D, ASYNC, CTAS, true>>(kBytes)) != cudaSuccess) return e;
+        decay_block_kernel<T, D, ASYNC, CTAS, true><<<ctas, kThreads, kBytes, s>>>(a);
+        return cudaGetLastError();
+    }
+    if ((e = allow_shared<decay_block_kernel<T, D, ASYNC, CTAS, false>>(kBytes)) != cudaSuccess) return e;
+    if (a.segments > 1) return launch_after(decay_block_kernel<T, D, ASYNC, CTAS, false>, ctas, kThreads, kBytes, s, a);
+    decay_block_kernel<T, D, ASYNC, CTAS, false><<<ctas, kThreads, kBytes, s>>>(a);
     return cudaGetLastError();
+}
+
+template <typename T, bool ASYNC> cudaError_t launch_blocks(const DecayArgs &a, cudaStream_t s) {
+    const int64_t units = static_cast<int64_t>(a.d / kN) * a.H * a.sequences * a.passes;
+    const int64_t grid = units * (a.parts_only ? a.segments - 1 : a.segments);
+    if (grid > 0x7fffffff) return cudaErrorInvalidValue;
+    if (a.d == 128) return launch_blocks<T, 128, ASYNC, 2>(a, grid, s);
+    return units * a.segments > 2 * sm_count_now() ? launch_blocks<T, 64, ASYNC, 3>(a, grid, s) : launch_blocks<T, 64, ASYNC, 2>(a, grid, s);
 }
 
 // ---------------------------------------------------------------- gradients of shared heads
@@ -399,7 +429,7 @@ Plan plan_segments(int64_t B, int64_t T, int H, int d, int64_t num_seqs, ccq_dty
     if (num_seqs < 1 || B * T < 1) return best;
     const bool cores = dtype == CCQ_BF16;
     const Cost c = cores ? Cost{128, d == 128 ? 3.45 : 2.4, d == 128 ? 4.0 : 2.8, 6.0, sm_count_now()}
-                         : Cost{kC, d == 128 ? 12.0 : 8.5, d == 128 ? 5.0 : 3.5, 6.0, 2 * sm_count_now()};
+                         : Cost{kC, d == 128 ? 10.5 : 8.0, d == 128 ? 5.0 : 3.5, 6.0, 2 * sm_count_now()};
     const int64_t ctas = num_seqs * H * (cores ? 1 : d / kN), blocks = (B * T / num_seqs + c.block - 1) / c.block;
     const int64_t kinds = passes > 1 ? 2 : 1;
     auto rounds = [&](int64_t n) { return static_cast<double>((n + c.resident - 1) / c.resident); };
@@ -517,10 +547,8 @@ ccq_status run_passes(DecayArgs &a, const Plan &plan, ccq_dtype dtype, bool core
 }  // namespace
 
 cudaError_t launch_decay_blocks(const DecayArgs &a, ccq_dtype dtype, cudaStream_t s) {
-    if (dtype == CCQ_BF16)
-        return a.d == 128 ? launch_blocks<__nv_bfloat16, 128, false>(a, s) : launch_blocks<__nv_bfloat16, 64, false>(a, s);
-    if (!a.vec) return a.d == 128 ? launch_blocks<float, 128, false>(a, s) : launch_blocks<float, 64, false>(a, s);
-    return a.d == 128 ? launch_blocks<float, 128, true>(a, s) : launch_blocks<float, 64, true>(a, s);
+    if (dtype == CCQ_BF16) return launch_blocks<__nv_bfloat16, false>(a, s);
+    return a.vec ? launch_blocks<float, true>(a, s) : launch_blocks<float, false>(a, s);
 }
 
 }  // namespace ccq
