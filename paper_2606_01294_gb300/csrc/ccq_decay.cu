@@ -4,11 +4,13 @@
 // decay_block_kernel: a CTA walks the tokens of one (sequence, head, segment) in blocks of 32 with a slice of 32 columns of
 // the state, in fp32 on the CUDA cores:
 //   P = Q K^T (32 x 32), masked and times g^|i - j|;  O = P V + diag(g^..) Q S;  S = g^n S + K^T diag(g^..) V.
-// 32 tokens cost 32 d (16 + 2 * 32) + 16 * 32 * 32 multiply-adds a CTA, of which P, formed again by each slice, is a fifth.
+// Half of the threads have the state and what is read from it (Q S), the others P and P V: between its two barriers a block is one chain
+// of either.  32 tokens cost 32 d (16 + 2 * 32) + 16 * 32 * 32 multiply-adds a CTA, of which P, formed again by each slice, is a fifth.
 // Aligned fp32 operands of the next block are copied while this one is computed.
-// Bound by the latency of a block's steps between its four barriers, 12 us with two CTAs an SM (a quarter of the CUDA cores' rate):
-// 16 x 2000 tokens of 16 heads of 128 in fp32 2.97 ms, 4 x 777 of 4 heads of 64 in 7 segments 47 us.  Slices of 32 columns rather
-// than whole heads, so that few heads still reach many SMs.
+// Bound by what a thread loads from shared memory (32 words a cycle for an SM that multiplies 128): so Q K^T and Q S are 4 x 8 a
+// thread over a quarter of d, summed by shuffles, and P V reads four columns of P at a time.  8 x 1000 tokens of 16 heads of 128 in
+// fp32: 532 us (797 with 2 x 4 a thread and one group), 8 x 1000 x 16 x 64 166 (287), 4 x 777 of 4 heads of 64 in 7 segments 34 (49).
+// Slices of 32 columns rather than whole heads, so that few heads still reach many SMs.
 #include <algorithm>
 #include <cmath>
 
@@ -21,15 +23,33 @@ constexpr int kC = 32;        // tokens of a block
 constexpr int kN = 32;        // columns of a CTA
 constexpr int kThreads = 256;
 constexpr int kPad = 4;
+constexpr int kRowPad = 16;   // of q and k: the two rows that eight lanes read lie in different halves of the banks
 
 template <int D, int BUFFERS> struct BlockShared {
     struct {
-        float q[kC][D + kPad], k[kC][D + kPad], v[kC][kN + kPad];
+        float q[kC][D + kRowPad], k[kC][D + kRowPad], v[kC][kN + kPad];
     } in[BUFFERS];
-    float p[kC][kN + kPad], o[kC][kN + kPad], s[D][kN + kPad];
+    float p[kC][kN + kPad], o[kC][kN + kPad];
+    float s[D][kN];       // chunks of four columns swizzled by the row, as state_chunk() says
     float power[kC + 1];  // g^n
     float2 keep[2];       // g^32 and g^n of the ragged block, as two floats
 };
+
+// Where the four columns 4 c .. of a row of the state lie in its row: lanes that read rows four apart meet in no bank.
+__device__ __forceinline__ int state_chunk(int row, int c) { return 4 * (c ^ (2 * (row >> 2 & 3))); }
+
+// Sums of 4 x 8 over four neighbouring lanes; lane l keeps columns 2 l and 2 l + 1.
+__device__ __forceinline__ void sum_lanes(float (&x)[4][8], int l, float (&y)[4][2]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            x[r][c] = (l & 2 ? x[r][c + 4] : x[r][c]) + __shfl_xor_sync(0xffffffffu, l & 2 ? x[r][c] : x[r][c + 4], 2);
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+            y[r][c] = (l & 1 ? x[r][c + 2] : x[r][c]) + __shfl_xor_sync(0xffffffffu, l & 1 ? x[r][c] : x[r][c + 2], 1);
+    }
+}
 
 // Rows begin .. begin + n of a head (of `width` channels from column c0) to shared memory, zeros up to kC.
 template <typename T, int W, int STRIDE>
@@ -74,14 +94,11 @@ __device__ __forceinline__ void copy_rows(float (*dst)[STRIDE], const DecayView 
     }
 }
 
-// ASYNC: fp32 operands on 16-byte boundaries, copied a block ahead.  CTAS an SM: for d = 64 three where the launch has more than two
-// for each SM (gradients of 16 x 2000 tokens, 16 heads 2.33 ms, 2.90 with two), else two, with the registers of the third (4 x 777
-// tokens of 4 heads 43 us, 47 with three).
-template <typename T, int D, bool ASYNC, int CTAS, bool PARTS>
-__global__ void __launch_bounds__(kThreads, CTAS) decay_block_kernel(const DecayArgs a) {
+// ASYNC: fp32 operands on 16-byte boundaries, copied a block ahead.
+template <typename T, int D, bool ASYNC, bool PARTS>
+__global__ void __launch_bounds__(kThreads, 2) decay_block_kernel(const DecayArgs a) {
     constexpr int kBuffers = ASYNC ? 2 : 1;
-    // (the launch after this one forms its tables and loads its first blocks meanwhile; with three CTAs an SM it would crowd some SMs)
-    if (PARTS && CTAS == 2) grid_release();
+    if (PARTS) grid_release();  // (the launch after this one forms its tables and loads its first blocks meanwhile)
     extern __shared__ float4 shared_raw[];
     BlockShared<D, kBuffers> &sh = *reinterpret_cast<BlockShared<D, kBuffers> *>(shared_raw);
     constexpr int kSlices = D / kN;
@@ -100,6 +117,8 @@ __global__ void __launch_bounds__(kThreads, CTAS) decay_block_kernel(const Decay
     const int tid = threadIdx.x, tx = tid % 8;
     const bool states = PARTS || tid >= kThreads / 2;  // these threads have the state and what is read from it, the others P and O
     const int ty = (PARTS ? tid : tid % (kThreads / 2)) / 8;
+    // of the two products over d: rows 4 ti .., eight columns by tj, and of each 16 channels the four from 4 tk
+    const int tk = tid % 4, tj = tid / 4 % 4, ti = tid % (kThreads / 2) / 16;
     const int c0 = slice * kN;
     const bool down = ps.descending != 0;
 
@@ -195,36 +214,44 @@ __global__ void __launch_bounds__(kThreads, CTAS) decay_block_kernel(const Decay
         if (!PARTS && states) {
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                *reinterpret_cast<float4 *>(&sh.s[R * ty + r][4 * tx]) = make_float4(S[r][0], S[r][1], S[r][2], S[r][3]);
+                *reinterpret_cast<float4 *>(&sh.s[R * ty + r][state_chunk(R * ty + r, tx)]) =
+                    make_float4(S[r][0], S[r][1], S[r][2], S[r][3]);
         }
         __syncthreads();
         float o[2][4] = {};  // rows 2 ty, 2 ty + 1, columns 4 tx .. 4 tx + 3
         if (states) {
             if constexpr (!PARTS) {
-                // diag(g^..) Q S
+                // diag(g^..) Q S: columns 4 tj .. and 16 + 4 tj ..
+                float x[4][8] = {}, y[4][2];
 #pragma unroll 2
-                for (int e = 0; e < D; e += 4) {
-                    float4 qv[2];
+                for (int e = 4 * tk; e < D; e += 16) {
+                    float4 qv[4];
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) qv[r] = *reinterpret_cast<const float4 *>(&in.q[2 * ty + r][e]);
+                    for (int r = 0; r < 4; ++r) qv[r] = *reinterpret_cast<const float4 *>(&in.q[4 * ti + r][e]);
 #pragma unroll
                     for (int f = 0; f < 4; ++f) {
-                        const float4 sv = *reinterpret_cast<const float4 *>(&sh.s[e + f][4 * tx]);
+                        const float4 s0 = *reinterpret_cast<const float4 *>(&sh.s[e + f][state_chunk(e, tj)]),
+                                     s1 = *reinterpret_cast<const float4 *>(&sh.s[e + f][state_chunk(e, tj + 4)]);
 #pragma unroll
-                        for (int r = 0; r < 2; ++r) {
+                        for (int r = 0; r < 4; ++r) {
                             const float w = f == 0 ? qv[r].x : f == 1 ? qv[r].y : f == 2 ? qv[r].z : qv[r].w;
-                            o[r][0] += w * sv.x;
-                            o[r][1] += w * sv.y;
-                            o[r][2] += w * sv.z;
-                            o[r][3] += w * sv.w;
+                            x[r][0] += w * s0.x;
+                            x[r][1] += w * s0.y;
+                            x[r][2] += w * s0.z;
+                            x[r][3] += w * s0.w;
+                            x[r][4] += w * s1.x;
+                            x[r][5] += w * s1.y;
+                            x[r][6] += w * s1.z;
+                            x[r][7] += w * s1.w;
                         }
                     }
                 }
+                sum_lanes(x, tk, y);
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int i = 2 * ty + r, m = down ? n - 1 - i : i + 1;
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 4 * ti + r, m = down ? n - 1 - i : i + 1;
                     const float f = m >= 0 ? sh.power[m] * ps.s_scale : 0.f;
-                    *reinterpret_cast<float4 *>(&sh.o[i][4 * tx]) = make_float4(o[r][0] * f, o[r][1] * f, o[r][2] * f, o[r][3] * f);
+                    *reinterpret_cast<float2 *>(&sh.o[i][16 * (tk >> 1) + 4 * tj + 2 * (tk & 1)]) = make_float2(y[r][0] * f, y[r][1] * f);
                 }
             }
             // S = g^n S + K^T diag(k_scale g^..) V, rows R ty .., columns 4 tx ..
@@ -233,67 +260,88 @@ __global__ void __launch_bounds__(kThreads, CTAS) decay_block_kernel(const Decay
             for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) S[r][c] = fmaf(S[r][c], keep.x, S[r][c] * keep.y);
-#pragma unroll 2
-            for (int jj = 0; jj < n; ++jj) {
-                const float u = sh.power[down ? jj + 1 : n - 1 - jj] * ps.k_scale;
-                float4 vv = *reinterpret_cast<const float4 *>(&in.v[jj][4 * tx]);
-                vv.x *= u;
-                vv.y *= u;
-                vv.z *= u;
-                vv.w *= u;
+#pragma unroll 1
+            for (int j0 = 0; j0 < n; j0 += 4) {  // (rows past n are zeros)
+                float4 vv[4];
+                Pack<float, kWide> kv[4][R / kWide];
 #pragma unroll
-                for (int r = 0; r < R; r += kWide) {
-                    const Pack<float, kWide> kv = load_plain<float, kWide>(&in.k[jj][R * ty + r]);
-                    float kk[kWide];
-                    unpack(kv, kk);
+                for (int e = 0; e < 4; ++e) {
+                    vv[e] = *reinterpret_cast<const float4 *>(&in.v[j0 + e][4 * tx]);
 #pragma unroll
-                    for (int e = 0; e < kWide; ++e) {
-                        S[r + e][0] += kk[e] * vv.x;
-                        S[r + e][1] += kk[e] * vv.y;
-                        S[r + e][2] += kk[e] * vv.z;
-                        S[r + e][3] += kk[e] * vv.w;
+                    for (int r = 0; r < R / kWide; ++r) kv[e][r] = load_plain<float, kWide>(&in.k[j0 + e][R * ty + kWide * r]);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float u = sh.power[max(down ? j0 + e + 1 : n - 1 - j0 - e, 0)] * ps.k_scale;
+                    vv[e].x *= u;
+                    vv[e].y *= u;
+                    vv[e].z *= u;
+                    vv[e].w *= u;
+#pragma unroll
+                    for (int r = 0; r < R / kWide; ++r) {
+                        float kk[kWide];
+                        unpack(kv[e][r], kk);
+#pragma unroll
+                        for (int f = 0; f < kWide; ++f) {
+                            S[kWide * r + f][0] += kk[f] * vv[e].x;
+                            S[kWide * r + f][1] += kk[f] * vv[e].y;
+                            S[kWide * r + f][2] += kk[f] * vv[e].z;
+                            S[kWide * r + f][3] += kk[f] * vv[e].w;
+                        }
                     }
                 }
             }
         } else if constexpr (!PARTS) {
-            // P: rows 2 ty, 2 ty + 1, columns tx + 8 c
-            float p[2][4] = {};
+            // P: columns tj + 4 c
+            float x[4][8] = {}, y[4][2];
 #pragma unroll 2
-            for (int e = 0; e < D; e += 4) {
-                float4 qv[2], kv[4];
+            for (int e = 4 * tk; e < D; e += 16) {
+                float4 qv[4];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) qv[r] = *reinterpret_cast<const float4 *>(&in.q[2 * ty + r][e]);
+                for (int r = 0; r < 4; ++r) qv[r] = *reinterpret_cast<const float4 *>(&in.q[4 * ti + r][e]);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) kv[c] = *reinterpret_cast<const float4 *>(&in.k[tx + 8 * c][e]);
+                for (int c = 0; c < 8; ++c) {
+                    const float4 kv = *reinterpret_cast<const float4 *>(&in.k[tj + 4 * c][e]);
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        p[r][c] += qv[r].x * kv[c].x + qv[r].y * kv[c].y + qv[r].z * kv[c].z + qv[r].w * kv[c].w;
+                    for (int r = 0; r < 4; ++r) x[r][c] += qv[r].x * kv.x + qv[r].y * kv.y + qv[r].z * kv.z + qv[r].w * kv.w;
+                }
             }
+            sum_lanes(x, tk, y);
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
+            for (int r = 0; r < 4; ++r) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int i = 2 * ty + r, jj = tx + 8 * c, gap = down ? jj - i : i - jj;
-                    sh.p[i][jj] = gap >= 0 ? p[r][c] * (sh.power[gap] * ps.p_scale) : 0.f;
+                for (int c = 0; c < 2; ++c) {
+                    const int i = 4 * ti + r, jj = tj + 4 * (2 * tk + c), gap = down ? jj - i : i - jj;
+                    sh.p[i][jj] = gap >= 0 ? y[r][c] * (sh.power[gap] * ps.p_scale) : 0.f;
                 }
             }
             __syncwarp();  // (a warp reads the rows that it has written)
-            // (a value that is not finite does not reach the rows before it: the sums end at the row)
-            const int from = down ? 2 * ty : 0, to = down ? n : min(n, 2 * ty + 2);
-            for (int jj = from; jj < to; ++jj) {
-                const float4 vv = *reinterpret_cast<const float4 *>(&in.v[jj][4 * tx]);
+            // O = P V, four columns of P at a time: those that all of the warp's eight rows keep, then those on the diagonal, where a
+            // value that is not finite must not reach the rows before it
+            const int row0 = ty / 4 * 8;
+            auto four = [&](int j0, bool diagonal) {
+                float4 vv[4], pv[2];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    if (down ? jj < 2 * ty + r : jj > 2 * ty + r) continue;
-                    const float w = sh.p[2 * ty + r][jj];
-                    o[r][0] += w * vv.x;
-                    o[r][1] += w * vv.y;
-                    o[r][2] += w * vv.z;
-                    o[r][3] += w * vv.w;
+                for (int r = 0; r < 2; ++r) pv[r] = *reinterpret_cast<const float4 *>(&sh.p[2 * ty + r][j0]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) vv[e] = *reinterpret_cast<const float4 *>(&in.v[j0 + e][4 * tx]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const bool kept = !diagonal || (down ? j0 + e >= 2 * ty + r : j0 + e <= 2 * ty + r);
+                        const float w = e == 0 ? pv[r].x : e == 1 ? pv[r].y : e == 2 ? pv[r].z : pv[r].w;
+                        o[r][0] = kept ? o[r][0] + w * vv[e].x : o[r][0];
+                        o[r][1] = kept ? o[r][1] + w * vv[e].y : o[r][1];
+                        o[r][2] = kept ? o[r][2] + w * vv[e].z : o[r][2];
+                        o[r][3] = kept ? o[r][3] + w * vv[e].w : o[r][3];
+                    }
                 }
-            }
+            };
+#pragma unroll 1
+            for (int j0 = down ? row0 + 8 : 0; j0 < (down ? n : row0); j0 += 4) four(j0, false);
+#pragma unroll 1
+            for (int j0 = row0; j0 < row0 + 8; j0 += 4) four(j0, true);
         }
         __syncthreads();
         if constexpr (!PARTS) {
@@ -337,27 +385,21 @@ __global__ void __launch_bounds__(kThreads, CTAS) decay_block_kernel(const Decay
     }
 }
 
-template <typename T, int D, bool ASYNC, int CTAS> cudaError_t launch_blocks(const DecayArgs &a, int64_t grid, cudaStream_t s) {
+template <typename T, int D, bool ASYNC> cudaError_t launch_blocks(const DecayArgs &a, cudaStream_t s) {
     constexpr int kBytes = sizeof(BlockShared<D, ASYNC ? 2 : 1>);
+    const int64_t grid = static_cast<int64_t>(D / kN) * (a.parts_only ? a.segments - 1 : a.segments) * a.H * a.sequences * a.passes;
+    if (grid > 0x7fffffff) return cudaErrorInvalidValue;
     const unsigned ctas = static_cast<unsigned>(grid);
     cudaError_t e;
     if (a.parts_only) {
-        if ((e = allow_shared<decay_block_kernel<T, D, ASYNC, CTAS, true>>(kBytes)) != cudaSuccess) return e;
-        decay_block_kernel<T, D, ASYNC, CTAS, true><<<ctas, kThreads, kBytes, s>>>(a);
+        if ((e = allow_shared<decay_block_kernel<T, D, ASYNC, true>>(kBytes)) != cudaSuccess) return e;
+        decay_block_kernel<T, D, ASYNC, true><<<ctas, kThreads, kBytes, s>>>(a);
         return cudaGetLastError();
     }
-    if ((e = allow_shared<decay_block_kernel<T, D, ASYNC, CTAS, false>>(kBytes)) != cudaSuccess) return e;
-    if (a.segments > 1) return launch_after(decay_block_kernel<T, D, ASYNC, CTAS, false>, ctas, kThreads, kBytes, s, a);
-    decay_block_kernel<T, D, ASYNC, CTAS, false><<<ctas, kThreads, kBytes, s>>>(a);
+    if ((e = allow_shared<decay_block_kernel<T, D, ASYNC, false>>(kBytes)) != cudaSuccess) return e;
+    if (a.segments > 1) return launch_after(decay_block_kernel<T, D, ASYNC, false>, ctas, kThreads, kBytes, s, a);
+    decay_block_kernel<T, D, ASYNC, false><<<ctas, kThreads, kBytes, s>>>(a);
     return cudaGetLastError();
-}
-
-template <typename T, bool ASYNC> cudaError_t launch_blocks(const DecayArgs &a, cudaStream_t s) {
-    const int64_t units = static_cast<int64_t>(a.d / kN) * a.H * a.sequences * a.passes;
-    const int64_t grid = units * (a.parts_only ? a.segments - 1 : a.segments);
-    if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-    if (a.d == 128) return launch_blocks<T, 128, ASYNC, 2>(a, grid, s);
-    return units * a.segments > 2 * sm_count_now() ? launch_blocks<T, 64, ASYNC, 3>(a, grid, s) : launch_blocks<T, 64, ASYNC, 2>(a, grid, s);
 }
 
 // ---------------------------------------------------------------- gradients of shared heads
@@ -412,7 +454,7 @@ template <typename T> __global__ void __launch_bounds__(256) decay_sum_kernel(co
 // Segments of each sequence, by a count of what a launch takes: rounds of resident CTAs times the blocks of a CTA, for the
 // passes and, with more than one segment, for the states before them (`kinds`, all segments but the last).  A block's times
 // are those measured with the GPU full.  1 x 16 x 20480 x 128 bf16: 482 us whole, 125 in 9 segments; the gradients of
-// 4 x 16 x 4096 x 128: 214 whole, 249 in 2; 1 x 8 x 4000 x 128 fp32: 1112 whole, 298 in 9.
+// 4 x 16 x 4096 x 128: 214 whole, 249 in 2; 1 x 8 x 4000 x 128 fp32: 174 in 9.
 struct Cost {
     int block;           // tokens
     double main, parts;  // microseconds a block
@@ -429,7 +471,7 @@ Plan plan_segments(int64_t B, int64_t T, int H, int d, int64_t num_seqs, ccq_dty
     if (num_seqs < 1 || B * T < 1) return best;
     const bool cores = dtype == CCQ_BF16;
     const Cost c = cores ? Cost{128, d == 128 ? 3.45 : 2.4, d == 128 ? 4.0 : 2.8, 6.0, sm_count_now()}
-                         : Cost{kC, d == 128 ? 10.5 : 8.0, d == 128 ? 5.0 : 3.5, 6.0, 2 * sm_count_now()};
+                         : Cost{kC, d == 128 ? 8.7 : 5.1, d == 128 ? 3.5 : 2.5, 6.0, 2 * sm_count_now()};
     const int64_t ctas = num_seqs * H * (cores ? 1 : d / kN), blocks = (B * T / num_seqs + c.block - 1) / c.block;
     const int64_t kinds = passes > 1 ? 2 : 1;
     auto rounds = [&](int64_t n) { return static_cast<double>((n + c.resident - 1) / c.resident); };
@@ -547,8 +589,10 @@ ccq_status run_passes(DecayArgs &a, const Plan &plan, ccq_dtype dtype, bool core
 }  // namespace
 
 cudaError_t launch_decay_blocks(const DecayArgs &a, ccq_dtype dtype, cudaStream_t s) {
-    if (dtype == CCQ_BF16) return launch_blocks<__nv_bfloat16, false>(a, s);
-    return a.vec ? launch_blocks<float, true>(a, s) : launch_blocks<float, false>(a, s);
+    if (dtype == CCQ_BF16)
+        return a.d == 128 ? launch_blocks<__nv_bfloat16, 128, false>(a, s) : launch_blocks<__nv_bfloat16, 64, false>(a, s);
+    if (!a.vec) return a.d == 128 ? launch_blocks<float, 128, false>(a, s) : launch_blocks<float, 64, false>(a, s);
+    return a.d == 128 ? launch_blocks<float, 128, true>(a, s) : launch_blocks<float, 64, true>(a, s);
 }
 
 }  // namespace ccq
