@@ -295,6 +295,57 @@ def test_long_sequences_in_segments(dtype, d, B, T, H):
     check_backward(g, q, k, v, ld, kept, d ** -0.5, dout, dST, dtype == BF16)
 
 
+# (on a GPU of 152 SMs, in bf16) 160 heads: a full round and 8 heads in segments; 192 passes of the gradients: 40 in segments
+@pytest.mark.parametrize("d,B,T,aligned", [(128, 10, 700, True), (64, 10, 513, True), (128, 10, 600, False), (128, 10, 511, True)])
+def test_more_heads_than_a_round(d, B, T, aligned):
+    """The sequences that full rounds leave over run in segments beside whole ones, in place as well."""
+    H = 16
+    q, k, v, ld, S0 = make(B, T, H, H, H, H, d, BF16, T)
+    if not aligned:  # (the fp32 kernel, which cuts all sequences or none)
+        q = torch.nn.functional.pad(q, (1, 1))[..., 1:-1]
+    kept = S0.clone()
+    o, ST = ops.decay_attention(q, k, v, ld, state=S0)
+    assert torch.equal(S0, kept)
+    check_forward(o, ST, q, k, v, ld, S0, d ** -0.5, aligned)
+    o2, again = ops.decay_attention(q, k, v, ld, state=S0, final_state=S0)
+    assert again is S0 and torch.equal(again, ST) and torch.equal(o2, o)
+
+
+def test_one_packed_sequence_of_more_heads_than_a_round():
+    q, k, v, ld, S0 = make(1, 700, 160, 160, 160, 160, 64, BF16, 5)
+    cu = torch.tensor([3, 680], device="cuda")
+    out = torch.full_like(q, 7.0)
+    o, ST = ops.decay_attention(q, k, v, ld, state=S0, cu_seqlens=cu, out=out)
+    check_forward(o[:, 3:680], ST, q[:, 3:680], k[:, 3:680], v[:, 3:680], ld, S0, 64 ** -0.5, True)
+    assert (o[:, :3] == 7).all() and (o[:, 680:] == 7).all()
+    dout, dST = torch.randn_like(q), torch.randn_like(S0)
+    g = ops.decay_attention_bwd(q, k, v, ld, dout, state=S0, dfinal_state=dST, cu_seqlens=cu)
+    part = {n: x[:, 3:680] if n != "dstate" else x for n, x in g.items()}
+    check_backward(part, q[:, 3:680], k[:, 3:680], v[:, 3:680], ld, S0, 64 ** -0.5, dout[:, 3:680], dST, True)
+
+
+@pytest.mark.parametrize("d,B,T,Hk,given", [(128, 4, 513, 16, True), (64, 4, 700, 4, True), (64, 4, 640, 16, False)])
+def test_gradients_of_more_passes_than_a_round(d, B, T, Hk, given):
+    H = 16
+    q, k, v, ld, S0 = make(B, T, H, H, Hk, Hk, d, BF16, T, given)
+    dout = torch.randn(B, T, H, d, device="cuda", generator=gen(8)).to(BF16)
+    dST = torch.randn(B, H, d, d, device="cuda", generator=gen(9)) if given else None
+    call = lambda: ops.decay_attention_bwd(q, k, v, ld, dout, state=S0, dfinal_state=dST)  # noqa: E731
+    g = call()
+    check_backward(g, q, k, v, ld, S0, d ** -0.5, dout, dST, True)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = call()
+    for _ in range(2):
+        graph.replay()
+        assert all(torch.equal(captured[n], g[n]) for n in g)
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    again = [ops.decay_attention_bwd(q, k, v, ld, dout, state=S0, dfinal_state=dST, stream=s) for s in (None, other)]
+    torch.cuda.current_stream().wait_stream(other)
+    assert all(torch.equal(r[n], g[n]) for r in again for n in g)
+
+
 @pytest.mark.parametrize("dtype", [FP32, BF16])
 def test_resumed_calls_and_steps(dtype):
     """A prompt in two calls, then tokens one by one, as the whole prompt in one call."""
