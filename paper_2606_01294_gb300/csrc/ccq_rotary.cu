@@ -24,6 +24,19 @@ struct RotaryTensor {
     int heads;
 };
 
+// n / d for 0 <= n < 2^31 as a product: with 2^s the first power of two from d on and m = floor(2^32 (2^s - d) / d) + 1,
+// n / d = (floor(m n / 2^32) + n) / 2^s (Granlund and Montgomery's method).
+struct Divisor {
+    uint32_t m, s;
+    Divisor() = default;
+    explicit Divisor(uint32_t d) {
+        s = 0;
+        while ((1ull << s) < d) ++s;
+        m = static_cast<uint32_t>(((1ull << 32) * ((1ull << s) - d)) / d + 1);
+    }
+    __device__ __forceinline__ int operator()(int n) const { return static_cast<int>((__umulhi(m, n) + static_cast<uint32_t>(n)) >> s); }
+};
+
 struct RotaryArgs {
     RotaryTensor t[2];
     int heads;             // of both tensors
@@ -36,6 +49,8 @@ struct RotaryArgs {
     int inverse;
     int tile;              // tokens of a CTA
     int turned, items;     // a head's rotated items, and with those that are copied
+    Divisor by_token, by_items, by_T, by_half;  // (a division by a number that is known here is several dozen instructions, by T
+                                                // in 64 bits a hundred: they took a third of the 3 x 3001 tokens' time)
 };
 
 // f 2^64 / (2 pi) mod 2^64, from the bits of f.
@@ -63,7 +78,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryArgs a) {
     const int64_t first = static_cast<int64_t>(blockIdx.x) * a.tile;
     const int tokens = static_cast<int>(min(static_cast<int64_t>(a.tile), a.tokens - first));
     for (int j = threadIdx.x; j < tokens * half; j += kThreads) {
-        const int t = j / half, i = j - t * half;
+        const int t = a.by_half(j), i = j - t * half;
         const double f = a.freqs[i];
         const uint64_t p = static_cast<uint64_t>(load_index(a.positions, a.position_bytes, first + t));
         const int32_t top = static_cast<int32_t>((p * turns_of(f)) >> 32);
@@ -75,7 +90,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryArgs a) {
     }
     __syncthreads();
     const int per_token = a.heads * a.items;
-    constexpr int K = N * sizeof(T) <= 4 ? 4 : 2;  // items at once
+    constexpr int K = N * sizeof(T) <= 4 || !PAIR ? 4 : 2;  // items at once
     const int total = tokens * per_token;
     for (int j0 = threadIdx.x; j0 < total; j0 += K * kThreads) {
         Pack<T, N> u[K], w[K];
@@ -84,13 +99,14 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryArgs a) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int j = min(j0 + k * kThreads, total - 1);  // (without conditions, so that all loads stay under way)
-            const int t = j / per_token, r = j - t * per_token;
-            int h = r / a.items;
+            const int t = a.by_token(j), r = j - t * per_token;
+            int h = a.by_items(r);
             const int c = r - h * a.items;
             const bool key = h >= a.t[0].heads;
             const RotaryTensor &x = a.t[key];
             if (key) h -= a.t[0].heads;
-            const int64_t row = first + t, b = row / a.T, at = row - b * a.T;
+            const int row = static_cast<int>(first) + t;  // (below 2^31)
+            const int64_t b = a.by_T(row), at = row - b * a.T;
             int64_t from = b * x.xb + at * x.xt + h * x.xh, to = b * x.yb + at * x.yt + h * x.yh;
             int lo;
             second[k] = 0;
@@ -162,6 +178,10 @@ cudaError_t launch(RotaryArgs &a, bool in_place, cudaStream_t s) {
     const int want = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(fill, (6 * kThreads) / per_token)));
     a.tile = std::max(1, std::min(want, kMostAngles / half));
     const int64_t grid = (a.tokens + a.tile - 1) / a.tile;
+    a.by_token = Divisor(per_token);
+    a.by_items = Divisor(a.items);
+    a.by_T = Divisor(static_cast<uint32_t>(a.T));
+    a.by_half = Divisor(half);
     rotary_kernel<T, N, PAIR, INTER><<<static_cast<unsigned>(grid), kThreads, a.tile * half * sizeof(float2), s>>>(a);
     return cudaGetLastError();
 }
