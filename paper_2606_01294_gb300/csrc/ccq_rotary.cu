@@ -5,8 +5,8 @@
 // exact whatever p (F_i is within 2 units of 2^-64 turns for f_i < 1, so 2^-33 turns at p = 2^30); the top 32 bits become
 // the argument of sincospif.  (The same in 64-bit floating point, at this GPU's rate for it, would take a fifth of the
 // prefill's time.)  A CTA computes the cosines and sines of its tokens once for all heads.
-// Bound by HBM, every element read once and written once: 8 x 4096 tokens of 16 + 16 heads of 128 in bf16 86 us, 6.2 TB/s, 92 % of a
-// copy.  A decode's 256 tokens take 3.4 us, a launch.
+// Bound by HBM, every element read once and written once: 8 x 4096 tokens of 16 + 16 heads of 128 in bf16 80 us, 6.7 TB/s, a copy's
+// rate.  A decode's 256 tokens take 3 us, a launch.
 #include <algorithm>
 
 #include "ccq_ops.cuh"
@@ -71,7 +71,7 @@ __device__ __forceinline__ uint64_t turns_of(double f) {
 template <typename T, int N, bool PAIR, bool INTER>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryArgs a) {
     // [tile][part / 2]: cos, sin; of the pairs of an access two by two, those of neighbouring accesses side by side, so that a warp's
-    // reads do not meet in a bank (8 x 4096 tokens, 32 heads of 128 in bf16: 90 -> 86 us)
+    // reads do not meet in a bank (8 x 4096 tokens, 32 heads of 128 in bf16: 90 us where they do, 86 so, both before the divisions went)
     extern __shared__ __align__(16) float2 turn[];
     constexpr int kPairs = PAIR ? N : N / 2;  // of an access
     const int half = a.part / 2, across = half / kPairs;
@@ -172,10 +172,11 @@ cudaError_t launch(RotaryArgs &a, bool in_place, cudaStream_t s) {
     a.turned = PAIR ? a.part / 2 / N : a.part / N;
     a.items = a.turned + (in_place ? 0 : (a.width - a.part) / N);
     const int half = a.part / 2;
-    // tokens of a CTA: a few accesses a thread where the tokens fill the GPU, one token (latency) where they do not
+    // tokens of a CTA: four accesses a thread where the tokens fill the GPU (3 x 3001 tokens interleaved 14 us, 16.5 with six, 22 with
+    // two; 8 x 4096 80, 81, 79), one token (latency) where they do not
     const int per_token = a.heads * a.items;
     const int64_t fill = a.tokens / (8 * sm_count_now());
-    const int want = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(fill, (6 * kThreads) / per_token)));
+    const int want = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(fill, (4 * kThreads) / per_token)));
     a.tile = std::max(1, std::min(want, kMostAngles / half));
     const int64_t grid = (a.tokens + a.tile - 1) / a.tile;
     a.by_token = Divisor(per_token);
