@@ -405,10 +405,9 @@ template <typename T, int D, bool ASYNC> cudaError_t launch_blocks(const DecayAr
 // ---------------------------------------------------------------- gradients of shared heads
 
 struct SumArgs {
-    const float *part;  // [rows][H][d]
     void *out[3];
     int64_t token[3], batch[3], head[3];
-    const float *parts[3];
+    const float *parts[3];  // [rows][H][d]
     int share[3];
     int count;
     int H, d;
@@ -417,34 +416,36 @@ struct SumArgs {
 
 // out[row, head, c] = sum over the heads that read it, in ascending order; one thread four channels.  Bound by HBM and L2: parts of
 // 3 x 1501 tokens, 16 heads of 64 twice (37 MB) 11 us.
-template <typename T> __global__ void __launch_bounds__(256) decay_sum_kernel(const SumArgs a, int vec) {
+template <typename Type> __global__ void __launch_bounds__(256) decay_sum_kernel(const SumArgs a, int vec) {
     const int which = blockIdx.x % a.count;
+    const unsigned shift = a.d == 128 ? 5 : 4;  // four channels a thread
+    const unsigned share = a.share[which], per_row = (a.H / share) << shift, rows = max(256 / per_row, 1u), blocks = gridDim.x / a.count;
+    const unsigned own = threadIdx.x / per_row, r0 = threadIdx.x - own * per_row, T = static_cast<unsigned>(a.T);
     grid_wait();  // (the passes' parts)
-    const int share = a.share[which], heads = a.H / share, quads = a.d / 4;
-    const int64_t total = a.rows * heads * quads;
-    const int64_t step = gridDim.x / a.count * 256ll;
-    for (int64_t i = blockIdx.x / a.count * 256ll + threadIdx.x; i < total; i += step) {
-        const int c = static_cast<int>(i % quads) * 4;
-        const int64_t r = i / quads;
-        const int h = static_cast<int>(r % heads);
-        const int64_t row = r / heads, b = row / a.T, t = row - b * a.T;
-        const float *src = a.parts[which] + (row * a.H + static_cast<int64_t>(h) * share) * a.d + c;
-        float f[4] = {};
-        for (int g = 0; g < share; ++g) {
-            const float4 u = __ldcs(reinterpret_cast<const float4 *>(src + static_cast<int64_t>(g) * a.d));
-            f[0] += u.x;
-            f[1] += u.y;
-            f[2] += u.z;
-            f[3] += u.w;
-        }
-        T *to = static_cast<T *>(a.out[which]) + b * a.batch[which] + t * a.token[which] + h * a.head[which] + c;
-        if (vec) {
-            Pack<T, 4> p;
-            pack(f, p);
-            store_stream<T, 4>(to, p);
-        } else {
+    if (own >= rows) return;
+    for (int64_t at = static_cast<int64_t>(blockIdx.x / a.count) * rows + own; at < a.rows; at += static_cast<int64_t>(blocks) * rows) {
+        const unsigned row = static_cast<unsigned>(at), b = row / T, t = row - b * T;
+        for (unsigned r = r0; r < per_row; r += 256) {
+            const unsigned h = r >> shift, c = (r - (h << shift)) * 4;
+            const float *src = a.parts[which] + (at * a.H + static_cast<int64_t>(h) * share) * a.d + c;
+            float f[4] = {};
+#pragma unroll 4
+            for (unsigned g = 0; g < share; ++g) {
+                const float4 u = __ldcs(reinterpret_cast<const float4 *>(src + static_cast<int64_t>(g) * a.d));
+                f[0] += u.x;
+                f[1] += u.y;
+                f[2] += u.z;
+                f[3] += u.w;
+            }
+            Type *to = static_cast<Type *>(a.out[which]) + b * a.batch[which] + t * a.token[which] + h * a.head[which] + c;
+            if (vec) {
+                Pack<Type, 4> p;
+                pack(f, p);
+                store_stream<Type, 4>(to, p);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) to[e] = from_f32<T>(f[e]);
+                for (int e = 0; e < 4; ++e) to[e] = from_f32<Type>(f[e]);
+            }
         }
     }
 }
