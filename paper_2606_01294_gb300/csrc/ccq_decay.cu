@@ -415,7 +415,7 @@ struct SumArgs {
 };
 
 // out[row, head, c] = sum over the heads that read it, in ascending order; one thread four channels.  Bound by HBM and L2: parts of
-// 3 x 1501 tokens, 16 heads of 64 twice (37 MB) 11 us.
+// 3 x 1501 tokens, 16 heads of 64 twice (37 MB) 10 us.
 template <typename Type> __global__ void __launch_bounds__(256) decay_sum_kernel(const SumArgs a, int vec) {
     const int which = blockIdx.x % a.count;
     const unsigned shift = a.d == 128 ? 5 : 4;  // four channels a thread
@@ -455,7 +455,7 @@ template <typename Type> __global__ void __launch_bounds__(256) decay_sum_kernel
 // Segments of each sequence, by a count of what a launch takes: rounds of resident CTAs times the blocks of a CTA, for the
 // passes and, with more than one segment, for the states before them (`kinds`, all segments but the last).  A block's times
 // are those measured with the GPU full.  1 x 16 x 20480 x 128 bf16: 482 us whole, 125 in 9 segments; the gradients of
-// 4 x 16 x 4096 x 128: 214 whole, 249 in 2; 1 x 8 x 4000 x 128 fp32: 174 in 9.
+// 4 x 16 x 4096 x 128: 197 whole, 249 in 2 each, 171 with 40 of 192 passes in 2; 1 x 8 x 4000 x 128 fp32: 174 in 9.
 struct Cost {
     int block;           // tokens
     double main, parts;  // microseconds a block

@@ -19,8 +19,8 @@
 //   LOAD  (warp 21)     one thread issues the TMA loads: a tile is loaded again when its last reader is through with it;
 //                       V in halves of 64 tokens, K in a ring of three halves
 // Bound by the steps of a chunk one after another, 3.4 us at d = 128 and 2.4 at 64, D through registers to S and its copy and A to P
-// among them, not by a unit: HBM 74 % of a copy, the tensor cores 53 %, issue 51 %.  bf16, 16 heads of 128: 8 x 4096 tokens 109 us
-// (decay_block_kernel: 4872), 1 x 20480 in segments 125, 64 packed prompts 237, gradients of 4 x 4096 198.  Why so: chunks of
+// among them, not by a unit: HBM 74 % of a copy, the tensor cores 40 to 53 %, issue 50 %; W, the longest stage, is 12 %.  bf16, 16 heads of 128: 8 x 4096 tokens 109 us
+// (decay_block_kernel: 3300), 1 x 20480 in segments 121, 64 packed prompts 238, gradients of 4 x 4096 171.  Why so: chunks of
 // 128 fill an accumulator's lanes; S stays in registers, as in tensor memory it would be read, scaled and written there each
 // chunk; a head has one CTA, for with two halves of V's columns both would form P and the split.
 // Rows past a sequence's end: TMA gives zeros past the tensor; rows of other packed sequences get W = 0, P = 0, and
