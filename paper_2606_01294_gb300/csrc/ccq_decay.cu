@@ -8,8 +8,10 @@
 // of either.  32 tokens cost 32 d (16 + 2 * 32) + 16 * 32 * 32 multiply-adds a CTA, of which P, formed again by each slice, is a fifth.
 // Aligned fp32 operands of the next block are copied while this one is computed.
 // Bound by what a thread loads from shared memory (32 words a cycle for an SM that multiplies 128): so Q K^T and Q S are 4 x 8 a
-// thread over a quarter of d, summed by shuffles, and P V reads four columns of P at a time.  8 x 1000 tokens of 16 heads of 128 in
-// fp32: 532 us (797 with 2 x 4 a thread and one group), 8 x 1000 x 16 x 64 166 (287), 4 x 777 of 4 heads of 64 in 7 segments 34 (49).
+// thread over a quarter of d, summed by shuffles, and P V reads four columns of P at a time.  What is left is instructions: Q S and the
+// state's increment are multiplied in pairs (531 -> 496 us; Q K^T in pairs, with twice the sums, is slower for d = 64).  8 x 1000
+// tokens of 16 heads of 128 in fp32: 496 us (797 with 2 x 4 a thread and one group), 8 x 1000 x 16 x 64 162 (287), 4 x 777 of 4 heads of
+// 64 in 7 segments 33 (49).
 // Slices of 32 columns rather than whole heads, so that few heads still reach many SMs.
 #include <algorithm>
 #include <cmath>
@@ -222,7 +224,8 @@ __global__ void __launch_bounds__(kThreads, 2) decay_block_kernel(const DecayArg
         if (states) {
             if constexpr (!PARTS) {
                 // diag(g^..) Q S: columns 4 tj .. and 16 + 4 tj ..
-                float x[4][8] = {}, y[4][2];
+                float x[4][8], y[4][2];
+                uint64_t x2[4][4] = {};
 #pragma unroll 2
                 for (int e = 4 * tk; e < D; e += 16) {
                     float4 qv[4];
@@ -235,17 +238,22 @@ __global__ void __launch_bounds__(kThreads, 2) decay_block_kernel(const DecayArg
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const float w = f == 0 ? qv[r].x : f == 1 ? qv[r].y : f == 2 ? qv[r].z : qv[r].w;
-                            x[r][0] += w * s0.x;
-                            x[r][1] += w * s0.y;
-                            x[r][2] += w * s0.z;
-                            x[r][3] += w * s0.w;
-                            x[r][4] += w * s1.x;
-                            x[r][5] += w * s1.y;
-                            x[r][6] += w * s1.z;
-                            x[r][7] += w * s1.w;
+                            const uint64_t ww = f2_make(w, w);
+                            x2[r][0] = f2_fma(ww, f2_make(s0.x, s0.y), x2[r][0]);
+                            x2[r][1] = f2_fma(ww, f2_make(s0.z, s0.w), x2[r][1]);
+                            x2[r][2] = f2_fma(ww, f2_make(s1.x, s1.y), x2[r][2]);
+                            x2[r][3] = f2_fma(ww, f2_make(s1.z, s1.w), x2[r][3]);
                         }
                     }
                 }
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const float2 f = f2_split(x2[r][c]);
+                        x[r][2 * c] = f.x;
+                        x[r][2 * c + 1] = f.y;
+                    }
                 sum_lanes(x, tk, y);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
@@ -283,10 +291,14 @@ __global__ void __launch_bounds__(kThreads, 2) decay_block_kernel(const DecayArg
                         unpack(kv[e][r], kk);
 #pragma unroll
                         for (int f = 0; f < kWide; ++f) {
-                            S[kWide * r + f][0] += kk[f] * vv[e].x;
-                            S[kWide * r + f][1] += kk[f] * vv[e].y;
-                            S[kWide * r + f][2] += kk[f] * vv[e].z;
-                            S[kWide * r + f][3] += kk[f] * vv[e].w;
+                            float *row = S[kWide * r + f];
+                            const uint64_t k2 = f2_make(kk[f], kk[f]);
+                            const float2 a2 = f2_split(f2_fma(k2, f2_make(vv[e].x, vv[e].y), f2_make(row[0], row[1])));
+                            const float2 b2 = f2_split(f2_fma(k2, f2_make(vv[e].z, vv[e].w), f2_make(row[2], row[3])));
+                            row[0] = a2.x;
+                            row[1] = a2.y;
+                            row[2] = b2.x;
+                            row[3] = b2.y;
                         }
                     }
                 }
@@ -455,7 +467,7 @@ template <typename Type> __global__ void __launch_bounds__(256) decay_sum_kernel
 // Segments of each sequence, by a count of what a launch takes: rounds of resident CTAs times the blocks of a CTA, for the
 // passes and, with more than one segment, for the states before them (`kinds`, all segments but the last).  A block's times
 // are those measured with the GPU full.  1 x 16 x 20480 x 128 bf16: 482 us whole, 125 in 9 segments; the gradients of
-// 4 x 16 x 4096 x 128: 197 whole, 249 in 2 each, 171 with 40 of 192 passes in 2; 1 x 8 x 4000 x 128 fp32: 174 in 9.
+// 4 x 16 x 4096 x 128: 197 whole, 249 in 2 each, 171 with 40 of 192 passes in 2; 1 x 8 x 4000 x 128 fp32: 162 in 9.
 struct Cost {
     int block;           // tokens
     double main, parts;  // microseconds a block
