@@ -125,7 +125,7 @@ CCQ_API ccq_status ccq_decay_attention(const ccq_heads *q, const ccq_heads *k, c
  * Gradients of ccq_decay_attention for a given dout [B, T, H, d] and, where it is not NULL, dST [num_seqs, H, d, d].
  * Nothing is kept from the forward.
  *   dq, dk, dv [B, T, heads, d] in dtype with the heads of q, k and v, apart from the inputs and each other: a head
- *              that several read gets their sum (formed in fp32, in ascending order).
+ *              that several read gets their sum (formed in fp32, in ascending order).  Tokens of no sequence get zeros.
  *   dS0        [num_seqs, H, d, d] fp32, or NULL.  Apart from S0 and dST.
  *   workspace  ccq_decay_attention_bwd_workspace_size() bytes, 16-byte aligned (NULL where that is 0).
  */

@@ -743,7 +743,7 @@ ccq_status ccq_decay_attention_bwd(const ccq_heads *q, const ccq_heads *k, const
     const size_t state_bytes = static_cast<size_t>(num_seqs) * H * d * d * 4;
     if ((st = check_states_apart("S0", S0, "dS0", dS0, state_bytes, false)) != CCQ_OK) return st;
     if ((st = check_states_apart("dST", dST, "dS0", dS0, state_bytes, false)) != CCQ_OK) return st;
-    if (num_seqs == 0) return CCQ_OK;
+    if (num_seqs == 0 && !(cu && T)) return CCQ_OK;
     if ((st = op_status_word(&a.status)) != CCQ_OK) return st;
     a.passes = 3;
     const DecayView Q = view_of(*q, H), K = view_of(*k, H), V = view_of(*v, H), O = view_of(*dout, H);
@@ -800,9 +800,24 @@ ccq_status ccq_decay_attention_bwd(const ccq_heads *q, const ccq_heads *k, const
     a.parts = static_cast<float *>(workspace);
     a.vec = access == 16 && access_out == 16;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    // Tokens of no sequence have no gradient: zeros where the passes write (the parts of shared heads, which are summed over all
+    // rows, among them).
+    if (cu && T) {
+        OutsideArgs rest = {};
+        for (int i = 0; i < 3; ++i) {
+            const DecayPass &p = a.pass[i];
+            rest.x[rest.count++] = outside_tensor(p.o, p.o_fp32 ? 4 : dtype_bytes(dtype), p.o_token, p.o_head, H, d);
+        }
+        rest.T = T;
+        rest.cu = cu;
+        rest.cu_bytes = cu_bytes;
+        rest.sequences = num_seqs;
+        if ((st = op_cuda(launch_outside(rest, s), "rows outside launch")) != CCQ_OK) return st;
+    }
     bool cores = dtype == CCQ_BF16 && a.vec && B * T > 0;
     for (int i = 0; i < 4; ++i) cores = cores && steps(*in[i], B, T) && (i > 2 || steps(*out[i], B, T));
-    if ((st = run_passes(a, plan, dtype, cores, B, 5u, s)) != CCQ_OK || !sum.count || !(B * T)) return st;
+    if (num_seqs && (st = run_passes(a, plan, dtype, cores, B, 5u, s)) != CCQ_OK) return st;
+    if (!sum.count || !(B * T)) return CCQ_OK;
     sum.H = H;
     sum.d = d;
     sum.rows = B * T;

@@ -143,6 +143,24 @@ __device__ __forceinline__ int64_t decay_part(const DecayArgs &a, int kind, int 
     return ((static_cast<int64_t>(kind) * a.split_pairs + pair) * a.segments + segment) * a.d * a.d;
 }
 
+// Tensors of [T, heads, width], strides in bytes, whose rows outside all packed sequences become zeros.
+struct OutsideTensor {
+    void *p;
+    int64_t token, head;
+    int heads, bytes;  // of a head's row
+    int wide;          // in accesses of 16 bytes
+};
+struct OutsideArgs {
+    OutsideTensor x[3];
+    int count;
+    int64_t T;
+    const void *cu;
+    int cu_bytes;
+    int64_t sequences;
+};
+OutsideTensor outside_tensor(void *p, int elem, int64_t token, int64_t head, int heads, int width);  // (strides in elements)
+cudaError_t launch_outside(const OutsideArgs &a, cudaStream_t s);
+
 cudaError_t launch_decay_chunks(const DecayArgs &a, int64_t B, cudaStream_t s);  // bf16 on the tensor cores
 cudaError_t launch_decay_blocks(const DecayArgs &a, ccq_dtype dtype, cudaStream_t s);
 

@@ -526,8 +526,8 @@ def decay_attention(q, k, v, log_decay, *, scale: Optional[float] = None, state=
 def decay_attention_bwd(q, k, v, log_decay, dout, *, scale: Optional[float] = None, state=None, dfinal_state=None,
                         cu_seqlens=None, out: Optional[dict] = None, workspace=None, stream=None):
     """Gradients of :func:`decay_attention` (ccq_decay_attention_bwd): a dict of dq, dk, dv (with q's, k's and v's heads) and,
-    with ``state`` or ``dfinal_state`` (the gradient of the states that the forward returned), dstate.  Only the
-    forward's inputs are needed.  ``out`` may hold preallocated tensors under those names."""
+    with ``state`` or ``dfinal_state`` (the gradient of the states that the forward returned), dstate.  Tokens that no packed
+    sequence holds get zeros.  Only the forward's inputs are needed.  ``out`` may hold preallocated tensors under those names."""
     if stream is not None:
         return _on_stream(stream, decay_attention_bwd, q, k, v, log_decay, dout, scale=scale, state=state,
                           dfinal_state=dfinal_state, cu_seqlens=cu_seqlens, out=out, workspace=workspace)
