@@ -73,6 +73,13 @@ typedef struct {
     int64_t heads;
 } ccq_heads;
 
+/*
+ * Zeros to the tokens of a packed batch that no sequence holds: x [1, T, heads, width] in dtype (its batch stride is not looked
+ * at), cu and num_seqs as for ccq_decay_attention.  The others are left as they are.
+ */
+CCQ_API ccq_status ccq_zero_outside(const ccq_heads *x, ccq_dtype dtype, int64_t T, int width, const void *cu,
+                                    int cu_bytes, int64_t num_seqs, void *stream);
+
 /* ------------------------------------------------------------ rotary positions */
 
 /*
@@ -106,7 +113,7 @@ CCQ_API ccq_status ccq_rotary(const ccq_heads *x, const ccq_heads *y, int count,
  *   ST         [num_seqs, H, d, d] fp32, or NULL: the states after the last tokens.  May be S0, else apart from it.
  *   cu         NULL: B sequences of T tokens (num_seqs = B).  Else B = 1 and sequence s is the tokens cu[s] to
  *              cu[s + 1] (a device array of num_seqs + 1, cu_bytes 4 or 8; 0 <= cu[s] <= cu[s + 1] <= T).
- *              Tokens of no sequence are left as they are in o.  An offset outside its range is held to it
+ *              Tokens of no sequence are left as they are in o (ccq_zero_outside clears them).  An offset outside its range is held to it
  *              and leaves CCQ_ERR_INDEX.
  *   workspace  ccq_decay_attention_workspace_size() bytes, 16-byte aligned (NULL where that is 0).
  * fp32 inputs, and bf16 ones whose addresses or strides are not multiples of 16 bytes, are computed in fp32.  Other

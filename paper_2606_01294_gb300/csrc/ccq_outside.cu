@@ -98,3 +98,32 @@ cudaError_t launch_outside(const OutsideArgs &a, cudaStream_t s) {
 }
 
 }  // namespace ccq
+
+using namespace ccq;
+
+extern "C" {
+
+ccq_status ccq_zero_outside(const ccq_heads *x, ccq_dtype dtype, int64_t T, int width, const void *cu, int cu_bytes,
+                            int64_t num_seqs, void *stream) {
+    if (!x) return op_fail(CCQ_ERR_INVALID_ARG, "x is NULL");
+    if (!valid_dtype(dtype)) return op_fail(CCQ_ERR_INVALID_ARG, "unknown dtype %d", static_cast<int>(dtype));
+    ccq_status st = check_tokens(1, T);
+    if (st != CCQ_OK) return st;
+    if (width < 1 || width > 65536) return op_fail(CCQ_ERR_INVALID_ARG, "head width %d: 1 to 65536", width);
+    if (num_seqs < 0 || num_seqs > (1 << 24))
+        return op_fail(CCQ_ERR_UNSUPPORTED, "%lld sequences: at most 2^24", static_cast<long long>(num_seqs));
+    if (cu_bytes != 4 && cu_bytes != 8) return op_fail(CCQ_ERR_INVALID_ARG, "cu_bytes=%d: 4 or 8", cu_bytes);
+    if ((st = op_pointer("cu", cu, cu_bytes)) != CCQ_OK) return st;
+    if ((st = check_heads("x", *x, dtype, 1, T, width, true)) != CCQ_OK) return st;
+    if (x->heads * width > (1 << 24)) return op_fail(CCQ_ERR_UNSUPPORTED, "at most 2^24 channels a token");
+    if (T == 0) return CCQ_OK;
+    OutsideArgs a = {};
+    a.x[a.count++] = outside_tensor(x->p, dtype_bytes(dtype), x->token, x->head, static_cast<int>(x->heads), width);
+    a.T = T;
+    a.cu = cu;
+    a.cu_bytes = cu_bytes;
+    a.sequences = num_seqs;
+    return op_cuda(launch_outside(a, static_cast<cudaStream_t>(stream)), "rows outside launch");
+}
+
+}  // extern "C"

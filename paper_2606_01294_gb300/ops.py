@@ -70,6 +70,8 @@ def _library() -> ctypes.CDLL:
                                 _VP, _VP, _L, _VP, _Z, _VP],
             "ccq_policy_loss_workspace_size": [_L, size],
             "ccq_token_logp": [_VP, _I, _L, _VP, _I, _L, _I, _F, _VP, _VP],
+            # x, dtype | T, width | cu, cu_bytes, num_seqs | stream
+            "ccq_zero_outside": [_VP, _I, _L, _I, _VP, _I, _L, _VP],
             # x, y (arrays), count, dtype | B, T, width, part | positions, bytes | freqs, amplitude, interleaved, inverse | stream
             "ccq_rotary": [_VP, _VP, _I, _I, _L, _L, _I, _I, _VP, _I, _VP, _F, _I, _I, _VP],
             # q, k, v, dtype | log_decay, scale, S0 | o, ST | B, T, H, d | cu, cu_bytes, num_seqs | ws | stream
@@ -475,7 +477,8 @@ def decay_attention(q, k, v, log_decay, *, scale: Optional[float] = None, state=
     """Linear attention with a constant decay for each head (ccq_decay_attention): with S = exp(log_decay) S + k v^T token by
     token, o = scale S^T q.  q, k, v [B, T, heads, d], d 64 or 128, bf16 or fp32 with any strides; fewer heads
     than log_decay's (fp32 [H], <= 0, a constant of the layer) are shared by consecutive ones.  ``scale``: d ** -0.5.
-    ``cu_seqlens``: CUDA offsets [N + 1] of sequences packed in one row (tokens of none are left as they are in ``out``).
+    ``cu_seqlens``: CUDA offsets [N + 1] of sequences packed in one row (tokens of none are zero in a new output, and left as
+    they are in ``out``).
     ``state`` [B or N, H, d, d] fp32: the states before the first tokens.  Returns (o [B, T, H, d], the states after the
     last tokens; None without ``return_state``); ``final_state`` may be ``state``."""
     if stream is not None:
@@ -499,6 +502,9 @@ def decay_attention(q, k, v, log_decay, *, scale: Optional[float] = None, state=
                 _FIVE(q.data_ptr(), *xq), _FIVE(k.data_ptr(), *xk), _FIVE(v.data_ptr(), *xv), code, log_decay.data_ptr(),
                 root if scale is None else scale, _ptr(state), _FIVE(out.data_ptr(), *xo), _ptr(final_state), *sizes,
                 _ptr(cu_seqlens), cu_bytes, seqs, _ptr(workspace), nbytes, raw))
+            if cu_seqlens is not None:
+                _check(_library().ccq_zero_outside(_FIVE(out.data_ptr(), *xo), code, shape[1], shape[3], cu_seqlens.data_ptr(), cu_bytes,
+                                                   seqs, raw))
             return out, final_state
     dev, B, T, H, d, (hq, hk, hv), cu, scale = _decay_args(q, k, v, log_decay, scale, cu_seqlens)
     shape = (cu[2], H, d, d)
@@ -508,7 +514,8 @@ def decay_attention(q, k, v, log_decay, *, scale: Optional[float] = None, state=
         _dense(final_state, "final_state", dev, torch.float32, shape)
     elif return_state:
         final_state = torch.empty(shape, dtype=torch.float32, device=dev)
-    if out is None:
+    new = out is None
+    if new:
         out = torch.empty((B, T, H, d), dtype=q.dtype, device=dev)
         ho = _FIVE(out.data_ptr(), T * H * d, H * d, d, H)
     else:
@@ -520,6 +527,8 @@ def decay_attention(q, k, v, log_decay, *, scale: Optional[float] = None, state=
     _check(_library().ccq_decay_attention(hq, hk, hv, code, log_decay.data_ptr(), scale, _ptr(state),
                                           ho, _ptr(final_state), B, T, H, d, *cu,
                                           _ptr(workspace), nbytes, raw))
+    if new and cu_seqlens is not None:
+        _check(_library().ccq_zero_outside(ho, code, T, d, *cu, raw))
     return out, final_state
 
 

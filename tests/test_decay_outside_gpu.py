@@ -1,6 +1,6 @@
 """Packed linear attention with a decay for each head: tokens that no sequence holds (padding before the first offset and behind
-the last, gaps that offsets going back leave).  Their gradients are zero, whatever the tensors and the workspace held.  All of it is
-exact: no tolerance."""
+the last, gaps that offsets going back leave).  Their gradients are zero, whatever the tensors and the workspace held; a new
+output is zero there, a given one is left as it was.  All of it is exact: no tolerance."""
 import pytest
 import torch
 
@@ -78,6 +78,28 @@ def test_gradients_of_tokens_outside_are_zero(dtype, H, Hk, cu, T):
 
 
 @pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("cu,T", CASES + BACK)
+def test_a_new_output_is_zero_outside(dtype, cu, T):
+    """... and one that is given keeps what it held."""
+    q, k, v, _, ld = make(T, 4, 4, 128, dtype, T)
+    held = held_by(cu, T)
+    offsets = torch.tensor(cu, device="cuda").long()
+    for x in (q, k, v):
+        x[:, ~held] = NAN
+    poisoned_memory((q.shape, dtype))
+    calls = [ops.decay_attention(q, k, v, ld, cu_seqlens=offsets)[0],
+             ops.decay_attention(q, k, v, ld, cu_seqlens=offsets.clamp(-2 ** 31, 2 ** 31 - 1).int(), return_state=False)[0]]
+    given = torch.full_like(q, 7.0)
+    ops.decay_attention(q, k, v, ld, cu_seqlens=offsets, out=given)
+    status((cu, T) in BACK)
+    for o in calls:
+        assert (o[:, ~held] == 0).all() and o.isfinite().all()
+    once = times_held(cu, T) == 1
+    assert torch.equal(calls[0][:, once], given[:, once])  # (in bf16 the second call's state has fewer bits: none is handed out)
+    assert (given[:, ~held] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
 def test_what_lies_between_the_rows_is_kept(dtype):
     """Gradients in slices of wider tensors, at addresses that no wide access fits: zeros go to the rows' own elements alone."""
     T, H, Hk, d = 150, 4, 2, 64
@@ -103,6 +125,8 @@ def test_many_sequences_and_much_padding(n):
     q, k, v, dout, ld = make(T, H, 1, d, BF16, n)
     out = {"dq": torch.full_like(q, NAN), "dk": torch.full_like(k, NAN), "dv": torch.full_like(v, NAN)}
     ops.decay_attention_bwd(q, k, v, ld, dout, cu_seqlens=cu, out=out)
+    poisoned_memory((q.shape, BF16))
+    out["o"] = ops.decay_attention(q, k, v, ld, cu_seqlens=cu)[0]
     ccq.device_status()
     for x in out.values():
         assert not x[:, :before].any() and not x[:, T - after:].any() and x.isfinite().all()
@@ -114,17 +138,17 @@ def test_captured_and_replayed_on_other_offsets():
     q, k, v, dout, ld = make(T, H, 2, d, BF16, 9)
     cu = torch.tensor([10, 100, 390], device="cuda")
     out = {"dq": torch.empty_like(q), "dk": torch.empty_like(k), "dv": torch.empty_like(v)}
-    call = lambda: ops.decay_attention_bwd(q, k, v, ld, dout, cu_seqlens=cu, out=out)  # noqa: E731
+    call = lambda: (ops.decay_attention_bwd(q, k, v, ld, dout, cu_seqlens=cu, out=out), ops.decay_attention(q, k, v, ld, cu_seqlens=cu)[0])  # noqa: E731
     call()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        call()
+        g, o = call()
     for offsets in ([10, 100, 390], [200, 300, 301], [0, 0, 0], [0, 5, 400]):
         cu.copy_(torch.tensor(offsets))
-        for x in out.values():
+        for x in (*out.values(), o):
             x.fill_(NAN)
         graph.replay()
         held = held_by(offsets, T)
-        for x in out.values():
+        for x in (*out.values(), o):
             assert (x[:, ~held] == 0).all() and x.isfinite().all()
     ccq.device_status()
