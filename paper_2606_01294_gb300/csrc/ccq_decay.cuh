@@ -134,6 +134,23 @@ __device__ __forceinline__ float2 decay_keep(const DecayLog &l, int n) {
     return make_float2(hi, static_cast<float>(p - hi));
 }
 
+// g as two floats, within 2^-23 log(g)^2 + 2^-49 of itself, without 64-bit arithmetic for slow decays (whose error would add up over the most
+// tokens): 1 + x + x^2 (1/2 + x/6 + ..), x exact, by the series of exp.
+__device__ __forceinline__ float2 decay_factor(const DecayLog &l) {
+    const float x = l.natural;
+    if (!(x >= -0.25f && x <= 0.f)) return decay_keep(l, 1);
+    float q = 1.f / 40320.f;
+    q = fmaf(q, x, 1.f / 5040.f);
+    q = fmaf(q, x, 1.f / 720.f);
+    q = fmaf(q, x, 1.f / 120.f);
+    q = fmaf(q, x, 1.f / 24.f);
+    q = fmaf(q, x, 1.f / 6.f);
+    q = fmaf(q, x, 0.5f);
+    q *= x * x;
+    const float first = 1.f + x, rest = (x - (first - 1.f)) + q, hi = first + rest;
+    return make_float2(hi, rest - (hi - first));
+}
+
 // Lets the launch after this one start where SMs are free.
 __device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

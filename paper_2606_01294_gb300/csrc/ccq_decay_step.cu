@@ -32,6 +32,7 @@ struct StepArgs {
 
 template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_step_kernel(const StepArgs a) {
     __shared__ float qs[D], ks[D], vs[kN];
+    __shared__ float2 factor;
     __shared__ float4 part[kRows / 4][kLanes];
     constexpr int kSlices = D / kN, R = D / kRows;
     const int slice = blockIdx.x % kSlices, bh = blockIdx.x / kSlices, b = bh / a.H, h = bh % a.H;
@@ -56,13 +57,15 @@ template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_s
         ks[tid] = to_f32(k[tid]);
     }
     if (tid < kN) vs[tid] = to_f32(v[tid]);
+    // g as two floats: one float's rounding would be off to the same side at every token and add up over a decode
+    if (tid == kThreads - 1) factor = decay_factor(decay_log2(a.log_decay, h));
     // a state that an earlier row of the batch has is that row's
     int taken = 0;
     if (a.slots && live)
         for (int i = tid; i < b; i += kThreads) taken |= load_index(a.slots, a.slot_bytes, i) == row;
     if (__syncthreads_or(taken)) live = false;
     if (!live && a.slots && row >= 0 && tid == 0) note_index(a.status);
-    const float g = decay_power(decay_log2(a.log_decay, h), 1);
+    const float2 g = factor;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     if (live) {
         const float4 vv = *reinterpret_cast<const float4 *>(&vs[4 * tx]);
@@ -70,10 +73,10 @@ template <typename T, int D> __global__ void __launch_bounds__(kThreads) decay_s
         for (int r = 0; r < R; ++r) {
             const int i = ty + kRows * r;
             const float kk = ks[i], qq = qs[i];
-            s[r].x = s[r].x * g + kk * vv.x;
-            s[r].y = s[r].y * g + kk * vv.y;
-            s[r].z = s[r].z * g + kk * vv.z;
-            s[r].w = s[r].w * g + kk * vv.w;
+            s[r].x = fmaf(s[r].x, g.x, fmaf(s[r].x, g.y, kk * vv.x));
+            s[r].y = fmaf(s[r].y, g.x, fmaf(s[r].y, g.y, kk * vv.y));
+            s[r].z = fmaf(s[r].z, g.x, fmaf(s[r].z, g.y, kk * vv.z));
+            s[r].w = fmaf(s[r].w, g.x, fmaf(s[r].w, g.y, kk * vv.w));
             o.x += qq * s[r].x;
             o.y += qq * s[r].y;
             o.z += qq * s[r].z;
