@@ -132,7 +132,15 @@ __global__ void __launch_bounds__(kThreads, 2) decay_block_kernel(const DecayArg
     if (tid <= kC) sh.power[tid] = decay_power(l2, tid);
     if (tid >= kThreads - 2) sh.keep[tid - (kThreads - 2)] = decay_keep(l2, tid == kThreads - 2 ? kC : ragged);
 
-    if (a.cu) __syncthreads();  // (the ranks' place becomes the first block's)
+    // the factors of the segments before this one, as two floats (up to 64 products; where P will lie)
+    float2 *seg_keep = reinterpret_cast<float2 *>(&sh.p[0][0]);
+    auto segment_tokens = [&](int g) {
+        const int64_t lo = min(per * g, blocks), hi = min(per * (g + 1), blocks);
+        return lo < hi ? static_cast<int>((hi - lo) * kC - ((down ? lo == 0 : hi == blocks) ? blocks * kC - span.length : 0)) : 0;
+    };
+    if (!PARTS && a.segments > 1 && tid < segment) seg_keep[tid] = decay_keep(l2, segment_tokens(tid));
+
+    if (a.cu || (!PARTS && a.segments > 1)) __syncthreads();  // (the ranks' place becomes the first block's)
     // tokens of block j in the pass's order: the ragged block is the sequence's last
     auto block_begin = [&](int64_t j) { return (down ? blocks - 1 - j : j) * kC; };
 
@@ -155,14 +163,14 @@ __global__ void __launch_bounds__(kThreads, 2) decay_block_kernel(const DecayArg
     float S[R][4];
     {
         const int64_t at = (static_cast<int64_t>(sequence) * a.H + h) * D * D;
-        auto add = [&](const float *m, bool transposed, float keep) {
+        auto add = [&](const float *m, bool transposed, float2 keep) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const int row = R * ty + r, col = c0 + 4 * tx + c;
                     const float f = m[transposed ? col * D + row : row * D + col];
-                    S[r][c] = keep == 0.f ? f : S[r][c] * keep + f;
+                    S[r][c] = keep.x == 0.f ? f : fmaf(S[r][c], keep.x, fmaf(S[r][c], keep.y, f));
                 }
             }
         };
@@ -172,7 +180,7 @@ __global__ void __launch_bounds__(kThreads, 2) decay_block_kernel(const DecayArg
             for (int c = 0; c < 4; ++c) S[r][c] = 0.f;
         if (!states) {
         } else if (a.segments == 1 || (PARTS && segment == 0)) {
-            if (ps.state_in) add(ps.state_in + at, ps.transposed, 0.f);
+            if (ps.state_in) add(ps.state_in + at, ps.transposed, make_float2(0.f, 0.f));
             if (PARTS) {
                 float *to = a.parts + decay_part(a, ps.kind, sequence, h, 0);
 #pragma unroll
@@ -185,14 +193,8 @@ __global__ void __launch_bounds__(kThreads, 2) decay_block_kernel(const DecayArg
                     for (int c = 0; c < 4; ++c) S[r][c] = 0.f;
             }
         } else if (!PARTS) {
-            for (int g = 0; g <= segment; ++g) {
-                // tokens of segment g - 1
-                const int64_t lo = min(per * (g - 1), blocks), hi = min(per * g, blocks);
-                int64_t n = 0;
-                if (g > 0 && hi > lo) n = (hi - lo) * kC - ((down ? lo == 0 : hi == blocks) ? blocks * kC - span.length : 0);
-                add(a.parts + decay_part(a, ps.kind, sequence, h, g), ps.parts_transposed,
-                    g == 0 ? 0.f : decay_power(l2, static_cast<int>(n)));
-            }
+            for (int g = 0; g <= segment; ++g)
+                add(a.parts + decay_part(a, ps.kind, sequence, h, g), ps.parts_transposed, g ? seg_keep[g - 1] : make_float2(0.f, 0.f));
         }
     }
 

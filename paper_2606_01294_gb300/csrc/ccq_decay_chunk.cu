@@ -230,6 +230,13 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
         fence_barrier_init();
     }
     if (warp == 0) tmem_alloc(tmem_slot, kTmemCols);
+    // the factors of the segments before this one, as two floats (up to 64 products; where o's tile will lie)
+    float2 *seg_keeps = reinterpret_cast<float2 *>(sm + M::kO);
+    if (!PARTS && segments > 1 && tid >= 32 * kIssueWarp && tid < 32 * kIssueWarp + static_cast<int>(segment)) {
+        const int g = tid - 32 * kIssueWarp, lo = min(per * g, chunks), hi = min(per * (g + 1), chunks);
+        const int n = lo < hi ? (hi - lo) * kC - ((down ? lo == 0 : hi == chunks) ? kC - ragged : 0) : 0;
+        seg_keeps[g] = decay_keep(l2, n);
+    }
     if (segments > 1) grid_wait();  // (the segments' parts)
     if (a.cu) __syncthreads();  // (the ranks' place becomes the table's)
     if (!PARTS && tid < 256) table[tid] = tid < 127 ? 0.f : ps.p_scale * decay_power(l2, tid - 127);
@@ -251,14 +258,14 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
         const int row = D == 128 ? 32 * (warp & 3) + lane : 16 * (warp & 3) + (lane & 15);
         const int col0 = D == 128 ? 64 * (warp >> 2) : 32 * (lane >> 4);
         uint64_t S[kCols / 2];
-        auto add = [&](const float *m, bool transposed, float keep) {
-            const uint64_t k2 = f2_make(keep, keep);
+        auto add = [&](const float *m, bool transposed, float2 keep) {
+            const uint64_t kx = f2_make(keep.x, keep.x), ky = f2_make(keep.y, keep.y);
             const float *at = m + (transposed ? row * D + col0 : col0 * D + row);
             const int step = transposed ? 1 : D;
 #pragma unroll
             for (int c = 0; c < kCols; c += 2) {
                 const uint64_t f = f2_make(at[c * step], at[(c + 1) * step]);
-                S[c / 2] = keep == 0.f ? f : f2_fma(S[c / 2], k2, f);
+                S[c / 2] = keep.x == 0.f ? f : f2_fma(S[c / 2], kx, f2_fma(S[c / 2], ky, f));
             }
         };
         auto put = [&](float *m) {
@@ -313,20 +320,15 @@ __global__ void __maxnreg__(kLaunchRegs) decay_chunk_kernel(const __grid_constan
         for (int c = 0; c < kCols / 2; ++c) S[c] = 0;
         const int64_t matrix = (static_cast<int64_t>(sequence) * a.H + h) * D * D;
         if (segments == 1 || (PARTS && segment == 0)) {
-            if (ps.state_in) add(ps.state_in + matrix, ps.transposed, 0.f);
+            if (ps.state_in) add(ps.state_in + matrix, ps.transposed, make_float2(0.f, 0.f));
             if (PARTS) {
                 put(a.parts + decay_part(a, ps.kind, sequence, h, 0));
 #pragma unroll
                 for (int c = 0; c < kCols / 2; ++c) S[c] = 0;
             }
         } else if (!PARTS) {
-            for (int g = 0; g <= static_cast<int>(segment); ++g) {
-                const int lo = min(per * (g - 1), chunks), hi = min(per * g, chunks);  // segment g - 1
-                int n = 0;
-                if (g > 0 && hi > lo) n = (hi - lo) * kC - ((down ? lo == 0 : hi == chunks) ? kC - ragged : 0);
-                add(a.parts + decay_part(a, ps.kind, sequence, h, g), ps.parts_transposed,
-                    g == 0 ? 0.f : decay_power(l2, n));
-            }
+            for (int g = 0; g <= static_cast<int>(segment); ++g)
+                add(a.parts + decay_part(a, ps.kind, sequence, h, g), ps.parts_transposed, g ? seg_keeps[g - 1] : make_float2(0.f, 0.f));
         }
         const int half = warp >> 2, row0 = 32 * (warp & 3), i = row0 + lane;  // of P: column half, row
         for (int r = 0; r < count; ++r) {

@@ -1,4 +1,11 @@
-"""What the step of linear attention with a decay for each head keeps of a state over thousands of tokens.  u = 2^-24."""
+"""What linear attention with a decay for each head keeps of a state over many tokens.
+
+With u = 2^-24.  A state that nothing is added to is g^n S0.  Each product with the factor rounds an entry by up to u of itself; the
+roundings of different entries are independent of each other (their bits are random) and take no side, so their mean over N
+entries after m products is near 0: its standard deviation is below u sqrt(m / 3) / sqrt(N), and 8 of these are allowed.  An error of the factor
+itself has the same sign in every entry and at every product and adds up to m times that error, which the mean shows.  The factor as two
+floats is off by 2^-47 of itself (half a unit of the second): m 2^-47 is allowed too.
+"""
 import math
 
 import pytest
@@ -9,6 +16,7 @@ from paper_2606_01294_gb300 import ccq, ops
 pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -24
+BF16, FP32 = torch.bfloat16, torch.float32
 
 
 @pytest.fixture(autouse=True)
@@ -22,6 +30,16 @@ def slow_decays(H, tokens):
     least = math.log2(tokens / 8)
     bits = least + (13 - least) * torch.arange(H, dtype=torch.float64) / max(1, H - 1)
     return torch.log1p(-torch.exp2(-bits)).float().cuda()
+
+
+def check_kept(state, start, log_decay, tokens, products, what):
+    """state = g^tokens start in every entry within m u, and the mean of the relative errors within its own bound."""
+    d = start.shape[-1]
+    ref = start.double() * torch.exp(log_decay.double() * tokens)[:, None, None]
+    err = state.double() / ref - 1
+    assert float(err.abs().max()) <= 1.01 * products * U + products * 2.0 ** -47, what
+    mean = err.mean((-1, -2)).abs().max()
+    assert float(mean) <= 8 * U * math.sqrt(products / 3) / d + products * 2.0 ** -47, f"{what}: mean {float(mean):.3g}"
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -76,3 +94,22 @@ def test_steps_and_a_prompt_keep_the_same():
     along = ((state.double() - exact) * exact).sum((-1, -2)) / (exact * exact).sum((-1, -2))
     room = 8 * 3 * U * (memory[..., 0, 0] / 3).sqrt() / d * largest.amax((-1, -2)) / exact.pow(2).mean((-1, -2)).sqrt()
     assert (along.abs() <= room).all(), (along / room).tolist()
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,T,H", [(1, 20480, 1), (1, 20480, 8), (1, 3001, 2), (8, 4096, 16)])
+def test_a_state_kept_through_a_prompt(dtype, d, B, T, H):
+    """Keys of zero: the state handed out is g^T of the one before, by a product for each chunk (128 tokens in bf16, 32 in fp32) and for
+    each segment of a sequence that is cut; so is the gradient of the state before, of the one behind."""
+    if dtype == FP32 and B == 8:
+        B = 2
+    ld = slow_decays(H, T)
+    start = torch.randn(B, H, d, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(T + d))
+    x = torch.randn(B, T, H, d, device="cuda").to(dtype)
+    zero = torch.zeros_like(x)
+    products = -(-T // (32 if dtype == FP32 else 128)) + 65
+    _, state = ops.decay_attention(x, zero, x, ld, state=start)
+    check_kept(state, start, ld, T, products, "state")
+    g = ops.decay_attention_bwd(zero, x, x, ld, x, dfinal_state=start)
+    check_kept(g["dstate"], start, ld, T, products, "dstate")
