@@ -1,4 +1,4 @@
-"""What linear attention with a decay for each head keeps of a state over many tokens.
+"""What linear attention with a decay for each head keeps of a state over many tokens, and the 24 bits of a state that is handed out.
 
 With u = 2^-24.  A state that nothing is added to is g^n S0.  Each product with the factor rounds an entry by up to u of itself; the
 roundings of different entries are independent of each other (their bits are random) and take no side, so their mean over N
@@ -113,3 +113,44 @@ def test_a_state_kept_through_a_prompt(dtype, d, B, T, H):
     check_kept(state, start, ld, T, products, "state")
     g = ops.decay_attention_bwd(zero, x, x, ld, x, dfinal_state=start)
     check_kept(g["dstate"], start, ld, T, products, "dstate")
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T", [2, 33, 128, 300])
+def test_a_state_handed_out_has_24_bits(dtype, d, T):
+    """One token with a value, the rest zeros: each entry of the state is one product, g^n k v.  The power is within 2^-22 of itself,
+    its product with k is rounded to 24 bits (u), the sum of the three terms' products is cut at most by a unit (2 u), each product with
+    a block's factor is rounded once (u; blocks of 32 tokens in fp32, of 128 in bf16): 2^-22 + (4 + blocks) u.  (Two bf16 terms would be
+    off by up to 2^-18, 64 u.)"""
+    H = 4
+    g = torch.Generator(device="cuda").manual_seed(T)
+    ld = torch.tensor([-0.0003, -0.01, -0.02, -0.037], device="cuda")
+    bound = 2.0 ** -22 + (4 + -(-T // (32 if dtype == FP32 else 128))) * U
+    for at in {0, T // 2, T - 2}:
+        k, v = (torch.zeros(1, T, H, d, device="cuda").to(dtype) for _ in range(2))
+        k[:, at], v[:, at] = (torch.randn(1, H, d, device="cuda", generator=g).to(dtype) for _ in range(2))
+        _, state = ops.decay_attention(k, k, v, ld)
+        exact = lambda n: (torch.exp(ld.double() * n)[:, None, None] * k[0, at].double()[..., None] * v[0, at].double()[:, None])[None]  # noqa: E731
+        ref = exact(T - 1 - at)
+        assert ((state.double() - ref).abs() <= bound * ref.abs()).all(), at
+        # the gradient of the state before: scale g^(n + 1) q dout
+        grads = ops.decay_attention_bwd(k, k, k, ld, v, dfinal_state=torch.zeros_like(state), scale=0.5)
+        ref = 0.5 * exact(at + 1)
+        assert ((grads["dstate"].double() - ref).abs() <= bound * ref.abs()).all(), at
+
+
+@pytest.mark.parametrize("Hk", [128, 64])
+def test_gradients_of_offsets_past_32_bits(Hk):
+    """The last of many rows, 2^31 elements and more in, of heads of their own and of shared ones; the rows before have no gradient."""
+    B, T, H, d = 9000, 16, 128, 128  # 2.36e9 elements
+    g = torch.Generator(device="cuda").manual_seed(Hk)
+    n = lambda h: torch.randn(1, T, h, d, device="cuda", generator=g).to(BF16)  # noqa: E731
+    q, k, v, dout = (torch.zeros(B, T, h, d, dtype=BF16, device="cuda") for h in (H, Hk, Hk, H))
+    for x in (q, k, v, dout):
+        x[-1:] = n(x.shape[2])
+    ld = torch.linspace(-0.3, -0.01, H, device="cuda")
+    grads = ops.decay_attention_bwd(q, k, v, ld, dout)
+    alone = ops.decay_attention_bwd(q[-1:], k[-1:], v[-1:], ld, dout[-1:])
+    for name, x in grads.items():
+        assert torch.equal(x[-1], alone[name][0]) and not x[0].any() and not x[-2].any() and alone[name].any(), name
