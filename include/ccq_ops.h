@@ -93,7 +93,8 @@ CCQ_API ccq_status ccq_zero_outside(const ccq_heads *x, ccq_dtype dtype, int64_t
  *              strides), else it lies apart from x and the other y.
  *   positions  [B, T], position_bytes 4 (int32) or 8 (int64); any values.
  *   freqs      [part / 2] radians a position, fp64 (any finite values).
- * An angle is formed to 2^-31 of a turn, whatever the position; products and sums are fp32, rounded once.
+ * An angle is formed to 2^-30 of a turn, whatever the position and the frequency, and rounded to fp32 as the argument of
+ * cosine and sine (2^-26 of a turn at most); products and sums are fp32, rounded once.
  */
 CCQ_API ccq_status ccq_rotary(const ccq_heads *x, const ccq_heads *y, int count, ccq_dtype dtype, int64_t B,
                               int64_t T, int width, int part, const void *positions, int position_bytes,

@@ -1,10 +1,10 @@
 // ccq_rotary.cu -- rotation of the heads of queries and keys by their positions (ccq_ops.h).
 //
 // The pair (a, b) of a token at position p turns by p f_i radians: a' = m (a cos - b sin), b' = m (a sin + b cos).
-// Angles are kept as 64-bit fractions of a turn: F_i = f_i 2^64 / (2 pi) mod 2^64 and p F_i mod 2^64 in integers,
-// exact whatever p (F_i is within 2 units of 2^-64 turns for f_i < 1, so 2^-33 turns at p = 2^30); the top 32 bits become
-// the argument of sincospif.  (The same in 64-bit floating point, at this GPU's rate for it, would take a fifth of the
-// prefill's time.)  A CTA computes the cosines and sines of its tokens once for all heads.
+// Angles are kept as 64-bit fractions of a turn: F_i = f_i 2^64 / (2 pi) mod 2^64 and p F_i mod 2^64 in integers, where F_i is within
+// 3 units of 2^-64 turns; the top 32 bits become the argument of sincospif, rounded to fp32.  Positions of more than 32 bits and
+// frequencies from 2 on, which lose more, take 128-bit fractions (far_angle).  (The same in 64-bit floating point, at this GPU's rate
+// for it, would take a fifth of the prefill's time.)  A CTA computes the cosines and sines of its tokens once for all heads.
 // Bound by HBM, every element read once and written once: 8 x 4096 tokens of 16 + 16 heads of 128 in bf16 80 us, 6.7 TB/s, a copy's
 // rate.  A decode's 256 tokens take 3 us, a launch.
 #include <algorithm>
@@ -53,7 +53,7 @@ struct RotaryArgs {
                                                 // in 64 bits a hundred: they took a third of the 3 x 3001 tokens' time)
 };
 
-// f 2^64 / (2 pi) mod 2^64, from the bits of f.
+// f 2^64 / (2 pi) mod 2^64 within 3 units, from the bits of f, for |f| < 2.
 __device__ __forceinline__ uint64_t turns_of(double f) {
     constexpr uint64_t kInvTwoPi = 2935890503282001226ull;  // 2^64 / (2 pi)
     const uint64_t bits = static_cast<uint64_t>(__double_as_longlong(f));
@@ -62,8 +62,41 @@ __device__ __forceinline__ uint64_t turns_of(double f) {
     m = e ? m | (1ull << 52) : 0;  // (a subnormal frequency turns by nothing)
     const uint64_t hi = __umul64hi(m << 11, kInvTwoPi);  // f = (m << 11) 2^(e - 1086): F = hi 2^(e - 1022)
     const int s = e - 1022;
-    const uint64_t F = s >= 64 || s <= -64 ? 0 : s >= 0 ? hi << s : hi >> -s;
+    const uint64_t F = s <= -64 ? 0 : s > 0 ? hi << s : hi >> -s;
     return bits >> 63 ? 0 - F : F;
+}
+
+// 1 / (2 pi), 64 bits a word, the first behind the point.
+__device__ constexpr uint64_t kInverseTurn[19] = {
+    0x28be60db9391054aull, 0x7f09d5f47d4d3770ull, 0x36d8a5664f10e410ull, 0x7f9458eaf7aef158ull, 0x6dc91b8e909374b8ull,
+    0x01924bba82746487ull, 0x3f877ac72c4a69cfull, 0xba208d7d4baed121ull, 0x3a671c09ad17df90ull, 0x4e64758e60d4ce7dull,
+    0x272117e2ef7e4a0eull, 0xc7fe25fff7816603ull, 0xfbcbc462d6829b47ull, 0xdb4d9fb3c9f2c26dull, 0xd3d18fd9a797fa8bull,
+    0x5d49eeb1faf97c5eull, 0xcf41ce7de294a4baull, 0x9afed7ec47e35742ull, 0x1580cc11bf1edaeaull};
+
+// The angle p f, in units of 2^-32 turns, for any p and any finite f = +-m 2^k: m, of 53 bits, times the 192 bits of 1 / (2 pi) from
+// the first whose product is no whole turn (Payne and Hanek's reduction) leaves 128 bits behind the point, and |p| takes 63 of them.
+__device__ __noinline__ int32_t far_angle(int64_t p, double f) {
+    const uint64_t bits = static_cast<uint64_t>(__double_as_longlong(f));
+    const int e = static_cast<int>((bits >> 52) & 0x7ff), k = e - 1075;
+    if (k <= -192) return 0;  // (below 2^-75 turns at any p)
+    const uint64_t m = (bits & 0xfffffffffffffull) | (1ull << 52);
+    const int first = k >> 6, shift = k & 63;
+    auto word = [](int j) { return j < 0 ? 0 : kInverseTurn[j]; };
+    uint64_t x[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        x[i] = shift ? word(first + i) << shift | word(first + i + 1) >> (64 - shift) : word(first + i);
+    const uint64_t mid = m * x[1], lo = mid + __umul64hi(m, x[2]), hi = m * x[0] + __umul64hi(m, x[1]) + (lo < mid);
+    const uint64_t n = p < 0 ? 0 - static_cast<uint64_t>(p) : static_cast<uint64_t>(p);
+    const uint64_t turn = n * hi + __umul64hi(n, lo);
+    return static_cast<int32_t>(((bits >> 63) != (p < 0) ? 0 - turn : turn) >> 32);
+}
+
+// The angle of every day, by one product: within 2^-30 of a turn, as 3 units of F times |p| <= 2^31 and the cut at 32 bits are.
+__device__ __forceinline__ int32_t angle_of(int64_t p, double f) {
+    const int exponent = __double2hiint(f) >> 20 & 0x7ff;  // (no comparison in 64 bits)
+    if (p != static_cast<int32_t>(p) || exponent > 1023) return far_angle(p, f);
+    return static_cast<int32_t>((static_cast<uint64_t>(p) * turns_of(f)) >> 32);
 }
 
 // N elements an access; PAIR: the two halves of N pairs as an access each (N = 1 interleaved: its two elements), else an
@@ -80,10 +113,9 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryArgs a) {
     for (int j = threadIdx.x; j < tokens * half; j += kThreads) {
         const int t = a.by_half(j), i = j - t * half;
         const double f = a.freqs[i];
-        const uint64_t p = static_cast<uint64_t>(load_index(a.positions, a.position_bytes, first + t));
-        const int32_t top = static_cast<int32_t>((p * turns_of(f)) >> 32);
+        const int32_t angle = angle_of(load_index(a.positions, a.position_bytes, first + t), f);
         float s, c;
-        sincospif(static_cast<float>(top) * 0x1p-31f, &s, &c);
+        sincospif(static_cast<float>(angle) * 0x1p-31f, &s, &c);
         if (!isfinite(f)) s = c = __int_as_float(0x7fffffff);
         const int e = i % kPairs, place = kPairs == 1 ? i : (e / 2 * across + i / kPairs) * 2 + e % 2;
         turn[t * half + place] = make_float2(c * a.amplitude, (a.inverse ? -s : s) * a.amplitude);
