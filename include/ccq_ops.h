@@ -64,7 +64,8 @@ CCQ_API ccq_status ccq_embed_grad_workspace_size(int64_t n, int64_t rows, int wi
 /*
  * Heads of tokens: channel c of head h of token (b, t) is p[b * batch + t * token + h * head + c].
  * Strides are in elements, 0 <= stride < 2^40 (those of extents of one are not looked at).  An input may
- * repeat itself (a stride of 0); an output's channels lie apart.  Tensors whose addresses and strides are
+ * repeat itself (a stride of 0); an output's channels lie apart, and an output that shares an element with a tensor it has to lie
+ * apart from is refused (slices that interleave do not).  Tensors whose addresses and strides are
  * multiples of 16 bytes are faster.
  */
 typedef struct {

@@ -653,6 +653,8 @@ ccq_status ccq_decay_attention(const ccq_heads *q, const ccq_heads *k, const ccq
     if (need && (st = op_pointer("workspace", workspace, 16)) != CCQ_OK) return st;
     if (workspace_bytes < need)
         return op_fail(CCQ_ERR_INVALID_ARG, "workspace of %zu bytes, needs %zu", workspace_bytes, need);
+    for (int i = 0; i < 3; ++i)
+        if ((st = check_apart("o", *o, names[i], *in[i], dtype_bytes(dtype), B, T, d)) != CCQ_OK) return st;
     const size_t state_bytes = static_cast<size_t>(num_seqs) * H * d * d * 4;
     if ((st = check_states_apart("S0", S0, "ST", ST, state_bytes, true)) != CCQ_OK) return st;
     if (num_seqs == 0) return CCQ_OK;
@@ -742,6 +744,11 @@ ccq_status ccq_decay_attention_bwd(const ccq_heads *q, const ccq_heads *k, const
     for (int i = 0; i < 3 && B * T; ++i)
         if (out[i]->p == out[(i + 1) % 3]->p)
             return op_fail(CCQ_ERR_INVALID_ARG, "%s is %s", outs[(i + 1) % 3], outs[i]);
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < 4; ++j)
+            if ((st = check_apart(outs[i], *out[i], names[j], *in[j], dtype_bytes(dtype), B, T, d)) != CCQ_OK) return st;
+        if ((st = check_apart(outs[(i + 1) % 3], *out[(i + 1) % 3], outs[i], *out[i], dtype_bytes(dtype), B, T, d)) != CCQ_OK) return st;
+    }
     const size_t state_bytes = static_cast<size_t>(num_seqs) * H * d * d * 4;
     if ((st = check_states_apart("S0", S0, "dS0", dS0, state_bytes, false)) != CCQ_OK) return st;
     if ((st = check_states_apart("dST", dST, "dS0", dS0, state_bytes, false)) != CCQ_OK) return st;

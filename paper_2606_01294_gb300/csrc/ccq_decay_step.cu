@@ -149,6 +149,8 @@ ccq_status ccq_decay_attention_step(const ccq_heads *q, const ccq_heads *k, cons
         if (in[i]->p == o->p) return op_fail(CCQ_ERR_INVALID_ARG, "o is %s: other blocks still read it", names[i]);
     StepArgs a = {};
     if ((st = op_status_word(&a.status)) != CCQ_OK) return st;
+    for (int i = 0; i < 3; ++i)
+        if ((st = check_apart("o", *o, names[i], *in[i], dtype_bytes(dtype), B, 1, d)) != CCQ_OK) return st;
     auto view = [H](const ccq_heads &x) { return DecayView{x.p, x.batch, 0, x.head, static_cast<int>(H / x.heads)}; };
     a.q = view(*q);
     a.k = view(*k);

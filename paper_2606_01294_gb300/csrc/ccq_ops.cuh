@@ -109,6 +109,82 @@ inline int heads_access(const ccq_heads &x, int elem, int64_t B, int64_t T, int 
     return most;
 }
 
+// Whether two tensors of heads have an element in common: whether offsets of b less offsets of a reach the distance of their
+// addresses.  The dimensions' steps are tried from the largest on (those of the same stride as one), a step as often as what is left
+// of the others still reaches the rest.  Slices of one tensor are told apart in a few tries, whatever interleaves; the answer is yes where
+// thousands of tries do not settle it.
+struct HeadsMeet {
+    struct {
+        __int128 stride, lo, hi;
+    } step[8];
+    __int128 lo[9], hi[9];  // of the steps from one on
+    bool all[9];            // whether these reach all that lies between
+    int count = 0, tries = 1 << 14;
+
+    void add(__int128 stride, __int128 lo_, __int128 hi_) {
+        if (!stride) return;
+        int i = 0;
+        while (i < count && step[i].stride > stride) ++i;
+        if (i < count && step[i].stride == stride) {
+            step[i].lo += lo_;
+            step[i].hi += hi_;
+            return;
+        }
+        for (int j = count++; j > i; --j) step[j] = step[j - 1];
+        step[i] = {stride, lo_, hi_};
+    }
+    bool reach(int i, __int128 rest) {
+        if (rest < lo[i] || rest > hi[i]) return false;
+        if (all[i] || --tries < 0) return true;
+        const auto &s = step[i];
+        // s.stride n within [rest - hi[i + 1], rest - lo[i + 1]]
+        const __int128 from = rest - hi[i + 1], to = rest - lo[i + 1];
+        __int128 n = from >= 0 ? (from + s.stride - 1) / s.stride : -(-from / s.stride);
+        for (n = n > s.lo ? n : s.lo; n <= s.hi && n * s.stride <= to; ++n)
+            if (reach(i + 1, rest - n * s.stride)) return true;
+        return false;
+    }
+    bool operator()(__int128 distance) {
+        lo[count] = hi[count] = 0;
+        all[count] = true;
+        for (int i = count - 1; i >= 0; --i) {
+            lo[i] = lo[i + 1] + step[i].stride * step[i].lo;
+            hi[i] = hi[i + 1] + step[i].stride * step[i].hi;
+            all[i] = all[i + 1] && step[i].stride <= hi[i + 1] - lo[i + 1] + 1;
+        }
+        return reach(0, distance);
+    }
+};
+
+inline bool heads_overlap(const ccq_heads &a, const ccq_heads &b, int elem, int64_t B, int64_t T, int64_t width) {
+    auto last = [&](const ccq_heads &x) {
+        return static_cast<__int128>(B > 1 ? x.batch : 0) * (B - 1) + static_cast<__int128>(T > 1 ? x.token : 0) * (T - 1) +
+               static_cast<__int128>(x.heads > 1 ? x.head : 0) * (x.heads - 1) + width - 1;
+    };
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
+    const __int128 distance = (static_cast<__int128>(pa) - static_cast<__int128>(pb)) / elem;  // (both are aligned to elements)
+    if (distance > last(b) || -distance > last(a)) return false;
+    HeadsMeet m;
+    for (const ccq_heads *x : {&a, &b}) {
+        const int sign = x == &b ? 1 : -1;
+        auto add = [&](int64_t stride, int64_t n) {
+            if (n > 1) m.add(stride, sign < 0 ? 1 - n : 0, sign < 0 ? 0 : n - 1);
+        };
+        add(x->batch, B);
+        add(x->token, T);
+        add(x->head, x->heads);
+        add(1, width);
+    }
+    return m(distance);
+}
+
+// An output apart from another tensor of the call, which other blocks read or write meanwhile.
+inline ccq_status check_apart(const char *out, const ccq_heads &y, const char *other, const ccq_heads &x, int elem, int64_t B, int64_t T,
+                              int64_t width) {
+    if (B * T == 0 || !heads_overlap(y, x, elem, B, T, width)) return CCQ_OK;
+    return op_fail(CCQ_ERR_INVALID_ARG, "%s overlaps %s", out, other);
+}
+
 inline int sm_count_now() {
     static std::atomic<int> counts[64];
     int dev = 0;

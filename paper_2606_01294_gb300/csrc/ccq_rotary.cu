@@ -289,6 +289,12 @@ ccq_status ccq_rotary(const ccq_heads *x, const ccq_heads *y, int count, ccq_dty
         if (count == 2 && (y[i].p == x[1 - i].p || y[0].p == y[1].p))
             return op_fail(CCQ_ERR_INVALID_ARG, "y[%d] is %s[%d]", i, y[i].p == x[1 - i].p ? "x" : "y", 1 - i);
     }
+    const char *xs[2] = {"x[0]", "x[1]"}, *ys[2] = {"y[0]", "y[1]"};
+    for (int i = 0; i < count; ++i)
+        for (int j = 0; j < count; ++j) {
+            if ((i != j || x[i].p != y[i].p) && (st = check_apart(ys[i], y[i], xs[j], x[j], elem, B, T, width)) != CCQ_OK) return st;
+            if (i < j && (st = check_apart(ys[j], y[j], ys[i], y[i], elem, B, T, width)) != CCQ_OK) return st;
+        }
     a.heads = static_cast<int>(heads);
     a.tokens = B * T;
     a.T = T;
