@@ -5,13 +5,14 @@
 // the state, in fp32 on the CUDA cores:
 //   P = Q K^T (32 x 32), masked and times g^|i - j|;  O = P V + diag(g^..) Q S;  S = g^n S + K^T diag(g^..) V.
 // Half of the threads have the state and what is read from it (Q S), the others P and P V: between its two barriers a block is one chain
-// of either.  32 tokens cost 32 d (16 + 2 * 32) + 16 * 32 * 32 multiply-adds a CTA, of which P, formed again by each slice, is a fifth.
+// of either.  32 tokens cost 32 d (32 + 2 * 32) + 20 * 32 * 32 multiply-adds a CTA, of which P, formed whole and again by each slice, is
+// a third.
 // Aligned fp32 operands of the next block are copied while this one is computed.
 // Bound by what a thread loads from shared memory (32 words a cycle for an SM that multiplies 128): so Q K^T and Q S are 4 x 8 a
 // thread over a quarter of d, summed by shuffles, and P V reads four columns of P at a time.  What is left is instructions: Q S and the
 // state's increment are multiplied in pairs (531 -> 496 us; Q K^T in pairs, with twice the sums, is slower for d = 64).  8 x 1000
-// tokens of 16 heads of 128 in fp32: 496 us (797 with 2 x 4 a thread and one group), 8 x 1000 x 16 x 64 162 (287), 4 x 777 of 4 heads of
-// 64 in 7 segments 33 (49).
+// tokens of 16 heads of 128 in fp32: 482 us (797 with 2 x 4 a thread and one group), 8 x 1000 x 16 x 64 159 (287), 4 x 777 of 4 heads of
+// 64 in 7 segments 29 (49).
 // Slices of 32 columns rather than whole heads, so that few heads still reach many SMs.
 #include <algorithm>
 #include <cmath>
@@ -468,7 +469,8 @@ template <typename Type> __global__ void __launch_bounds__(256) decay_sum_kernel
 
 // Segments of each sequence, by a count of what a launch takes: rounds of resident CTAs times the blocks of a CTA, for the
 // passes and, with more than one segment, for the states before them (`kinds`, all segments but the last).  A block's times
-// are those measured with the GPU full.  1 x 16 x 20480 x 128 bf16: 482 us whole, 125 in 9 segments; the gradients of
+// are those measured with the GPU full.  What is not counted: the adding of earlier segments' states, one after another (64 KB of each for
+// d = 128), which few heads with dozens of segments feel.  1 x 16 x 20480 x 128 bf16: 482 us whole, 122 in 9 segments; the gradients of
 // 4 x 16 x 4096 x 128: 197 whole, 249 in 2 each, 171 with 40 of 192 passes in 2; 1 x 8 x 4000 x 128 fp32: 162 in 9.
 struct Cost {
     int block;           // tokens

@@ -20,9 +20,12 @@
 //                       V in halves of 64 tokens, K in a ring of three halves
 // Bound by the steps of a chunk one after another, 3.4 us at d = 128 and 2.4 at 64, D through registers to S and its copy and A to P
 // among them, not by a unit: HBM 74 % of a copy, the tensor cores 40 to 53 %, issue 50 %; W, the longest stage, is 12 %.  bf16, 16 heads of 128: 8 x 4096 tokens 109 us
-// (decay_block_kernel: 3300), 1 x 20480 in segments 121, 64 packed prompts 238, gradients of 4 x 4096 171.  Why so: chunks of
+// (decay_block_kernel: 3150), 1 x 20480 in segments 122, 64 packed prompts 241, gradients of 4 x 4096 172.  Why so: chunks of
 // 128 fill an accumulator's lanes; S stays in registers, as in tensor memory it would be read, scaled and written there each
 // chunk; a head has one CTA, for with two halves of V's columns both would form P and the split.
+// What is rounded to fewer bits than fp32: P and the copy of S that queries read, as bf16 operands (relative error of o against 64 bits 2.3e-3;
+// 1.7e-3 where o alone is rounded).  In two bf16 terms each they would cost P V and Q S twice, a third more products, and S's second term 32 KB
+// of shared memory, of which none is left at d = 128.  S itself is not rounded: fp32, its factors two floats, its increment's terms as below.
 // Rows past a sequence's end: TMA gives zeros past the tensor; rows of other packed sequences get W = 0, P = 0, and
 // zeros in V (0 times what is not finite would not be 0).
 #include "ccq_decay.cuh"

@@ -3,7 +3,8 @@
 // state = g state + k v^T, o = scale state^T q: each state is read and written once, 8 d^2 bytes a head, and nothing else
 // counts: bound by HBM.  A CTA takes 32 columns of a head's state, so that a small batch still reaches many SMs; its 128
 // threads hold the slice in registers (all loads under way at once), and the partial sums of o cross threads once.
-// 256 x 16 states of 64 KB: 80 to 83 us, 6.5 TB/s, 96 % of a copy; 2 x 4 of 128: 2.1 us, a launch.
+// 256 x 16 states of 64 KB: 80 to 83 us, 6.5 TB/s, 96 % of a copy; 2 x 4 of 128: 2.1 us, a launch.  With slots, every CTA looks for its
+// state among the rows before it: 3 % more for 1024 rows of 16 heads, 10 % for 4096, 40 % for 16384 of 4 heads, 4 times the time for 65536 of one.
 #include <cmath>
 
 #include "ccq_decay.cuh"
