@@ -154,3 +154,29 @@ def test_gradients_of_offsets_past_32_bits(Hk):
     alone = ops.decay_attention_bwd(q[-1:], k[-1:], v[-1:], ld, dout[-1:])
     for name, x in grads.items():
         assert torch.equal(x[-1], alone[name][0]) and not x[0].any() and not x[-2].any() and alone[name].any(), name
+
+
+def test_states_past_32_bits():
+    """States of 2^31 elements and more, as a pool for steps and before and after many short prompts: the last rows as by themselves."""
+    rows, H, d = 9000, 16, 128  # 2.36e9 elements
+    g = torch.Generator(device="cuda").manual_seed(6)
+    pool = torch.zeros(rows, H, d, d, device="cuda")
+    pool[-2:] = torch.randn(2, H, d, d, device="cuda", generator=g)
+    before = pool[-2:].clone()
+    ld = torch.linspace(-0.3, -0.01, H, device="cuda")
+    q, k, v = (torch.randn(2, H, d, device="cuda", generator=g).to(BF16) for _ in range(3))
+    alone = before.clone()
+    expect = ops.decay_attention_step(q, k, v, ld, alone)
+    o = ops.decay_attention_step(q, k, v, ld, pool, slots=torch.tensor([rows - 2, rows - 1], device="cuda"))
+    assert torch.equal(o, expect) and torch.equal(pool[-2:], alone) and not pool[:-2].any()
+    for dtype in (BF16, FP32):
+        x = torch.zeros(rows, 3, H, d, device="cuda", dtype=dtype)
+        x[-2:] = torch.randn(2, 3, H, d, device="cuda", generator=g).to(dtype)
+        expect, state = ops.decay_attention(x[-2:], x[-2:], x[-2:], ld, state=pool[-2:])
+        o, states = ops.decay_attention(x, x, x, ld, state=pool)
+        assert torch.equal(o[-2:], expect) and torch.equal(states[-2:], state) and not states[:-2].any() and not o[:-2].any()
+        expect = ops.decay_attention_bwd(x[-2:], x[-2:], x[-2:], ld, x[-2:], state=pool[-2:], dfinal_state=state)
+        grads = ops.decay_attention_bwd(x, x, x, ld, x, state=pool, dfinal_state=states)
+        for n in expect:
+            assert torch.equal(grads[n][-2:], expect[n]) and not grads[n][:-2].any(), n
+        del x, o, states, grads
